@@ -1,0 +1,461 @@
+"""The operators of the update side of a GRPO step, as timed cases.
+
+A rollout leaves tokens (padded with -1), lengths, logits and advantages.  The
+update scores the tokens (log probability, entropy, most likely alternatives),
+forms the clipped group-relative loss, and carries its gradient back into the
+logits and, at the other end of the model, into the embedding rows.  The cases
+are those calls from the tiny fp32 model of the smoke test to the widths and
+vocabulary of the 7B, 14B and 72B decoders.
+
+Each operator has a plain form (``own`` false): elementary torch operations in
+32 bits.  ``exact`` is the definition in 64 bits, a few rows at a time.
+"""
+import math
+
+import torch
+
+own = False
+DEV = "cuda:0"
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
+MEAN_SEQUENCE, MEAN_TOKEN, MEAN_FIXED = 0, 1, 2
+INF = float("inf")
+
+
+def listed():
+    return [
+        # a decode step of the tiny fp32 model: eight rows, where only latency counts
+        {"name": "logprobs_tiny", "kind": "logprobs", "rows": 8, "vocab": 1024, "dtype": "fp32", "temperature": 1.0, "top": 0, "extra": 0, "pad": 0.0},
+        # after the draw of a decode step of the 7B benchmark: 64 sequences in flight, a few alternatives kept
+        {"name": "logprobs_decode_7b", "kind": "logprobs", "rows": 64, "vocab": 152064, "dtype": "fp32", "temperature": 0.9, "top": 8, "extra": 0, "pad": 0.0},
+        # the same at the 14B benchmark's 256 sequences, with as many alternatives as an answer usually carries
+        {"name": "logprobs_decode_14b", "kind": "logprobs", "rows": 256, "vocab": 152064, "dtype": "fp32", "temperature": 1.0, "top": 20, "extra": 0, "pad": 0.0},
+        # old and reference log probabilities for an update: 4,096 tokens of completions of unequal length, bf16 logits
+        {"name": "logprobs_update_7b", "kind": "logprobs", "rows": 4096, "vocab": 152064, "dtype": "bf16", "temperature": 0.9, "top": 0, "extra": 0, "pad": 0.125},
+        # the gradient of the same micro-batch; the rows of groups without reward variance have none
+        {"name": "logprobs_backward_7b", "kind": "logprobs_backward", "rows": 4096, "vocab": 152064, "dtype": "bf16", "temperature": 0.9, "extra": 0, "pad": 0.125, "still": 0.125},
+        # fp32 logits of an odd vocabulary inside a wider matrix, an odd number of rows
+        {"name": "logprobs_backward_odd", "kind": "logprobs_backward", "rows": 259, "vocab": 32003, "dtype": "fp32", "temperature": 1.0, "extra": 29, "pad": 0.0, "still": 0.0},
+        # the loss over the 7B benchmark's wave: 64 completions of up to 512 tokens, no reference model
+        {"name": "loss_7b", "kind": "loss", "groups": 8, "G": 8, "max_len": 512, "mean": MEAN_SEQUENCE, "ref": False, "entropy": False},
+        # a large batch of long completions with reference and entropy terms, mean over tokens
+        {"name": "loss_long", "kind": "loss", "groups": 128, "G": 16, "max_len": 4096, "mean": MEAN_TOKEN, "ref": True, "entropy": True},
+        # the tokens of one decode step of the 7B benchmark
+        {"name": "embedding_decode_7b", "kind": "embedding", "tokens": 64, "vocab": 152064, "dim": 3584, "table": "bf16", "out": "fp32", "pad": 0.0},
+        # prompts and completions of a whole 7B wave (64 x 768), widened to the fp32 residual stream
+        {"name": "embedding_update_7b", "kind": "embedding", "tokens": 49152, "vocab": 152064, "dim": 3584, "table": "bf16", "out": "fp32", "pad": 0.125},
+        # the tiny model's gradient: a small table, every id many times
+        {"name": "embedding_backward_tiny", "kind": "embedding_backward", "tokens": 2048, "vocab": 1024, "dim": 128, "grad": "fp32", "table": "fp32", "pad": 0.0},
+        # the gradient of the whole 7B wave: bf16 gradients into the fp32 table
+        {"name": "embedding_backward_7b", "kind": "embedding_backward", "tokens": 49152, "vocab": 152064, "dim": 3584, "grad": "bf16", "table": "fp32", "pad": 0.125},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    kind = rng.choice(["logprobs", "logprobs", "logprobs", "logprobs_backward", "logprobs_backward", "loss", "loss",
+                       "embedding", "embedding_backward", "embedding_backward"])
+    if kind.startswith("logprobs"):
+        vocab = rng.choice([1024, 4099, 32003, 50257, 152064, 152064, 152064, _log(rng, 64, 160000)])
+        dtype = rng.choice(["fp32", "bf16"])
+        # at most the bytes of 4,096 rows of the largest vocabulary in bf16
+        rows = _log(rng, 1, min(40000, 4096 * 152064 // vocab // (2 if dtype == "fp32" else 1)))
+        case = {"kind": kind, "rows": rows, "vocab": vocab, "dtype": dtype, "temperature": rng.choice([1.0, 0.9, 0.7, 1.3]),
+                "extra": rng.choice([0, 0, 0, 1, 8, 61]), "pad": rng.choice([0.0, 0.0, 0.25])}
+        if kind == "logprobs":
+            # alternatives are kept while generating, for a few hundred rows at most
+            case["top"] = rng.choice([0, 1, 5, 20, 32]) if rows <= 512 else 0
+        else:
+            case["still"] = rng.choice([0.0, 0.0, 0.25])
+        return case
+    if kind == "loss":
+        G = rng.choice([1, 2, 4, 8, 16])
+        groups = _log(rng, 1, 128)
+        return {"kind": kind, "groups": groups, "G": G, "max_len": _log(rng, 1, 4096),
+                "mean": rng.choice([MEAN_SEQUENCE, MEAN_TOKEN, MEAN_FIXED]), "ref": rng.random() < 0.6, "entropy": rng.random() < 0.5}
+    vocab, dim = rng.choice([(1024, 128), (2064, 544), (2064, 640), (152064, 3584), (152064, 3584), (152064, 5120), (32003, 1000)])
+    tokens = _log(rng, 1, min(200000, 49152 * 3584 // dim))
+    case = {"kind": kind, "tokens": tokens, "vocab": vocab, "dim": dim, "pad": rng.choice([0.0, 0.25]),
+            "table": rng.choice(["fp32", "bf16"])}
+    if vocab * dim > 152064 * 3584:
+        case["table"] = "bf16"
+    case["out" if kind == "embedding" else "grad"] = rng.choice(["fp32", "bf16"])
+    return case
+
+
+# ---------------------------------------------------------------------------
+# inputs
+# ---------------------------------------------------------------------------
+def _gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed * 2 + 1)
+
+
+def _rows_of(case, key, n):
+    return int(n * case.get(key, 0.0))
+
+
+def _logits(case, g):
+    """Rows as a model gives them: a spread of a few units, some rows almost certain of one id, and the ids behind the
+    tokenizer's last one banned."""
+    n, V = case["rows"], case["vocab"]
+    t = TYPES[case["dtype"]]
+    z = torch.randn((n, V + case["extra"]), generator=g, device=DEV, dtype=t)
+    z *= 2.5
+    tokens = torch.randint(0, max(1, V - V // 256), (n,), generator=g, device=DEV, dtype=torch.int32)
+    sure = torch.rand(n, generator=g, device=DEV) < 0.5
+    rows = sure.nonzero().flatten()
+    z[rows, tokens[rows].long()] = 16.0
+    if V // 256:
+        z[:, V - V // 256:V] = -INF
+    pad = torch.randperm(n, generator=g, device=DEV)[:_rows_of(case, "pad", n)]
+    tokens[pad] = -1
+    return z, tokens
+
+
+def _ids(case, g):
+    """Token ids as text has them: few ids make up much of it (id v about as often as 1 / (v + 1))."""
+    n, V = case["tokens"], case["vocab"]
+    u = torch.rand(n, generator=g, device=DEV, dtype=torch.float64)
+    ids = (torch.exp(u * math.log(V + 1.0)) - 1.0).to(torch.int32).clamp_(0, V - 1)
+    ids[torch.randperm(n, generator=g, device=DEV)[:_rows_of(case, "pad", n)]] = -1
+    return ids
+
+
+def _empty(*shape, dtype=torch.float32):
+    return torch.empty(shape, device=DEV, dtype=dtype)
+
+
+def prepare(case, seed):
+    g = _gen(seed)
+    st = {"case": case}
+    kind = case["kind"]
+    if kind == "logprobs":
+        st["z"], st["tokens"] = _logits(case, g)
+        n, k = case["rows"], case["top"]
+        if own:
+            import paper_2608_11226_amd as R
+
+            st["out"] = [_empty(n), _empty(n), _empty(n)] + ([_empty(n, k, dtype=torch.int32), _empty(n, k)] if k else [])
+            st["bytes"] = R.rollout_token_logprobs_workspace(n, case["vocab"], k)
+            st["ws"] = _empty(max(1, st["bytes"]), dtype=torch.uint8)
+    elif kind == "logprobs_backward":
+        st["z"], st["tokens"] = _logits(case, g)
+        n = case["rows"]
+        lse, H = _statistics(st["z"], case)
+        st["lse"], st["H"] = lse.float(), H.float()
+        # advantages over lengths; a little weight on the entropy
+        st["g"] = torch.randn(n, generator=g, device=DEV) / n
+        st["h"] = torch.full((n,), -0.001 / n, device=DEV)
+        still = torch.randperm(n, generator=g, device=DEV)[:_rows_of(case, "still", n)]
+        st["g"][still] = 0.0
+        st["h"][still] = 0.0
+        if own:
+            st["out"] = [_empty(n, case["vocab"], dtype=TYPES[case["dtype"]])]
+    elif kind == "loss":
+        S, N = case["groups"] * case["G"], case["max_len"]
+        old = -torch.empty((S, N), device=DEV).exponential_(1.0, generator=g)
+        st["old"] = old
+        st["lp"] = old + 0.2 * torch.randn((S, N), generator=g, device=DEV)
+        st["ref"] = old + 0.2 * torch.randn((S, N), generator=g, device=DEV) if case["ref"] else None
+        st["H"] = 2.0 * torch.rand((S, N), generator=g, device=DEV) if case["entropy"] else None
+        st["adv"] = torch.randn(S, generator=g, device=DEV)
+        # lengths evenly spread from 0 to max_len, in any order: their sum does not depend on the seed
+        st["len"] = _lengths(case).to(DEV)[torch.randperm(S, generator=g, device=DEV)]
+        if own:
+            import paper_2608_11226_amd as R
+
+            st["out"] = [_empty(1), _empty(5), _empty(S, N)] + ([_empty(S, N)] if case["entropy"] else [])
+            st["bytes"] = R.grpo_policy_loss_workspace(S, N)
+            st["ws"] = _empty(max(1, st["bytes"]), dtype=torch.uint8)
+    elif kind == "embedding":
+        st["E"] = torch.randn((case["vocab"], case["dim"]), generator=g, device=DEV, dtype=TYPES[case["table"]])
+        st["E"] *= 0.02
+        st["ids"] = _ids(case, g)
+        if own:
+            st["out"] = [_empty(case["tokens"], case["dim"], dtype=TYPES[case["out"]])]
+    else:
+        st["g"] = torch.randn((case["tokens"], case["dim"]), generator=g, device=DEV, dtype=TYPES[case["grad"]])
+        st["g"] *= 0.01
+        st["ids"] = _ids(case, g)
+        if own:
+            import paper_2608_11226_amd as R
+
+            st["out"] = [_empty(case["vocab"], case["dim"], dtype=TYPES[case["table"]])]
+            st["bytes"] = R.rollout_embedding_backward_workspace(case["tokens"], case["vocab"], case["dim"])
+            st["ws"] = _empty(max(1, st["bytes"]), dtype=torch.uint8)
+    return st
+
+
+def _lengths(case):
+    S, N = case["groups"] * case["G"], case["max_len"]
+    if S == 1:
+        return torch.tensor([N], dtype=torch.int32)
+    return (torch.arange(S, dtype=torch.int64) * N // (S - 1)).to(torch.int32)
+
+
+LOSS = {"clip_low": 0.2, "clip_high": 0.28, "kl": 0.04, "ent": 0.001}
+SCALE = 1.25
+
+
+# ---------------------------------------------------------------------------
+# one pass
+# ---------------------------------------------------------------------------
+def run(st):
+    kind = st["case"]["kind"]
+    return _own(kind, st) if own else PLAIN[kind](st)
+
+
+def _own(kind, st):
+    import paper_2608_11226_amd as R
+
+    case, out = st["case"], st["out"]
+    code = {"fp32": R.DTYPE_FP32, "bf16": R.DTYPE_BF16}
+    stream = torch.cuda.current_stream().cuda_stream
+    if kind == "logprobs":
+        k = case["top"]
+        R.rollout_token_logprobs(st["z"], code[case["dtype"]], case["vocab"] + case["extra"], case["rows"], case["vocab"],
+                                 case["temperature"], st["tokens"], k, out[0], out[1], out[2], out[3] if k else None,
+                                 out[4] if k else None, st["ws"], st["bytes"], stream)
+    elif kind == "logprobs_backward":
+        R.rollout_token_logprobs_backward(st["z"], code[case["dtype"]], case["vocab"] + case["extra"], case["rows"],
+                                          case["vocab"], case["temperature"], st["tokens"], st["lse"], st["H"], st["g"],
+                                          st["h"], out[0], case["vocab"], stream)
+    elif kind == "loss":
+        S, N = case["groups"] * case["G"], case["max_len"]
+        R.grpo_policy_loss(st["lp"], st["old"], st["ref"], st["H"], st["adv"], st["len"], S, N, LOSS["clip_low"],
+                           LOSS["clip_high"], LOSS["kl"] if case["ref"] else 0.0, LOSS["ent"] if case["entropy"] else 0.0,
+                           case["mean"], out[0], out[1], out[2], out[3] if case["entropy"] else None, st["ws"],
+                           st["bytes"], stream)
+    elif kind == "embedding":
+        R.rollout_embedding(st["E"], code[case["table"]], case["vocab"], case["dim"], st["ids"], case["tokens"], SCALE,
+                            out[0], code[case["out"]], stream)
+    else:
+        R.rollout_embedding_backward(st["g"], code[case["grad"]], st["ids"], case["tokens"], case["vocab"], case["dim"],
+                                     SCALE, 0, out[0], code[case["table"]], st["ws"], st["bytes"], stream)
+    return out
+
+
+def _plain_logprobs(st):
+    case = st["case"]
+    V, k = case["vocab"], case["top"]
+    z = st["z"][:, :V].float()
+    y = z / case["temperature"]
+    m = y.amax(1, keepdim=True)
+    d = y - m
+    e = torch.exp(d)
+    s = e.sum(1, keepdim=True)
+    H = torch.log(s) - torch.where(e > 0, e * d, 0.0).sum(1, keepdim=True) / s
+    lse = m + torch.log(s)
+    pad = st["tokens"] < 0
+    t = st["tokens"].clamp(min=0).long()
+    logp = d.gather(1, t[:, None]) - torch.log(s)
+    out = [logp[:, 0].masked_fill(pad, 0.0), H[:, 0].masked_fill(pad, 0.0), lse[:, 0].masked_fill(pad, 0.0)]
+    if k:
+        # by value, equal ones by id
+        ids = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :k]
+        top = d.gather(1, ids) - torch.log(s)
+        out += [ids.to(torch.int32).masked_fill(pad[:, None], -1), top.masked_fill(pad[:, None], 0.0)]
+    return out
+
+
+def _plain_logprobs_backward(st):
+    case = st["case"]
+    V, T = case["vocab"], case["temperature"]
+    dead = (st["tokens"] < 0) | ((st["g"] == 0) & (st["h"] == 0))
+    lp = st["z"][:, :V].float() / T - st["lse"][:, None]
+    p = torch.exp(lp)
+    dz = -p * (st["g"][:, None] + st["h"][:, None] * (torch.where(p > 0, lp, 0.0) + st["H"][:, None]))
+    t = st["tokens"].clamp(min=0).long()[:, None]
+    dz.scatter_add_(1, t, st["g"][:, None])
+    return [(dz / T).masked_fill(dead[:, None], 0.0).to(st["z"].dtype)]
+
+
+def _plain_loss(st):
+    case = st["case"]
+    S, N = st["lp"].shape
+    A = st["adv"][:, None]
+    live = torch.arange(N, device=DEV)[None, :] < st["len"][:, None]
+    count = st["len"].sum().float()
+    if case["mean"] == MEAN_SEQUENCE:
+        w = 1.0 / (S * st["len"].clamp(min=1).float())[:, None]
+    elif case["mean"] == MEAN_TOKEN:
+        w = 1.0 / count.clamp(min=1.0)
+    else:
+        w = torch.full((1, 1), 1.0 / (S * N), device=DEV)
+    # which side of the clipping border a token is on is decided in 64 bits, and so are the sums
+    d = st["lp"].double() - st["old"].double()
+    high = (A > 0) & (d > math.log1p(LOSS["clip_high"])) & live
+    low = (A < 0) & (d < math.log1p(-LOSS["clip_low"])) & live
+    r = torch.exp(d.float())
+    surr = torch.where(high, (1.0 + LOSS["clip_high"]) * A, torch.where(low, (1.0 - LOSS["clip_low"]) * A, r * A))
+    tok = -surr
+    grad = torch.where(high | low, 0.0, -A * r)
+    kl = torch.zeros_like(r)
+    if case["ref"]:
+        x = st["ref"] - st["lp"]
+        kl = torch.expm1(x) - x
+        tok = tok + LOSS["kl"] * kl
+        grad = grad - LOSS["kl"] * torch.expm1(x)
+    H = torch.zeros_like(r)
+    if case["entropy"]:
+        H = st["H"]
+        tok = tok - LOSS["ent"] * H
+    loss = (torch.where(live, tok, 0.0) * w).double().sum()
+    stats = [(torch.where(live, q, 0.0)).double().sum() / count.clamp(min=1.0) for q in (r, kl, low.float(), high.float(), H)]
+    out = [loss.float()[None], torch.stack(stats).float(), torch.where(live, grad * w, 0.0)]
+    if case["entropy"]:
+        out.append(torch.where(live, -LOSS["ent"] * w, 0.0))
+    return out
+
+
+def _plain_embedding(st):
+    pad = st["ids"] < 0
+    rows = st["E"][st["ids"].clamp(min=0).long()].float() * SCALE
+    return [rows.masked_fill(pad[:, None], 0.0).to(TYPES[st["case"]["out"]])]
+
+
+def _plain_embedding_backward(st):
+    case = st["case"]
+    kept = (st["ids"] >= 0).nonzero().flatten()
+    total = torch.zeros((case["vocab"], case["dim"]), device=DEV)
+    total.index_add_(0, st["ids"][kept].long(), st["g"][kept].float())
+    return [(total * SCALE).to(TYPES[case["table"]])]
+
+
+PLAIN = {"logprobs": _plain_logprobs, "logprobs_backward": _plain_logprobs_backward, "loss": _plain_loss,
+         "embedding": _plain_embedding, "embedding_backward": _plain_embedding_backward}
+
+
+# ---------------------------------------------------------------------------
+# work
+# ---------------------------------------------------------------------------
+def work(case):
+    kind = case["kind"]
+    if kind in ("logprobs", "logprobs_backward"):
+        n, V = case["rows"], case["vocab"]
+        es = 2 if case["dtype"] == "bf16" else 4
+        live = n - _rows_of(case, "pad", n)
+        if kind == "logprobs":
+            return {"bytes": live * V * es + n * (16 + 8 * case["top"]), "flops": live * V * 6}
+        # a padded row or one without a gradient is only written
+        read = live - int(_rows_of(case, "still", n) * live / n)
+        return {"bytes": (read + n) * V * es + n * 20, "flops": read * V * 8}
+    if kind == "loss":
+        S, N = case["groups"] * case["G"], case["max_len"]
+        live = int(_lengths(case).sum())
+        arrays = 2 + int(case["ref"]) + int(case["entropy"])
+        return {"bytes": live * 4 * arrays + S * N * 4 * (1 + int(case["entropy"])) + S * 8, "flops": live * 30}
+    n, V, dim = case["tokens"], case["vocab"], case["dim"]
+    es = {k: 2 if case.get(k) == "bf16" else 4 for k in ("table", "out", "grad")}
+    live = n - _rows_of(case, "pad", n)
+    if kind == "embedding":
+        v = torch.arange(V, dtype=torch.float64)
+        p = torch.log((v + 2.0) / (v + 1.0)) / math.log(V + 1.0)
+        distinct = float((1.0 - (1.0 - p) ** live).sum())
+        return {"bytes": int(distinct * dim * es["table"]) + n * dim * es["out"] + n * 4, "flops": n * dim}
+    return {"bytes": live * dim * es["grad"] + V * dim * es["table"] + n * 4, "flops": live * dim}
+
+
+# ---------------------------------------------------------------------------
+# the definition in 64 bits
+# ---------------------------------------------------------------------------
+def _chunks(n, width):
+    step = max(1, (1 << 26) // width)
+    return [(a, min(n, a + step)) for a in range(0, n, step)]
+
+
+def _statistics(z, case):
+    """log sum exp and entropy of every row, 64 bits."""
+    n, V = case["rows"], case["vocab"]
+    lse, H = _empty(n, dtype=torch.float64), _empty(n, dtype=torch.float64)
+    for a, b in _chunks(n, V):
+        y = z[a:b, :V].double() / case["temperature"]
+        lse[a:b] = torch.logsumexp(y, 1)
+        q = y - lse[a:b, None]
+        p = torch.exp(q)
+        H[a:b] = -(p * q.clamp(min=-1e4)).sum(1)
+    return lse, H
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "logprobs":
+        n, V, k = case["rows"], case["vocab"], case["top"]
+        lse, H = _statistics(st["z"], case)
+        logp = _empty(n, dtype=torch.float64)
+        ids, top = _empty(n, k, dtype=torch.int32), _empty(n, k, dtype=torch.float64)
+        for i, t in enumerate(st["tokens"].tolist() if n <= 512 else []):
+            if t < 0:
+                logp[i], H[i], lse[i], ids[i], top[i] = 0.0, 0.0, 0.0, -1, 0.0
+                continue
+            row = st["z"][i, :V].double()
+            logp[i] = row[t] / case["temperature"] - lse[i]
+            # the k largest by repeated search, the first id among equal ones
+            for j in range(k):
+                v = row.max()
+                w = (row == v).nonzero()[0, 0]
+                ids[i, j] = w
+                top[i, j] = v / case["temperature"] - lse[i]
+                row[w] = -INF
+        if n > 512:
+            t = st["tokens"].long()
+            for a, b in _chunks(n, V):
+                at = torch.arange(a, b, device=DEV)
+                logp[a:b] = st["z"][at, t[a:b].clamp(min=0)].double() / case["temperature"] - lse[a:b]
+            for q in (logp, H, lse):
+                q[t < 0] = 0.0
+        return [logp, H, lse] + ([ids, top] if k else [])
+    if kind == "logprobs_backward":
+        n, V, T = case["rows"], case["vocab"], case["temperature"]
+        g, h, lse, H = (st[q].double() for q in ("g", "h", "lse", "H"))
+        t = st["tokens"].long()
+        out = _empty(n, V, dtype=torch.float64)
+        for a, b in _chunks(n, V):
+            q = st["z"][a:b, :V].double() / T - lse[a:b, None]
+            p = torch.exp(q)
+            onehot = torch.zeros_like(p)
+            live = (t[a:b] >= 0) & ~((g[a:b] == 0) & (h[a:b] == 0))
+            onehot[live.nonzero().flatten(), t[a:b][live]] = 1.0
+            v = (g[a:b, None] * (onehot - p) - h[a:b, None] * p * (q.clamp(min=-1e4) + H[a:b, None])) / T
+            v[~live] = 0.0
+            out[a:b] = v
+        return [out]
+    if kind == "loss":
+        S, N = st["lp"].shape
+        lp, old, adv = st["lp"].double(), st["old"].double(), st["adv"].double()[:, None]
+        L = st["len"].double()[:, None]
+        count = max(1.0, float(L.sum()))
+        mask = (torch.arange(N, device=DEV)[None] < L).double()
+        w = mask * {MEAN_SEQUENCE: 1.0 / (S * L.clamp(min=1.0)), MEAN_TOKEN: 1.0 / count, MEAN_FIXED: 1.0 / (S * N)}[case["mean"]]
+        r = torch.exp(lp - old)
+        kept = r.clamp(1.0 - LOSS["clip_low"], 1.0 + LOSS["clip_high"])
+        surr = torch.minimum(r * adv, kept * adv)
+        high = ((adv > 0) & (r > 1.0 + LOSS["clip_high"])).double() * mask
+        low = ((adv < 0) & (r < 1.0 - LOSS["clip_low"])).double() * mask
+        x = st["ref"].double() - lp if case["ref"] else torch.zeros_like(r)
+        kl = torch.expm1(x) - x
+        H = st["H"].double() if case["entropy"] else torch.zeros_like(r)
+        c = LOSS["ent"] if case["entropy"] else 0.0
+        b = LOSS["kl"] if case["ref"] else 0.0
+        loss = (w * (-surr + b * kl - c * H)).sum()[None]
+        stats = torch.stack([(q * mask).sum() / count for q in (r, kl, low, high, H)])
+        out = [loss, stats, w * (-adv * r * (1.0 - high - low) - b * torch.expm1(x))]
+        return out + ([-c * w] if case["entropy"] else [])
+    if kind == "embedding":
+        n, dim = case["tokens"], case["dim"]
+        out = torch.zeros((n, dim), device=DEV, dtype=torch.float64)
+        for a, b in _chunks(n, dim):
+            ids = st["ids"][a:b].long()
+            at = (ids >= 0).nonzero().flatten()
+            out[a + at] = SCALE * st["E"][ids[at]].double()
+        return [out]
+    V, dim = case["vocab"], case["dim"]
+    out = torch.zeros((V, dim), device=DEV, dtype=torch.float64)
+    for a, b in _chunks(case["tokens"], dim):
+        ids = st["ids"][a:b].long()
+        at = (ids >= 0).nonzero().flatten()
+        out.index_add_(0, ids[at], SCALE * st["g"][a:b][at].double())
+    return [out]
