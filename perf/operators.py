@@ -137,14 +137,14 @@ def prepare(case, seed):
         if own:
             import paper_2608_11226_amd as R
 
-            st["out"] = [_empty(n), _empty(n), _empty(n)] + ([_empty(n, k, dtype=torch.int32), _empty(n, k)] if k else [])
+            st["out"] = [_empty(n), _empty(n), _empty(n, 2)] + ([_empty(n, k, dtype=torch.int32), _empty(n, k)] if k else [])
             st["bytes"] = R.rollout_token_logprobs_workspace(n, case["vocab"], k)
             st["ws"] = _empty(max(1, st["bytes"]), dtype=torch.uint8)
     elif kind == "logprobs_backward":
         st["z"], st["tokens"] = _logits(case, g)
         n = case["rows"]
-        lse, H = _statistics(st["z"], case)
-        st["lse"], st["H"] = lse.float(), H.float()
+        stats, H = _statistics(st["z"], case)
+        st["stats"], st["H"] = stats.float(), H.float()
         # advantages over lengths; a little weight on the entropy
         st["g"] = torch.randn(n, generator=g, device=DEV) / n
         st["h"] = torch.full((n,), -0.001 / n, device=DEV)
@@ -220,7 +220,7 @@ def _own(kind, st):
                                  out[4] if k else None, st["ws"], st["bytes"], stream)
     elif kind == "logprobs_backward":
         R.rollout_token_logprobs_backward(st["z"], code[case["dtype"]], case["vocab"] + case["extra"], case["rows"],
-                                          case["vocab"], case["temperature"], st["tokens"], st["lse"], st["H"], st["g"],
+                                          case["vocab"], case["temperature"], st["tokens"], st["stats"], st["H"], st["g"],
                                           st["h"], out[0], case["vocab"], stream)
     elif kind == "loss":
         S, N = case["groups"] * case["G"], case["max_len"]
@@ -241,22 +241,21 @@ def _plain_logprobs(st):
     case = st["case"]
     V, k = case["vocab"], case["top"]
     z = st["z"][:, :V].float()
-    y = z / case["temperature"]
-    m = y.amax(1, keepdim=True)
-    d = y - m
+    m = z.amax(1, keepdim=True)
+    d = (z - m) / case["temperature"]
     e = torch.exp(d)
     s = e.sum(1, keepdim=True)
     H = torch.log(s) - torch.where(e > 0, e * d, 0.0).sum(1, keepdim=True) / s
-    lse = m + torch.log(s)
-    pad = st["tokens"] < 0
+    pad = (st["tokens"] < 0)[:, None]
     t = st["tokens"].clamp(min=0).long()
     logp = d.gather(1, t[:, None]) - torch.log(s)
-    out = [logp[:, 0].masked_fill(pad, 0.0), H[:, 0].masked_fill(pad, 0.0), lse[:, 0].masked_fill(pad, 0.0)]
+    out = [logp.masked_fill(pad, 0.0)[:, 0], H.masked_fill(pad, 0.0)[:, 0],
+           torch.cat([m, torch.log(s)], 1).masked_fill(pad, 0.0)]
     if k:
         # by value, equal ones by id
         ids = torch.sort(z, dim=1, descending=True, stable=True)[1][:, :k]
         top = d.gather(1, ids) - torch.log(s)
-        out += [ids.to(torch.int32).masked_fill(pad[:, None], -1), top.masked_fill(pad[:, None], 0.0)]
+        out += [ids.to(torch.int32).masked_fill(pad, -1), top.masked_fill(pad, 0.0)]
     return out
 
 
@@ -264,7 +263,7 @@ def _plain_logprobs_backward(st):
     case = st["case"]
     V, T = case["vocab"], case["temperature"]
     dead = (st["tokens"] < 0) | ((st["g"] == 0) & (st["h"] == 0))
-    lp = st["z"][:, :V].float() / T - st["lse"][:, None]
+    lp = (st["z"][:, :V].float() - st["stats"][:, :1]) / T - st["stats"][:, 1:]
     p = torch.exp(lp)
     dz = -p * (st["g"][:, None] + st["h"][:, None] * (torch.where(p > 0, lp, 0.0) + st["H"][:, None]))
     t = st["tokens"].clamp(min=0).long()[:, None]
@@ -338,10 +337,10 @@ def work(case):
         es = 2 if case["dtype"] == "bf16" else 4
         live = n - _rows_of(case, "pad", n)
         if kind == "logprobs":
-            return {"bytes": live * V * es + n * (16 + 8 * case["top"]), "flops": live * V * 6}
+            return {"bytes": live * V * es + n * (20 + 8 * case["top"]), "flops": live * V * 6}
         # a padded row or one without a gradient is only written
         read = live - int(_rows_of(case, "still", n) * live / n)
-        return {"bytes": (read + n) * V * es + n * 20, "flops": read * V * 8}
+        return {"bytes": (read + n) * V * es + n * 24, "flops": read * V * 8}
     if kind == "loss":
         S, N = case["groups"] * case["G"], case["max_len"]
         live = int(_lengths(case).sum())
@@ -367,16 +366,17 @@ def _chunks(n, width):
 
 
 def _statistics(z, case):
-    """log sum exp and entropy of every row, 64 bits."""
+    """Largest logit, log sum exp of the scaled distances to it, and entropy of every row, 64 bits."""
     n, V = case["rows"], case["vocab"]
-    lse, H = _empty(n, dtype=torch.float64), _empty(n, dtype=torch.float64)
+    stats, H = _empty(n, 2, dtype=torch.float64), _empty(n, dtype=torch.float64)
     for a, b in _chunks(n, V):
-        y = z[a:b, :V].double() / case["temperature"]
-        lse[a:b] = torch.logsumexp(y, 1)
-        q = y - lse[a:b, None]
-        p = torch.exp(q)
-        H[a:b] = -(p * q.clamp(min=-1e4)).sum(1)
-    return lse, H
+        row = z[a:b, :V].double()
+        stats[a:b, 0] = row.amax(1)
+        row = (row - stats[a:b, :1]) / case["temperature"]
+        stats[a:b, 1] = torch.logsumexp(row, 1)
+        row -= stats[a:b, 1:]
+        H[a:b] = -(torch.exp(row) * row.clamp(min=-1e4)).sum(1)
+    return stats, H
 
 
 def exact(case, seed):
@@ -384,37 +384,38 @@ def exact(case, seed):
     kind = case["kind"]
     if kind == "logprobs":
         n, V, k = case["rows"], case["vocab"], case["top"]
-        lse, H = _statistics(st["z"], case)
+        T = case["temperature"]
+        stats, H = _statistics(st["z"], case)
         logp = _empty(n, dtype=torch.float64)
         ids, top = _empty(n, k, dtype=torch.int32), _empty(n, k, dtype=torch.float64)
         for i, t in enumerate(st["tokens"].tolist() if n <= 512 else []):
             if t < 0:
-                logp[i], H[i], lse[i], ids[i], top[i] = 0.0, 0.0, 0.0, -1, 0.0
+                logp[i], H[i], stats[i], ids[i], top[i] = 0.0, 0.0, 0.0, -1, 0.0
                 continue
             row = st["z"][i, :V].double()
-            logp[i] = row[t] / case["temperature"] - lse[i]
+            logp[i] = (row[t] - stats[i, 0]) / T - stats[i, 1]
             # the k largest by repeated search, the first id among equal ones
             for j in range(k):
                 v = row.max()
                 w = (row == v).nonzero()[0, 0]
                 ids[i, j] = w
-                top[i, j] = v / case["temperature"] - lse[i]
+                top[i, j] = (v - stats[i, 0]) / T - stats[i, 1]
                 row[w] = -INF
         if n > 512:
             t = st["tokens"].long()
             for a, b in _chunks(n, V):
                 at = torch.arange(a, b, device=DEV)
-                logp[a:b] = st["z"][at, t[a:b].clamp(min=0)].double() / case["temperature"] - lse[a:b]
-            for q in (logp, H, lse):
+                logp[a:b] = (st["z"][at, t[a:b].clamp(min=0)].double() - stats[a:b, 0]) / T - stats[a:b, 1]
+            for q in (logp, H, stats):
                 q[t < 0] = 0.0
-        return [logp, H, lse] + ([ids, top] if k else [])
+        return [logp, H, stats] + ([ids, top] if k else [])
     if kind == "logprobs_backward":
         n, V, T = case["rows"], case["vocab"], case["temperature"]
-        g, h, lse, H = (st[q].double() for q in ("g", "h", "lse", "H"))
+        g, h, stats, H = (st[q].double() for q in ("g", "h", "stats", "H"))
         t = st["tokens"].long()
         out = _empty(n, V, dtype=torch.float64)
         for a, b in _chunks(n, V):
-            q = st["z"][a:b, :V].double() / T - lse[a:b, None]
+            q = (st["z"][a:b, :V].double() - stats[a:b, :1]) / T - stats[a:b, 1:]
             p = torch.exp(q)
             onehot = torch.zeros_like(p)
             live = (t[a:b] >= 0) & ~((g[a:b] == 0) & (h[a:b] == 0))
