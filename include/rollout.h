@@ -282,6 +282,76 @@ rollout_status rollout_sample_noalloc(const float* d_logits, int32_t n_seqs, int
                                       void* hip_stream);
 
 /* ------------------------------------------------------------------------ */
+/* The update side of a GRPO step                                            */
+/* ------------------------------------------------------------------------ */
+/*
+ * After the rollout a step scores its tokens, forms the clipped loss over the
+ * groups' advantages and carries its gradient back (section 3's update phase,
+ * of which the paper gives no arithmetic: the definitions are below).  These
+ * entry points need no context.  hip_stream is a hipStream_t of the current
+ * device (NULL = its default stream; a stream of another device: EINVAL), and
+ * every buffer is the caller's, on that device.  A workspace is device memory
+ * aligned to 16 bytes, at least as large as the call's _workspace query says
+ * for the same sizes; nothing is kept in it from one call to the next, and
+ * calls that may run at the same time (two streams, two captured graphs) need
+ * one each.  Nothing is allocated or waited for, so every call can be captured
+ * into a HIP graph.  Messages: rollout_last_error(NULL).
+ *
+ * dtype of a matrix: ROLLOUT_DTYPE_FP32 or ROLLOUT_DTYPE_BF16.  Arithmetic is
+ * fp32 or wider, outputs are rounded once (to nearest, ties to even).  Results
+ * do not depend on scheduling: no floating-point atomics.
+ * A token id < 0 is padding (rollout_generate_eos fills with -1).
+ */
+
+/*
+ * Log probabilities of given tokens under softmax(z / temperature), with the
+ * rows' entropies and most likely alternatives.  d_logits: n_rows rows of vocab
+ * values of dtype, row_stride elements apart (>= vocab; rows may start at any
+ * element); d_tokens int32 [n_rows].  Outputs, each fp32 and NULL if not
+ * wanted:
+ *   d_logp [n_rows]      log p of the row's token;
+ *   d_entropy [n_rows]   -sum p log p;
+ *   d_stats [n_rows, 2]  max z, and log sum exp((z - max z) / temperature): what the
+ *                        gradient needs.  (Their sum, the log-sum-exp of the row, would
+ *                        lose the second where the logits stand far from zero.)
+ *   d_top_ids int32, d_top_logp [n_rows, n_top]  the n_top ids with the largest
+ *                        logits, equal ones by lowest id, and their log p; both needed
+ *                        when n_top > 0 (at most 32 and vocab), unused when it is 0.
+ * The distribution is the whole one: a draw's top-p does not enter.
+ * Padding rows are not read and get zeros (top ids -1).  A token >= vocab gets
+ * log p NaN.  Logits of -inf have probability 0; a row of nothing else has log p
+ * -inf, entropy 0, statistics -inf and the lowest ids as alternatives.  A row
+ * with NaN or +inf gets NaN everywhere and top ids -1.  d_tokens NULL: no row
+ * is padding, and d_logp must be NULL.
+ * Errors: EINVAL (sizes, types, alignment, NULL buffers, temperature not > 0, no
+ * output), EUNSUPPORTED (vocab above 2^30, or above 2^20 with n_top > 0), ENOMEM
+ * (workspace too small), EDEVICE.
+ */
+rollout_status rollout_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t* h_bytes);
+rollout_status rollout_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                                      int32_t vocab, float temperature, const int32_t* d_tokens, int32_t n_top,
+                                      float* d_logp, float* d_entropy, float* d_stats, int32_t* d_top_ids,
+                                      float* d_top_logp, void* d_workspace, uint64_t workspace_bytes,
+                                      void* hip_stream);
+
+/*
+ * Gradient of the above with respect to the logits.  With p = softmax(z / T), H
+ * its entropy, g = d_grad_logp and h = d_grad_entropy (fp32 [n_rows]; h NULL: 0):
+ *   dz_i = (g (1[i = token] - p_i) - h p_i (log p_i + H)) / T
+ * into d_grad_logits, n_rows rows of vocab values of dtype, grad_stride elements
+ * apart; it may be d_logits itself at the same stride (any other overlap:
+ * EINVAL).  d_stats and d_entropy (needed only with h) are the forward call's.
+ * What lies between the rows is left alone.  Rows that are padding, have g = h = 0
+ * or hold nothing but -inf get zeros and are not read; a token >= vocab makes
+ * its row NaN.  Errors: EINVAL, EUNSUPPORTED (vocab above 2^30), EDEVICE.
+ */
+rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                                               int32_t vocab, float temperature, const int32_t* d_tokens,
+                                               const float* d_stats, const float* d_entropy, const float* d_grad_logp,
+                                               const float* d_grad_entropy, void* d_grad_logits, int64_t grad_stride,
+                                               void* hip_stream);
+
+/* ------------------------------------------------------------------------ */
 /* Inspection and measurement                                                */
 /* ------------------------------------------------------------------------ */
 

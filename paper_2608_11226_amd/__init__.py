@@ -27,6 +27,7 @@ EXPORTED = (
     "grpo_advantages", "rollout_generate", "rollout_sync", "rollout_destroy", "rollout_last_error",
     "rollout_export_weight", "rollout_profile_decode_step", "rollout_generate_eos", "rollout_length_rewards",
     "rollout_sample_noalloc", "rollout_profile_projections",
+    "rollout_token_logprobs_workspace", "rollout_token_logprobs", "rollout_token_logprobs_backward",
 )
 NOALLOC_SCRATCH_BYTES = 64 << 20  # ROLLOUT_SAMPLE_NOALLOC_SCRATCH_BYTES
 # include/occupancy.h: power metrics and threshold policy of the occupancy controller (host code)
@@ -94,6 +95,7 @@ def _load():
 
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, f32, u64, f64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_uint64, ctypes.c_double
+    i64, pu64 = ctypes.c_int64, ctypes.POINTER(u64)
     sig = {
         "rollout_plan": ([ctypes.POINTER(ModelConfig), i32, ctypes.POINTER(Plan)], i32),
         "rollout_init": ([ctypes.POINTER(ModelConfig), vp, u64, vp, ctypes.POINTER(vp)], i32),
@@ -112,6 +114,9 @@ def _load():
         "rollout_length_rewards": ([vp, i32, i32, vp, vp, vp], i32),
         "rollout_sample_noalloc": ([vp, i32, i32, f32, f32, vp, vp, vp], i32),
         "rollout_profile_projections": ([vp, i32, vp, ctypes.POINTER(ProjectionProfile)], i32),
+        "rollout_token_logprobs_workspace": ([i32, i32, i32, pu64], i32),
+        "rollout_token_logprobs": ([vp, i32, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp, u64, vp], i32),
+        "rollout_token_logprobs_backward": ([vp, i32, i64, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp], i32),
         "occ_rolling_mean": ([vp, ctypes.c_int64, f64, f64, vp], i32),
         "occ_violation": ([vp, ctypes.c_int64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f64)], i32),
         "occ_normalize_budget": ([f64, f64, f64], f64),
@@ -206,6 +211,69 @@ def rollout_generate_eos(ctx, prompts, n_prompts: int, prompt_len: int, group_si
 
 def rollout_length_rewards(lengths, n: int, target: int, rewards, total_tokens=None, stream=None):
     _check(lib.rollout_length_rewards(_ptr(lengths), n, target, _ptr(rewards), _ptr(total_tokens), _ptr(stream)))
+
+
+# The update side of a GRPO step: no context, caller-owned workspaces.  A tensor passed for a buffer has to be on the
+# current device, of the buffer's type, contiguous and large enough (a strided matrix of logits: large enough for its
+# last row); an integer address is passed on as it is.
+_DTYPES = {DTYPE_FP32: "torch.float32", DTYPE_BF16: "torch.bfloat16"}
+
+
+def _buf(name: str, x, dtype: str, n: int, strided: bool = False) -> int | None:
+    """Device pointer of a buffer of n elements of dtype."""
+    if x is None or not hasattr(x, "data_ptr"):
+        return _ptr(x)
+    import torch
+
+    if dtype != "any" and str(x.dtype) != dtype:
+        raise RolloutError(EINVAL, f"{name} must be {dtype}, not {x.dtype}")
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
+    if strided:
+        if x.stride(-1) != 1 and x.shape[-1] > 1:
+            raise RolloutError(EINVAL, f"the rows of {name} are not contiguous")
+        have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+    elif not x.is_contiguous():
+        raise RolloutError(EINVAL, f"{name} is not contiguous")
+    else:
+        have = x.numel() * (x.element_size() if dtype == "any" else 1)
+    if have < n:
+        raise RolloutError(EINVAL, f"{name} holds {have} elements, the call needs {n}")
+    return x.data_ptr()
+
+
+def _rows(name: str, x, dtype: int, n_rows: int, stride: int, vocab: int) -> int | None:
+    return _buf(name, x, _DTYPES.get(dtype, f"of dtype 0 or 1 (got {dtype})"), (n_rows - 1) * stride + vocab, strided=True)
+
+
+def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) -> int:
+    out = ctypes.c_uint64(0)
+    _check(lib.rollout_token_logprobs_workspace(n_rows, vocab, n_top, ctypes.byref(out)))
+    return out.value
+
+
+def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float, tokens,
+                           n_top: int = 0, logp=None, entropy=None, stats=None, top_ids=None, top_logp=None,
+                           workspace=None, workspace_bytes: int = 0, stream=None):
+    f = "torch.float32"
+    _check(lib.rollout_token_logprobs(
+        _rows("logits", logits, dtype, n_rows, row_stride, vocab), dtype, row_stride, n_rows, vocab, temperature,
+        _buf("tokens", tokens, "torch.int32", n_rows), n_top, _buf("logp", logp, f, n_rows),
+        _buf("entropy", entropy, f, n_rows), _buf("stats", stats, f, 2 * n_rows),
+        _buf("top_ids", top_ids, "torch.int32", n_rows * n_top), _buf("top_logp", top_logp, f, n_rows * n_top),
+        _buf("workspace", workspace, "any", workspace_bytes), workspace_bytes, _ptr(stream)))
+
+
+def rollout_token_logprobs_backward(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float,
+                                    tokens, stats, entropy, grad_logp, grad_entropy, grad_logits, grad_stride: int,
+                                    stream=None):
+    f = "torch.float32"
+    _check(lib.rollout_token_logprobs_backward(
+        _rows("logits", logits, dtype, n_rows, row_stride, vocab), dtype, row_stride, n_rows, vocab, temperature,
+        _buf("tokens", tokens, "torch.int32", n_rows), _buf("stats", stats, f, 2 * n_rows),
+        _buf("entropy", entropy, f, n_rows), _buf("grad_logp", grad_logp, f, n_rows),
+        _buf("grad_entropy", grad_entropy, f, n_rows),
+        _rows("grad_logits", grad_logits, dtype, n_rows, grad_stride, vocab), grad_stride, _ptr(stream)))
 
 
 def rollout_sync(ctx):

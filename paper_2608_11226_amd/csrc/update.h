@@ -1,0 +1,118 @@
+// The operators of a GRPO step's update side: token log probabilities and their gradient (logprobs.hip), the clipped
+// group loss (grpo.hip), embedding lookup and its gradient (embedding.hip).  Launchers called by the C entry points in
+// update.hip, and device helpers that these kernels share.
+#pragma once
+
+#include "internal.h"
+
+namespace rollout {
+
+constexpr int kMaxTop = 32;            // alternatives of a row
+constexpr int kMaxTopVocab = 1 << 20;  // widest row that alternatives are taken from
+
+struct LogprobArgs {
+  const void* z;
+  int64_t stride;
+  int rows, vocab;
+  float temperature;
+  const int32_t* tokens;
+  int top;
+  float* logp;
+  float* entropy;
+  float* stats;
+  int32_t* top_ids;
+  float* top_logp;
+};
+size_t logprobs_workspace(int rows, int vocab, int top);
+hipError_t launch_logprobs(hipStream_t s, int dtype, const LogprobArgs& a, void* ws);
+
+struct LogprobGradArgs {
+  const void* z;
+  int64_t stride;
+  int rows, vocab;
+  float temperature;
+  const int32_t* tokens;
+  const float* stats;
+  const float* entropy;
+  const float* g;
+  const float* h;
+  void* dz;
+  int64_t dz_stride;
+};
+hipError_t launch_logprobs_backward(hipStream_t s, int dtype, const LogprobGradArgs& a);
+
+}  // namespace rollout
+
+#ifdef __HIPCC__
+namespace rollout {
+
+// 16 bytes of a row that starts at any element: rows of an odd width begin anywhere, and the hardware takes such
+// loads and stores whole.
+template <typename T>
+struct Chunk16;
+template <>
+struct Chunk16<float> {
+  static constexpr int N = 4;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(4), may_alias));
+};
+template <>
+struct Chunk16<uint16_t> {
+  static constexpr int N = 8;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(2), may_alias));
+};
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T>
+__device__ __forceinline__ u32x4 load16(const T* p) {
+  return *reinterpret_cast<const typename Chunk16<T>::Raw*>(p);
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, u32x4 v) {
+  *reinterpret_cast<typename Chunk16<T>::Raw*>(p) = v;
+}
+
+__device__ __forceinline__ void unpack16(u32x4 r, float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void unpack16(u32x4 r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(r[i] << 16);
+    v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+  }
+}
+// round to nearest, ties to even; a NaN stays one
+__device__ __forceinline__ uint16_t round_bf16(float f) {
+  return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+__device__ __forceinline__ u32x4 pack16(const float (&v)[4]) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(v[i]);
+  return r;
+}
+__device__ __forceinline__ u32x4 pack16(const float (&v)[8]) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (uint32_t)round_bf16(v[2 * i]) | ((uint32_t)round_bf16(v[2 * i + 1]) << 16);
+  return r;
+}
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t* p, float v) { *p = round_bf16(v); }
+
+// Maximum of one unsigned value per lane, the same in every lane (lane moves without LDS; a lane with no source adds 0).
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+#define ROLLOUT_MAX_STEP(ctrl, rows) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false))
+  ROLLOUT_MAX_STEP(0x111, 0xf);  // row_shr:1, 2, 4, 8
+  ROLLOUT_MAX_STEP(0x112, 0xf);
+  ROLLOUT_MAX_STEP(0x114, 0xf);
+  ROLLOUT_MAX_STEP(0x118, 0xf);
+  ROLLOUT_MAX_STEP(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
+  ROLLOUT_MAX_STEP(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
+#undef ROLLOUT_MAX_STEP
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+}  // namespace rollout
+#endif

@@ -1,0 +1,140 @@
+// C entry points of the update side of a GRPO step: token log probabilities and their gradient, the clipped group
+// loss, embedding lookup and its gradient.  They need no context: buffers and workspaces are the caller's, and the
+// stream is an argument.
+#include "update.h"
+
+#include <algorithm>
+#include <cmath>
+#include <string>
+
+#include <rocprofiler-sdk-roctx/roctx.h>
+
+using namespace rollout;
+
+namespace {
+
+struct Range {
+  explicit Range(const char* name) { roctxRangePush(name); }
+  ~Range() { roctxRangePop(); }
+  Range(const Range&) = delete;
+  Range& operator=(const Range&) = delete;
+};
+
+rollout_status fail(rollout_status st, const std::string& msg) {
+  set_last_error(msg);
+  return st;
+}
+
+constexpr int32_t kMaxVocab = 1 << 30;
+
+bool is_float_type(int32_t dtype) { return dtype == ROLLOUT_DTYPE_FP32 || dtype == ROLLOUT_DTYPE_BF16; }
+bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+
+// [a, a + a_bytes) and [b, b + b_bytes) share a byte
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+  return x < y + b_bytes && y < x + a_bytes;
+}
+
+// the stream (NULL: the default one) belongs to the current device
+rollout_status check_stream(void* hip_stream) {
+  int dev = -1, sdev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return fail(ROLLOUT_EDEVICE, std::string("hipGetDevice: ") + hipGetErrorString(e));
+  if (!hip_stream) return ROLLOUT_OK;
+  e = hipStreamGetDevice((hipStream_t)hip_stream, &sdev);
+  if (e != hipSuccess) return fail(ROLLOUT_EDEVICE, std::string("hipStreamGetDevice: ") + hipGetErrorString(e));
+  if (sdev != dev) return fail(ROLLOUT_EINVAL, "the stream belongs to another device than the current one");
+  return ROLLOUT_OK;
+}
+
+rollout_status check_workspace(const void* ws, uint64_t bytes, size_t need) {
+  if (bytes < need)
+    return fail(ROLLOUT_ENOMEM, "workspace of " + std::to_string(bytes) + " bytes; the call needs " + std::to_string(need));
+  if (need && !ws) return fail(ROLLOUT_EINVAL, "the workspace is NULL");
+  if (need && !aligned_to(ws, 16)) return fail(ROLLOUT_EINVAL, "the workspace must be aligned to 16 bytes");
+  return ROLLOUT_OK;
+}
+
+rollout_status launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) return fail(ROLLOUT_EDEVICE, std::string(what) + ": " + hipGetErrorString(e));
+  return ROLLOUT_OK;
+}
+
+// what both directions of the log probabilities ask of a matrix of logits
+rollout_status check_rows(const void* z, int32_t dtype, int64_t stride, int32_t rows, int32_t vocab, float temperature) {
+  if (!is_float_type(dtype)) return fail(ROLLOUT_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
+  if (rows < 1 || vocab < 1) return fail(ROLLOUT_EINVAL, "n_rows and vocab must be >= 1");
+  if (vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab above 2^30");
+  if (stride < vocab) return fail(ROLLOUT_EINVAL, "row_stride must be at least vocab");
+  if (stride > INT64_MAX / 8 / rows) return fail(ROLLOUT_EINVAL, "row_stride too large");
+  if (!z) return fail(ROLLOUT_EINVAL, "logits must be non-NULL");
+  if (!aligned_to(z, elem_bytes(dtype))) return fail(ROLLOUT_EINVAL, "logits are not aligned to their type");
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite((float)(2.0 / (double)temperature)))
+    return fail(ROLLOUT_EINVAL, "temperature must be > 0, and its reciprocal finite");
+  return ROLLOUT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+rollout_status rollout_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t* h_bytes) {
+  if (!h_bytes) return fail(ROLLOUT_EINVAL, "the result pointer is NULL");
+  if (n_rows < 1 || vocab < 1) return fail(ROLLOUT_EINVAL, "n_rows and vocab must be >= 1");
+  if (vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab above 2^30");
+  if (n_top < 0 || n_top > kMaxTop || n_top > vocab) return fail(ROLLOUT_EINVAL, "n_top must be in [0, 32] and at most vocab");
+  if (n_top && vocab > kMaxTopVocab) return fail(ROLLOUT_EUNSUPPORTED, "alternatives of more than 2^20 ids");
+  *h_bytes = logprobs_workspace(n_rows, vocab, n_top);
+  return ROLLOUT_OK;
+}
+
+rollout_status rollout_token_logprobs(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                                      int32_t vocab, float temperature, const int32_t* d_tokens, int32_t n_top,
+                                      float* d_logp, float* d_entropy, float* d_stats, int32_t* d_top_ids,
+                                      float* d_top_logp, void* d_workspace, uint64_t workspace_bytes,
+                                      void* hip_stream) {
+  Range range("rollout_token_logprobs");
+  rollout_status st = check_rows(d_logits, dtype, row_stride, n_rows, vocab, temperature);
+  if (st != ROLLOUT_OK) return st;
+  uint64_t need = 0;
+  st = rollout_token_logprobs_workspace(n_rows, vocab, n_top, &need);
+  if (st != ROLLOUT_OK) return st;
+  if (n_top && (!d_top_ids || !d_top_logp)) return fail(ROLLOUT_EINVAL, "alternatives asked for without their outputs");
+  if (!d_tokens && d_logp) return fail(ROLLOUT_EINVAL, "log probabilities asked for without tokens");
+  if (!d_logp && !d_entropy && !d_stats && !n_top) return fail(ROLLOUT_EINVAL, "no output asked for");
+  st = check_workspace(d_workspace, workspace_bytes, need);
+  if (st != ROLLOUT_OK) return st;
+  st = check_stream(hip_stream);
+  if (st != ROLLOUT_OK) return st;
+  const LogprobArgs a = {d_logits, row_stride, n_rows, vocab, temperature, d_tokens, n_top,
+                         d_logp, d_entropy, d_stats, d_top_ids, d_top_logp};
+  return launched(launch_logprobs((hipStream_t)hip_stream, dtype, a, d_workspace), "token logprobs");
+}
+
+rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows,
+                                               int32_t vocab, float temperature, const int32_t* d_tokens,
+                                               const float* d_stats, const float* d_entropy, const float* d_grad_logp,
+                                               const float* d_grad_entropy, void* d_grad_logits, int64_t grad_stride,
+                                               void* hip_stream) {
+  Range range("rollout_token_logprobs_backward");
+  rollout_status st = check_rows(d_logits, dtype, row_stride, n_rows, vocab, temperature);
+  if (st != ROLLOUT_OK) return st;
+  if (!d_tokens || !d_stats || !d_grad_logp || !d_grad_logits) return fail(ROLLOUT_EINVAL, "NULL buffer");
+  if (d_grad_entropy && !d_entropy) return fail(ROLLOUT_EINVAL, "a gradient of the entropies needs the entropies");
+  if (grad_stride < vocab) return fail(ROLLOUT_EINVAL, "grad_stride must be at least vocab");
+  if (grad_stride > INT64_MAX / 8 / n_rows) return fail(ROLLOUT_EINVAL, "grad_stride too large");
+  const size_t es = elem_bytes(dtype);
+  if (!aligned_to(d_grad_logits, es)) return fail(ROLLOUT_EINVAL, "gradients are not aligned to their type");
+  const bool in_place = d_grad_logits == d_logits && grad_stride == row_stride;
+  if (!in_place && overlap(d_logits, ((size_t)(n_rows - 1) * row_stride + vocab) * es, d_grad_logits,
+                           ((size_t)(n_rows - 1) * grad_stride + vocab) * es))
+    return fail(ROLLOUT_EINVAL, "the gradients overlap the logits without being in their place");
+  st = check_stream(hip_stream);
+  if (st != ROLLOUT_OK) return st;
+  const LogprobGradArgs a = {d_logits, row_stride, n_rows, vocab, temperature, d_tokens, d_stats,
+                             d_entropy, d_grad_logp, d_grad_entropy, d_grad_logits, grad_stride};
+  return launched(launch_logprobs_backward((hipStream_t)hip_stream, dtype, a), "token logprobs backward");
+}
+
+}  // extern "C"
