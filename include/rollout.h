@@ -351,6 +351,66 @@ rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dty
                                                const float* d_grad_entropy, void* d_grad_logits, int64_t grad_stride,
                                                void* hip_stream);
 
+/*
+ * The clipped policy loss over groups of completions, and its gradient.  All matrices
+ * are fp32 [n_seqs, max_len], sequence s being completion s of the rollout and
+ * its tokens 0 .. len_s - 1 counted (d_lengths int32 [n_seqs] as rollout_generate_eos
+ * leaves them, taken into [0, max_len]; NULL: max_len each); what lies
+ * behind them is not used and gets gradient 0.  With lp = d_logp, A = d_adv[s]
+ * (grpo_advantages), r = exp(lp - old), x = ref - lp:
+ *   tok  = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl_coef (exp(x) - 1 - x) - entropy_coef H
+ *   loss = sum_s w_s sum_t tok,  w_s by mean:
+ *     ROLLOUT_MEAN_SEQUENCE  1 / (n_seqs len_s)      each completion weighs the same
+ *     ROLLOUT_MEAN_TOKEN     1 / sum len             each token weighs the same
+ *     ROLLOUT_MEAN_FIXED     1 / (n_seqs max_len)    lengths do not enter
+ *   (a divisor of 0 counts as 1: nothing but empty sequences has loss 0)
+ *   dlp  = w_s (-A r where the ratio is not clipped - kl_coef (exp(x) - 1)),  dH = -entropy_coef w_s
+ * A token is clipped where A > 0 and r > 1 + clip_high, or A < 0 and r < 1 - clip_low;
+ * with A = 0 the first term is 0 whatever the ratio.  d_old_logp NULL: the
+ * log probabilities themselves, held constant (r = 1).  d_ref_logp NULL: no penalty
+ * (kl_coef must be 0).  d_entropy NULL: no entropy term (entropy_coef must be 0).
+ * Outputs, each NULL if not wanted: d_loss fp32 [1]; d_stats fp32 [5], means over the counted
+ * tokens of r, of exp(x) - 1 - x, of tokens clipped below, clipped above, of H; d_grad_logp,
+ * d_grad_entropy fp32 [n_seqs, max_len], that must not overlap an input.  Sums are fp64.
+ * Errors: EINVAL (sizes, clip_low outside [0, 1], clip_high < 0, coefficients, mean,
+ * NULL buffers, overlap, no output), EUNSUPPORTED (2^31 tokens or more), ENOMEM
+ * (workspace too small), EDEVICE.
+ */
+#define ROLLOUT_MEAN_SEQUENCE 0
+#define ROLLOUT_MEAN_TOKEN 1
+#define ROLLOUT_MEAN_FIXED 2
+rollout_status grpo_policy_loss_workspace(int32_t n_seqs, int32_t max_len, uint64_t* h_bytes);
+rollout_status grpo_policy_loss(const float* d_logp, const float* d_old_logp, const float* d_ref_logp,
+                                const float* d_entropy, const float* d_adv, const int32_t* d_lengths, int32_t n_seqs,
+                                int32_t max_len, float clip_low, float clip_high, float kl_coef, float entropy_coef,
+                                int32_t mean, float* d_loss, float* d_stats, float* d_grad_logp, float* d_grad_entropy,
+                                void* d_workspace, uint64_t workspace_bytes, void* hip_stream);
+
+/*
+ * Embedding lookup: d_out [n_tokens, dim] of out_dtype, row n being scale times row
+ * d_tokens[n] of d_table [vocab, dim] of table_dtype (tensor 0 of rollout_export_weight,
+ * say).  Padding gives zeros, an id >= vocab NaN.  Both matrices are dense and do not
+ * overlap.  Errors: EINVAL (sizes, types, alignment, NULL buffers, overlap, scale not finite),
+ * EUNSUPPORTED (vocab or dim above 2^30, n_tokens above 2^31 - 4097), EDEVICE.
+ */
+rollout_status rollout_embedding(const void* d_table, int32_t table_dtype, int32_t vocab, int32_t dim,
+                                 const int32_t* d_tokens, int32_t n_tokens, float scale, void* d_out, int32_t out_dtype,
+                                 void* hip_stream);
+
+/*
+ * Its gradient: row v of d_grad_table [vocab, dim] of table_dtype becomes scale times the
+ * sum of the rows of d_grad [n_tokens, dim] of grad_dtype whose token is v.  With accumulate
+ * 0 every row is written (rows without tokens with zeros); with 1 the sum is added
+ * to what the row holds, rounded once, and rows without tokens are left alone.
+ * Ids outside [0, vocab) contribute nothing.  Tokens are sorted by id and a row's are
+ * added in fp32 in an order that their positions fix.  Errors as above, and ENOMEM (workspace too small).
+ */
+rollout_status rollout_embedding_backward_workspace(int32_t n_tokens, int32_t vocab, int32_t dim, uint64_t* h_bytes);
+rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype, const int32_t* d_tokens, int32_t n_tokens,
+                                          int32_t vocab, int32_t dim, float scale, int32_t accumulate, void* d_grad_table,
+                                          int32_t table_dtype, void* d_workspace, uint64_t workspace_bytes,
+                                          void* hip_stream);
+
 /* ------------------------------------------------------------------------ */
 /* Inspection and measurement                                                */
 /* ------------------------------------------------------------------------ */

@@ -28,7 +28,10 @@ EXPORTED = (
     "rollout_export_weight", "rollout_profile_decode_step", "rollout_generate_eos", "rollout_length_rewards",
     "rollout_sample_noalloc", "rollout_profile_projections",
     "rollout_token_logprobs_workspace", "rollout_token_logprobs", "rollout_token_logprobs_backward",
+    "grpo_policy_loss_workspace", "grpo_policy_loss",
+    "rollout_embedding", "rollout_embedding_backward_workspace", "rollout_embedding_backward",
 )
+MEAN_SEQUENCE, MEAN_TOKEN, MEAN_FIXED = 0, 1, 2  # ROLLOUT_MEAN_*
 NOALLOC_SCRATCH_BYTES = 64 << 20  # ROLLOUT_SAMPLE_NOALLOC_SCRATCH_BYTES
 # include/occupancy.h: power metrics and threshold policy of the occupancy controller (host code)
 EXPORTED_OCC = (
@@ -117,6 +120,11 @@ def _load():
         "rollout_token_logprobs_workspace": ([i32, i32, i32, pu64], i32),
         "rollout_token_logprobs": ([vp, i32, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp, u64, vp], i32),
         "rollout_token_logprobs_backward": ([vp, i32, i64, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp], i32),
+        "grpo_policy_loss_workspace": ([i32, i32, pu64], i32),
+        "grpo_policy_loss": ([vp, vp, vp, vp, vp, vp, i32, i32, f32, f32, f32, f32, i32, vp, vp, vp, vp, vp, u64, vp], i32),
+        "rollout_embedding": ([vp, i32, i32, i32, vp, i32, f32, vp, i32, vp], i32),
+        "rollout_embedding_backward_workspace": ([i32, i32, i32, pu64], i32),
+        "rollout_embedding_backward": ([vp, i32, vp, i32, i32, i32, f32, i32, vp, i32, vp, u64, vp], i32),
         "occ_rolling_mean": ([vp, ctypes.c_int64, f64, f64, vp], i32),
         "occ_violation": ([vp, ctypes.c_int64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f64)], i32),
         "occ_normalize_budget": ([f64, f64, f64], f64),
@@ -214,36 +222,36 @@ def rollout_length_rewards(lengths, n: int, target: int, rewards, total_tokens=N
 
 
 # The update side of a GRPO step: no context, caller-owned workspaces.  A tensor passed for a buffer has to be on the
-# current device, of the buffer's type, contiguous and large enough (a strided matrix of logits: large enough for its
-# last row); an integer address is passed on as it is.
-_DTYPES = {DTYPE_FP32: "torch.float32", DTYPE_BF16: "torch.bfloat16"}
-
-
-def _buf(name: str, x, dtype: str, n: int, strided: bool = False) -> int | None:
-    """Device pointer of a buffer of n elements of dtype."""
-    if x is None or not hasattr(x, "data_ptr"):
-        return _ptr(x)
+# current device, of the buffer's type, contiguous (the rows of logits may be strided) and large enough; an integer
+# address is passed on as it is.
+def _checker():
     import torch
 
-    if dtype != "any" and str(x.dtype) != dtype:
-        raise RolloutError(EINVAL, f"{name} must be {dtype}, not {x.dtype}")
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
-        raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
-    if strided:
-        if x.stride(-1) != 1 and x.shape[-1] > 1:
-            raise RolloutError(EINVAL, f"the rows of {name} are not contiguous")
-        have = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
-    elif not x.is_contiguous():
-        raise RolloutError(EINVAL, f"{name} is not contiguous")
-    else:
-        have = x.numel() * (x.element_size() if dtype == "any" else 1)
-    if have < n:
-        raise RolloutError(EINVAL, f"{name} holds {have} elements, the call needs {n}")
-    return x.data_ptr()
+    types = {"f": torch.float32, "i": torch.int32, DTYPE_FP32: torch.float32, DTYPE_BF16: torch.bfloat16}
+    device = None
 
+    def buf(name: str, x, kind, n: int) -> int | None:
+        """Device pointer of a buffer of n elements of a kind (n bytes of any type where kind is None)."""
+        nonlocal device
+        if x is None or not isinstance(x, torch.Tensor):
+            return _ptr(x)
+        want = types.get(kind)
+        if kind is not None and x.dtype != want:
+            raise RolloutError(EINVAL, f"{name} must be {want or 'of dtype 0 (fp32) or 1 (bf16)'}, not {x.dtype}")
+        if device is None:
+            device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+        if x.get_device() != device or device < 0:
+            raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
+        have = x.numel() if kind is not None else x.numel() * x.element_size()
+        if not x.is_contiguous():
+            if not name.endswith("logits") or x.stride(-1) != 1:
+                raise RolloutError(EINVAL, f"{name} is not contiguous")
+            have = sum((k - 1) * s for k, s in zip(x.shape, x.stride())) + 1 if have else 0
+        if have < n:
+            raise RolloutError(EINVAL, f"{name} holds {have} elements, the call needs {n}")
+        return x.data_ptr()
 
-def _rows(name: str, x, dtype: int, n_rows: int, stride: int, vocab: int) -> int | None:
-    return _buf(name, x, _DTYPES.get(dtype, f"of dtype 0 or 1 (got {dtype})"), (n_rows - 1) * stride + vocab, strided=True)
+    return buf
 
 
 def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) -> int:
@@ -255,25 +263,67 @@ def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) ->
 def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float, tokens,
                            n_top: int = 0, logp=None, entropy=None, stats=None, top_ids=None, top_logp=None,
                            workspace=None, workspace_bytes: int = 0, stream=None):
-    f = "torch.float32"
+    buf = _checker()
     _check(lib.rollout_token_logprobs(
-        _rows("logits", logits, dtype, n_rows, row_stride, vocab), dtype, row_stride, n_rows, vocab, temperature,
-        _buf("tokens", tokens, "torch.int32", n_rows), n_top, _buf("logp", logp, f, n_rows),
-        _buf("entropy", entropy, f, n_rows), _buf("stats", stats, f, 2 * n_rows),
-        _buf("top_ids", top_ids, "torch.int32", n_rows * n_top), _buf("top_logp", top_logp, f, n_rows * n_top),
-        _buf("workspace", workspace, "any", workspace_bytes), workspace_bytes, _ptr(stream)))
+        buf("logits", logits, dtype, (n_rows - 1) * row_stride + vocab), dtype, row_stride, n_rows, vocab, temperature,
+        buf("tokens", tokens, "i", n_rows), n_top, buf("logp", logp, "f", n_rows), buf("entropy", entropy, "f", n_rows),
+        buf("stats", stats, "f", 2 * n_rows), buf("top_ids", top_ids, "i", n_rows * n_top),
+        buf("top_logp", top_logp, "f", n_rows * n_top), buf("workspace", workspace, None, workspace_bytes),
+        workspace_bytes, _ptr(stream)))
 
 
 def rollout_token_logprobs_backward(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float,
                                     tokens, stats, entropy, grad_logp, grad_entropy, grad_logits, grad_stride: int,
                                     stream=None):
-    f = "torch.float32"
+    buf = _checker()
     _check(lib.rollout_token_logprobs_backward(
-        _rows("logits", logits, dtype, n_rows, row_stride, vocab), dtype, row_stride, n_rows, vocab, temperature,
-        _buf("tokens", tokens, "torch.int32", n_rows), _buf("stats", stats, f, 2 * n_rows),
-        _buf("entropy", entropy, f, n_rows), _buf("grad_logp", grad_logp, f, n_rows),
-        _buf("grad_entropy", grad_entropy, f, n_rows),
-        _rows("grad_logits", grad_logits, dtype, n_rows, grad_stride, vocab), grad_stride, _ptr(stream)))
+        buf("logits", logits, dtype, (n_rows - 1) * row_stride + vocab), dtype, row_stride, n_rows, vocab, temperature,
+        buf("tokens", tokens, "i", n_rows), buf("stats", stats, "f", 2 * n_rows), buf("entropy", entropy, "f", n_rows),
+        buf("grad_logp", grad_logp, "f", n_rows), buf("grad_entropy", grad_entropy, "f", n_rows),
+        buf("grad_logits", grad_logits, dtype, (n_rows - 1) * grad_stride + vocab), grad_stride, _ptr(stream)))
+
+
+def grpo_policy_loss_workspace(n_seqs: int, max_len: int) -> int:
+    out = ctypes.c_uint64(0)
+    _check(lib.grpo_policy_loss_workspace(n_seqs, max_len, ctypes.byref(out)))
+    return out.value
+
+
+def grpo_policy_loss(logp, old_logp, ref_logp, entropy, adv, lengths, n_seqs: int, max_len: int, clip_low: float,
+                     clip_high: float, kl_coef: float, entropy_coef: float, mean: int, loss=None, stats=None,
+                     grad_logp=None, grad_entropy=None, workspace=None, workspace_bytes: int = 0, stream=None):
+    buf = _checker()
+    n = n_seqs * max_len
+    _check(lib.grpo_policy_loss(
+        buf("logp", logp, "f", n), buf("old_logp", old_logp, "f", n), buf("ref_logp", ref_logp, "f", n),
+        buf("entropy", entropy, "f", n), buf("adv", adv, "f", n_seqs), buf("lengths", lengths, "i", n_seqs), n_seqs,
+        max_len, clip_low, clip_high, kl_coef, entropy_coef, mean, buf("loss", loss, "f", 1), buf("stats", stats, "f", 5),
+        buf("grad_logp", grad_logp, "f", n), buf("grad_entropy", grad_entropy, "f", n),
+        buf("workspace", workspace, None, workspace_bytes), workspace_bytes, _ptr(stream)))
+
+
+def rollout_embedding(table, table_dtype: int, vocab: int, dim: int, tokens, n_tokens: int, scale: float, out,
+                      out_dtype: int, stream=None):
+    buf = _checker()
+    _check(lib.rollout_embedding(
+        buf("table", table, table_dtype, vocab * dim), table_dtype, vocab, dim, buf("tokens", tokens, "i", n_tokens),
+        n_tokens, scale, buf("out", out, out_dtype, n_tokens * dim), out_dtype, _ptr(stream)))
+
+
+def rollout_embedding_backward_workspace(n_tokens: int, vocab: int, dim: int) -> int:
+    out = ctypes.c_uint64(0)
+    _check(lib.rollout_embedding_backward_workspace(n_tokens, vocab, dim, ctypes.byref(out)))
+    return out.value
+
+
+def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, vocab: int, dim: int, scale: float,
+                               accumulate: int, grad_table, table_dtype: int, workspace=None, workspace_bytes: int = 0,
+                               stream=None):
+    buf = _checker()
+    _check(lib.rollout_embedding_backward(
+        buf("grad", grad, grad_dtype, n_tokens * dim), grad_dtype, buf("tokens", tokens, "i", n_tokens), n_tokens, vocab,
+        dim, scale, accumulate, buf("grad_table", grad_table, table_dtype, vocab * dim), table_dtype,
+        buf("workspace", workspace, None, workspace_bytes), workspace_bytes, _ptr(stream)))
 
 
 def rollout_sync(ctx):

@@ -5,6 +5,8 @@
 
 #include "internal.h"
 
+#include <algorithm>
+
 namespace rollout {
 
 constexpr int kMaxTop = 32;            // alternatives of a row
@@ -40,6 +42,39 @@ struct LogprobGradArgs {
   int64_t dz_stride;
 };
 hipError_t launch_logprobs_backward(hipStream_t s, int dtype, const LogprobGradArgs& a);
+
+struct PolicyLossArgs {
+  const float *logp, *old, *ref, *entropy, *adv;
+  const int32_t* lengths;
+  int seqs, max_len;
+  float clip_low, clip_high, kl_coef, entropy_coef;
+  int mean;  // ROLLOUT_MEAN_*
+  float *loss, *stats, *grad_logp, *grad_entropy;
+};
+size_t policy_loss_workspace(int seqs, int max_len);
+hipError_t launch_policy_loss(hipStream_t s, const PolicyLossArgs& a, void* ws);
+
+struct EmbeddingArgs {
+  const void* table;
+  int vocab, dim;
+  const int32_t* tokens;
+  int n;
+  float scale;
+  void* out;
+};
+hipError_t launch_embedding(hipStream_t s, int table_dtype, int out_dtype, const EmbeddingArgs& a);
+
+struct EmbeddingGradArgs {
+  const void* g;
+  const int32_t* tokens;
+  int n, vocab, dim;
+  float scale;
+  bool accumulate;
+  void* table;
+};
+constexpr int kMaxEmbeddingTokens = 0x7FFFFFFF - 4096;
+size_t embedding_backward_workspace(int n, int vocab, int dim);
+hipError_t launch_embedding_backward(hipStream_t s, int grad_dtype, int table_dtype, const EmbeddingGradArgs& a, void* ws);
 
 }  // namespace rollout
 

@@ -75,6 +75,16 @@ rollout_status check_rows(const void* z, int32_t dtype, int64_t stride, int32_t 
   return ROLLOUT_OK;
 }
 
+// what lookup and gradient ask of a table and a matrix of rows
+rollout_status check_table(int32_t table_dtype, int32_t row_dtype, int32_t vocab, int32_t dim, int32_t n, float scale) {
+  if (!is_float_type(table_dtype) || !is_float_type(row_dtype)) return fail(ROLLOUT_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
+  if (vocab < 1 || dim < 1 || n < 1) return fail(ROLLOUT_EINVAL, "vocab, dim and n_tokens must be >= 1");
+  if (vocab > kMaxVocab || dim > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab or dim above 2^30");
+  if (n > kMaxEmbeddingTokens) return fail(ROLLOUT_EUNSUPPORTED, "more than 2^31 - 4097 tokens");
+  if (!std::isfinite(scale)) return fail(ROLLOUT_EINVAL, "scale must be finite");
+  return ROLLOUT_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -135,6 +145,97 @@ rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dty
   const LogprobGradArgs a = {d_logits, row_stride, n_rows, vocab, temperature, d_tokens, d_stats,
                              d_entropy, d_grad_logp, d_grad_entropy, d_grad_logits, grad_stride};
   return launched(launch_logprobs_backward((hipStream_t)hip_stream, dtype, a), "token logprobs backward");
+}
+
+rollout_status grpo_policy_loss_workspace(int32_t n_seqs, int32_t max_len, uint64_t* h_bytes) {
+  if (!h_bytes) return fail(ROLLOUT_EINVAL, "the result pointer is NULL");
+  if (n_seqs < 1 || max_len < 1) return fail(ROLLOUT_EINVAL, "n_seqs and max_len must be >= 1");
+  if ((int64_t)n_seqs * max_len > INT32_MAX) return fail(ROLLOUT_EUNSUPPORTED, "more than 2^31 - 1 tokens");
+  *h_bytes = policy_loss_workspace(n_seqs, max_len);
+  return ROLLOUT_OK;
+}
+
+rollout_status grpo_policy_loss(const float* d_logp, const float* d_old_logp, const float* d_ref_logp,
+                                const float* d_entropy, const float* d_adv, const int32_t* d_lengths, int32_t n_seqs,
+                                int32_t max_len, float clip_low, float clip_high, float kl_coef, float entropy_coef,
+                                int32_t mean, float* d_loss, float* d_stats, float* d_grad_logp, float* d_grad_entropy,
+                                void* d_workspace, uint64_t workspace_bytes, void* hip_stream) {
+  Range range("grpo_policy_loss");
+  uint64_t need = 0;
+  rollout_status st = grpo_policy_loss_workspace(n_seqs, max_len, &need);
+  if (st != ROLLOUT_OK) return st;
+  if (!d_logp || !d_adv) return fail(ROLLOUT_EINVAL, "log probabilities and advantages must be non-NULL");
+  if (!(clip_low >= 0.f && clip_low <= 1.f)) return fail(ROLLOUT_EINVAL, "clip_low must be in [0, 1]");
+  if (!(clip_high >= 0.f) || !std::isfinite(clip_high)) return fail(ROLLOUT_EINVAL, "clip_high must be >= 0");
+  if (!std::isfinite(kl_coef) || !std::isfinite(entropy_coef)) return fail(ROLLOUT_EINVAL, "coefficients must be finite");
+  if (kl_coef != 0.f && !d_ref_logp) return fail(ROLLOUT_EINVAL, "kl_coef without reference log probabilities");
+  if ((entropy_coef != 0.f || d_grad_entropy) && !d_entropy) return fail(ROLLOUT_EINVAL, "an entropy term without entropies");
+  if (mean != ROLLOUT_MEAN_SEQUENCE && mean != ROLLOUT_MEAN_TOKEN && mean != ROLLOUT_MEAN_FIXED)
+    return fail(ROLLOUT_EINVAL, "mean must be 0 (sequence), 1 (token) or 2 (fixed)");
+  if (!d_loss && !d_stats && !d_grad_logp && !d_grad_entropy) return fail(ROLLOUT_EINVAL, "no output asked for");
+  const size_t whole = (size_t)n_seqs * max_len * 4;
+  float* outs[] = {d_grad_logp, d_grad_entropy};
+  const float* ins[] = {d_logp, d_old_logp, d_ref_logp, d_entropy};
+  for (float* o : outs)
+    for (const float* i : ins)
+      if (o && i && overlap(o, whole, i, whole)) return fail(ROLLOUT_EINVAL, "a gradient overlaps an input");
+  if (d_grad_logp && d_grad_entropy && overlap(d_grad_logp, whole, d_grad_entropy, whole))
+    return fail(ROLLOUT_EINVAL, "the gradients overlap");
+  st = check_workspace(d_workspace, workspace_bytes, need);
+  if (st != ROLLOUT_OK) return st;
+  st = check_stream(hip_stream);
+  if (st != ROLLOUT_OK) return st;
+  const PolicyLossArgs a = {d_logp, d_old_logp, d_ref_logp, d_entropy, d_adv, d_lengths, n_seqs, max_len, clip_low,
+                            clip_high, kl_coef, entropy_coef, mean, d_loss, d_stats, d_grad_logp, d_grad_entropy};
+  return launched(launch_policy_loss((hipStream_t)hip_stream, a, d_workspace), "policy loss");
+}
+
+rollout_status rollout_embedding(const void* d_table, int32_t table_dtype, int32_t vocab, int32_t dim,
+                                 const int32_t* d_tokens, int32_t n_tokens, float scale, void* d_out, int32_t out_dtype,
+                                 void* hip_stream) {
+  Range range("rollout_embedding");
+  rollout_status st = check_table(table_dtype, out_dtype, vocab, dim, n_tokens, scale);
+  if (st != ROLLOUT_OK) return st;
+  if (!d_table || !d_tokens || !d_out) return fail(ROLLOUT_EINVAL, "NULL buffer");
+  if (!aligned_to(d_table, elem_bytes(table_dtype)) || !aligned_to(d_out, elem_bytes(out_dtype)))
+    return fail(ROLLOUT_EINVAL, "a matrix is not aligned to its type");
+  if (overlap(d_table, (size_t)vocab * dim * elem_bytes(table_dtype), d_out, (size_t)n_tokens * dim * elem_bytes(out_dtype)))
+    return fail(ROLLOUT_EINVAL, "the output overlaps the table");
+  st = check_stream(hip_stream);
+  if (st != ROLLOUT_OK) return st;
+  const EmbeddingArgs a = {d_table, vocab, dim, d_tokens, n_tokens, scale, d_out};
+  return launched(launch_embedding((hipStream_t)hip_stream, table_dtype, out_dtype, a), "embedding");
+}
+
+rollout_status rollout_embedding_backward_workspace(int32_t n_tokens, int32_t vocab, int32_t dim, uint64_t* h_bytes) {
+  if (!h_bytes) return fail(ROLLOUT_EINVAL, "the result pointer is NULL");
+  const rollout_status st = check_table(ROLLOUT_DTYPE_FP32, ROLLOUT_DTYPE_FP32, vocab, dim, n_tokens, 1.f);
+  if (st != ROLLOUT_OK) return st;
+  *h_bytes = embedding_backward_workspace(n_tokens, vocab, dim);
+  return ROLLOUT_OK;
+}
+
+rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype, const int32_t* d_tokens, int32_t n_tokens,
+                                          int32_t vocab, int32_t dim, float scale, int32_t accumulate, void* d_grad_table,
+                                          int32_t table_dtype, void* d_workspace, uint64_t workspace_bytes,
+                                          void* hip_stream) {
+  Range range("rollout_embedding_backward");
+  rollout_status st = check_table(table_dtype, grad_dtype, vocab, dim, n_tokens, scale);
+  if (st != ROLLOUT_OK) return st;
+  if (accumulate != 0 && accumulate != 1) return fail(ROLLOUT_EINVAL, "accumulate must be 0 or 1");
+  if (!d_grad || !d_tokens || !d_grad_table) return fail(ROLLOUT_EINVAL, "NULL buffer");
+  if (!aligned_to(d_grad, elem_bytes(grad_dtype)) || !aligned_to(d_grad_table, elem_bytes(table_dtype)))
+    return fail(ROLLOUT_EINVAL, "a matrix is not aligned to its type");
+  if (overlap(d_grad, (size_t)n_tokens * dim * elem_bytes(grad_dtype), d_grad_table,
+              (size_t)vocab * dim * elem_bytes(table_dtype)))
+    return fail(ROLLOUT_EINVAL, "the table's gradient overlaps the tokens' gradients");
+  st = check_workspace(d_workspace, workspace_bytes, embedding_backward_workspace(n_tokens, vocab, dim));
+  if (st != ROLLOUT_OK) return st;
+  st = check_stream(hip_stream);
+  if (st != ROLLOUT_OK) return st;
+  const EmbeddingGradArgs a = {d_grad, d_tokens, n_tokens, vocab, dim, scale, accumulate != 0, d_grad_table};
+  return launched(launch_embedding_backward((hipStream_t)hip_stream, grad_dtype, table_dtype, a, d_workspace),
+                  "embedding backward");
 }
 
 }  // extern "C"

@@ -75,3 +75,64 @@ def test_tensors_are_checked():
     refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host), text="current device")
     refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host.double()), text="float32")
     refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, tokens=torch.zeros(4, dtype=torch.int64)), text="int32")
+    refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host.bfloat16(), dtype=7), text="dtype 0")
+
+
+LOSS = dict(lp=A, old=B, ref=C, H=D, adv=E, lengths=F, S=4, N=16, lo=0.2, hi=0.3, kl=0.1, ent=0.01, mean=0, loss=G, stats=G + 64,
+            dlp=H, dH=H + (1 << 20), ws=H + (2 << 20), ws_bytes=1 << 20, stream=None)
+
+
+@pytest.mark.parametrize("code,change,text", [
+    (R.EINVAL, dict(S=0), "n_seqs"), (R.EINVAL, dict(N=0), "max_len"), (R.EUNSUPPORTED, dict(S=1 << 16, N=1 << 15), "2^31"),
+    (R.EINVAL, dict(lp=None), "non-NULL"), (R.EINVAL, dict(adv=None), "non-NULL"),
+    (R.EINVAL, dict(lo=-0.1), "clip_low"), (R.EINVAL, dict(lo=1.1), "clip_low"), (R.EINVAL, dict(lo=float("nan")), "clip_low"),
+    (R.EINVAL, dict(hi=-0.1), "clip_high"), (R.EINVAL, dict(hi=float("inf")), "clip_high"),
+    (R.EINVAL, dict(kl=float("nan")), "finite"), (R.EINVAL, dict(ent=float("inf")), "finite"),
+    (R.EINVAL, dict(ref=None), "reference"), (R.EINVAL, dict(H=None), "entropies"), (R.EINVAL, dict(H=None, ent=0.0), "entropies"),
+    (R.EINVAL, dict(mean=3), "mean"), (R.EINVAL, dict(mean=-1), "mean"),
+    (R.EINVAL, dict(loss=None, stats=None, dlp=None, dH=None), "no output"),
+    (R.EINVAL, dict(dlp=A), "overlaps an input"), (R.EINVAL, dict(dlp=B + 252), "overlaps an input"),
+    (R.EINVAL, dict(dH=D - 252), "overlaps an input"), (R.EINVAL, dict(dH=H), "gradients overlap"),
+    (R.ENOMEM, dict(ws_bytes=8), "workspace"), (R.EINVAL, dict(ws=None), "workspace"), (R.EINVAL, dict(ws=H + 8), "16 bytes"),
+])
+def test_policy_loss_refusals(code, change, text):
+    refuse(code, R.grpo_policy_loss, *call(LOSS, **change), text=text)
+
+
+LOOKUP = dict(table=A, tdt=0, V=100, dim=8, tokens=B, n=5, scale=1.0, out=C, odt=1, stream=None)
+
+
+@pytest.mark.parametrize("code,change,text", [
+    (R.EINVAL, dict(tdt=2), "dtype"), (R.EINVAL, dict(odt=-1), "dtype"), (R.EINVAL, dict(V=0), "vocab"),
+    (R.EINVAL, dict(dim=0), "dim"), (R.EINVAL, dict(n=0), "n_tokens"), (R.EUNSUPPORTED, dict(V=(1 << 30) + 1), "2^30"),
+    (R.EUNSUPPORTED, dict(n=2**31 - 1), "4097"), (R.EINVAL, dict(scale=float("nan")), "scale"),
+    (R.EINVAL, dict(table=None), "NULL"), (R.EINVAL, dict(tokens=None), "NULL"), (R.EINVAL, dict(out=None), "NULL"),
+    (R.EINVAL, dict(table=A + 2), "aligned"), (R.EINVAL, dict(out=C + 1), "aligned"),
+    (R.EINVAL, dict(out=A + 3198), "overlaps"), (R.EINVAL, dict(out=A - 78), "overlaps"),
+])
+def test_embedding_refusals(code, change, text):
+    refuse(code, R.rollout_embedding, *call(LOOKUP, **change), text=text)
+
+
+GRAD = dict(g=A, gdt=1, tokens=B, n=5, V=100, dim=8, scale=1.0, acc=0, table=C, tdt=0, ws=D, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("code,change,text", [
+    (R.EINVAL, dict(tdt=2), "dtype"), (R.EINVAL, dict(gdt=2), "dtype"), (R.EINVAL, dict(V=0), "vocab"), (R.EINVAL, dict(n=0), "n_tokens"),
+    (R.EINVAL, dict(acc=2), "accumulate"), (R.EINVAL, dict(scale=float("inf")), "scale"),
+    (R.EINVAL, dict(g=None), "NULL"), (R.EINVAL, dict(tokens=None), "NULL"), (R.EINVAL, dict(table=None), "NULL"),
+    (R.EINVAL, dict(g=A + 1), "aligned"), (R.EINVAL, dict(table=C + 2), "aligned"),
+    (R.EINVAL, dict(table=A + 76), "overlaps"), (R.EINVAL, dict(table=A - 3196), "overlaps"),
+    (R.ENOMEM, dict(ws_bytes=100), "workspace"), (R.EINVAL, dict(ws=None), "NULL"), (R.EINVAL, dict(ws=D + 4), "16 bytes"),
+])
+def test_embedding_backward_refusals(code, change, text):
+    refuse(code, R.rollout_embedding_backward, *call(GRAD, **change), text=text)
+
+
+def test_workspaces_of_loss_and_embedding():
+    assert R.grpo_policy_loss_workspace(1, 1) > 0
+    assert R.rollout_embedding_backward_workspace(5, 100, 8) > 0
+    refuse(R.EINVAL, R.grpo_policy_loss_workspace, 0, 4)
+    refuse(R.EINVAL, R.rollout_embedding_backward_workspace, 0, 4, 4)
+    assert R.lib.grpo_policy_loss_workspace(1, 1, None) == R.EINVAL
+    assert R.lib.rollout_embedding_backward_workspace(1, 1, 1, None) == R.EINVAL
