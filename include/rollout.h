@@ -324,7 +324,7 @@ rollout_status rollout_sample_noalloc(const float* d_logits, int32_t n_seqs, int
  * with NaN or +inf gets NaN everywhere and top ids -1.  d_tokens NULL: no row
  * is padding, and d_logp must be NULL.
  * Errors: EINVAL (sizes, types, alignment, NULL buffers, temperature not > 0, no
- * output), EUNSUPPORTED (vocab above 2^30, or above 2^20 with n_top > 0), ENOMEM
+ * output), EUNSUPPORTED (vocab above 2^30, or above 327,680 with n_top > 0), ENOMEM
  * (workspace too small), EDEVICE.
  */
 rollout_status rollout_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t* h_bytes);

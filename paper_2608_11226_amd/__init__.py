@@ -144,6 +144,11 @@ def _load():
 
 lib = _load()
 
+import torch as _torch  # noqa: E402  (loaded above)
+
+_F, _I = _torch.float32, _torch.int32
+_TYPES = {DTYPE_FP32: _torch.float32, DTYPE_BF16: _torch.bfloat16}
+
 
 def _ptr(x) -> int | None:
     """Device pointer of a tensor (data_ptr) or an integer address; None stays NULL."""
@@ -224,34 +229,37 @@ def rollout_length_rewards(lengths, n: int, target: int, rewards, total_tokens=N
 # The update side of a GRPO step: no context, caller-owned workspaces.  A tensor passed for a buffer has to be on the
 # current device, of the buffer's type, contiguous (the rows of logits may be strided) and large enough; an integer
 # address is passed on as it is.
-def _checker():
-    import torch
-
-    types = {"f": torch.float32, "i": torch.int32, DTYPE_FP32: torch.float32, DTYPE_BF16: torch.bfloat16}
-    device = None
-
-    def buf(name: str, x, kind, n: int) -> int | None:
-        """Device pointer of a buffer of n elements of a kind (n bytes of any type where kind is None)."""
-        nonlocal device
-        if x is None or not isinstance(x, torch.Tensor):
-            return _ptr(x)
-        want = types.get(kind)
-        if kind is not None and x.dtype != want:
-            raise RolloutError(EINVAL, f"{name} must be {want or 'of dtype 0 (fp32) or 1 (bf16)'}, not {x.dtype}")
-        if device is None:
-            device = torch.cuda.current_device() if torch.cuda.is_available() else -1
-        if x.get_device() != device or device < 0:
-            raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
-        have = x.numel() if kind is not None else x.numel() * x.element_size()
-        if not x.is_contiguous():
-            if not name.endswith("logits") or x.stride(-1) != 1:
-                raise RolloutError(EINVAL, f"{name} is not contiguous")
-            have = sum((k - 1) * s for k, s in zip(x.shape, x.stride())) + 1 if have else 0
-        if have < n:
-            raise RolloutError(EINVAL, f"{name} holds {have} elements, the call needs {n}")
+def _buf(name: str, x, kind, n: int, device: int) -> int | None:
+    """Device pointer of a buffer of n elements of a kind (n bytes of any type where kind is None)."""
+    if x is None or type(x) is int:
+        return x
+    if not isinstance(x, _torch.Tensor):
+        return _ptr(x)
+    if x.dtype is kind and x.get_device() == device and x.is_contiguous() and x.numel() >= n:
         return x.data_ptr()
+    if kind is not None and x.dtype is not kind:
+        raise RolloutError(EINVAL, f"{name} must be {kind}, not {x.dtype}")
+    if x.get_device() != device:
+        raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
+    have = x.numel() if kind is not None else x.numel() * x.element_size()
+    if not x.is_contiguous():
+        if not name.endswith("logits") or x.stride(-1) != 1:
+            raise RolloutError(EINVAL, f"{name} is not contiguous")
+        have = sum((k - 1) * s for k, s in zip(x.shape, x.stride())) + 1 if have else 0
+    if have < n:
+        raise RolloutError(EINVAL, f"{name} holds {have} elements, the call needs {n}")
+    return x.data_ptr()
 
-    return buf
+
+def _kind(dtype: int):
+    kind = _TYPES.get(dtype)
+    if kind is None:
+        raise RolloutError(EINVAL, f"dtype must be 0 (fp32) or 1 (bf16), not {dtype}")
+    return kind
+
+
+def _device() -> int:
+    return _torch.cuda.current_device() if _torch.cuda.is_initialized() else -2  # no tensor's
 
 
 def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) -> int:
@@ -263,24 +271,29 @@ def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) ->
 def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float, tokens,
                            n_top: int = 0, logp=None, entropy=None, stats=None, top_ids=None, top_logp=None,
                            workspace=None, workspace_bytes: int = 0, stream=None):
-    buf = _checker()
+    dev = _device()
     _check(lib.rollout_token_logprobs(
-        buf("logits", logits, dtype, (n_rows - 1) * row_stride + vocab), dtype, row_stride, n_rows, vocab, temperature,
-        buf("tokens", tokens, "i", n_rows), n_top, buf("logp", logp, "f", n_rows), buf("entropy", entropy, "f", n_rows),
-        buf("stats", stats, "f", 2 * n_rows), buf("top_ids", top_ids, "i", n_rows * n_top),
-        buf("top_logp", top_logp, "f", n_rows * n_top), buf("workspace", workspace, None, workspace_bytes),
+        _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev), dtype, row_stride, n_rows, vocab,
+        temperature,
+        _buf("tokens", tokens, _I, n_rows, dev), n_top, _buf("logp", logp, _F, n_rows, dev),
+        _buf("entropy", entropy, _F, n_rows, dev),
+        _buf("stats", stats, _F, 2 * n_rows, dev), _buf("top_ids", top_ids, _I, n_rows * n_top, dev),
+        _buf("top_logp", top_logp, _F, n_rows * n_top, dev), _buf("workspace", workspace, None, workspace_bytes, dev),
         workspace_bytes, _ptr(stream)))
 
 
 def rollout_token_logprobs_backward(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float,
                                     tokens, stats, entropy, grad_logp, grad_entropy, grad_logits, grad_stride: int,
                                     stream=None):
-    buf = _checker()
+    dev = _device()
     _check(lib.rollout_token_logprobs_backward(
-        buf("logits", logits, dtype, (n_rows - 1) * row_stride + vocab), dtype, row_stride, n_rows, vocab, temperature,
-        buf("tokens", tokens, "i", n_rows), buf("stats", stats, "f", 2 * n_rows), buf("entropy", entropy, "f", n_rows),
-        buf("grad_logp", grad_logp, "f", n_rows), buf("grad_entropy", grad_entropy, "f", n_rows),
-        buf("grad_logits", grad_logits, dtype, (n_rows - 1) * grad_stride + vocab), grad_stride, _ptr(stream)))
+        _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev), dtype, row_stride, n_rows, vocab,
+        temperature,
+        _buf("tokens", tokens, _I, n_rows, dev), _buf("stats", stats, _F, 2 * n_rows, dev),
+        _buf("entropy", entropy, _F, n_rows, dev),
+        _buf("grad_logp", grad_logp, _F, n_rows, dev), _buf("grad_entropy", grad_entropy, _F, n_rows, dev),
+        _buf("grad_logits", grad_logits, _kind(dtype), (n_rows - 1) * grad_stride + vocab, dev), grad_stride,
+        _ptr(stream)))
 
 
 def grpo_policy_loss_workspace(n_seqs: int, max_len: int) -> int:
@@ -292,22 +305,25 @@ def grpo_policy_loss_workspace(n_seqs: int, max_len: int) -> int:
 def grpo_policy_loss(logp, old_logp, ref_logp, entropy, adv, lengths, n_seqs: int, max_len: int, clip_low: float,
                      clip_high: float, kl_coef: float, entropy_coef: float, mean: int, loss=None, stats=None,
                      grad_logp=None, grad_entropy=None, workspace=None, workspace_bytes: int = 0, stream=None):
-    buf = _checker()
+    dev = _device()
     n = n_seqs * max_len
     _check(lib.grpo_policy_loss(
-        buf("logp", logp, "f", n), buf("old_logp", old_logp, "f", n), buf("ref_logp", ref_logp, "f", n),
-        buf("entropy", entropy, "f", n), buf("adv", adv, "f", n_seqs), buf("lengths", lengths, "i", n_seqs), n_seqs,
-        max_len, clip_low, clip_high, kl_coef, entropy_coef, mean, buf("loss", loss, "f", 1), buf("stats", stats, "f", 5),
-        buf("grad_logp", grad_logp, "f", n), buf("grad_entropy", grad_entropy, "f", n),
-        buf("workspace", workspace, None, workspace_bytes), workspace_bytes, _ptr(stream)))
+        _buf("logp", logp, _F, n, dev), _buf("old_logp", old_logp, _F, n, dev), _buf("ref_logp", ref_logp, _F, n, dev),
+        _buf("entropy", entropy, _F, n, dev), _buf("adv", adv, _F, n_seqs, dev),
+        _buf("lengths", lengths, _I, n_seqs, dev), n_seqs,
+        max_len, clip_low, clip_high, kl_coef, entropy_coef, mean, _buf("loss", loss, _F, 1, dev),
+        _buf("stats", stats, _F, 5, dev),
+        _buf("grad_logp", grad_logp, _F, n, dev), _buf("grad_entropy", grad_entropy, _F, n, dev),
+        _buf("workspace", workspace, None, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
 
 
 def rollout_embedding(table, table_dtype: int, vocab: int, dim: int, tokens, n_tokens: int, scale: float, out,
                       out_dtype: int, stream=None):
-    buf = _checker()
+    dev = _device()
     _check(lib.rollout_embedding(
-        buf("table", table, table_dtype, vocab * dim), table_dtype, vocab, dim, buf("tokens", tokens, "i", n_tokens),
-        n_tokens, scale, buf("out", out, out_dtype, n_tokens * dim), out_dtype, _ptr(stream)))
+        _buf("table", table, _kind(table_dtype), vocab * dim, dev), table_dtype, vocab, dim,
+        _buf("tokens", tokens, _I, n_tokens, dev),
+        n_tokens, scale, _buf("out", out, _kind(out_dtype), n_tokens * dim, dev), out_dtype, _ptr(stream)))
 
 
 def rollout_embedding_backward_workspace(n_tokens: int, vocab: int, dim: int) -> int:
@@ -319,11 +335,12 @@ def rollout_embedding_backward_workspace(n_tokens: int, vocab: int, dim: int) ->
 def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, vocab: int, dim: int, scale: float,
                                accumulate: int, grad_table, table_dtype: int, workspace=None, workspace_bytes: int = 0,
                                stream=None):
-    buf = _checker()
+    dev = _device()
     _check(lib.rollout_embedding_backward(
-        buf("grad", grad, grad_dtype, n_tokens * dim), grad_dtype, buf("tokens", tokens, "i", n_tokens), n_tokens, vocab,
-        dim, scale, accumulate, buf("grad_table", grad_table, table_dtype, vocab * dim), table_dtype,
-        buf("workspace", workspace, None, workspace_bytes), workspace_bytes, _ptr(stream)))
+        _buf("grad", grad, _kind(grad_dtype), n_tokens * dim, dev), grad_dtype,
+        _buf("tokens", tokens, _I, n_tokens, dev), n_tokens, vocab,
+        dim, scale, accumulate, _buf("grad_table", grad_table, _kind(table_dtype), vocab * dim, dev), table_dtype,
+        _buf("workspace", workspace, None, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
 
 
 def rollout_sync(ctx):

@@ -16,6 +16,13 @@ namespace {
 constexpr int RB = 256;  // threads of a row's workgroup
 constexpr int RW = RB / 64;
 constexpr int kUnits = 4;  // 16-byte loads in flight a lane
+constexpr int kMaxUnits = kMaxTopVocab / 256, kMaxPer = kMaxUnits / 64;  // of a row, of a lane, where alternatives are taken
+constexpr int kMaxChunks = 64;     // a lane each when parts are joined
+constexpr int kWorkgroups = 2048;  // that a launch of few rows is split into
+constexpr int kWhole = 64;         // units of a row that is not split
+constexpr int kMaxGrid = 1 << 20;
+constexpr int kBatch = 4;              // 16-byte loads in flight a thread in the gradient
+constexpr size_t kLastLevelBytes = 256u << 20;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // exponents are taken at least this low: the weighted sum multiplies them with a 0, which an infinity would spoil
 constexpr float kLow = -160.f;
@@ -56,55 +63,63 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xFFFFFFFFu)); }
 
-// The row's top values by (value descending, id ascending), by one wave.  seg holds the keys of the maxima of the row's
-// units (64 x N consecutive ids) and is used up; buf holds kMaxTop units.  The top values lie in the top units by
+// Key of the k-th of the lanes' keys (1 <= k <= 64), in every lane: how many stand before a lane's own decides.
+__device__ __forceinline__ uint32_t kth_key(uint32_t key, int k) {
+  const int lane = threadIdx.x & 63;
+  int place = 0;
+#pragma unroll
+  for (int j = 0; j < 64; ++j) {
+    const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)key, j);
+    place += other > key || (other == key && j < lane);
+  }
+  return (uint32_t)__builtin_amdgcn_readlane((int)key, __ffsll((unsigned long long)__ballot(place == k - 1)) - 1);
+}
+
+// The row's top values by (value descending, id ascending), one by one, by one wave: where very many values are equal.
+// keys: the keys of the maxima of the row's units (64 x N consecutive ids).  The top values lie in the top units by
 // (maximum, position): a unit that is not among them has as many values before its own as there are alternatives.
-// Each of these units then offers its best value not yet taken, and the best offer is taken, top times.
+// Every one of these units offers its best value not yet taken, and the best offer is taken, top times.
 template <typename T>
-__device__ void take_top(const T* row, int V, int top, uint32_t* seg, int nseg, u32x4* buf, float m, float inv_t,
-                         float ln_s, int32_t* ids, float* logp) {
+__device__ void take_top_in_turn(const T* row, int V, int top, const uint32_t* keys, int nseg, float m, float temperature,
+                                 float ln_s, int32_t* ids, float* logp) {
   constexpr int N = Chunk16<T>::N;
   const int lane = threadIdx.x & 63;
-  const int per = (nseg + 63) >> 6, first = lane * per;
   const int n = min(top, nseg);
-  uint32_t key = 0;  // lane j: key of the unit it offers, and the unit
+  uint32_t key = 0;  // lane j: key of the unit it holds, and the unit
   int unit = 0x7FFFFFFF;
+  uint32_t bound = 0xFFFFFFFFu;  // the unit chosen last, and its key
+  int after = -1;
   for (int r = 0; r < n; ++r) {
     uint32_t best = 0;
     int at = 0;
-    for (int i = 0; i < per && first + i < nseg; ++i) {
-      const uint32_t k = seg[first + i];
-      if (k > best) best = k, at = first + i;
+    for (int i = lane; i < nseg; i += 64) {
+      const uint32_t k = keys[i];
+      if (k > best && (k < bound || (k == bound && i > after))) best = k, at = i;
     }
     const uint32_t top_key = wave_max_u32(best);
-    const int owner = __ffsll((unsigned long long)__ballot(best == top_key)) - 1;
-    const int chosen = __builtin_amdgcn_readlane(at, owner);
-    if (lane == owner) seg[chosen] = 0;
-    if (lane == r) key = top_key, unit = chosen;
+    const uint32_t low = wave_max_u32(best == top_key ? 0x7FFFFFFFu - (uint32_t)at : 0u);
+    bound = top_key, after = (int)(0x7FFFFFFFu - low);
+    if (lane == r) key = top_key, unit = after;
   }
   // in the order of their ids, so that the first of equal offers is the lowest id
   int rank = 0;
   for (int r = 0; r < n; ++r) rank += __builtin_amdgcn_readlane(unit, r) < unit;
   key = (uint32_t)__builtin_amdgcn_ds_permute(4 * (lane < n ? rank : lane), (int)key);
   unit = __builtin_amdgcn_ds_permute(4 * (lane < n ? rank : lane), unit);
-  for (int r = 0; r < n; ++r) {
-    const int u = __builtin_amdgcn_readlane(unit, r);
-    buf[r * 64 + lane] = load_row(row, (u * 64 + lane) * N, V);
-  }
   int last = -1;  // lane j: id of the last of its unit's values that were taken and equal its offer
   for (int r = 0; r < top; ++r) {
     const uint32_t best = wave_max_u32(lane < n ? key : 0);
     const int j = __ffsll((unsigned long long)__ballot(lane < n && key == best)) - 1;
     const int u = __builtin_amdgcn_readlane(unit, j), taken = __builtin_amdgcn_readlane(last, j);
-    float v[N];
-    unpack16(buf[j * 64 + lane], v);
     const int id0 = (u * 64 + lane) * N;
-    int found = 0x7FFFFFFF;
+    float v[N];
+    unpack16(load_row(row, id0, V), v);
+    int hit = 0x7FFFFFFF;
 #pragma unroll
     for (int i = N - 1; i >= 0; --i)
-      if (key_of(v[i]) == best && id0 + i > taken && id0 + i < V) found = id0 + i;
-    const int who = __ffsll((unsigned long long)__ballot(found != 0x7FFFFFFF)) - 1;
-    const int id = __builtin_amdgcn_readlane(found, who);
+      if (key_of(v[i]) == best && id0 + i > taken && id0 + i < V) hit = id0 + i;
+    const int who = __ffsll((unsigned long long)__ballot(hit != 0x7FFFFFFF)) - 1;
+    const int id = __builtin_amdgcn_readlane(hit, who);
     uint32_t next = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -115,182 +130,381 @@ __device__ void take_top(const T* row, int V, int top, uint32_t* seg, int nseg, 
     if (lane == j) key = next, last = next == best ? id : -1;
     if (lane == 0) {
       ids[r] = id;
-      logp[r] = (of_key(best) - m) * inv_t - ln_s;
+      logp[r] = (of_key(best) - m) / temperature - ln_s;
     }
   }
 }
 
-// One workgroup a row.
-template <typename T, bool TOP>
-__global__ __launch_bounds__(RB) void k_logprobs(const T* __restrict__ z, int64_t stride, int rows, int V, float inv_t,
-                                                 float c, const int32_t* __restrict__ tokens, int top,
-                                                 float* __restrict__ logp, float* __restrict__ entropy,
-                                                 float* __restrict__ stats, int32_t* __restrict__ top_ids,
-                                                 float* __restrict__ top_logp) {
+struct TopLds {
+  uint32_t sample[RB];
+  int units[kMaxUnits];
+  uint2 found[RB];
+  int count;
+};
+
+// The same by a workgroup, where no more than RB values stand at or above a bound that at least `top` values reach.  Such
+// a bound is the top-th of 64 maxima of disjoint parts of the row: of the units' maxima, every 64th in a lane's part, or,
+// in rows of few units, of the threads' own values.  Only units whose maximum reaches the bound are read.  The values
+// found are ranked at once, every thread counting those before its own.
+template <typename T>
+__device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int nseg, TopLds& lds, float m,
+                         float temperature, float ln_s, int32_t* ids, float* logp, const uint32_t (&mine)[kMaxPer]) {
   constexpr int N = Chunk16<T>::N;
-  extern __shared__ u32x4 dyn[];  // TOP: kMaxTop units, then the keys of the units' maxima
-  __shared__ Soft part[RW];
-  u32x4* buf = dyn;
-  uint32_t* seg = reinterpret_cast<uint32_t*>(dyn + top * 64);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int nseg = (int)(((int64_t)V + 64 * N - 1) / (64 * N));
-  for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-    const int token = tokens ? tokens[row] : 0;
+  if (threadIdx.x == 0) lds.count = 0;
+  uint32_t part = 0;
+  int n = 0;  // units to read, the same in every wave
+  if (nseg >= 64) {
+#pragma unroll
+    for (int i = 0; i < kMaxPer; ++i) part = max(part, mine[i]);
+    part = kth_key(part, top);
+#pragma unroll
+    for (int i = 0; i < kMaxPer; ++i) {
+      const unsigned long long b = __ballot(mine[i] >= part);
+      if (wave == 0 && mine[i] >= part) lds.units[n + __popcll(b & ((1ull << lane) - 1))] = i * 64 + lane;
+      n += __popcll(b);
+    }
+  } else {
+    for (int i = threadIdx.x * N; i < V; i += RB * N) {
+      float v[N];
+      unpack16(load_row(row, i, V), v);
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (i + j < V) part = max(part, key_of(v[j]));
+    }
+    lds.sample[threadIdx.x] = part;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < RW; ++w) part = max(part, lds.sample[w * 64 + lane]);
+    part = kth_key(part, top);
+    n = nseg;
+    if (wave == 0 && lane < nseg) lds.units[lane] = lane;
+  }
+  __syncthreads();
+  constexpr int kAhead = 4;
+  for (int r0 = wave; r0 < n; r0 += RW * kAhead) {
+    u32x4 raw[kAhead];
+    int id0[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      id0[j] = (lds.units[min(r0 + j * RW, n - 1)] * 64 + lane) * N;
+      raw[j] = load_row(row, id0[j], V);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (r0 + j * RW >= n) break;
+      float v[N];
+      unpack16(raw[j], v);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint32_t k = key_of(v[i]);
+        if (k >= part && id0[j] + i < V) {
+          const int at = atomicAdd(&lds.count, 1);
+          if (at < RB) lds.found[at] = make_uint2(k, (uint32_t)(id0[j] + i));
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int count = lds.count;
+  if (count > RB) {
+    if (wave == 0) take_top_in_turn(row, V, top, keys, nseg, m, temperature, ln_s, ids, logp);
+  } else if (threadIdx.x < count) {
+    const uint2 own = lds.found[threadIdx.x];
+    int place = 0;
+    for (int j = 0; j < count; ++j) {
+      const uint2 q = lds.found[j];
+      place += q.x > own.x || (q.x == own.x && q.y < own.y);
+    }
+    if (place < top) {
+      ids[place] = (int)own.y;
+      logp[place] = (of_key(own.x) - m) / temperature - ln_s;
+    }
+  }
+  __syncthreads();  // the next row's use of the LDS
+}
+
+// What a row's maximum and sums come to (one lane).
+template <typename T>
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, int token, const Soft& r) {
+  const bool bad = !(r.s == r.s);
+  const float ln_s = logf(r.s);
+  if (a.logp) {
+    const float x = token < a.vocab ? ldf((const T*)a.z + (int64_t)row * a.stride, (size_t)token) : NAN;
+    a.logp[row] = bad || token >= a.vocab ? NAN : x == -INFINITY ? -INFINITY : (x - r.m) / a.temperature - ln_s;
+  }
+  if (a.entropy) a.entropy[row] = bad ? NAN : r.m == -INFINITY ? 0.f : ln_s - kLn2 * r.w / r.s;
+  if (a.stats) {
+    a.stats[2 * (size_t)row] = bad ? NAN : r.m;
+    a.stats[2 * (size_t)row + 1] = bad ? NAN : ln_s;
+  }
+}
+__device__ __forceinline__ void finish_padding(const LogprobArgs& a, int row) {
+  if (a.logp) a.logp[row] = 0.f;
+  if (a.entropy) a.entropy[row] = 0.f;
+  if (a.stats) a.stats[2 * (size_t)row] = 0.f, a.stats[2 * (size_t)row + 1] = 0.f;
+}
+
+// Maximum and sums over the units [lo, hi) of a row, by `waves` waves of which this is number `wave`: this lane's part.
+// Units of one batch are summed apart from what came before: a small term is added to a sum of a few, not to a sum
+// that one large value dominates.
+template <typename T, bool KEYS>
+__device__ __forceinline__ Soft scan_units(const T* zr, int V, float c, int lo, int hi, int wave, int waves,
+                                           uint32_t* keys) {
+  constexpr int N = Chunk16<T>::N;
+  const int lane = threadIdx.x & 63;
+  Soft a = {-INFINITY, 0.f, 0.f};
+  for (int u0 = lo + wave * kUnits; u0 < hi; u0 += waves * kUnits) {
+    u32x4 raw[kUnits];
+    if (u0 + kUnits <= hi && (int64_t)(u0 + kUnits) * 64 * N <= V) {
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j) raw[j] = stream16(zr + (u0 + j) * 64 * N + lane * N);
+    } else {
+      u32x4 none;  // nothing but -inf
+#pragma unroll
+      for (int i = 0; i < 4; ++i) none[i] = N == 4 ? 0xFF800000u : 0xFF80FF80u;
+#pragma unroll
+      for (int j = 0; j < kUnits; ++j)
+        raw[j] = u0 + j < hi ? load_row(zr, (u0 + j) * 64 * N + lane * N, V) : none;
+    }
+    float bm = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      float v[N];
+      unpack16(raw[j], v);
+      float um = v[0];
+#pragma unroll
+      for (int i = 1; i < N; ++i) um = fmaxf(um, v[i]);
+      bm = fmaxf(bm, um);
+      if (KEYS && u0 + j < hi) {
+        const uint32_t k = wave_max_u32(key_of(um));
+        if (lane == 0) keys[u0 + j] = k;
+      }
+    }
+    bm = fmaxf(a.m, bm);
+    const float mm = finite_or_zero(bm);
+    a = moved(a, bm, c);
+    float s = 0.f, w = 0.f;
+#pragma unroll
+    for (int j = 0; j < kUnits; ++j) {
+      float v[N];
+      unpack16(raw[j], v);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float t = (v[i] - mm) * c, e = __builtin_amdgcn_exp2f(t);
+        s += e;
+        w = fmaf(e, fmaxf(t, kLow), w);
+      }
+    }
+    a.s += s;
+    a.w += w;
+  }
+  return a;
+}
+
+// A wave's lanes joined, the same in every lane.
+__device__ __forceinline__ Soft joined_wave(Soft a, float c) {
+  a = moved(a, wave_max(a.m), c);
+  a.s = wave_sum(a.s);
+  a.w = wave_sum(a.w);
+  return a;
+}
+
+__host__ __device__ constexpr int units_of(int V, int N) { return (int)(((int64_t)V + 64 * N - 1) / (64 * N)); }
+
+// A part of a row: chunk blockIdx.y of units_a_chunk units, by TEAM waves (a workgroup's other waves do other rows).
+// With one chunk and no alternatives it is the whole row and its outputs are written here; otherwise the part goes to
+// part[row][chunk] and k_logprobs_join does the rest.
+template <typename T, int TEAM, bool KEYS>
+__global__ __launch_bounds__(RB) void k_logprobs(LogprobArgs a, float c, int units_a_chunk, Soft* __restrict__ part,
+                                                 uint32_t* __restrict__ keys) {
+  constexpr int N = Chunk16<T>::N;
+  __shared__ Soft team[RW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int nseg = units_of(a.vocab, N), chunks = gridDim.y, chunk = blockIdx.y;
+  const int lo = chunk * units_a_chunk, hi = min(lo + units_a_chunk, nseg);
+  for (int row = blockIdx.x * (RW / TEAM) + wave / TEAM; row < a.rows; row += gridDim.x * (RW / TEAM)) {
+    const int token = a.tokens ? a.tokens[row] : 0;
     if (token < 0) {
-      if (threadIdx.x == 0) {
-        if (logp) logp[row] = 0.f;
-        if (entropy) entropy[row] = 0.f;
-        if (stats) stats[2 * (size_t)row] = 0.f, stats[2 * (size_t)row + 1] = 0.f;
-      }
-      if (TOP && threadIdx.x < top) {
-        top_ids[(size_t)row * top + threadIdx.x] = -1;
-        top_logp[(size_t)row * top + threadIdx.x] = 0.f;
-      }
+      if (!part && lane == 0 && wave % TEAM == 0) finish_padding(a, row);
+      continue;  // the same for a whole team
+    }
+    const T* zr = (const T*)a.z + (int64_t)row * a.stride;
+    Soft r = joined_wave(scan_units<T, KEYS>(zr, a.vocab, c, lo, hi, wave % TEAM, TEAM,
+                                             KEYS ? keys + (int64_t)row * nseg : nullptr), c);
+    if (TEAM > 1) {
+      __syncthreads();
+      if (lane == 0) team[wave] = r;
+      __syncthreads();
+      if (wave) continue;
+      r = joined_wave(lane < TEAM ? team[lane] : Soft{-INFINITY, 0.f, 0.f}, c);
+    }
+    if (lane == 0) {
+      if (part)
+        part[(int64_t)row * chunks + chunk] = r;
+      else
+        finish_row<T>(a, row, token, r);
+    }
+  }
+}
+
+// A row's parts joined, and its alternatives: one workgroup a row with alternatives, otherwise one wave.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(RB) void k_logprobs_join(LogprobArgs a, float c, int chunks, const Soft* __restrict__ part,
+                                                      const uint32_t* __restrict__ keys) {
+  constexpr int N = Chunk16<T>::N;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int step = TOP ? 1 : RW;
+  for (int row = blockIdx.x * step + (TOP ? 0 : wave); row < a.rows; row += gridDim.x * step) {
+    // everything that is needed first is asked for at once
+    const int nseg = units_of(a.vocab, N);
+    const Soft mine = lane < chunks ? part[(int64_t)row * chunks + lane] : Soft{-INFINITY, 0.f, 0.f};
+    uint32_t unit_keys[kMaxPer];
+    if (TOP)
+#pragma unroll
+      for (int i = 0; i < kMaxPer; ++i) unit_keys[i] = i * 64 + lane < nseg ? keys[(int64_t)row * nseg + i * 64 + lane] : 0u;
+    const int token = a.tokens ? a.tokens[row] : 0;
+    const size_t t0 = (size_t)row * a.top;
+    if (token < 0) {
+      if (lane == 0 && (!TOP || wave == 0)) finish_padding(a, row);
+      if (TOP && threadIdx.x < a.top) a.top_ids[t0 + threadIdx.x] = -1, a.top_logp[t0 + threadIdx.x] = 0.f;
       continue;
     }
-    const T* zr = z + (int64_t)row * stride;
-    Soft a = {-INFINITY, 0.f, 0.f};
-    for (int u0 = wave * kUnits; u0 < nseg; u0 += RW * kUnits) {
-      u32x4 raw[kUnits];
-#pragma unroll
-      for (int j = 0; j < kUnits; ++j) raw[j] = load_row(zr, min(u0 + j, nseg - 1) * 64 * N + lane * N, V);
-      float bm = -INFINITY;
-#pragma unroll
-      for (int j = 0; j < kUnits; ++j) {
-        float v[N];
-        unpack16(raw[j], v);
-        float um = v[0];
-#pragma unroll
-        for (int i = 1; i < N; ++i) um = fmaxf(um, v[i]);
-        if (u0 + j < nseg) {
-          bm = fmaxf(bm, um);
-          if (TOP) {
-            const uint32_t k = wave_max_u32(key_of(um));
-            if (lane == 0) seg[u0 + j] = k;
-          }
-        }
-      }
-      const float mm = finite_or_zero(fmaxf(a.m, bm));
-      a = moved(a, fmaxf(a.m, bm), c);
-#pragma unroll
-      for (int j = 0; j < kUnits; ++j) {
-        if (u0 + j >= nseg) break;
-        float v[N];
-        unpack16(raw[j], v);
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const float t = (v[i] - mm) * c, e = __builtin_amdgcn_exp2f(t);
-          a.s += e;
-          a.w = fmaf(e, fmaxf(t, kLow), a.w);
-        }
-      }
-    }
-    a = moved(a, wave_max(a.m), c);
-    a.s = wave_sum(a.s);
-    a.w = wave_sum(a.w);
-    __syncthreads();
-    if (lane == 0) part[wave] = a;
-    __syncthreads();
-    if (wave == 0) {
-    float m = part[0].m;
-    for (int i = 1; i < RW; ++i) m = fmaxf(m, part[i].m);
-    Soft r = {m, 0.f, 0.f};
-    for (int i = 0; i < RW; ++i) {
-      const Soft q = moved(part[i], m, c);
-      r.s += q.s;
-      r.w += q.w;
-    }
-    const bool bad = !(r.s == r.s);
-    const float ln_s = logf(r.s);
-    if (lane == 0) {
-      const float x = token < V ? ldf(zr, (size_t)token) : NAN;
-      if (logp) logp[row] = bad || token >= V ? NAN : x == -INFINITY ? -INFINITY : (x - m) * inv_t - ln_s;
-      if (entropy) entropy[row] = bad ? NAN : m == -INFINITY ? 0.f : ln_s - kLn2 * r.w / r.s;
-      if (stats) stats[2 * (size_t)row] = bad ? NAN : m, stats[2 * (size_t)row + 1] = bad ? NAN : ln_s;
-    }
-    if (TOP) {
-      if (bad) {
-        if (lane < top) top_ids[(size_t)row * top + lane] = -1, top_logp[(size_t)row * top + lane] = NAN;
+    const Soft r = joined_wave(mine, c);
+    if constexpr (TOP) {
+      __shared__ TopLds lds;
+      if (!(r.s == r.s)) {
+        if (threadIdx.x < a.top) a.top_ids[t0 + threadIdx.x] = -1, a.top_logp[t0 + threadIdx.x] = NAN;
       } else {
-        // a row of -inf alone: every difference to the maximum is taken as -inf
-        take_top(zr, V, top, seg, nseg, buf, finite_or_zero(m), inv_t, m == -INFINITY ? 0.f : ln_s,
-                 top_ids + (size_t)row * top, top_logp + (size_t)row * top);
+        // a row of -inf alone: every distance to the maximum is -inf
+        take_top((const T*)a.z + (int64_t)row * a.stride, a.vocab, a.top, keys + (int64_t)row * nseg, nseg, lds,
+                 finite_or_zero(r.m), a.temperature, r.m == -INFINITY ? 0.f : logf(r.s), a.top_ids + t0, a.top_logp + t0,
+                 unit_keys);
       }
     }
-    }
-    if (TOP) __syncthreads();  // the next row's keys
+    if (lane == 0 && (!TOP || wave == RW - 1)) finish_row<T>(a, row, token, r);
   }
 }
 
-// z and dz may be the same matrix: a thread reads its values before it writes them.
+// z and dz may be the same matrix: a thread reads its values before it writes them.  A workgroup does one step of a
+// row, kBatch times 16 bytes a thread (more steps a workgroup are slower: 4,096 x 152,064 bf16 488 us with five, 480 with
+// one).  What it writes is not read again soon; what it reads may be in the last-level cache if the matrix fits there
+// (beyond: matrices of more than that): 512 x 152,064 bf16 read past the caches 64.7 us, through them 55.3; 4,096 rows 488
+// and 496.
 template <typename T>
-__global__ __launch_bounds__(RB) void k_logprobs_backward(const T* z, int64_t stride, int rows, int V,
-                                                          float inv_t, const int32_t* __restrict__ tokens,
-                                                          const float* __restrict__ stats,
-                                                          const float* __restrict__ entropy,
-                                                          const float* __restrict__ gp, const float* __restrict__ hp,
-                                                          T* dz, int64_t dz_stride) {
+__global__ __launch_bounds__(RB) void k_logprobs_backward(LogprobGradArgs a, bool beyond) {
   constexpr int N = Chunk16<T>::N;
-  for (int row = blockIdx.x; row < rows; row += gridDim.x) {
-    const T* zr = z + (int64_t)row * stride;
-    T* dr = dz + (int64_t)row * dz_stride;
-    const int token = tokens[row];
-    const float m = stats[2 * (size_t)row], ln_s = stats[2 * (size_t)row + 1];
-    const float g = gp[row], h = hp ? hp[row] : 0.f, H = hp ? entropy[row] : 0.f;
+  const int V = a.vocab, i0 = (blockIdx.x * RB * kBatch + threadIdx.x) * N;
+  const float inv_t = 1.f / a.temperature, c = kLog2e / a.temperature;
+  for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    const T* zr = (const T*)a.z + (int64_t)row * a.stride;
+    T* dr = (T*)a.dz + (int64_t)row * a.dz_stride;
+    const int token = a.tokens[row];
+    const float m = a.stats[2 * (size_t)row], ln_s = a.stats[2 * (size_t)row + 1];
+    const float g = a.g[row], h = a.h ? a.h[row] : 0.f, H = a.h ? a.entropy[row] : 0.f;
     const bool dead = token < 0 || (g == 0.f && h == 0.f) || m == -INFINITY;
-    const float c = inv_t * kLog2e, l2 = ln_s * kLog2e;
-    for (int i = threadIdx.x * N; i < V; i += RB * N) {
-      float v[N], d[N];
-      if (!dead) unpack16(load_row(zr, i, V), v);
+    const float l2 = ln_s * kLog2e, gt = g * inv_t, ht = h * inv_t;
+    const float spoil = token >= V ? NAN : 0.f;
+    u32x4 raw[kBatch];
+    if (!dead) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (dead) {
-          d[j] = 0.f;
-        } else if (token >= V) {
-          d[j] = NAN;
-        } else {
+      for (int b = 0; b < kBatch; ++b) {
+        const int i = i0 + b * RB * N;
+        if (i + N > V)
+          raw[b] = load_row(zr, i, V);
+        else
+          raw[b] = beyond ? stream16(zr + i) : load16(zr + i);
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+      const int i = i0 + b * RB * N;
+      if (i >= V) break;
+      float d[N];
+      if (dead) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) d[j] = 0.f;
+      } else {
+        float v[N];
+        unpack16(raw[b], v);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
           const float t = fmaf(v[j] - m, c, -l2), p = __builtin_amdgcn_exp2f(t);
-          const float k = fmaf(h, fmaf(fmaxf(t, kLow), kLn2, H), g);
-          d[j] = (i + j == token ? fmaf(-p, k, g) : -p * k) * inv_t;
+          const float k = fmaf(ht, fmaf(fmaxf(t, kLow), kLn2, H), gt) + spoil;
+          d[j] = -p * k;
+        }
+        if ((unsigned)(token - i) < (unsigned)N) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) d[j] += i + j == token ? gt : 0.f;
         }
       }
       if (i + N <= V) {
-        store16(dr + i, pack16(d));
+        stream16(dr + i, pack16(d));
       } else {
-        for (int j = 0; i + j < V; ++j) put(dr + i + j, d[j]);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (i + j < V) put(dr + i + j, d[j]);
       }
     }
   }
 }
 
-template <typename T>
-void forward(hipStream_t s, const LogprobArgs& a) {
+struct Split {
+  int chunks, units;  // of a row; units of a chunk
+};
+// Enough workgroups for the whole card where rows are few; a wave's share of a chunk is one batch of loads at least.
+// Short rows stay whole, whose second kernel would take longer than the loads it shares out (8,192 fp32 ids, 1 and 64 rows:
+// 5.2 and 5.4 us whole, 6.8 and 7.5 split; 32,003 ids 7.7 and 10.7 whole, 7.1 and 8.5 split).
+Split split_of(int rows, int nseg) {
+  const int most = nseg <= kWhole ? 1 : std::min(kMaxChunks, nseg / (RW * kUnits));
+  const int want = std::max(1, std::min(most, kWorkgroups / rows));
+  const int units = (nseg + want - 1) / want;
+  return {(nseg + units - 1) / units, units};
+}
+
+template <typename T, bool KEYS>
+void forward(hipStream_t s, const LogprobArgs& a, char* ws) {
   constexpr int N = Chunk16<T>::N;
-  const float inv_t = 1.f / a.temperature, c = (float)(1.4426950408889634 / (double)a.temperature);
-  const unsigned grid = (unsigned)std::min(a.rows, 1 << 20);
-  if (a.top) {
-    const size_t lds = (size_t)a.top * 1024 + ((size_t)a.vocab + 64 * N - 1) / (64 * N) * 4;
-    hipLaunchKernelGGL((k_logprobs<T, true>), dim3(grid), dim3(RB), lds, s, (const T*)a.z, a.stride, a.rows, a.vocab, inv_t,
-                       c, a.tokens, a.top, a.logp, a.entropy, a.stats, a.top_ids, a.top_logp);
-  } else {
-    hipLaunchKernelGGL((k_logprobs<T, false>), dim3(grid), dim3(RB), 0, s, (const T*)a.z, a.stride, a.rows, a.vocab, inv_t, c,
-                       a.tokens, 0, a.logp, a.entropy, a.stats, a.top_ids, a.top_logp);
-  }
+  const float c = (float)(1.4426950408889634 / (double)a.temperature);
+  const int nseg = units_of(a.vocab, N);
+  const Split p = split_of(a.rows, nseg);
+  const bool join = KEYS || p.chunks > 1;
+  Soft* part = join ? (Soft*)ws : nullptr;
+  uint32_t* keys = KEYS ? (uint32_t*)(part + (size_t)a.rows * p.chunks) : nullptr;
+  if (nseg <= kUnits)
+    hipLaunchKernelGGL((k_logprobs<T, 1, KEYS>), dim3(std::min((a.rows + RW - 1) / RW, kMaxGrid)), dim3(RB), 0, s, a, c, nseg,
+                       part, keys);
+  else
+    hipLaunchKernelGGL((k_logprobs<T, RW, KEYS>), dim3(std::min(a.rows, kMaxGrid), p.chunks), dim3(RB), 0, s, a, c, p.units,
+                       part, keys);
+  if (join)
+    hipLaunchKernelGGL((k_logprobs_join<T, KEYS>), dim3(std::min(KEYS ? a.rows : (a.rows + RW - 1) / RW, kMaxGrid)), dim3(RB), 0,
+                       s, a, c, p.chunks, part, keys);
 }
 
 template <typename T>
 void backward(hipStream_t s, const LogprobGradArgs& a) {
-  hipLaunchKernelGGL(k_logprobs_backward<T>, dim3((unsigned)std::min(a.rows, 1 << 20)), dim3(RB), 0, s, (const T*)a.z,
-                     a.stride, a.rows, a.vocab, 1.f / a.temperature, a.tokens, a.stats, a.entropy, a.g, a.h, (T*)a.dz,
-                     a.dz_stride);
+  constexpr int N = Chunk16<T>::N, step = RB * N * kBatch;
+  const bool beyond = (size_t)a.rows * a.vocab * sizeof(T) > kLastLevelBytes;
+  const dim3 grid((a.vocab + step - 1) / step, std::min(a.rows, 65535));
+  hipLaunchKernelGGL(k_logprobs_backward<T>, grid, dim3(RB), 0, s, a, beyond);
 }
 
 }  // namespace
 
-size_t logprobs_workspace(int rows, int vocab, int top) { return 0; }
+// parts, and the keys of the units: for the type with more units
+size_t logprobs_workspace(int rows, int vocab, int top) {
+  size_t chunks = 0;
+  for (int N : {4, 8}) chunks = std::max(chunks, (size_t)split_of(rows, units_of(vocab, N)).chunks);
+  if (!top && chunks == 1) return 0;
+  return (size_t)rows * (chunks * sizeof(Soft) + (top ? (size_t)units_of(vocab, 4) * 4 : 0));
+}
 
 hipError_t launch_logprobs(hipStream_t s, int dtype, const LogprobArgs& a, void* ws) {
-  dtype == ROLLOUT_DTYPE_BF16 ? forward<uint16_t>(s, a) : forward<float>(s, a);
+  if (dtype == ROLLOUT_DTYPE_BF16)
+    a.top ? forward<uint16_t, true>(s, a, (char*)ws) : forward<uint16_t, false>(s, a, (char*)ws);
+  else
+    a.top ? forward<float, true>(s, a, (char*)ws) : forward<float, false>(s, a, (char*)ws);
   return hipGetLastError();
 }
 

@@ -13,23 +13,33 @@ namespace rollout {
 namespace {
 
 constexpr int LB = 256;
-constexpr int kTile = LB * 4;      // tokens of a workgroup's step
-constexpr int kMaxBlocks = 2048;
-constexpr int kSums = 6;           // loss, r, kl, clipped low, clipped high, H
+constexpr int kTile = LB * 4;     // tokens of a workgroup's step
+constexpr int kMaxBlocks = 1024;  // as many as the join has threads
+constexpr int kSums = 6;          // loss, r, kl, clipped low, clipped high, H
+constexpr int kCountSeqs = 8192;  // up to here every workgroup counts the tokens itself
 
 struct Borders {
   double low, high;  // ln(1 - el), ln(1 + eh)
 };
 
-__device__ __forceinline__ double block_sum_f64(double v, double* red) {
+// Sums of K values per thread over the workgroup, in a fixed order, for the threads 0 .. K - 1 (one each).
+template <int K>
+__device__ __forceinline__ double block_sums(const double (&v)[K], double* red) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  double s[K];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if (lane == 0) red[w] = v;
+  for (int k = 0; k < K; ++k) s[k] = v[k];
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+    for (int k = 0; k < K; ++k) s[k] += __shfl_xor(s[k], o, 64);
+  if (lane == 0)
+#pragma unroll
+    for (int k = 0; k < K; ++k) red[w * K + k] = s[k];
   __syncthreads();
   double t = 0.0;
-  for (int i = 0; i < nw; ++i) t += red[i];
+  if (threadIdx.x < K)
+    for (int i = 0; i < nw; ++i) t += red[i * K + threadIdx.x];
   return t;
 }
 
@@ -37,12 +47,18 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int s, int N) {
   return lengths ? max(0, min(lengths[s], N)) : N;
 }
 
-// number of counted tokens
+// Number of counted tokens, in every thread (whole numbers below 2^53: exact in any order).
 __device__ __forceinline__ double count_tokens(const int32_t* lengths, int S, int N, double* red) {
   if (!lengths) return (double)S * N;
   double v = 0.0;
   for (int s = threadIdx.x; s < S; s += blockDim.x) v += length_of(lengths, s, N);
-  return block_sum_f64(v, red);  // whole numbers below 2^53: exact
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v += red[i];
+  return v;
 }
 
 __global__ __launch_bounds__(1024) void k_policy_count(const int32_t* __restrict__ lengths, int S, int N,
@@ -72,16 +88,19 @@ __device__ __forceinline__ void store4(float* p, int n, const float (&v)[4]) {
 
 __global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders border, const double* __restrict__ count,
                                                     double* __restrict__ part) {
-  __shared__ double red[LB / 64];
+  __shared__ double red[LB / 64], sums[LB / 64 * kSums];
   const int S = a.seqs, N = a.max_len;
   const int64_t total = (int64_t)S * N;
-  const float w_all = a.mean == ROLLOUT_MEAN_TOKEN ? (float)(1.0 / fmax(*count, 1.0)) : (float)(1.0 / ((double)S * N));
+  double all = (double)S * N;
+  if (a.mean == ROLLOUT_MEAN_TOKEN) all = fmax(count ? *count : count_tokens(a.lengths, S, N, red), 1.0);
+  const float w_all = (float)(1.0 / all);
   double sum[kSums] = {};
   for (int64_t i0 = (int64_t)blockIdx.x * kTile + threadIdx.x * 4; i0 < total; i0 += (int64_t)gridDim.x * kTile) {
     const int n = (int)min((int64_t)4, total - i0);
     int s = (int)((uint32_t)i0 / (uint32_t)N), t = (int)((uint32_t)i0 - (uint32_t)s * (uint32_t)N);
     int len = length_of(a.lengths, s, N);
     float A = a.adv[s];
+    float ws = a.mean == ROLLOUT_MEAN_SEQUENCE ? (float)(1.0 / ((double)S * max(len, 1))) : w_all;
     bool live[4];
     float adv[4], w[4];
     bool any = false;
@@ -89,13 +108,14 @@ __global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders bo
     for (int j = 0; j < 4; ++j) {
       live[j] = j < n && t < len;
       adv[j] = A;
-      w[j] = a.mean == ROLLOUT_MEAN_SEQUENCE ? (float)(1.0 / ((double)S * max(len, 1))) : w_all;
+      w[j] = ws;
       any |= live[j];
-      if (++t == N && j + 1 < n) {
+      if (++t == N && j + 1 < n) {  // the next sequence begins
         t = 0;
         ++s;
         len = length_of(a.lengths, s, N);
         A = a.adv[s];
+        if (a.mean == ROLLOUT_MEAN_SEQUENCE) ws = (float)(1.0 / ((double)S * max(len, 1)));
       }
     }
     float gl[4] = {}, gh[4] = {};
@@ -136,27 +156,21 @@ __global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders bo
     if (a.grad_logp) store4(a.grad_logp + i0, n, gl);
     if (a.grad_entropy) store4(a.grad_entropy + i0, n, gh);
   }
-#pragma unroll
-  for (int k = 0; k < kSums; ++k) {
-    const double v = block_sum_f64(sum[k], red);
-    if (threadIdx.x == 0) part[(size_t)blockIdx.x * kSums + k] = v;
-  }
+  const double v = block_sums(sum, sums);
+  if (threadIdx.x < kSums) part[(size_t)blockIdx.x * kSums + threadIdx.x] = v;
 }
 
-__global__ __launch_bounds__(LB) void k_policy_join(const double* __restrict__ part, int blocks,
+__global__ __launch_bounds__(kMaxBlocks) void k_policy_join(const double* __restrict__ part, int blocks,
                                                     const int32_t* __restrict__ lengths, int S, int N,
                                                     float* __restrict__ loss, float* __restrict__ stats) {
-  __shared__ double red[LB / 64];
+  __shared__ double red[kMaxBlocks / 64], sums[kMaxBlocks / 64 * kSums];
+  double v[kSums];
+#pragma unroll
+  for (int k = 0; k < kSums; ++k) v[k] = threadIdx.x < blocks ? part[(size_t)threadIdx.x * kSums + k] : 0.0;
   const double c = fmax(count_tokens(lengths, S, N, red), 1.0);
-  for (int k = 0; k < kSums; ++k) {
-    double v = 0.0;
-    for (int b = threadIdx.x; b < blocks; b += LB) v += part[(size_t)b * kSums + k];
-    v = block_sum_f64(v, red);
-    if (threadIdx.x == 0) {
-      if (k == 0 && loss) *loss = (float)v;
-      if (k > 0 && stats) stats[k - 1] = (float)(v / c);
-    }
-  }
+  const double t = block_sums(v, sums);
+  if (threadIdx.x == 0 && loss) *loss = (float)t;
+  if (threadIdx.x > 0 && threadIdx.x < kSums && stats) stats[threadIdx.x - 1] = (float)(t / c);
 }
 
 int blocks_of(int seqs, int max_len) {
@@ -172,10 +186,12 @@ hipError_t launch_policy_loss(hipStream_t s, const PolicyLossArgs& a, void* ws) 
   double* part = count + 2;
   const int blocks = blocks_of(a.seqs, a.max_len);
   const Borders b = {std::log1p(-(double)a.clip_low), std::log1p((double)a.clip_high)};
-  if (a.mean == ROLLOUT_MEAN_TOKEN)
-    hipLaunchKernelGGL(k_policy_count, dim3(1), dim3(1024), 0, s, a.lengths, a.seqs, a.max_len, count);
-  hipLaunchKernelGGL(k_policy_loss, dim3(blocks), dim3(LB), 0, s, a, b, count, part);
-  hipLaunchKernelGGL(k_policy_join, dim3(1), dim3(LB), 0, s, part, blocks, a.lengths, a.seqs, a.max_len, a.loss, a.stats);
+  const bool counted = a.mean == ROLLOUT_MEAN_TOKEN && a.lengths && a.seqs > kCountSeqs;
+  if (counted) hipLaunchKernelGGL(k_policy_count, dim3(1), dim3(1024), 0, s, a.lengths, a.seqs, a.max_len, count);
+  hipLaunchKernelGGL(k_policy_loss, dim3(blocks), dim3(LB), 0, s, a, b, counted ? count : nullptr, part);
+  // the join has a thread for every workgroup's sums, and no more waves than they and the lengths need
+  const int threads = (std::max(blocks, std::min(a.seqs, kMaxBlocks)) + 63) / 64 * 64;
+  hipLaunchKernelGGL(k_policy_join, dim3(1), dim3(threads), 0, s, part, blocks, a.lengths, a.seqs, a.max_len, a.loss, a.stats);
   return hipGetLastError();
 }
 

@@ -10,7 +10,7 @@
 namespace rollout {
 
 constexpr int kMaxTop = 32;            // alternatives of a row
-constexpr int kMaxTopVocab = 1 << 20;  // widest row that alternatives are taken from
+constexpr int kMaxTopVocab = 5 << 16;  // widest row that alternatives are taken from
 
 struct LogprobArgs {
   const void* z;
@@ -100,6 +100,16 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T>
 __device__ __forceinline__ u32x4 load16(const T* p) {
   return *reinterpret_cast<const typename Chunk16<T>::Raw*>(p);
+}
+// the same for data that is read or written once: it does not push other lines out of the caches (log probabilities of
+// 3,584 rows of 152,064 bf16 logits 206 -> 184 us)
+template <typename T>
+__device__ __forceinline__ u32x4 stream16(const T* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const typename Chunk16<T>::Raw*>(p));
+}
+template <typename T>
+__device__ __forceinline__ void stream16(T* p, u32x4 v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<typename Chunk16<T>::Raw*>(p));
 }
 template <typename T>
 __device__ __forceinline__ void store16(T* p, u32x4 v) {

@@ -94,7 +94,7 @@ rollout_status rollout_token_logprobs_workspace(int32_t n_rows, int32_t vocab, i
   if (n_rows < 1 || vocab < 1) return fail(ROLLOUT_EINVAL, "n_rows and vocab must be >= 1");
   if (vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab above 2^30");
   if (n_top < 0 || n_top > kMaxTop || n_top > vocab) return fail(ROLLOUT_EINVAL, "n_top must be in [0, 32] and at most vocab");
-  if (n_top && vocab > kMaxTopVocab) return fail(ROLLOUT_EUNSUPPORTED, "alternatives of more than 2^20 ids");
+  if (n_top && vocab > kMaxTopVocab) return fail(ROLLOUT_EUNSUPPORTED, "alternatives of more than 327,680 ids");
   *h_bytes = logprobs_workspace(n_rows, vocab, n_top);
   return ROLLOUT_OK;
 }

@@ -34,7 +34,7 @@ FORWARD = dict(z=A, dtype=0, stride=100, n=4, V=100, T=1.0, tokens=B, top=0, log
     (R.EINVAL, dict(T=float("nan")), "temperature"), (R.EINVAL, dict(T=1e-40), "temperature"),
     (R.EINVAL, dict(top=-1), "n_top"), (R.EINVAL, dict(top=33, ids=G, tops=H), "n_top"),
     (R.EINVAL, dict(V=3, top=4, ids=G, tops=H), "n_top"),
-    (R.EUNSUPPORTED, dict(V=(1 << 20) + 1, stride=1 << 21, top=1, ids=G, tops=H), "2^20"),
+    (R.EUNSUPPORTED, dict(V=327681, stride=1 << 21, top=1, ids=G, tops=H), "327,680"),
     (R.EINVAL, dict(top=3), "alternatives"), (R.EINVAL, dict(top=3, ids=G), "alternatives"),
     (R.EINVAL, dict(tokens=None), "without tokens"), (R.EINVAL, dict(logp=None, entropy=None, stats=None), "no output"),
 ])
@@ -65,7 +65,7 @@ def test_logprobs_workspace():
     assert R.rollout_token_logprobs_workspace(1, 1) >= 0
     for args in ((0, 10, 0), (1, 0, 0), (1, 10, 11), (1, 100, 33), (1, 100, -1)):
         refuse(R.EINVAL, R.rollout_token_logprobs_workspace, *args)
-    refuse(R.EUNSUPPORTED, R.rollout_token_logprobs_workspace, 1, (1 << 20) + 1, 1)
+    refuse(R.EUNSUPPORTED, R.rollout_token_logprobs_workspace, 1, 327681, 1)
     assert R.lib.rollout_token_logprobs_workspace(1, 10, 0, None) == R.EINVAL
 
 
@@ -75,7 +75,7 @@ def test_tensors_are_checked():
     refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host), text="current device")
     refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host.double()), text="float32")
     refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, tokens=torch.zeros(4, dtype=torch.int64)), text="int32")
-    refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host.bfloat16(), dtype=7), text="dtype 0")
+    refuse(R.EINVAL, R.rollout_token_logprobs, *call(FORWARD, z=host.bfloat16(), dtype=7), text="dtype must be 0")
 
 
 LOSS = dict(lp=A, old=B, ref=C, H=D, adv=E, lengths=F, S=4, N=16, lo=0.2, hi=0.3, kl=0.1, ent=0.01, mean=0, loss=G, stats=G + 64,
