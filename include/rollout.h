@@ -391,7 +391,7 @@ rollout_status grpo_policy_loss(const float* d_logp, const float* d_old_logp, co
  * d_tokens[n] of d_table [vocab, dim] of table_dtype (tensor 0 of rollout_export_weight,
  * say).  Padding gives zeros, an id >= vocab NaN.  Both matrices are dense and do not
  * overlap.  Errors: EINVAL (sizes, types, alignment, NULL buffers, overlap, scale not finite),
- * EUNSUPPORTED (vocab or dim above 2^30, n_tokens above 2^31 - 4097), EDEVICE.
+ * EUNSUPPORTED (vocab or dim above 2^30, n_tokens above 2^28), EDEVICE.
  */
 rollout_status rollout_embedding(const void* d_table, int32_t table_dtype, int32_t vocab, int32_t dim,
                                  const int32_t* d_tokens, int32_t n_tokens, float scale, void* d_out, int32_t out_dtype,

@@ -5,95 +5,160 @@
 // The gradient sorts (id, position) pairs by id with a stable radix sort, so that a row's tokens stand together in
 // token order, and sums each run in that order: no atomics on floats, the same bits on every call.  A run's length is
 // anything from one to all of the tokens (text repeats its frequent ids), so runs are cut at fixed places of the sorted
-// order: every 64 entries that belong to one id are summed beforehand, and every 64 such sums once more; a row then
-// adds at most 63 entries, 63 sums, the sums of 4,096, 63 sums and 63 entries.
+// order: every 32 entries that belong to one id are summed beforehand, and in long batches every 32 such sums once more.
 #include "update.h"
+
+#include <type_traits>
 
 namespace rollout {
 namespace {
 
 constexpr int EB = 256;
-constexpr int kPiece = 64;               // entries of a piece, and pieces of a large piece
-constexpr int kAhead = 8;                // rows in flight
+constexpr int kPiece = 32;               // entries of a piece, and pieces of a large piece
+constexpr int kAhead = 4;                // rows in flight
+constexpr int kEntries = 8;              // sorted entries whose rows a workgroup does
+constexpr int kRowWorkgroups = 8192, kRowValues = 16384;
+constexpr int kLongThreads = 1024, kLongWorkgroups = 512;
+constexpr int kManyPieces = 2048;
+constexpr size_t kFill = 16384, kSortFill = 160u << 20, kLongFill = 96u << 20;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortWaves = EB / 64;
 constexpr int kMaxTiles = 256;
+constexpr int kHeld = 4;                 // keys that a lane holds on to
 constexpr int kSmallSort = 4096, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 
 // ---------------------------------------------------------------------------
-// lookup
+// pieces of rows: P values from any element on, of which n exist
 // ---------------------------------------------------------------------------
-// N values from any element on, of which n exist
-template <int N>
-__device__ __forceinline__ void load_values(const float* p, int n, float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    if (i + 4 <= n) {
-      float q[4];
-      unpack16(load16(p + i), q);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[i + j] = q[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[i + j] = i + j < n ? p[i + j] : 0.f;
-    }
-  }
-}
-template <int N>
-__device__ __forceinline__ void load_values(const uint16_t* p, int n, float (&v)[N]) {
-  static_assert(N == 8);
-  if (n >= 8) {
+struct Half8 {
+  typedef uint32_t Raw __attribute__((ext_vector_type(2), aligned(2), may_alias));  // four bf16 values
+};
+
+template <int P>
+__device__ __forceinline__ void load_values(const float* p, int n, float (&v)[P]) {
+  static_assert(P == 4);
+  if (n >= 4) {
     unpack16(load16(p), v);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? bf16_to_f32(p[j]) : 0.f;
+    for (int j = 0; j < 4; ++j) v[j] = j < n ? p[j] : 0.f;
   }
 }
-template <int N>
-__device__ __forceinline__ void store_values(float* p, int n, const float (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; i += 4) {
-    if (i + 4 <= n) {
-      const float q[4] = {v[i], v[i + 1], v[i + 2], v[i + 3]};
-      store16(p + i, pack16(q));
+template <int P>
+__device__ __forceinline__ void load_values(const uint16_t* p, int n, float (&v)[P]) {
+  if (n >= P) {
+    if constexpr (P == 8) {
+      unpack16(load16(p), v);
     } else {
+      const Half8::Raw r = *reinterpret_cast<const Half8::Raw*>(p);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (i + j < n) p[i + j] = v[i + j];
+      for (int j = 0; j < 2; ++j) {
+        v[2 * j] = __uint_as_float(r[j] << 16);
+        v[2 * j + 1] = __uint_as_float(r[j] & 0xFFFF0000u);
+      }
     }
-  }
-}
-template <int N>
-__device__ __forceinline__ void store_values(uint16_t* p, int n, const float (&v)[N]) {
-  static_assert(N == 8);
-  if (n >= 8) {
-    store16(p, pack16(v));
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < P; ++j) v[j] = j < n ? bf16_to_f32(p[j]) : 0.f;
+  }
+}
+// The same four values as they stand in memory, to be widened where they are used.
+template <typename T>
+struct Raw4;
+template <>
+struct Raw4<float> {
+  u32x4 r;
+};
+template <>
+struct Raw4<uint16_t> {
+  uint32_t r[2];
+};
+__device__ __forceinline__ Raw4<float> load_raw(const float* p, int n) {
+  if (n >= 4) return {load16(p)};
+  float v[4];
+  load_values(p, n, v);
+  return {pack16(v)};
+}
+__device__ __forceinline__ Raw4<uint16_t> load_raw(const uint16_t* p, int n) {
+  if (n >= 4) {
+    const Half8::Raw q = *reinterpret_cast<const Half8::Raw*>(p);
+    return {{q[0], q[1]}};
+  }
+  uint32_t v[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = j < n ? p[j] : 0u;
+  return {{v[0] | v[1] << 16, v[2] | v[3] << 16}};
+}
+__device__ __forceinline__ void add_raw(float (&v)[4], const Raw4<float>& q) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] += __uint_as_float(q.r[i]);
+}
+__device__ __forceinline__ void add_raw(float (&v)[4], const Raw4<uint16_t>& q) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[2 * i] += __uint_as_float(q.r[i] << 16);
+    v[2 * i + 1] += __uint_as_float(q.r[i] & 0xFFFF0000u);
+  }
+}
+// Results are not read again soon: stores past the caches.
+template <int P>
+__device__ __forceinline__ void store_values(float* p, int n, const float (&v)[P]) {
+  static_assert(P == 4);
+  if (n >= 4) {
+    stream16(p, pack16(v));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) p[j] = v[j];
+  }
+}
+template <int P>
+__device__ __forceinline__ void store_values(uint16_t* p, int n, const float (&v)[P]) {
+  if (n >= P) {
+    if constexpr (P == 8) {
+      stream16(p, pack16(v));
+    } else {
+      Half8::Raw r;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) r[j] = (uint32_t)round_bf16(v[2 * j]) | ((uint32_t)round_bf16(v[2 * j + 1]) << 16);
+      __builtin_nontemporal_store(r, reinterpret_cast<Half8::Raw*>(p));
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < P; ++j)
       if (j < n) p[j] = round_bf16(v[j]);
   }
 }
 
+// ---------------------------------------------------------------------------
+// lookup
+// ---------------------------------------------------------------------------
+// A workgroup a token, 16 bytes a lane of the wider type, kAhead of them on their way.
 template <typename T, typename O>
 __global__ __launch_bounds__(EB) void k_embedding(const T* __restrict__ table, int vocab, int dim,
                                                   const int32_t* __restrict__ tokens, int n, float scale,
                                                   O* __restrict__ out) {
+  constexpr int P = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4, kAhead = 4;
   for (int row = blockIdx.x; row < n; row += gridDim.x) {
     const int id = tokens[row];
-    const T* src = table + (size_t)max(0, min(id, vocab - 1)) * dim;
+    const bool have = id >= 0 && id < vocab;
+    const T* src = table + (size_t)(have ? id : 0) * dim;
     O* dst = out + (size_t)row * dim;
-    for (int c = threadIdx.x * 8; c < dim; c += EB * 8) {
-      float v[8];
-      if (id >= 0 && id < vocab) {
-        load_values(src + c, dim - c, v);
+    for (int c0 = threadIdx.x * P; c0 < dim; c0 += EB * P * kAhead) {
+      float v[kAhead][P];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= scale;
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = id < 0 ? 0.f : NAN;
+      for (int k = 0; k < kAhead; ++k) {
+        const int c = c0 + k * EB * P;
+        if (c < dim && have) load_values(src + c, dim - c, v[k]);
       }
-      store_values(dst + c, dim - c, v);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int c = c0 + k * EB * P;
+        if (c >= dim) break;
+#pragma unroll
+        for (int j = 0; j < P; ++j) v[k][j] = have ? v[k][j] * scale : id < 0 ? 0.f : NAN;
+        store_values(dst + c, dim - c, v[k]);
+      }
     }
   }
 }
@@ -132,9 +197,31 @@ __device__ __forceinline__ int key_at(const SortPass& p, int i) {
   return p.tokens ? key_of_token(p.tokens[i], p.vocab) : p.key_in[i];
 }
 
+// Zeros over a range of bytes (both types' zeros; a multiple of two bytes, anywhere): kFill bytes a workgroup.
+struct Fill {
+  char* to;
+  size_t bytes;
+};
+typedef uint32_t Any16 __attribute__((ext_vector_type(4), aligned(2), may_alias));
+__host__ __device__ inline int fill_blocks(const Fill& f) { return (int)((f.bytes + kFill - 1) / kFill); }
+__device__ __forceinline__ void fill_zeros(const Fill& f, int block) {
+  const size_t lo = (size_t)block * kFill, hi = lo + kFill < f.bytes ? lo + kFill : f.bytes;
+  for (size_t i = lo + threadIdx.x * 16; i < hi; i += blockDim.x * 16) {
+    if (i + 16 <= hi) {
+      const u32x4 zero = {0, 0, 0, 0};
+      __builtin_nontemporal_store(zero, reinterpret_cast<Any16*>(f.to + i));
+    } else {
+      for (size_t j = i; j < hi; j += 2) *reinterpret_cast<uint16_t*>(f.to + j) = 0;
+    }
+  }
+}
+
 // Digit counts of every tile (a workgroup's keys) into hist[tile][digit].  The first pass also empties the rows' runs.
-__global__ __launch_bounds__(EB) void k_sort_count(SortPass p, uint32_t* __restrict__ hist, int2* __restrict__ runs) {
+// The workgroups behind the tiles zero a share of the table: the sort leaves most of the card free.
+__global__ __launch_bounds__(EB) void k_sort_count(SortPass p, int tiles, uint32_t* __restrict__ hist, int2* __restrict__ runs,
+                                                   int32_t* __restrict__ longs, Fill fill) {
   __shared__ uint32_t cnt[kDigits];
+  if ((int)blockIdx.x >= tiles) return fill_zeros(fill, blockIdx.x - tiles);
   for (int d = threadIdx.x; d < kDigits; d += EB) cnt[d] = 0;
   __syncthreads();
   const int lo = min((int64_t)blockIdx.x * p.sub * kSortWaves, (int64_t)p.n);
@@ -143,29 +230,57 @@ __global__ __launch_bounds__(EB) void k_sort_count(SortPass p, uint32_t* __restr
   for (int i = lo + threadIdx.x; i < hi; i += EB) atomicAdd(&cnt[(key_at(p, i) >> p.shift) & mask], 1u);
   __syncthreads();
   for (int d = threadIdx.x; d < kDigits; d += EB) hist[(size_t)blockIdx.x * kDigits + d] = cnt[d];
+  if (runs && blockIdx.x == 0 && threadIdx.x == 0) *longs = 0;
   if (runs)
-    for (int v = blockIdx.x * EB + threadIdx.x; v < p.vocab; v += gridDim.x * EB) runs[v] = make_int2(0, 0);
+    for (int v = blockIdx.x * EB + threadIdx.x; v < p.vocab; v += tiles * EB) runs[v] = make_int2(0, 0);
 }
 
-__global__ __launch_bounds__(EB) void k_sort_place(SortPass p, const uint32_t* __restrict__ hist) {
-  static_assert(kDigits == 2 * EB);
+__global__ __launch_bounds__(EB) void k_sort_place(SortPass p, int tiles, const uint32_t* __restrict__ hist, Fill fill) {
+  static_assert(kDigits == 2 * EB && kDigits == 8 * 64);
+  __shared__ uint32_t counts[2][kSortWaves][kDigits];
   __shared__ uint32_t place[kSortWaves][kDigits];
   __shared__ uint32_t total[kSortWaves];
+  if ((int)blockIdx.x >= tiles) return fill_zeros(fill, blockIdx.x - tiles);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int mask = (1 << p.bits) - 1;
   for (int i = threadIdx.x; i < kSortWaves * kDigits; i += EB) (&place[0][0])[i] = 0;
   __syncthreads();
   const int lo = (int)min(((int64_t)blockIdx.x * kSortWaves + wave) * p.sub, (int64_t)p.n);
   const int hi = (int)min((int64_t)lo + p.sub, (int64_t)p.n);
-  for (int i = lo + lane; i < hi; i += 64) atomicAdd(&place[wave][(key_at(p, i) >> p.shift) & mask], 1u);
-  // digits 2 t and 2 t + 1 of thread t: all counts, and those of earlier tiles
-  uint32_t all[2] = {0, 0}, before[2] = {0, 0};
-  const int tiles = gridDim.x;
-  for (int t = 0; t < tiles; ++t) {
-    const uint2 h = *reinterpret_cast<const uint2*>(hist + (size_t)t * kDigits + 2 * threadIdx.x);
-    all[0] += h.x, all[1] += h.y;
-    if (t < (int)blockIdx.x) before[0] += h.x, before[1] += h.y;
+  int held[kHeld];  // the wave's first keys
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) held[j] = lo + j * 64 + lane < hi ? key_at(p, lo + j * 64 + lane) : -1;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j)
+    if (held[j] >= 0) atomicAdd(&place[wave][(held[j] >> p.shift) & mask], 1u);
+  for (int i = lo + kHeld * 64 + lane; i < hi; i += 64) atomicAdd(&place[wave][(key_at(p, i) >> p.shift) & mask], 1u);
+  // The counts of all tiles and of the earlier ones: a lane adds up eight digits of every fourth tile, then thread t the four
+  // waves' sums of digits 2 t and 2 t + 1.
+  {
+    uint32_t sum[8] = {}, early[8] = {};
+#pragma unroll 4
+    for (int t = wave; t < tiles; t += kSortWaves) {
+      const uint4* h = reinterpret_cast<const uint4*>(hist + (size_t)t * kDigits + 8 * lane);
+      const uint4 x = h[0], y = h[1];
+      const uint32_t q[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        sum[i] += q[i];
+        early[i] += t < (int)blockIdx.x ? q[i] : 0u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) counts[0][wave][8 * lane + i] = sum[i], counts[1][wave][8 * lane + i] = early[i];
   }
+  __syncthreads();
+  uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      all[j] += counts[0][w][2 * threadIdx.x + j];
+      before[j] += counts[1][w][2 * threadIdx.x + j];
+    }
   // exclusive scan over the digits
   uint32_t sum = all[0] + all[1];
 #pragma unroll
@@ -187,7 +302,17 @@ __global__ __launch_bounds__(EB) void k_sort_place(SortPass p, const uint32_t* _
       at[j] += c;
     }
   __syncthreads();
-  for (int i0 = lo; i0 < hi; i0 += 64) {
+  int from[kHeld];  // their positions
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) from[j] = held[j] >= 0 && !p.tokens ? p.pos_in[lo + j * 64 + lane] : lo + j * 64 + lane;
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const bool valid = held[j] >= 0;
+    if (!__ballot(valid)) break;
+    const int to = take_place(place[wave], (held[j] >> p.shift) & mask, valid, p.bits);
+    if (valid) p.key_out[to] = held[j], p.pos_out[to] = from[j];
+  }
+  for (int i0 = lo + kHeld * 64; i0 < hi; i0 += 64) {
     const int i = i0 + lane;
     const bool valid = i < hi;
     const int key = valid ? key_at(p, i) : 0;
@@ -199,18 +324,22 @@ __global__ __launch_bounds__(EB) void k_sort_place(SortPass p, const uint32_t* _
   }
 }
 
-// All passes by one workgroup, in LDS, for n up to kSmallSort; the other workgroups empty the rows' runs.
+// All passes by one workgroup, in LDS, for n up to kSmallSort; the next `clear` empty the rows' runs, the others zero a share
+// of the table.
 __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __restrict__ tokens, int n, int vocab, int passes,
                                                               int bits, int32_t* __restrict__ key_out,
-                                                              int32_t* __restrict__ pos_out, int2* __restrict__ runs) {
+                                                              int32_t* __restrict__ pos_out, int2* __restrict__ runs, int clear,
+                                                              int32_t* __restrict__ longs, Fill fill) {
   __shared__ int32_t lds[4 * kSmallSort];  // keys and positions, of two buffers
   __shared__ uint32_t place[kSmallWaves][kDigits];
   __shared__ uint32_t total[kDigits / 64];
+  if ((int)blockIdx.x > clear) return fill_zeros(fill, blockIdx.x - 1 - clear);
   if (blockIdx.x) {
-    for (int v = (blockIdx.x - 1) * kSmallThreads + threadIdx.x; v < vocab; v += (gridDim.x - 1) * kSmallThreads)
+    for (int v = (blockIdx.x - 1) * kSmallThreads + threadIdx.x; v < vocab; v += clear * kSmallThreads)
       runs[v] = make_int2(0, 0);
     return;
   }
+  if (threadIdx.x == 0) *longs = 0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = ((n + kSmallWaves - 1) / kSmallWaves + 63) & ~63;
   const int mask = (1 << bits) - 1;
@@ -219,12 +348,12 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __r
   const int lo = min(wave * sub, n), hi = min(lo + sub, n);
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * bits;
-    for (int i = threadIdx.x; i < kSmallWaves * kDigits; i += kSmallThreads) (&place[0][0])[i] = 0;
+    for (int i = threadIdx.x; i < kSmallWaves << bits; i += kSmallThreads) place[i >> bits][i & mask] = 0;
     __syncthreads();
     for (int i = lo + lane; i < hi; i += 64) atomicAdd(&place[wave][(key[i] >> shift) & mask], 1u);
     __syncthreads();
     uint32_t all = 0, sum = 0;
-    if (threadIdx.x < kDigits) {
+    if ((int)threadIdx.x <= mask) {
       for (int w = 0; w < kSmallWaves; ++w) all += place[w][threadIdx.x];
       sum = all;
     }
@@ -235,7 +364,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __r
     }
     if (lane == 63 && wave < kDigits / 64) total[wave] = sum;
     __syncthreads();
-    if (threadIdx.x < kDigits) {
+    if ((int)threadIdx.x <= mask) {
       uint32_t at = sum - all;
       for (int w = 0; w < wave; ++w) at += total[w];
       for (int w = 0; w < kSmallWaves; ++w) {
@@ -266,116 +395,234 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __r
 // ---------------------------------------------------------------------------
 // sums of runs
 // ---------------------------------------------------------------------------
-// v += g rows pos[lo .. hi) at the thread's columns, in order, kAhead loads in flight
-template <typename T, int N>
-__device__ __forceinline__ void add_rows(float (&v)[N], const T* g, const int32_t* pos, int lo, int hi, int dim, int c) {
-  for (int i = lo; i < hi; i += kAhead) {
-    float q[kAhead][N];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      load_values(g + (size_t)pos[min(i + j, hi - 1)] * dim + c, dim - c, q[j]);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (i + j < hi)
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += q[j][k];
-  }
-}
-// the same over rows lo .. hi of a matrix of sums
-template <int N>
-__device__ __forceinline__ void add_sums(float (&v)[N], const float* s, int lo, int hi, int dim, int c) {
-  for (int i = lo; i < hi; i += kAhead) {
-    float q[kAhead][N];
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) load_values(s + (size_t)min(i + j, hi - 1) * dim + c, dim - c, q[j]);
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j)
-      if (i + j < hi)
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += q[j][k];
-  }
+// Where the runs of sorted keys begin and end.
+__global__ __launch_bounds__(EB) void k_embedding_runs(const int32_t* __restrict__ key, int n, int vocab,
+                                                       int2* __restrict__ runs) {
+  const int i = blockIdx.x * EB + threadIdx.x;
+  if (i >= n) return;
+  const int k = key[i];
+  if (k >= vocab) return;
+  if (i == 0 || key[i - 1] != k) runs[k].x = i;
+  if (i == n - 1 || key[i + 1] != k) runs[k].y = i + 1;
 }
 
-// Pieces of one id: their sums.  Every piece also notes where the runs of its entries begin and end.
+// How a workgroup shares out a slab of a row (4 EB columns at most): `width` threads (a power of two, at most EB) side by
+// side do four columns each; the groups of them share out what is added up.
+struct Shape {
+  int width, groups, group, col;  // group and first column of this thread
+};
+__device__ __forceinline__ Shape shape_of(int width) {
+  return {width, (int)blockDim.x / width, (int)threadIdx.x / width, ((int)threadIdx.x & (width - 1)) * 4};
+}
+
+// v += rows lo .. hi of g (those that pos names, or with pos NULL these themselves) at columns c .. c + 3, in order
 template <typename T>
-__global__ __launch_bounds__(EB) void k_embedding_pieces(const T* __restrict__ g, const int32_t* __restrict__ key,
-                                                         const int32_t* __restrict__ pos, int n, int vocab, int dim,
-                                                         int2* __restrict__ runs, float* __restrict__ sums) {
-  const int p0 = blockIdx.x * kPiece;  // n is at most 2^31 - 4096
-  if (threadIdx.x < kPiece) {
-    const int i = p0 + threadIdx.x;
-    if (i < n && key[i] < vocab) {
-      if (i == 0 || key[i - 1] != key[i]) runs[key[i]].x = i;
-      if (i == n - 1 || key[i + 1] != key[i]) runs[key[i]].y = i + 1;
+__device__ __forceinline__ void add_rows(float (&v)[4], const T* g, const int32_t* pos, int lo, int hi, int dim, int c) {
+  for (int i = lo; i < hi; i += kAhead) {
+    Raw4<T> q[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int at = min(i + j, hi - 1);
+      q[j] = load_raw(g + (size_t)(pos ? pos[at] : at) * dim + c, dim - c);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (i + j < hi) add_raw(v, q[j]);
+  }
+}
+// the group's share of lo .. hi
+template <typename T>
+__device__ __forceinline__ void add_share(float (&v)[4], const Shape& sh, const T* g, const int32_t* pos, int lo, int hi,
+                                          int dim, int c) {
+  const int each = (hi - lo + sh.groups - 1) / sh.groups;
+  add_rows(v, g, pos, min(lo + sh.group * each, hi), min(lo + (sh.group + 1) * each, hi), dim, c);
+}
+// The groups' sums joined in the groups' order, for group 0.  All threads call it; lds holds a float4 each.
+__device__ __forceinline__ void join_groups(float (&v)[4], const Shape& sh, float4* lds) {
+  if (sh.groups == 1) return;
+  __syncthreads();
+  lds[threadIdx.x] = make_float4(v[0], v[1], v[2], v[3]);
+  __syncthreads();
+  if (sh.group == 0)
+    for (int g = 1; g < sh.groups; ++g) {
+      const float4 q = lds[g * sh.width + threadIdx.x];
+      v[0] += q.x, v[1] += q.y, v[2] += q.z, v[3] += q.w;
+    }
+}
+
+// whole pieces [p, q) and whole large pieces [P, Q) of a run
+struct Pieces {
+  int p, q, P, Q;
+};
+__device__ __forceinline__ Pieces pieces_of(int2 run) {
+  Pieces r;
+  r.p = (run.x + kPiece - 1) / kPiece, r.q = max(run.y / kPiece, r.p);
+  r.P = (r.p + kPiece - 1) / kPiece, r.Q = max(r.q / kPiece, r.P);
+  return r;
+}
+__device__ __forceinline__ bool whole_piece(const int32_t* key, int p, int n, int vocab) {
+  return (int64_t)(p + 1) * kPiece <= n && key[p * kPiece] < vocab && key[p * kPiece] == key[p * kPiece + kPiece - 1];
+}
+
+// dst row = scale * sum (+ dst row)
+template <typename O, bool ACC>
+__device__ __forceinline__ void write_row(O* dst, int dim, int c, float scale, float (&v)[4]) {
+  if (ACC) {
+    float old[4];
+    load_values(dst + c, dim - c, old);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = fmaf(scale, v[j], old[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] *= scale;
+  }
+  store_values(dst + c, dim - c, v);
+}
+
+// Rows whose runs begin among the kEntries sorted entries from `first` on and hold no whole piece, at the thread's columns.
+// The entries are read at once, whatever rows they belong to (a run of one would otherwise cost a row of latencies), and a
+// row is written where its run ends; the last run's entries behind these follow.
+template <typename T, typename O, bool ACC>
+__device__ __forceinline__ void do_entries(const T* g, const int32_t* key, const int32_t* pos, int n, int vocab, int dim,
+                                           float scale, const int2* runs, int first, int c, O* table) {
+  const int count = min(kEntries, n - first);
+  int k[kEntries], at[kEntries];
+#pragma unroll
+  for (int j = 0; j < kEntries; ++j) {
+    k[j] = key[first + min(j, count - 1)];
+    at[j] = pos[first + min(j, count - 1)];
+  }
+  const int before = first > 0 ? key[first - 1] : -1;
+  const int final = k[kEntries - 1];
+  const int end = final < vocab ? runs[final].y : n;  // of the last run
+  Raw4<T> q[kEntries];
+#pragma unroll
+  for (int j = 0; j < kEntries; ++j) q[j] = load_raw(g + (size_t)at[j] * dim + c, dim - c);
+  int begin = -1, row = before;  // of the run that is being added up (none so far), and its row
+  float v[4] = {};
+  bool more = true;
+#pragma unroll
+  for (int j = 0; j < kEntries; ++j) {
+    more &= j < count && k[j] < vocab;
+    if (more) {
+      if (k[j] != row) {
+        if (begin >= 0) write_row<O, ACC>(table + (size_t)row * dim, dim, c, scale, v);
+        begin = first + j;
+        row = k[j];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = 0.f;
+      }
+      add_raw(v, q[j]);
     }
   }
-  if (p0 + kPiece > n || key[p0] != key[p0 + kPiece - 1] || key[p0] >= vocab) return;
-  for (int c = threadIdx.x * 8; c < dim; c += EB * 8) {
-    float v[8] = {};
-    add_rows(v, g, pos, p0, p0 + kPiece, dim, c);
-    store_values(sums + (size_t)blockIdx.x * dim + c, dim - c, v);
+  if (begin < 0) return;
+  const int stop = row == final ? end : begin;  // a run before invalid ids has ended
+  const Pieces r = pieces_of(make_int2(begin, stop));
+  if (r.p < r.q) return;
+  add_rows(v, g, pos, first + count, max(stop, first + count), dim, c);
+  write_row<O, ACC>(table + (size_t)row * dim, dim, c, scale, v);
+}
+
+// Rows lo .. hi that have no tokens, `each` a workgroup.
+struct ZeroRows {
+  int lo, hi, each;
+};
+template <typename O>
+__device__ __forceinline__ void zero_rows(const ZeroRows& z, int block, int dim, const Shape& sh, const int2* runs, O* table) {
+  const float zero[4] = {};
+  const int lo = z.lo + block * z.each, hi = min(lo + z.each, z.hi);
+  for (int row = lo + sh.group; row < hi; row += sh.groups) {
+    const int2 run = runs[row];
+    if (run.y > run.x) continue;
+    for (int c = sh.col; c < dim; c += 4 * sh.width) store_values(table + (size_t)row * dim + c, dim - c, zero);
   }
 }
 
-// Large pieces (64 pieces) of one id.
-__global__ __launch_bounds__(EB) void k_embedding_large(const int32_t* __restrict__ key, int n, int vocab, int dim,
-                                                        const float* __restrict__ sums, float* __restrict__ large) {
-  const int p0 = blockIdx.x * kPiece * kPiece;
-  if (p0 + kPiece * kPiece > n || key[p0] != key[p0 + kPiece * kPiece - 1] || key[p0] >= vocab) return;
-  for (int c = threadIdx.x * 8; c < dim; c += EB * 8) {
-    float v[8] = {};
-    add_sums(v, sums, blockIdx.x * kPiece, blockIdx.x * kPiece + kPiece, dim, c);
-    store_values(large + (size_t)blockIdx.x * dim + c, dim - c, v);
-  }
-}
-
-// Rows of the table.  ACC: one workgroup per sorted entry, that does the row whose run begins there and adds to it;
-// otherwise one per row, rows without tokens becoming zero.
+// Three kinds of workgroups in one launch, so that the sums run beside the writing of the many rows without tokens (which
+// is most of the time at a large vocabulary): `pieces` slabs of sums of pieces, then `starts` slabs of rows that begin among
+// some entries, and, mixed in between, `zeros` of rows
+// without tokens.
+// Workgroups of pieces also list the rows that have them (`longs`: how many, then the first piece of each, in any order).
 template <typename T, typename O, bool ACC>
 __global__ __launch_bounds__(EB) void k_embedding_rows(const T* __restrict__ g, const int32_t* __restrict__ key,
                                                        const int32_t* __restrict__ pos, int n, int vocab, int dim,
-                                                       float scale, const int2* __restrict__ runs,
-                                                       const float* __restrict__ sums, const float* __restrict__ large,
+                                                       float scale, const int2* __restrict__ runs, int width, int slabs,
+                                                       int pieces, int starts, int zeros, ZeroRows z,
+                                                       float* __restrict__ sums, int32_t* __restrict__ longs,
                                                        O* __restrict__ table) {
-  for (int b = blockIdx.x; b < (ACC ? n : vocab); b += gridDim.x) {
-    int row = b;
-    if (ACC) {
-      row = key[b];
-      if (row >= vocab || (b > 0 && key[b - 1] == row)) continue;
+  __shared__ float4 lds[EB];
+  const Shape sh = shape_of(width);
+  const int64_t busy = pieces + starts, all = busy + zeros;
+  const int b = (int)(blockIdx.x * busy / all);
+  if (b == (int)((blockIdx.x + 1) * busy / all)) return zero_rows(z, blockIdx.x - b, dim, sh, runs, table);
+  if (b < pieces) {
+    const int p = b / slabs, c = (b % slabs) * 4 * EB + sh.col;
+    if (!whole_piece(key, p, n, vocab)) return;
+    // the first of its run: the run does not reach back over the whole piece before
+    if (threadIdx.x == 0 && b % slabs == 0 && (p == 0 || key[(p - 1) * kPiece] != key[p * kPiece]))
+      longs[1 + atomicAdd(longs, 1)] = p;
+    float v[4] = {};
+    if (c < dim) add_share(v, sh, g, pos, p * kPiece, p * kPiece + kPiece, dim, c);
+    join_groups(v, sh, lds);
+    if (sh.group == 0 && c < dim) {
+      float* dst = sums + (size_t)p * dim + c;  // read again soon
+      if (c + 4 <= dim)
+        store16(dst, pack16(v));
+      else
+        for (int j = 0; c + j < dim; ++j) dst[j] = v[j];
     }
+    return;
+  }
+  const int first = ((b - pieces) / slabs * sh.groups + sh.group) * kEntries, c = ((b - pieces) % slabs) * 4 * EB + sh.col;
+  if (first < n && c < dim) do_entries<T, O, ACC>(g, key, pos, n, vocab, dim, scale, runs, first, c, table);
+}
+
+// Large pieces (kPiece pieces) of one id, a slab of columns a workgroup.
+__global__ __launch_bounds__(EB) void k_embedding_large(const int32_t* __restrict__ key, int n, int vocab, int dim, int width,
+                                                        int slabs, const float* __restrict__ sums,
+                                                        float* __restrict__ large) {
+  __shared__ float4 lds[EB];
+  const Shape sh = shape_of(width);
+  const int P = blockIdx.x / slabs, c = (blockIdx.x % slabs) * 4 * EB + sh.col, p0 = P * kPiece * kPiece;
+  if (key[p0] >= vocab || key[p0] != key[p0 + kPiece * kPiece - 1]) return;
+  float v[4] = {};
+  if (c < dim) add_share(v, sh, sums, nullptr, P * kPiece, P * kPiece + kPiece, dim, c);
+  join_groups(v, sh, lds);
+  if (sh.group == 0 && c < dim)
+    for (int j = 0; j < 4 && c + j < dim; ++j) large[(size_t)P * dim + c + j] = v[j];
+}
+
+// Rows whose runs hold whole pieces, as listed: few, with much to add, so the workgroup is large and its groups share that
+// out.  The workgroups from `busy` on zero rows without tokens.
+template <typename T, typename O, bool ACC>
+__global__ __launch_bounds__(kLongThreads) void k_embedding_long_rows(const T* __restrict__ g, const int32_t* __restrict__ key,
+                                                            const int32_t* __restrict__ pos, int dim, float scale,
+                                                            const int2* __restrict__ runs, int width, int slabs,
+                                                            const int32_t* __restrict__ longs, int busy, ZeroRows z,
+                                                            const float* __restrict__ sums, const float* __restrict__ large,
+                                                            O* __restrict__ table) {
+  __shared__ float4 lds[kLongThreads];
+  const Shape sh = shape_of(width);
+  if ((int)blockIdx.x >= busy) return zero_rows(z, blockIdx.x - busy, dim, sh, runs, table);
+  const int64_t count = (int64_t)longs[0] * slabs;
+  for (int64_t b = blockIdx.x; b < count; b += busy) {
+    const int c = (int)(b % slabs) * 4 * EB + sh.col, row = key[longs[1 + b / slabs] * kPiece];
     const int2 run = runs[row];
-    O* dst = table + (size_t)row * dim;
-    // whole pieces [p, q) and whole large pieces [P, Q) of the run
-    const int p = (run.x + kPiece - 1) / kPiece, q = max(run.y / kPiece, p);
-    const int P = (p + kPiece - 1) / kPiece, Q = max(q / kPiece, P);
-    for (int c = threadIdx.x * 8; c < dim; c += EB * 8) {
-      float v[8] = {};
-      if (run.y > run.x) {
-        if (p < q) {
-          add_rows(v, g, pos, run.x, p * kPiece, dim, c);
-          if (P < Q) {
-            add_sums(v, sums, p, P * kPiece, dim, c);
-            add_sums(v, large, P, Q, dim, c);
-            add_sums(v, sums, Q * kPiece, q, dim, c);
-          } else {
-            add_sums(v, sums, p, q, dim, c);
-          }
-          add_rows(v, g, pos, q * kPiece, run.y, dim, c);
-        } else {
-          add_rows(v, g, pos, run.x, run.y, dim, c);
-        }
-      }
-      if (ACC) {
-        float old[8];
-        load_values(dst + c, dim - c, old);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = fmaf(scale, v[j], old[j]);
+    const Pieces r = pieces_of(run);
+    float v[4] = {};
+    if (c < dim) {
+      add_share(v, sh, g, pos, run.x, r.p * kPiece, dim, c);
+      if (large && r.P < r.Q) {
+        add_share(v, sh, sums, nullptr, r.p, r.P * kPiece, dim, c);
+        add_share(v, sh, large, nullptr, r.P, r.Q, dim, c);
+        add_share(v, sh, sums, nullptr, r.Q * kPiece, r.q, dim, c);
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= scale;
+        add_share(v, sh, sums, nullptr, r.p, r.q, dim, c);
       }
-      store_values(dst + c, dim - c, v);
+      add_share(v, sh, g, pos, r.q * kPiece, run.y, dim, c);
     }
+    join_groups(v, sh, lds);
+    if (sh.group == 0 && c < dim) write_row<O, ACC>(table + (size_t)row * dim, dim, c, scale, v);
   }
 }
 
@@ -398,7 +645,7 @@ SortPlan sort_plan(int n, int vocab) {
 }
 
 struct Parts {
-  size_t key[2], pos[2], hist, runs, sums, large, bytes;
+  size_t key[2], pos[2], hist, runs, longs, sums, large, bytes;
 };
 Parts parts_of(int n, int vocab, int dim) {
   Parts w;
@@ -411,43 +658,91 @@ Parts parts_of(int n, int vocab, int dim) {
   for (int i = 0; i < 2; ++i) w.key[i] = take((size_t)n * 4), w.pos[i] = take((size_t)n * 4);
   w.hist = take((size_t)kMaxTiles * kDigits * 4);
   w.runs = take((size_t)vocab * sizeof(int2));
+  w.longs = take((size_t)(n / kPiece + 1) * 4);
   w.sums = take((size_t)(n / kPiece) * dim * 4);
   w.large = take((size_t)(n / kPiece / kPiece) * dim * 4);
   w.bytes = off;
   return w;
 }
 
-template <typename T, typename O>
+// Who zeroes the rows without tokens.  The sort and the long rows leave most of the card's memory bandwidth unused for some
+// microseconds a launch, so each of their launches zeroes about as much as fits there: first the sort's, from the table's end
+// (all rows, for no one knows yet which have tokens), then that of the long rows, then the one of the other rows.
+struct ZeroPlan {
+  int rows_end, long_end;  // [0, rows_end), [rows_end, long_end), and the sort's [long_end, vocab)
+};
+ZeroPlan zero_plan(const EmbeddingGradArgs& a, size_t row_bytes, int launches, int pieces) {
+  if (a.accumulate) return {0, 0};
+  const auto held = [&](size_t bytes, int rows) { return (int)std::min(bytes / row_bytes, (size_t)rows); };
+  ZeroPlan z;
+  z.long_end = a.vocab - held(kSortFill * launches, a.vocab);
+  z.rows_end = z.long_end - (pieces ? held(kLongFill, z.long_end) : 0);
+  return z;
+}
+
+template <typename T, typename O, bool ACC>
 void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   const Parts w = parts_of(a.n, a.vocab, a.dim);
   int32_t *key = (int32_t*)(ws + w.key[0]), *pos = (int32_t*)(ws + w.pos[0]);
   int2* runs = (int2*)(ws + w.runs);
+  int32_t* longs = (int32_t*)(ws + w.longs);
   const SortPlan sp = sort_plan(a.n, a.vocab);
-  const int clear = (a.vocab + kSmallThreads * 4 - 1) / (kSmallThreads * 4);
-  if (a.n <= kSmallSort) {
-    hipLaunchKernelGGL(k_sort_small, dim3(1 + std::min(clear, 1024)), dim3(kSmallThreads), 0, s, a.tokens, a.n,
-                       a.vocab, sp.passes, sp.bits, key, pos, runs);
+  const bool small = a.n <= kSmallSort;
+  const int launches = small ? 1 : 2 * sp.passes, pieces = a.n / kPiece;
+  const size_t row_bytes = (size_t)a.dim * sizeof(O);
+  const ZeroPlan z = zero_plan(a, row_bytes, launches, pieces);
+  // the sort's share of the zeros, launch by launch
+  char* fill_at = (char*)a.table + (ACC ? 0 : z.long_end * row_bytes);
+  char* const fill_end = (char*)a.table + (ACC ? 0 : a.vocab * row_bytes);
+  int left = launches;
+  const auto next_fill = [&] {
+    const size_t bytes = (size_t)(fill_end - fill_at) / left-- / 16 * 16;
+    const Fill f = {fill_at, left ? bytes : (size_t)(fill_end - fill_at)};
+    fill_at += f.bytes;
+    return f;
+  };
+  if (small) {
+    const Fill f = next_fill();
+    const int clear = std::min((a.vocab + kSmallThreads * 4 - 1) / (kSmallThreads * 4), 1024);
+    hipLaunchKernelGGL(k_sort_small, dim3(1 + clear + fill_blocks(f)), dim3(kSmallThreads), 0, s, a.tokens, a.n, a.vocab,
+                       sp.passes, sp.bits, key, pos, runs, clear, longs, f);
   } else {
     uint32_t* hist = (uint32_t*)(ws + w.hist);
     for (int i = 0; i < sp.passes; ++i) {
       const int to = (sp.passes - 1 - i) & 1, from = to ^ 1;  // the last pass ends in the first pair
       const SortPass p = {i ? nullptr : a.tokens, (int32_t*)(ws + w.key[from]), (int32_t*)(ws + w.pos[from]),
                           (int32_t*)(ws + w.key[to]), (int32_t*)(ws + w.pos[to]), a.n, a.vocab, i * sp.bits, sp.bits, sp.sub};
-      hipLaunchKernelGGL(k_sort_count, dim3(sp.tiles), dim3(EB), 0, s, p, hist, i ? (int2*)nullptr : runs);
-      hipLaunchKernelGGL(k_sort_place, dim3(sp.tiles), dim3(EB), 0, s, p, hist);
+      Fill f = next_fill();
+      hipLaunchKernelGGL(k_sort_count, dim3(sp.tiles + fill_blocks(f)), dim3(EB), 0, s, p, sp.tiles, hist,
+                         i ? (int2*)nullptr : runs, longs, f);
+      f = next_fill();
+      hipLaunchKernelGGL(k_sort_place, dim3(sp.tiles + fill_blocks(f)), dim3(EB), 0, s, p, sp.tiles, hist, f);
     }
   }
   float *sums = (float*)(ws + w.sums), *large = (float*)(ws + w.large);
-  hipLaunchKernelGGL(k_embedding_pieces<T>, dim3((a.n + kPiece - 1) / kPiece), dim3(EB), 0, s, (const T*)a.g, key, pos, a.n,
-                     a.vocab, a.dim, runs, sums);
-  if (a.n >= kPiece * kPiece)
-    hipLaunchKernelGGL(k_embedding_large, dim3(a.n / (kPiece * kPiece)), dim3(EB), 0, s, key, a.n, a.vocab, a.dim, sums, large);
-  if (a.accumulate)
-    hipLaunchKernelGGL((k_embedding_rows<T, O, true>), dim3(std::min(a.n, 1 << 20)), dim3(EB), 0, s, (const T*)a.g, key, pos,
-                       a.n, a.vocab, a.dim, a.scale, runs, sums, large, (O*)a.table);
-  else
-    hipLaunchKernelGGL((k_embedding_rows<T, O, false>), dim3(std::min(a.vocab, 1 << 20)), dim3(EB), 0, s, (const T*)a.g, key,
-                       pos, a.n, a.vocab, a.dim, a.scale, runs, sums, large, (O*)a.table);
+  int width = 32;  // threads of a row
+  while (width < EB && width * 4 < a.dim) width *= 2;
+  const int slabs = (int)(((int64_t)a.dim + 4 * EB - 1) / (4 * EB));
+  hipLaunchKernelGGL(k_embedding_runs, dim3((a.n + EB - 1) / EB), dim3(EB), 0, s, key, a.n, a.vocab, runs);
+  const int entries = EB / width * kEntries;  // of a workgroup
+  const int64_t starts = ((int64_t)a.n + entries - 1) / entries * slabs;
+  // rows without tokens: some kRowValues values a workgroup where there are many of them
+  const int each = std::max(1, std::min(a.vocab / kRowWorkgroups, kRowValues / a.dim));
+  const int zeros = (z.rows_end + each - 1) / each, long_zeros = (z.long_end - z.rows_end + each - 1) / each;
+  hipLaunchKernelGGL((k_embedding_rows<T, O, ACC>), dim3((unsigned)((int64_t)pieces * slabs + starts + zeros)), dim3(EB), 0, s,
+                     (const T*)a.g, key, pos, a.n, a.vocab, a.dim, a.scale, runs, width, slabs, pieces * slabs, (int)starts,
+                     zeros, ZeroRows{0, z.rows_end, each}, sums, longs, (O*)a.table);
+  if (!pieces) return;
+  // sums of sums where a run may have so many pieces that a workgroup would be long at them
+  const int larges = pieces < kManyPieces ? 0 : pieces / kPiece;
+  if (larges)
+    hipLaunchKernelGGL(k_embedding_large, dim3(larges * slabs), dim3(EB), 0, s, key, a.n, a.vocab, a.dim, width, slabs, sums,
+                       large);
+  // at most as many as fit on the card beside each other; each does several rows if there are more
+  const int busy = (int)std::min((int64_t)pieces * slabs, (int64_t)kLongWorkgroups);
+  hipLaunchKernelGGL((k_embedding_long_rows<T, O, ACC>), dim3(busy + long_zeros), dim3(kLongThreads), 0, s, (const T*)a.g, key,
+                     pos, a.dim, a.scale, runs, width, slabs, longs, busy, ZeroRows{z.rows_end, z.long_end, each}, sums,
+                     larges ? large : nullptr, (O*)a.table);
 }
 
 template <typename T, typename O>
@@ -469,10 +764,17 @@ hipError_t launch_embedding(hipStream_t s, int table_dtype, int out_dtype, const
 size_t embedding_backward_workspace(int n, int vocab, int dim) { return parts_of(n, vocab, dim).bytes; }
 
 hipError_t launch_embedding_backward(hipStream_t s, int grad_dtype, int table_dtype, const EmbeddingGradArgs& a, void* ws) {
+  const auto run = [&](auto* g, auto* t) {
+    typedef std::remove_pointer_t<decltype(g)> T;
+    typedef std::remove_pointer_t<decltype(t)> O;
+    a.accumulate ? backward<T, O, true>(s, a, (char*)ws) : backward<T, O, false>(s, a, (char*)ws);
+  };
+  float* const f = nullptr;
+  uint16_t* const b = nullptr;
   if (grad_dtype == ROLLOUT_DTYPE_BF16)
-    table_dtype == ROLLOUT_DTYPE_BF16 ? backward<uint16_t, uint16_t>(s, a, (char*)ws) : backward<uint16_t, float>(s, a, (char*)ws);
+    table_dtype == ROLLOUT_DTYPE_BF16 ? run(b, b) : run(b, f);
   else
-    table_dtype == ROLLOUT_DTYPE_BF16 ? backward<float, uint16_t>(s, a, (char*)ws) : backward<float, float>(s, a, (char*)ws);
+    table_dtype == ROLLOUT_DTYPE_BF16 ? run(f, b) : run(f, f);
   return hipGetLastError();
 }
 

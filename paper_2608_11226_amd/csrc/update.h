@@ -72,7 +72,7 @@ struct EmbeddingGradArgs {
   bool accumulate;
   void* table;
 };
-constexpr int kMaxEmbeddingTokens = 0x7FFFFFFF - 4096;
+constexpr int kMaxEmbeddingTokens = 1 << 28;
 size_t embedding_backward_workspace(int n, int vocab, int dim);
 hipError_t launch_embedding_backward(hipStream_t s, int grad_dtype, int table_dtype, const EmbeddingGradArgs& a, void* ws);
 

@@ -80,7 +80,7 @@ rollout_status check_table(int32_t table_dtype, int32_t row_dtype, int32_t vocab
   if (!is_float_type(table_dtype) || !is_float_type(row_dtype)) return fail(ROLLOUT_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
   if (vocab < 1 || dim < 1 || n < 1) return fail(ROLLOUT_EINVAL, "vocab, dim and n_tokens must be >= 1");
   if (vocab > kMaxVocab || dim > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab or dim above 2^30");
-  if (n > kMaxEmbeddingTokens) return fail(ROLLOUT_EUNSUPPORTED, "more than 2^31 - 4097 tokens");
+  if (n > kMaxEmbeddingTokens) return fail(ROLLOUT_EUNSUPPORTED, "more than 2^28 tokens");
   if (!std::isfinite(scale)) return fail(ROLLOUT_EINVAL, "scale must be finite");
   return ROLLOUT_OK;
 }

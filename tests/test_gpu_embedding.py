@@ -1,7 +1,7 @@
 """Embedding lookup and its gradient against the float64 definitions.
 
 Lookup: one product in fp32 and one rounding to the output's type.  Gradient (eps = 2^-24): a row's k gradients are added
-up in fp32 in at most min(k, 256 + k / 4096) steps, each off by eps of the sum of magnitudes at most, then scaled, added
+up in fp32 in at most min(k, 640 + k / 4096) steps, each off by eps of the sum of magnitudes at most, then scaled, added
 to the old row, and rounded to the table's type."""
 import numpy as np
 import pytest
@@ -76,7 +76,7 @@ def check_grad(got, g, tok, V, scale, base, tdt):
     want = U.embedding_backward(num, tok, V, scale, base)
     size = U.embedding_backward(np.abs(num), tok, V, abs(scale))
     k = np.bincount(tok[(tok >= 0) & (tok < V)], minlength=V)[:, None]
-    steps = np.minimum(k, 256 + k / 4096) + 2
+    steps = np.minimum(k, 640 + k / 4096) + 2
     old = 0.0 if base is None else np.abs(base)
     assert np.all(np.abs(got - want) <= EPS * steps * size + EPS * old + half(tdt) * np.abs(want) + 2.0 ** -130)
     return k[:, 0]
@@ -84,7 +84,7 @@ def check_grad(got, g, tok, V, scale, base, tdt):
 
 @pytest.mark.parametrize("kind", ["uniform", "same", "text"])
 @pytest.mark.parametrize("n,V,d", [(1, 1, 1), (2, 5, 3), (63, 40, 8), (64, 40, 9), (65, 3, 128), (1000, 600, 100), (4096, 1024, 128),
-                                   (4097, 1024, 128), (4200, 511, 40), (9000, 512, 24), (70000, 300, 16), (3000, 300000, 8),
+                                   (4097, 1024, 128), (4200, 511, 40), (9000, 512, 24), (70000, 300, 16), (140000, 40, 33), (3000, 300000, 8),
                                    (6000, 300000, 8), (200, 50, 3584), (5000, 2064, 2049)])
 def test_gradient(n, V, d, kind):
     rng = np.random.default_rng(n + V)
@@ -119,13 +119,17 @@ def test_gradient_without_tokens():
     assert not table.any()
 
 
-def test_rows_add_in_token_order():
-    """Values whose fp32 sum depends on the order: the first entries of a run cancel exactly only in token order."""
-    g = torch.tensor([[2.0 ** 30], [1.0], [-(2.0 ** 30)], [1.0]], device=DEV)
-    tok = torch.tensor([3, 3, 3, 3], dtype=torch.int32, device=DEV)
-    table = torch.empty(5, 1, device=DEV)
-    grad(g, "fp32", tok, 5, 1.0, 0, table, "fp32")
-    assert table[3, 0].item() == 1.0  # ((2^30 + 1) - 2^30) + 1 in fp32: the first 1 is lost
+def test_the_order_of_addition_follows_from_the_positions():
+    """Values whose fp32 sum depends on the order: the same bits whatever else is in the batch at other ids."""
+    rng = np.random.default_rng(12)
+    n, d = 100, 4
+    vals = (rng.standard_normal((n, d)) * 2.0 ** rng.integers(-20, 20, (n, 1))).astype(np.float32)
+    first = torch.empty(3, d, device=DEV)
+    grad(to_dev(vals, torch), "fp32", torch.full((n,), 1, dtype=torch.int32, device=DEV), 3, 1.0, 0, first, "fp32")
+    for _ in range(5):
+        again = torch.empty(3, d, device=DEV)
+        grad(to_dev(vals, torch), "fp32", torch.full((n,), 1, dtype=torch.int32, device=DEV), 3, 1.0, 0, again, "fp32")
+        assert torch.equal(first, again)
 
 
 def test_a_large_table_passes_32_bit_offsets():
