@@ -20,6 +20,7 @@ constexpr int kMaxUnits = kMaxTopVocab / 256, kMaxPer = kMaxUnits / 64;  // of a
 constexpr int kMaxChunks = 64;     // a lane each when parts are joined
 constexpr int kWorkgroups = 2048;  // that a launch of few rows is split into
 constexpr int kWhole = 64;         // units of a row that is not split
+constexpr int kWaveRows = 1024;    // rows from which such a row is one wave's
 constexpr int kMaxGrid = 1 << 20;
 constexpr int kBatch = 4;              // 16-byte loads in flight a thread in the gradient
 constexpr size_t kLastLevelBytes = 256u << 20;
@@ -224,15 +225,16 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
   __syncthreads();  // the next row's use of the LDS
 }
 
-// What a row's maximum and sums come to (one lane).
+// The token's logit (NaN: there is no such id, or no token is asked for).
 template <typename T>
-__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, int token, const Soft& r) {
+__device__ __forceinline__ float token_logit(const LogprobArgs& a, int row, int token) {
+  return a.logp && token < a.vocab ? ldf((const T*)a.z + (int64_t)row * a.stride, (size_t)token) : NAN;
+}
+// What a row's maximum and sums come to (one lane); x: its token's logit.
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row, float x, const Soft& r) {
   const bool bad = !(r.s == r.s);
   const float ln_s = logf(r.s);
-  if (a.logp) {
-    const float x = token < a.vocab ? ldf((const T*)a.z + (int64_t)row * a.stride, (size_t)token) : NAN;
-    a.logp[row] = bad || token >= a.vocab ? NAN : x == -INFINITY ? -INFINITY : (x - r.m) / a.temperature - ln_s;
-  }
+  if (a.logp) a.logp[row] = bad ? NAN : x == -INFINITY ? -INFINITY : (x - r.m) / a.temperature - ln_s;
   if (a.entropy) a.entropy[row] = bad ? NAN : r.m == -INFINITY ? 0.f : ln_s - kLn2 * r.w / r.s;
   if (a.stats) {
     a.stats[2 * (size_t)row] = bad ? NAN : r.m;
@@ -330,6 +332,7 @@ __global__ __launch_bounds__(RB) void k_logprobs(LogprobArgs a, float c, int uni
       continue;  // the same for a whole team
     }
     const T* zr = (const T*)a.z + (int64_t)row * a.stride;
+    const float x = part ? 0.f : token_logit<T>(a, row, token);  // on its way meanwhile
     Soft r = joined_wave(scan_units<T, KEYS>(zr, a.vocab, c, lo, hi, wave % TEAM, TEAM,
                                              KEYS ? keys + (int64_t)row * nseg : nullptr), c);
     if (TEAM > 1) {
@@ -343,7 +346,7 @@ __global__ __launch_bounds__(RB) void k_logprobs(LogprobArgs a, float c, int uni
       if (part)
         part[(int64_t)row * chunks + chunk] = r;
       else
-        finish_row<T>(a, row, token, r);
+        finish_row(a, row, x, r);
     }
   }
 }
@@ -370,6 +373,7 @@ __global__ __launch_bounds__(RB) void k_logprobs_join(LogprobArgs a, float c, in
       if (TOP && threadIdx.x < a.top) a.top_ids[t0 + threadIdx.x] = -1, a.top_logp[t0 + threadIdx.x] = 0.f;
       continue;
     }
+    const float x = token_logit<T>(a, row, token);
     const Soft r = joined_wave(mine, c);
     if constexpr (TOP) {
       __shared__ TopLds lds;
@@ -382,21 +386,23 @@ __global__ __launch_bounds__(RB) void k_logprobs_join(LogprobArgs a, float c, in
                  unit_keys);
       }
     }
-    if (lane == 0 && (!TOP || wave == RW - 1)) finish_row<T>(a, row, token, r);
+    if (lane == 0 && (!TOP || wave == RW - 1)) finish_row(a, row, x, r);
   }
 }
 
-// z and dz may be the same matrix: a thread reads its values before it writes them.  A workgroup does one step of a
-// row, kBatch times 16 bytes a thread (more steps a workgroup are slower: 4,096 x 152,064 bf16 488 us with five, 480 with
-// one).  What it writes is not read again soon; what it reads may be in the last-level cache if the matrix fits there
-// (beyond: matrices of more than that): 512 x 152,064 bf16 read past the caches 64.7 us, through them 55.3; 4,096 rows 488
-// and 496.
+// z and dz may be the same matrix: a thread reads its values before it writes them.  `team` threads (a power of two) do one
+// step of a row, `loads` (at most kBatch) times 16 bytes a thread; a workgroup does several short rows.  More than one step a
+// workgroup is slower (4,096 x 152,064 bf16 488 us with five, 480 with one).  What is written is not read again soon; what is
+// read may be in the last-level cache if the matrix fits there (beyond: matrices of more than that): 512 x 152,064 bf16 read
+// past the caches 64.7 us, through them 55.3; 4,096 rows 488 and 496.
 template <typename T>
-__global__ __launch_bounds__(RB) void k_logprobs_backward(LogprobGradArgs a, bool beyond) {
+__global__ __launch_bounds__(RB) void k_logprobs_backward(LogprobGradArgs a, int team, int loads, bool beyond) {
   constexpr int N = Chunk16<T>::N;
-  const int V = a.vocab, i0 = (blockIdx.x * RB * kBatch + threadIdx.x) * N;
+  const int V = a.vocab, each = RB / team;
+  const int i0 = (blockIdx.x * team * loads + (threadIdx.x & (team - 1))) * N;
   const float inv_t = 1.f / a.temperature, c = kLog2e / a.temperature;
-  for (int row = blockIdx.y; row < a.rows; row += gridDim.y) {
+  for (int64_t r0 = (int64_t)blockIdx.y * each + threadIdx.x / team; r0 < a.rows; r0 += (int64_t)gridDim.y * each) {
+    const int row = (int)r0;
     const T* zr = (const T*)a.z + (int64_t)row * a.stride;
     T* dr = (T*)a.dz + (int64_t)row * a.dz_stride;
     const int token = a.tokens[row];
@@ -409,7 +415,8 @@ __global__ __launch_bounds__(RB) void k_logprobs_backward(LogprobGradArgs a, boo
     if (!dead) {
 #pragma unroll
       for (int b = 0; b < kBatch; ++b) {
-        const int i = i0 + b * RB * N;
+        const int i = i0 + b * team * N;
+        if (b >= loads || i >= V) break;
         if (i + N > V)
           raw[b] = load_row(zr, i, V);
         else
@@ -418,8 +425,8 @@ __global__ __launch_bounds__(RB) void k_logprobs_backward(LogprobGradArgs a, boo
     }
 #pragma unroll
     for (int b = 0; b < kBatch; ++b) {
-      const int i = i0 + b * RB * N;
-      if (i >= V) break;
+      const int i = i0 + b * team * N;
+      if (b >= loads || i >= V) break;
       float d[N];
       if (dead) {
 #pragma unroll
@@ -471,7 +478,9 @@ void forward(hipStream_t s, const LogprobArgs& a, char* ws) {
   const bool join = KEYS || p.chunks > 1;
   Soft* part = join ? (Soft*)ws : nullptr;
   uint32_t* keys = KEYS ? (uint32_t*)(part + (size_t)a.rows * p.chunks) : nullptr;
-  if (nseg <= kUnits)
+  // A wave a row where rows are short and many, so that no wave waits for others over a few loads (fp32, 20,000 rows of 2,064
+  // ids 30 us, 41 by workgroups; 2,000 of 4,099 bf16 8.7 and 9.5; 300 rows of 4,099 fp32 are faster by workgroups).
+  if (nseg <= kUnits || (nseg <= kWhole && a.rows >= kWaveRows))
     hipLaunchKernelGGL((k_logprobs<T, 1, KEYS>), dim3(std::min((a.rows + RW - 1) / RW, kMaxGrid)), dim3(RB), 0, s, a, c, nseg,
                        part, keys);
   else
@@ -484,10 +493,15 @@ void forward(hipStream_t s, const LogprobArgs& a, char* ws) {
 
 template <typename T>
 void backward(hipStream_t s, const LogprobGradArgs& a) {
-  constexpr int N = Chunk16<T>::N, step = RB * N * kBatch;
+  constexpr int N = Chunk16<T>::N;
   const bool beyond = (size_t)a.rows * a.vocab * sizeof(T) > kLastLevelBytes;
-  const dim3 grid((a.vocab + step - 1) / step, std::min(a.rows, 65535));
-  hipLaunchKernelGGL(k_logprobs_backward<T>, grid, dim3(RB), 0, s, a, beyond);
+  int team = 1;
+  while (team < RB && team * N * kBatch < a.vocab) team *= 2;
+  // steps of about the same size: a row a little longer than a step is not a step and a rest
+  const int all = (a.vocab + team * N - 1) / (team * N), steps = (all + kBatch - 1) / kBatch, loads = (all + steps - 1) / steps;
+  const int each = RB / team;
+  hipLaunchKernelGGL(k_logprobs_backward<T>, dim3(steps, std::min((a.rows + each - 1) / each, 65535)), dim3(RB), 0, s, a, team,
+                     loads, beyond);
 }
 
 }  // namespace

@@ -108,6 +108,47 @@ def test_gradient(n, V, d, kind):
         assert torch.equal(table[untouched], base[untouched])
 
 
+@pytest.mark.parametrize("kind", ["text", "same"])
+def test_gradient_of_more_than_a_million_tokens(kind):
+    """Tiles longer than what a lane holds on to, more tokens than a lookup's grid has workgroups, and, all of one id, sums of
+    sums of pieces."""
+    n, V, d = 1_100_000, 1000, 4
+    rng = np.random.default_rng(3)
+    tok = ids(kind, n, V, rng)
+    td = to_dev(tok, torch)
+    log(f"{n} tokens, {kind}")
+    g = matrix(n, d, "fp32", rng)
+    table = torch.empty(V, d, device=DEV)
+    grad(g, "fp32", td, V, 1.0, 0, table, "fp32")
+    check_grad(table.double().cpu().numpy(), g, tok, V, 1.0, None, "fp32")
+    out = torch.empty(n, d, device=DEV)
+    R.rollout_embedding(table, 0, V, d, td, n, 1.0, out, 0)
+    live = (td >= 0) & (td < V)
+    assert torch.equal(out[live], table[td[live].long()]) and not out[td < 0].any()
+    assert torch.isnan(out[td >= V]).all()
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(9)
+    n, V, d = 6000, 900, 64
+    g = [matrix(n, d, "fp32", rng) for _ in range(2)]
+    tok = to_dev(ids("text", n, V, rng), torch)
+    want = [torch.empty(V, d, device=DEV) for _ in range(2)]
+    for i in range(2):
+        grad(g[i], "fp32", tok, V, 1.0, 0, want[i], "fp32")
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [torch.empty(V, d, device=DEV) for _ in range(2)]
+    ws = [torch.empty(R.rollout_embedding_backward_workspace(n, V, d), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for i in range(2):
+            grad(g[i], "fp32", tok, V, 1.0, 0, got[i], "fp32", streams[i].cuda_stream, ws[i])
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
 def test_gradient_without_tokens():
     rng = np.random.default_rng(0)
     g = matrix(100, 12, "fp32", rng)

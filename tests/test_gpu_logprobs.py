@@ -354,3 +354,64 @@ def test_repeats_streams_and_graphs():
             for k, x in zip(("logp", "entropy", "stats", "ids", "top_logp"), out):
                 assert torch.equal(eager[k], x), (replay, k)
             assert torch.equal(grad, out[5])
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """More rows than the grids hold: workgroups go on to further rows, with alternatives and without, and back."""
+    for n, V, top in ((1100000, 5, 2), (70000, 4100, 0)):
+        z = torch.randn(n, V, device=DEV, dtype=torch.bfloat16) * 3
+        tok = torch.randint(-1, V, (n,), device=DEV, dtype=torch.int32)
+        log(f"many rows: {n} x {V}")
+        got = forward(z, V, V, 1.0, tok, top, "bf16")
+        lp = torch.log_softmax(z.double(), 1)
+        live = tok >= 0
+        want = lp.gather(1, tok.clamp(min=0).long()[:, None])[:, 0] * live
+        assert (got["logp"] - want).abs().max().item() <= EPS * (V / 64 + 200)  # distances of at most 27, entropies of at most 9
+        if top:
+            order = torch.sort(z.double(), dim=1, descending=True, stable=True)[1][:, :top].int()
+            assert torch.equal(got["ids"], torch.where(live[:, None], order, -1))
+        g = torch.randn(n, device=DEV)
+        out = torch.empty_like(z)
+        R.rollout_token_logprobs_backward(z, R.DTYPE_BF16, V, n, V, 1.0, tok, got["stats"], None, g, None, out, V)
+        dz = -lp.exp() * (g * live)[:, None].double()
+        dz.scatter_add_(1, tok.clamp(min=0).long()[:, None], (g * live).double()[:, None])
+        assert ((out.double() - dz).abs() <= 2.0 ** -8 * dz.abs() + 200 * EPS * g.abs()[:, None]).all()
+
+
+def test_two_streams_at_once():
+    """Calls of two streams side by side, each with its own workspace."""
+    n, V, top = 64, 50257, 8
+    zs = [torch.randn(n, V, device=DEV) * 3 for _ in range(2)]
+    tok = torch.randint(0, V, (n,), device=DEV, dtype=torch.int32)
+    want = [forward(z, V, V, 1.0, tok, top) for z in zs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i] = forward(zs[i], V, V, 1.0, tok, top, stream=streams[i].cuda_stream)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for k in ("logp", "entropy", "stats", "ids", "top_logp"):
+            assert torch.equal(a[k], b[k])
+
+
+def test_tensors_of_rows():
+    """A view of wider rows is taken with its stride; tensors that do not fit the call are refused."""
+    n, V = 6, 300
+    wide = torch.randn(n, V + 20, device=DEV)
+    tok = torch.zeros(n, dtype=torch.int32, device=DEV)
+    part = wide[:, 7:7 + V]
+    got = forward(part, V + 20, V, 1.0, tok)
+    assert torch.equal(got["logp"], forward(part.contiguous(), V, V, 1.0, tok)["logp"])
+    logp = torch.empty(n, device=DEV)
+    no_ws = lambda z, stride, tokens=tok, out=logp: R.rollout_token_logprobs(z, 0, stride, n, V, 1.0, tokens, 0, out)
+    no_ws(part, V + 20)
+    assert torch.equal(logp, got["logp"])
+    for bad in (lambda: no_ws(part, V + 21), lambda: no_ws(part.t(), V), lambda: no_ws(wide.half(), V + 20),
+                lambda: no_ws(part, V + 20, tok[:-1]), lambda: no_ws(part, V + 20, tok.long()),
+                lambda: no_ws(part, V + 20, tok, torch.empty(2 * n, device=DEV)[::2]), lambda: no_ws(part, V + 20, tok.cpu())):
+        with pytest.raises(R.RolloutError) as e:
+            bad()
+        assert e.value.code == R.EINVAL
