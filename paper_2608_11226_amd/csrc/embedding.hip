@@ -15,7 +15,7 @@ namespace {
 
 constexpr int EB = 256;
 constexpr int kPiece = 32;               // entries of a piece, and pieces of a large piece
-constexpr int kAhead = 4;                // rows in flight
+constexpr int kAhead = 8;                // rows in flight
 constexpr int kEntries = 8;              // sorted entries whose rows a workgroup does
 constexpr int kRowWorkgroups = 8192, kRowValues = 16384;
 constexpr int kLongThreads = 1024, kLongWorkgroups = 512;
@@ -324,10 +324,19 @@ __global__ __launch_bounds__(EB) void k_sort_place(SortPass p, int tiles, const 
   }
 }
 
-// All passes by one workgroup, in LDS, for n up to kSmallSort; the next `clear` empty the rows' runs, the others zero a share
-// of the table.
+// Where the runs of sorted keys begin and end: what entry i knows of it.
+__device__ __forceinline__ void note_run(const int32_t* key, int i, int n, int vocab, int2* runs) {
+  const int k = key[i];
+  if (k >= vocab) return;
+  if (i == 0 || key[i - 1] != k) runs[k].x = i;
+  if (i == n - 1 || key[i + 1] != k) runs[k].y = i + 1;
+}
+
+// All passes by one workgroup, in LDS, for n up to kSmallSort.  The next `clear` empty the rows' runs; without them (no one will
+// ask for a row without tokens, the whole table being zeroed here) the runs are found here too.  The others zero a share of the
+// table.
 __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __restrict__ tokens, int n, int vocab, int passes,
-                                                              int bits, int32_t* __restrict__ key_out,
+                                                              int bits, int32_t* key_out,
                                                               int32_t* __restrict__ pos_out, int2* __restrict__ runs, int clear,
                                                               int32_t* __restrict__ longs, Fill fill) {
   __shared__ int32_t lds[4 * kSmallSort];  // keys and positions, of two buffers
@@ -390,20 +399,18 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __r
     key = key2, key2 = t;
     t = pos, pos = pos2, pos2 = t;
   }
+  if (clear) return;
+  __syncthreads();  // the sorted keys are in memory, and this workgroup's own
+  for (int i = threadIdx.x; i < n; i += kSmallThreads) note_run(key_out, i, n, vocab, runs);
 }
 
 // ---------------------------------------------------------------------------
 // sums of runs
 // ---------------------------------------------------------------------------
-// Where the runs of sorted keys begin and end.
 __global__ __launch_bounds__(EB) void k_embedding_runs(const int32_t* __restrict__ key, int n, int vocab,
                                                        int2* __restrict__ runs) {
   const int i = blockIdx.x * EB + threadIdx.x;
-  if (i >= n) return;
-  const int k = key[i];
-  if (k >= vocab) return;
-  if (i == 0 || key[i - 1] != k) runs[k].x = i;
-  if (i == n - 1 || key[i + 1] != k) runs[k].y = i + 1;
+  if (i < n) note_run(key, i, n, vocab, runs);
 }
 
 // How a workgroup shares out a slab of a row (4 EB columns at most): `width` threads (a power of two, at most EB) side by
@@ -422,8 +429,8 @@ __device__ __forceinline__ void add_rows(float (&v)[4], const T* g, const int32_
     Raw4<T> q[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      const int at = min(i + j, hi - 1);
-      q[j] = load_raw(g + (size_t)(pos ? pos[at] : at) * dim + c, dim - c);
+      const int at = i + j;
+      if (at < hi) q[j] = load_raw(g + (size_t)(pos ? pos[at] : at) * dim + c, dim - c);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j)
@@ -691,6 +698,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   const int launches = small ? 1 : 2 * sp.passes, pieces = a.n / kPiece;
   const size_t row_bytes = (size_t)a.dim * sizeof(O);
   const ZeroPlan z = zero_plan(a, row_bytes, launches, pieces);
+  const bool runs_known = small && z.long_end == 0;  // by the sort itself
   // the sort's share of the zeros, launch by launch
   char* fill_at = (char*)a.table + (ACC ? 0 : z.long_end * row_bytes);
   char* const fill_end = (char*)a.table + (ACC ? 0 : a.vocab * row_bytes);
@@ -703,7 +711,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   };
   if (small) {
     const Fill f = next_fill();
-    const int clear = std::min((a.vocab + kSmallThreads * 4 - 1) / (kSmallThreads * 4), 1024);
+    const int clear = runs_known ? 0 : std::min((a.vocab + kSmallThreads * 4 - 1) / (kSmallThreads * 4), 1024);
     hipLaunchKernelGGL(k_sort_small, dim3(1 + clear + fill_blocks(f)), dim3(kSmallThreads), 0, s, a.tokens, a.n, a.vocab,
                        sp.passes, sp.bits, key, pos, runs, clear, longs, f);
   } else {
@@ -723,7 +731,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   int width = 32;  // threads of a row
   while (width < EB && width * 4 < a.dim) width *= 2;
   const int slabs = (int)(((int64_t)a.dim + 4 * EB - 1) / (4 * EB));
-  hipLaunchKernelGGL(k_embedding_runs, dim3((a.n + EB - 1) / EB), dim3(EB), 0, s, key, a.n, a.vocab, runs);
+  if (!runs_known) hipLaunchKernelGGL(k_embedding_runs, dim3((a.n + EB - 1) / EB), dim3(EB), 0, s, key, a.n, a.vocab, runs);
   const int entries = EB / width * kEntries;  // of a workgroup
   const int64_t starts = ((int64_t)a.n + entries - 1) / entries * slabs;
   // rows without tokens: some kRowValues values a workgroup where there are many of them

@@ -182,7 +182,7 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
     if (wave == 0 && lane < nseg) lds.units[lane] = lane;
   }
   __syncthreads();
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 8;
   for (int r0 = wave; r0 < n; r0 += RW * kAhead) {
     u32x4 raw[kAhead];
     int id0[kAhead];
@@ -213,9 +213,13 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
   } else if (threadIdx.x < count) {
     const uint2 own = lds.found[threadIdx.x];
     int place = 0;
-    for (int j = 0; j < count; ++j) {
-      const uint2 q = lds.found[j];
-      place += q.x > own.x || (q.x == own.x && q.y < own.y);
+    for (int j0 = 0; j0 < count; j0 += 8) {
+      uint2 q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[j] = lds.found[j0 + j];  // RB is a multiple of 8
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        place += j0 + j < count && (q[j].x > own.x || (q[j].x == own.x && q[j].y < own.y));
     }
     if (place < top) {
       ids[place] = (int)own.y;
@@ -306,9 +310,9 @@ __device__ __forceinline__ Soft scan_units(const T* zr, int V, float c, int lo, 
 
 // A wave's lanes joined, the same in every lane.
 __device__ __forceinline__ Soft joined_wave(Soft a, float c) {
-  a = moved(a, wave_max(a.m), c);
-  a.s = wave_sum(a.s);
-  a.w = wave_sum(a.w);
+  a = moved(a, wave_max_f32(a.m), c);
+  a.s = wave_sum_f32(a.s);
+  a.w = wave_sum_f32(a.w);
   return a;
 }
 

@@ -146,17 +146,34 @@ __device__ __forceinline__ u32x4 pack16(const float (&v)[8]) {
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t* p, float v) { *p = round_bf16(v); }
 
-// Maximum of one unsigned value per lane, the same in every lane (lane moves without LDS; a lane with no source adds 0).
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#define ROLLOUT_MAX_STEP(ctrl, rows) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false))
-  ROLLOUT_MAX_STEP(0x111, 0xf);  // row_shr:1, 2, 4, 8
-  ROLLOUT_MAX_STEP(0x112, 0xf);
-  ROLLOUT_MAX_STEP(0x114, 0xf);
-  ROLLOUT_MAX_STEP(0x118, 0xf);
-  ROLLOUT_MAX_STEP(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
-  ROLLOUT_MAX_STEP(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
-#undef ROLLOUT_MAX_STEP
+// Reductions of one value per lane by lane moves, without LDS, the result the same in every lane: shifts of 1, 2, 4 and 8
+// lanes within each row of 16, then row 0's result into row 1 and row 2's into row 3, then the first two rows' into the
+// others; a lane with no source takes `none`.  Lane 63 then has all of them.
+template <typename F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, uint32_t none, F f) {
+#define ROLLOUT_STEP(ctrl, rows) \
+  v = f(v, (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, ctrl, rows, 0xf, false))
+  ROLLOUT_STEP(0x111, 0xf);  // row_shr:1, 2, 4, 8
+  ROLLOUT_STEP(0x112, 0xf);
+  ROLLOUT_STEP(0x114, 0xf);
+  ROLLOUT_STEP(0x118, 0xf);
+  ROLLOUT_STEP(0x142, 0xa);  // row_bcast:15 into rows 1 and 3
+  ROLLOUT_STEP(0x143, 0xc);  // row_bcast:31 into rows 2 and 3
+#undef ROLLOUT_STEP
   return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  return wave_reduce(v, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+__device__ __forceinline__ float wave_max_f32(float v) {
+  return __uint_as_float(wave_reduce(__float_as_uint(v), 0xFF800000u, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  return __uint_as_float(wave_reduce(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
 }
 
 }  // namespace rollout
