@@ -16,8 +16,10 @@ constexpr int LB = 256;
 constexpr int kTile = LB * 4;     // tokens of a workgroup's step
 constexpr int kMaxBlocks = 1536;  // of 8.4 M tokens: 37 us, 38 with 1,024, 41 with 2,048
 constexpr int kJoin = 1024;       // threads that join their sums, at most
-constexpr int kSums = 6;          // loss, r, kl, clipped low, clipped high, H
-constexpr int kCountSeqs = 8192;  // up to here every workgroup counts the tokens itself
+constexpr int kSums = 7;          // loss, r, kl, clipped low, clipped high, H, tokens
+// Every workgroup adds up to this many numbers itself to know how many tokens there are (1,024 sequences of 128: 12.2 us, with
+// a kernel before it that counts 13.8; 4,096 of 1,024: 25.0 and 24.4); more lengths are first added up in this many sums.
+constexpr int kCountSeqs = 2048, kCountBlocks = 256;
 
 struct Borders {
   double low, high;  // ln(1 - el), ln(1 + eh)
@@ -48,25 +50,27 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int s, int N) {
   return lengths ? max(0, min(lengths[s], N)) : N;
 }
 
-// Number of counted tokens, in every thread (whole numbers below 2^53: exact in any order).
-__device__ __forceinline__ double count_tokens(const int32_t* lengths, int S, int N, double* red) {
-  if (!lengths) return (double)S * N;
-  double v = 0.0;
-  for (int s = threadIdx.x; s < S; s += blockDim.x) v += length_of(lengths, s, N);
+// Sum of n lengths, in every thread (less than 2^31: exact in any order).
+__device__ __forceinline__ int add_lengths(const int32_t* lengths, int lo, int hi, int N, int32_t* red) {
+  int v = 0;
+#pragma unroll 4
+  for (int s = lo + threadIdx.x; s < hi; s += LB) v += length_of(lengths, s, N);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = 0.0;
-  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v += red[i];
+  v = 0;
+#pragma unroll
+  for (int i = 0; i < LB / 64; ++i) v += red[i];
   return v;
 }
 
-__global__ __launch_bounds__(1024) void k_policy_count(const int32_t* __restrict__ lengths, int S, int N,
-                                                       double* __restrict__ count) {
-  __shared__ double red[16];
-  const double c = count_tokens(lengths, S, N, red);
-  if (threadIdx.x == 0) *count = c;
+__global__ __launch_bounds__(LB) void k_policy_count(const int32_t* __restrict__ lengths, int S, int N, int each,
+                                                     int32_t* __restrict__ counts) {
+  __shared__ int32_t red[LB / 64];
+  const int lo = min((int64_t)blockIdx.x * each, (int64_t)S), hi = (int)min((int64_t)lo + each, (int64_t)S);
+  const int v = add_lengths(lengths, lo, hi, N, red);
+  if (threadIdx.x == 0) counts[blockIdx.x] = v;
 }
 
 __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4]) {
@@ -118,7 +122,7 @@ __device__ __forceinline__ Step load_step(const PolicyLossArgs& a, int64_t i0, i
 
 struct Sums {
   double loss = 0.0, r = 0.0, kl = 0.0, H = 0.0;
-  int low = 0, high = 0;
+  int low = 0, high = 0, tokens = 0;
 };
 
 __device__ __forceinline__ void use_step(const PolicyLossArgs& a, const Borders& border, float w_all, const Step& q, Sums& sum) {
@@ -152,6 +156,7 @@ __device__ __forceinline__ void use_step(const PolicyLossArgs& a, const Borders&
         sum.r += (double)r;
         sum.low += low;
         sum.high += high;
+        sum.tokens += 1;
         gl[j] = g * w;
         gh[j] = -a.entropy_coef * w;
       }
@@ -168,35 +173,37 @@ __device__ __forceinline__ void use_step(const PolicyLossArgs& a, const Borders&
   if (a.grad_entropy) store4(a.grad_entropy + q.i0, q.n, gh);
 }
 
-// A thread does four tokens at a time.
-__global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders border, const double* __restrict__ count,
-                                                    double* __restrict__ part) {
-  __shared__ double red[LB / 64], sums[LB / 64 * kSums];
+// A thread does four tokens at a time.  counts: n_counts numbers that add up to the tokens (the lengths, or sums of them).
+__global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders border, const int32_t* __restrict__ counts,
+                                                    int n_counts, double* __restrict__ part) {
+  __shared__ int32_t red[LB / 64];
+  __shared__ double sums[LB / 64 * kSums];
   const int S = a.seqs, N = a.max_len;
   const int64_t total = (int64_t)S * N, stride = (int64_t)gridDim.x * kTile;
   Sums sum;
-  double all = (double)S * N;
-  if (a.mean == ROLLOUT_MEAN_TOKEN) all = fmax(count ? *count : count_tokens(a.lengths, S, N, red), 1.0);
+  double all = (double)total;
+  if (a.mean == ROLLOUT_MEAN_TOKEN && a.lengths)
+    all = max(add_lengths(counts, 0, n_counts, counts == a.lengths ? N : 0x7FFFFFFF, red), 1);
   const float w_all = (float)(1.0 / all);
   for (int64_t i0 = (int64_t)blockIdx.x * kTile + threadIdx.x * 4; i0 < total; i0 += stride)
     use_step(a, border, w_all, load_step(a, i0, total), sum);
-  const double each[kSums] = {sum.loss, sum.r, sum.kl, (double)sum.low, (double)sum.high, sum.H};
+  const double each[kSums] = {sum.loss, sum.r, sum.kl, (double)sum.low, (double)sum.high, sum.H, (double)sum.tokens};
   const double v = block_sums(each, sums);
   if (threadIdx.x < kSums) part[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = v;
 }
 
-__global__ __launch_bounds__(kJoin) void k_policy_join(const double* __restrict__ part, int blocks,
-                                                    const int32_t* __restrict__ lengths, int S, int N,
-                                                    float* __restrict__ loss, float* __restrict__ stats) {
-  __shared__ double red[kJoin / 64], sums[kJoin / 64 * kSums];
+__global__ __launch_bounds__(kJoin) void k_policy_join(const double* __restrict__ part, int blocks, float* __restrict__ loss,
+                                                       float* __restrict__ stats) {
+  __shared__ double sums[kJoin / 64 * kSums], all[kSums];
   double v[kSums] = {};
   for (int b = threadIdx.x; b < blocks; b += blockDim.x)
 #pragma unroll
     for (int k = 0; k < kSums; ++k) v[k] += part[(size_t)k * blocks + b];
-  const double c = fmax(count_tokens(lengths, S, N, red), 1.0);
   const double t = block_sums(v, sums);
+  if (threadIdx.x < kSums) all[threadIdx.x] = t;
+  __syncthreads();
   if (threadIdx.x == 0 && loss) *loss = (float)t;
-  if (threadIdx.x > 0 && threadIdx.x < kSums && stats) stats[threadIdx.x - 1] = (float)(t / c);
+  if (threadIdx.x > 0 && threadIdx.x < kSums - 1 && stats) stats[threadIdx.x - 1] = (float)(t / fmax(all[kSums - 1], 1.0));
 }
 
 int blocks_of(int seqs, int max_len) {
@@ -205,19 +212,27 @@ int blocks_of(int seqs, int max_len) {
 
 }  // namespace
 
-size_t policy_loss_workspace(int seqs, int max_len) { return 16 + (size_t)blocks_of(seqs, max_len) * kSums * 8; }
+size_t policy_loss_workspace(int seqs, int max_len) {
+  return kCountBlocks * 4 + (size_t)blocks_of(seqs, max_len) * kSums * 8;
+}
 
 hipError_t launch_policy_loss(hipStream_t s, const PolicyLossArgs& a, void* ws) {
-  double* count = (double*)ws;
-  double* part = count + 2;
+  int32_t* sums = (int32_t*)ws;
+  double* part = (double*)(sums + kCountBlocks);
   const int blocks = blocks_of(a.seqs, a.max_len);
   const Borders b = {std::log1p(-(double)a.clip_low), std::log1p((double)a.clip_high)};
-  const bool counted = a.mean == ROLLOUT_MEAN_TOKEN && a.lengths && a.seqs > kCountSeqs;
-  if (counted) hipLaunchKernelGGL(k_policy_count, dim3(1), dim3(1024), 0, s, a.lengths, a.seqs, a.max_len, count);
-  hipLaunchKernelGGL(k_policy_loss, dim3(blocks), dim3(LB), 0, s, a, b, counted ? count : nullptr, part);
-  // no more waves than the sums and the lengths need
-  const int threads = (std::min(std::max(blocks, a.seqs), kJoin) + 63) / 64 * 64;
-  hipLaunchKernelGGL(k_policy_join, dim3(1), dim3(threads), 0, s, part, blocks, a.lengths, a.seqs, a.max_len, a.loss, a.stats);
+  const int32_t* counts = a.lengths;
+  int n_counts = a.seqs;
+  if (a.mean == ROLLOUT_MEAN_TOKEN && a.lengths && a.seqs > kCountSeqs) {
+    const int each = std::max(kCountSeqs, (a.seqs + kCountBlocks - 1) / kCountBlocks);
+    n_counts = (a.seqs + each - 1) / each;
+    hipLaunchKernelGGL(k_policy_count, dim3(n_counts), dim3(LB), 0, s, a.lengths, a.seqs, a.max_len, each, sums);
+    counts = sums;
+  }
+  hipLaunchKernelGGL(k_policy_loss, dim3(blocks), dim3(LB), 0, s, a, b, counts, n_counts, part);
+  if (a.loss || a.stats)
+    hipLaunchKernelGGL(k_policy_join, dim3(1), dim3((std::min(blocks, kJoin) + 63) / 64 * 64), 0, s, part, blocks, a.loss,
+                       a.stats);
   return hipGetLastError();
 }
 

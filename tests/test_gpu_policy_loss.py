@@ -69,7 +69,7 @@ def check(out, lp, old, ref, H, adv, lengths, lo, hi, kl, ent, mean):
         assert np.all(np.abs(got[3] - dH) <= 3 * EPS * np.abs(dH) + 2.0 ** -140)
 
 
-SIZES = [(1, 1), (1, 7), (3, 1), (5, 3), (4, 4), (64, 512), (7, 1023), (3, 2049), (1000, 2), (33, 130), (2, 9001), (20000, 3)]
+SIZES = [(1, 1), (1, 7), (3, 1), (5, 3), (4, 4), (64, 512), (7, 1023), (3, 2049), (1000, 2), (33, 130), (2, 9001), (20000, 3), (600000, 1)]
 
 
 @pytest.mark.parametrize("S,N", SIZES)
