@@ -18,11 +18,13 @@ constexpr int RW = RB / 64;
 constexpr int kUnits = 4;  // 16-byte loads in flight a lane
 constexpr int kMaxUnits = kMaxTopVocab / 256, kMaxPer = kMaxUnits / 64;  // of a row, of a lane, where alternatives are taken
 constexpr int kMaxChunks = 64;     // a lane each when parts are joined
-constexpr int kWorkgroups = 2048;  // that a launch of few rows is split into
+// Workgroups that a launch of few rows is split into: 515 bf16 rows of 152,064 39.5 us with 1,024, 36.1 with 2,048, 36.4 with
+// 8,192; 256 fp32 rows with alternatives 44.4, 41.9 and 46.9 at the time.
+constexpr int kWorkgroups = 2048;
 constexpr int kWhole = 64;         // units of a row that is not split
 constexpr int kWaveRows = 1024;    // rows from which such a row is one wave's
 constexpr int kMaxGrid = 1 << 20;
-constexpr int kBatch = 4;              // 16-byte loads in flight a thread in the gradient
+constexpr int kBatch = 4;          // 16-byte loads in flight a thread in the gradient
 constexpr size_t kLastLevelBytes = 256u << 20;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // exponents are taken at least this low: the weighted sum multiplies them with a 0, which an infinity would spoil

@@ -17,9 +17,10 @@ constexpr int kTile = LB * 4;     // tokens of a workgroup's step
 constexpr int kMaxBlocks = 1536;  // of 8.4 M tokens: 37 us, 38 with 1,024, 41 with 2,048
 constexpr int kJoin = 1024;       // threads that join their sums, at most
 constexpr int kSums = 7;          // loss, r, kl, clipped low, clipped high, H, tokens
-// Every workgroup adds up to this many numbers itself to know how many tokens there are (1,024 sequences of 128: 12.2 us, with
-// a kernel before it that counts 13.8; 4,096 of 1,024: 25.0 and 24.4); more lengths are first added up in this many sums.
-constexpr int kCountSeqs = 2048, kCountBlocks = 256;
+// Every workgroup adds up to this many lengths itself to know how many tokens there are; more are first added up in
+// kCountBlocks sums by a kernel before it (4,096 sequences of 64: 10.5 us by itself, 12 with the kernel; 16,384 of 16: 15.6 and
+// 12).
+constexpr int kCountSeqs = 8192, kCountBlocks = 256;
 
 struct Borders {
   double low, high;  // ln(1 - el), ln(1 + eh)
@@ -224,7 +225,7 @@ hipError_t launch_policy_loss(hipStream_t s, const PolicyLossArgs& a, void* ws) 
   const int32_t* counts = a.lengths;
   int n_counts = a.seqs;
   if (a.mean == ROLLOUT_MEAN_TOKEN && a.lengths && a.seqs > kCountSeqs) {
-    const int each = std::max(kCountSeqs, (a.seqs + kCountBlocks - 1) / kCountBlocks);
+    const int each = std::max(2048, (a.seqs + kCountBlocks - 1) / kCountBlocks);
     n_counts = (a.seqs + each - 1) / each;
     hipLaunchKernelGGL(k_policy_count, dim3(n_counts), dim3(LB), 0, s, a.lengths, a.seqs, a.max_len, each, sums);
     counts = sums;
