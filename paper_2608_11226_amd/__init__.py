@@ -146,7 +146,7 @@ lib = _load()
 
 import torch as _torch  # noqa: E402  (loaded above)
 
-_F, _I = _torch.float32, _torch.int32
+_F, _I, _U8 = _torch.float32, _torch.int32, _torch.uint8
 _TYPES = {DTYPE_FP32: _torch.float32, DTYPE_BF16: _torch.bfloat16}
 
 
@@ -228,20 +228,20 @@ def rollout_length_rewards(lengths, n: int, target: int, rewards, total_tokens=N
 
 # The update side of a GRPO step: no context, caller-owned workspaces.  A tensor passed for a buffer has to be on the
 # current device, of the buffer's type, contiguous (the rows of logits may be strided) and large enough; an integer
-# address is passed on as it is.
+# address is passed on as it is.  Workspaces are uint8 tensors.
 def _buf(name: str, x, kind, n: int, device: int) -> int | None:
-    """Device pointer of a buffer of n elements of a kind (n bytes of any type where kind is None)."""
+    """Device pointer of a buffer of n elements of a torch type."""
     if x is None or type(x) is int:
         return x
-    if not isinstance(x, _torch.Tensor):
+    if not hasattr(x, "is_contiguous"):
         return _ptr(x)
-    if x.dtype is kind and x.get_device() == device and x.is_contiguous() and x.numel() >= n:
+    if x.dtype is kind and x.is_contiguous() and x.numel() >= n and x.get_device() == device:
         return x.data_ptr()
-    if kind is not None and x.dtype is not kind:
+    if x.dtype is not kind:
         raise RolloutError(EINVAL, f"{name} must be {kind}, not {x.dtype}")
     if x.get_device() != device:
         raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
-    have = x.numel() if kind is not None else x.numel() * x.element_size()
+    have = x.numel()
     if not x.is_contiguous():
         if not name.endswith("logits") or x.stride(-1) != 1:
             raise RolloutError(EINVAL, f"{name} is not contiguous")
@@ -278,7 +278,7 @@ def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, voc
         _buf("tokens", tokens, _I, n_rows, dev), n_top, _buf("logp", logp, _F, n_rows, dev),
         _buf("entropy", entropy, _F, n_rows, dev),
         _buf("stats", stats, _F, 2 * n_rows, dev), _buf("top_ids", top_ids, _I, n_rows * n_top, dev),
-        _buf("top_logp", top_logp, _F, n_rows * n_top, dev), _buf("workspace", workspace, None, workspace_bytes, dev),
+        _buf("top_logp", top_logp, _F, n_rows * n_top, dev), _buf("workspace", workspace, _U8, workspace_bytes, dev),
         workspace_bytes, _ptr(stream)))
 
 
@@ -314,7 +314,7 @@ def grpo_policy_loss(logp, old_logp, ref_logp, entropy, adv, lengths, n_seqs: in
         max_len, clip_low, clip_high, kl_coef, entropy_coef, mean, _buf("loss", loss, _F, 1, dev),
         _buf("stats", stats, _F, 5, dev),
         _buf("grad_logp", grad_logp, _F, n, dev), _buf("grad_entropy", grad_entropy, _F, n, dev),
-        _buf("workspace", workspace, None, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
+        _buf("workspace", workspace, _U8, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
 
 
 def rollout_embedding(table, table_dtype: int, vocab: int, dim: int, tokens, n_tokens: int, scale: float, out,
@@ -340,7 +340,7 @@ def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, voc
         _buf("grad", grad, _kind(grad_dtype), n_tokens * dim, dev), grad_dtype,
         _buf("tokens", tokens, _I, n_tokens, dev), n_tokens, vocab,
         dim, scale, accumulate, _buf("grad_table", grad_table, _kind(table_dtype), vocab * dim, dev), table_dtype,
-        _buf("workspace", workspace, None, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
+        _buf("workspace", workspace, _U8, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
 
 
 def rollout_sync(ctx):

@@ -174,6 +174,13 @@ __device__ __forceinline__ void use_step(const PolicyLossArgs& a, const Borders&
   if (a.grad_entropy) store4(a.grad_entropy + q.i0, q.n, gh);
 }
 
+// Loss and statistics from the whole sums, which the first kSums threads hold.
+__device__ __forceinline__ void write_sums(double v, float* loss, float* stats) {
+  const double tokens = fmax(__shfl(v, kSums - 1, 64), 1.0);
+  if (threadIdx.x == 0 && loss) *loss = (float)v;
+  if (threadIdx.x > 0 && threadIdx.x < kSums - 1 && stats) stats[threadIdx.x - 1] = (float)(v / tokens);
+}
+
 // A thread does four tokens at a time.  counts: n_counts numbers that add up to the tokens (the lengths, or sums of them).
 __global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders border, const int32_t* __restrict__ counts,
                                                     int n_counts, double* __restrict__ part) {
@@ -190,21 +197,21 @@ __global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders bo
     use_step(a, border, w_all, load_step(a, i0, total), sum);
   const double each[kSums] = {sum.loss, sum.r, sum.kl, (double)sum.low, (double)sum.high, sum.H, (double)sum.tokens};
   const double v = block_sums(each, sums);
-  if (threadIdx.x < kSums) part[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = v;
+  if (gridDim.x > 1) {
+    if (threadIdx.x < kSums) part[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = v;
+  } else {
+    write_sums(v, a.loss, a.stats);  // the only workgroup
+  }
 }
 
 __global__ __launch_bounds__(kJoin) void k_policy_join(const double* __restrict__ part, int blocks, float* __restrict__ loss,
                                                        float* __restrict__ stats) {
-  __shared__ double sums[kJoin / 64 * kSums], all[kSums];
+  __shared__ double sums[kJoin / 64 * kSums];
   double v[kSums] = {};
   for (int b = threadIdx.x; b < blocks; b += blockDim.x)
 #pragma unroll
     for (int k = 0; k < kSums; ++k) v[k] += part[(size_t)k * blocks + b];
-  const double t = block_sums(v, sums);
-  if (threadIdx.x < kSums) all[threadIdx.x] = t;
-  __syncthreads();
-  if (threadIdx.x == 0 && loss) *loss = (float)t;
-  if (threadIdx.x > 0 && threadIdx.x < kSums - 1 && stats) stats[threadIdx.x - 1] = (float)(t / fmax(all[kSums - 1], 1.0));
+  write_sums(block_sums(v, sums), loss, stats);
 }
 
 int blocks_of(int seqs, int max_len) {
@@ -231,7 +238,7 @@ hipError_t launch_policy_loss(hipStream_t s, const PolicyLossArgs& a, void* ws) 
     counts = sums;
   }
   hipLaunchKernelGGL(k_policy_loss, dim3(blocks), dim3(LB), 0, s, a, b, counts, n_counts, part);
-  if (a.loss || a.stats)
+  if (blocks > 1 && (a.loss || a.stats))
     hipLaunchKernelGGL(k_policy_join, dim3(1), dim3((std::min(blocks, kJoin) + 63) / 64 * 64), 0, s, part, blocks, a.loss,
                        a.stats);
   return hipGetLastError();
