@@ -343,22 +343,15 @@ __device__ __forceinline__ void note_run(const int32_t* key, int i, int n, int v
   if (i == n - 1 || key[i + 1] != k) runs[k].y = i + 1;
 }
 
-// All passes by one workgroup, in LDS, for n up to kSmallSort.  The next `clear` empty the rows' runs; without them (no one will
-// ask for a row without tokens, the whole table being zeroed here) the runs are found here too.  The others zero a share of the
-// table.
+// All passes by one workgroup, in LDS, for n up to kSmallSort, and the runs; the other workgroups zero the table.
 __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __restrict__ tokens, int n, int vocab, int passes,
                                                               int bits, int32_t* key_out,
-                                                              int32_t* __restrict__ pos_out, int2* __restrict__ runs, int clear,
+                                                              int32_t* __restrict__ pos_out, int2* __restrict__ runs,
                                                               int32_t* __restrict__ longs, Fill fill) {
   __shared__ int32_t lds[4 * kSmallSort];  // keys and positions, of two buffers
   __shared__ uint32_t place[kSmallWaves][kDigits];
   __shared__ uint32_t total[kDigits / 64];
-  if ((int)blockIdx.x > clear) return fill_zeros(fill, blockIdx.x - 1 - clear);
-  if (blockIdx.x) {
-    for (int v = (blockIdx.x - 1) * kSmallThreads + threadIdx.x; v < vocab; v += clear * kSmallThreads)
-      runs[v] = make_int2(0, 0);
-    return;
-  }
+  if (blockIdx.x) return fill_zeros(fill, blockIdx.x - 1);
   if (threadIdx.x == 0) *longs = 0;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int sub = ((n + kSmallWaves - 1) / kSmallWaves + 63) & ~63;
@@ -410,7 +403,6 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __r
     key = key2, key2 = t;
     t = pos, pos = pos2, pos2 = t;
   }
-  if (clear) return;
   __syncthreads();  // the sorted keys are in memory, and this workgroup's own
   for (int i = threadIdx.x; i < n; i += kSmallThreads) note_run(key_out, i, n, vocab, runs);
 }
@@ -683,14 +675,16 @@ Parts parts_of(int n, int vocab, int dim) {
   return w;
 }
 
-// Who zeroes the rows without tokens.  The sort and the long rows leave most of the card's memory bandwidth unused for some
-// microseconds a launch, so each of their launches zeroes about as much as fits there: first the sort's, from the table's end
-// (all rows, for no one knows yet which have tokens), then that of the long rows, then the one of the other rows.
+// Who zeroes the rows without tokens.  The small sort's launch zeroes the whole table beside it, for few rows are then written
+// twice (300 tokens into 152,064 x 3,584 fp32 414 -> 374 us).  The other sort and the long rows leave most of the card's memory
+// bandwidth unused for some microseconds a launch, so each of their launches zeroes about as much as fits there: first the
+// sort's, from the table's end (all rows, for no one knows yet which have tokens), then that of the long rows, then the one of
+// the other rows.
 struct ZeroPlan {
   int rows_end, long_end;  // [0, rows_end), [rows_end, long_end), and the sort's [long_end, vocab)
 };
-ZeroPlan zero_plan(const EmbeddingGradArgs& a, size_t row_bytes, int launches, int pieces) {
-  if (a.accumulate) return {0, 0};
+ZeroPlan zero_plan(const EmbeddingGradArgs& a, size_t row_bytes, bool small, int launches, int pieces) {
+  if (a.accumulate || small) return {0, 0};
   const auto held = [&](size_t bytes, int rows) { return (int)std::min(bytes / row_bytes, (size_t)rows); };
   ZeroPlan z;
   z.long_end = a.vocab - held(kSortFill * launches, a.vocab);
@@ -708,8 +702,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   const bool small = a.n <= kSmallSort;
   const int launches = small ? 1 : 2 * sp.passes, pieces = a.n / kPiece;
   const size_t row_bytes = (size_t)a.dim * sizeof(O);
-  const ZeroPlan z = zero_plan(a, row_bytes, launches, pieces);
-  const bool runs_known = small && z.long_end == 0;  // by the sort itself
+  const ZeroPlan z = zero_plan(a, row_bytes, small, launches, pieces);
   // the sort's share of the zeros, launch by launch
   char* fill_at = (char*)a.table + (ACC ? 0 : z.long_end * row_bytes);
   char* const fill_end = (char*)a.table + (ACC ? 0 : a.vocab * row_bytes);
@@ -722,9 +715,8 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   };
   if (small) {
     const Fill f = next_fill();
-    const int clear = runs_known ? 0 : std::min((a.vocab + kSmallThreads * 4 - 1) / (kSmallThreads * 4), 1024);
-    hipLaunchKernelGGL(k_sort_small, dim3(1 + clear + fill_blocks(f)), dim3(kSmallThreads), 0, s, a.tokens, a.n, a.vocab,
-                       sp.passes, sp.bits, key, pos, runs, clear, longs, f);
+    hipLaunchKernelGGL(k_sort_small, dim3(1 + fill_blocks(f)), dim3(kSmallThreads), 0, s, a.tokens, a.n, a.vocab, sp.passes,
+                       sp.bits, key, pos, runs, longs, f);
   } else {
     uint32_t* hist = (uint32_t*)(ws + w.hist);
     for (int i = 0; i < sp.passes; ++i) {
@@ -742,7 +734,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   int width = 32;  // threads of a row
   while (width < EB && width * 4 < a.dim) width *= 2;
   const int slabs = (int)(((int64_t)a.dim + 4 * EB - 1) / (4 * EB));
-  if (!runs_known) hipLaunchKernelGGL(k_embedding_runs, dim3((a.n + EB - 1) / EB), dim3(EB), 0, s, key, a.n, a.vocab, runs);
+  if (!small) hipLaunchKernelGGL(k_embedding_runs, dim3((a.n + EB - 1) / EB), dim3(EB), 0, s, key, a.n, a.vocab, runs);
   const int entries = EB / width * kEntries;  // of a workgroup
   const int64_t starts = ((int64_t)a.n + entries - 1) / entries * slabs;
   // rows without tokens: some kRowValues values a workgroup where there are many of them
