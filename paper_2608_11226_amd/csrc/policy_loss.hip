@@ -14,8 +14,10 @@ namespace {
 
 constexpr int LB = 256;
 constexpr int kTile = LB * 4;     // tokens of a workgroup's step
-constexpr int kMaxBlocks = 1536;  // of 8.4 M tokens: 37 us, 38 with 1,024, 41 with 2,048
-constexpr int kJoin = 1024;       // threads that join their sums, at most
+// Odd: the steps of a workgroup are kMaxBlocks tiles apart and shall not all fall on the same part of completions, whose ends
+// have nothing to do (of 8.4 M tokens: 28.7 us, 30.2 with 1,536; 29.1 and 32.2 with 1,023 and 1,791).
+constexpr int kMaxBlocks = 1279;
+constexpr int kJoin = 512;         // threads that join their sums, at most (256 to 512 4.0 us, 1,024 5.5)
 constexpr int kSums = 7;          // loss, r, kl, clipped low, clipped high, H, tokens
 // Every workgroup adds up to this many lengths itself to know how many tokens there are; more are first added up in
 // kCountBlocks sums by a kernel before it (4,096 sequences of 64: 10.5 us by itself, 12 with the kernel; 16,384 of 16: 15.6 and
