@@ -3,9 +3,14 @@
 //   out_n = scale E[id_n];     dE_v = scale sum over n with id_n = v of g_n   (+ the old dE_v)
 //
 // The gradient sorts (id, position) pairs by id with a stable radix sort, so that a row's tokens stand together in
-// token order, and sums each run in that order: no atomics on floats, the same bits on every call.  A run's length is
-// anything from one to all of the tokens (text repeats its frequent ids), so runs are cut at fixed places of the sorted
-// order: every 32 entries that belong to one id are summed beforehand, and in long batches every 32 such sums once more.
+// token order, and adds up each run in an order that follows from its place alone: no atomics on floats, the same bits on every
+// call.  A run's length is anything from one to all of the tokens (text repeats its frequent ids), so runs are cut at fixed
+// places of the sorted order: every 32 entries that belong to one id are summed beforehand, and in long batches every 32 such
+// sums once more.
+//
+// Both are bound by HBM where there is much to move: 49,152 rows of 3,584 looked up in 186 us (705 MB written beside some 150 MB
+// of scattered rows), their gradient into 152,064 fp32 rows in 494 us (2.18 GB, most of it zeros, beside 308 MB of gathered
+// rows: 5.0 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 9.5, rows 8.6, long rows 5.1 us).
 #include "update.h"
 
 #include <type_traits>
@@ -144,7 +149,8 @@ __device__ __forceinline__ void store_values(uint16_t* p, int n, const float (&v
 // ---------------------------------------------------------------------------
 // lookup
 // ---------------------------------------------------------------------------
-// A workgroup a token, 16 bytes a lane of the wider type, kAhead of them on their way.
+// A workgroup a token, 16 bytes a lane of the wider type, kAhead of them on their way (a wave a token: 197 to 201 us instead
+// of 186 in the case above).
 template <typename T, typename O>
 __global__ __launch_bounds__(EB) void k_embedding(const T* __restrict__ table, int vocab, int dim,
                                                   const int32_t* __restrict__ tokens, int n, float scale,
@@ -227,6 +233,8 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, int block) {
   }
 }
 
+// A pass of the sort is two launches: the digits of every tile (a workgroup's keys) counted, then every workgroup adds up the
+// other tiles' counts itself and places its keys.  49,152 tokens take 4.8 and 8.2 us a pass without the zeros beside them.
 // Digit counts of every tile (a workgroup's keys) into hist[tile][digit].  The first pass also empties the rows' runs.
 // The workgroups behind the tiles zero a share of the table: the sort leaves most of the card free.
 __global__ __launch_bounds__(EB) void k_sort_count(SortPass p, int tiles, uint32_t* __restrict__ hist, int2* __restrict__ runs,

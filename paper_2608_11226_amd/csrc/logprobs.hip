@@ -8,6 +8,10 @@
 // One pass over the row with the running maximum, sum and weighted sum of every lane, each corrected when its maximum
 // moves (2^((m_old - m_new) c)), joined at the end in a fixed order.  z - m is taken before the scaling: it is exact
 // near the maximum and cannot overflow where a mask holds the type's lowest value.
+//
+// Both directions are bound by HBM: 4,096 rows of 152,064 bf16 logits (an eighth of them padding) are read at 6.2 TB/s (177
+// us), with the vector ALU busy four fifths of that time (nine instructions an element, the exponential among them), and
+// their gradient is read and written at 5.9 TB/s (375 us).  A large copy reaches 4.75 TB/s on this card, a fill 6.9.
 #include "update.h"
 
 namespace rollout {
@@ -357,7 +361,9 @@ __global__ __launch_bounds__(RB) void k_logprobs(LogprobArgs a, float c, int uni
   }
 }
 
-// A row's parts joined, and its alternatives: one workgroup a row with alternatives, otherwise one wave.
+// A row's parts joined, and its alternatives: one workgroup a row with alternatives, otherwise one wave.  Bound by its chain
+// of reads (parts and keys, units, the token's logit) and by the ranking: 64 rows with 8 alternatives 7.8 us, 256 with 20 10.3,
+// of which 4 are the launch and the first reads.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(RB) void k_logprobs_join(LogprobArgs a, float c, int chunks, const Soft* __restrict__ part,
                                                       const uint32_t* __restrict__ keys) {

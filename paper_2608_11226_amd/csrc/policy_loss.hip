@@ -7,6 +7,10 @@
 // Which side of a clipping border a token is on is decided on the exact difference in 64 bits, against the border's
 // logarithm, so that it does not hang on the rounding of an exponential.  Terms are fp32; their sums are fp64, added up
 // per thread, per workgroup, and over the workgroups by a second kernel, always in the same order.
+//
+// Bound by HBM where there are many tokens (2,048 sequences of 4,096 places, half of them tokens, with reference and
+// entropies: 67 MB read and 67 written in 28.4 us, 4.7 TB/s, and 4 us for the join), by its two launches where there are few
+// (64 of 512: 5.3 and 2.0 us).
 #include "update.h"
 
 namespace rollout {
