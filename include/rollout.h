@@ -324,7 +324,7 @@ rollout_status rollout_sample_noalloc(const float* d_logits, int32_t n_seqs, int
  * with NaN or +inf gets NaN everywhere and top ids -1.  d_tokens NULL: no row
  * is padding, and d_logp must be NULL.
  * Errors: EINVAL (sizes, types, alignment, NULL buffers, temperature not > 0, no
- * output), EUNSUPPORTED (vocab above 2^30, or above 327,680 with n_top > 0), ENOMEM
+ * output), EUNSUPPORTED (n_rows or vocab above 2^30, vocab above 327,680 with n_top > 0), ENOMEM
  * (workspace too small), EDEVICE.
  */
 rollout_status rollout_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t* h_bytes);
@@ -343,7 +343,7 @@ rollout_status rollout_token_logprobs(const void* d_logits, int32_t dtype, int64
  * EINVAL).  d_stats and d_entropy (needed only with h) are the forward call's.
  * What lies between the rows is left alone.  Rows that are padding, have g = h = 0
  * or hold nothing but -inf get zeros and are not read; a token >= vocab makes
- * its row NaN.  Errors: EINVAL, EUNSUPPORTED (vocab above 2^30), EDEVICE.
+ * its row NaN.  Errors: EINVAL, EUNSUPPORTED (n_rows or vocab above 2^30), EDEVICE.
  */
 rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_rows,
                                                int32_t vocab, float temperature, const int32_t* d_tokens,
@@ -403,7 +403,8 @@ rollout_status rollout_embedding(const void* d_table, int32_t table_dtype, int32
  * 0 every row is written (rows without tokens with zeros); with 1 the sum is added
  * to what the row holds, rounded once, and rows without tokens are left alone.
  * Ids outside [0, vocab) contribute nothing.  Tokens are sorted by id and a row's are
- * added in fp32 in an order that their positions fix.  Errors as above, and ENOMEM (workspace too small).
+ * added in fp32 in an order that their positions fix.  Errors as above, EUNSUPPORTED also where
+ * n_tokens ceil(dim / 1024) is above 2^25, and ENOMEM (workspace too small).
  */
 rollout_status rollout_embedding_backward_workspace(int32_t n_tokens, int32_t vocab, int32_t dim, uint64_t* h_bytes);
 rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype, const int32_t* d_tokens, int32_t n_tokens,

@@ -36,6 +36,7 @@ constexpr int kManyPieces = 2048;
 // Bytes of zeros that a launch of the sort writes beside it (none 526 us, 80 MB 497, 160 MB 493, 320 MB 496; 5,000 tokens into
 // a bf16 table 231, 203, 201 and 226), that of the long rows (none 535 us, 96 or 200 MB 530 at the time), and a workgroup.
 constexpr size_t kSortFill = 160u << 20, kLongFill = 96u << 20, kFill = 16384;
+constexpr int kMaxFillBlocks = 1 << 20;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortWaves = EB / 64;
 constexpr int kMaxTiles = 256;
@@ -214,15 +215,15 @@ __device__ __forceinline__ int key_at(const SortPass& p, int i) {
   return p.tokens ? key_of_token(p.tokens[i], p.vocab) : p.key_in[i];
 }
 
-// Zeros over a range of bytes (both types' zeros; a multiple of two bytes, anywhere): kFill bytes a workgroup.
+// Zeros over a range of bytes (both types' zeros; a multiple of two bytes, anywhere): `each` of them a workgroup.
 struct Fill {
   char* to;
-  size_t bytes;
+  size_t bytes, each;
 };
 typedef uint32_t Any16 __attribute__((ext_vector_type(4), aligned(2), may_alias));
-__host__ __device__ inline int fill_blocks(const Fill& f) { return (int)((f.bytes + kFill - 1) / kFill); }
+int fill_blocks(const Fill& f) { return (int)((f.bytes + f.each - 1) / f.each); }
 __device__ __forceinline__ void fill_zeros(const Fill& f, int block) {
-  const size_t lo = (size_t)block * kFill, hi = lo + kFill < f.bytes ? lo + kFill : f.bytes;
+  const size_t lo = (size_t)block * f.each, hi = lo + f.each < f.bytes ? lo + f.each : f.bytes;
   for (size_t i = lo + threadIdx.x * 16; i < hi; i += blockDim.x * 16) {
     if (i + 16 <= hi) {
       const u32x4 zero = {0, 0, 0, 0};
@@ -233,10 +234,11 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, int block) {
   }
 }
 
-// A pass of the sort is two launches: the digits of every tile (a workgroup's keys) counted, then every workgroup adds up the
-// other tiles' counts itself and places its keys.  49,152 tokens take 4.8 and 8.2 us a pass without the zeros beside them.
-// Digit counts of every tile (a workgroup's keys) into hist[tile][digit].  The first pass also empties the rows' runs.
+// A pass of the sort is two launches: the digits of every tile (a workgroup's keys) are counted, then every workgroup adds up
+// the other tiles' counts itself and places its keys.  49,152 tokens take 4.8 and 8.2 us a pass without the zeros beside them.
 // The workgroups behind the tiles zero a share of the table: the sort leaves most of the card free.
+//
+// Digit counts into hist[tile][digit].  The first pass also empties the rows' runs and the list of long rows.
 __global__ __launch_bounds__(EB) void k_sort_count(SortPass p, int tiles, uint32_t* __restrict__ hist, int2* __restrict__ runs,
                                                    int32_t* __restrict__ longs, Fill fill) {
   __shared__ uint32_t cnt[kDigits];
@@ -558,9 +560,8 @@ __device__ __forceinline__ void zero_rows(const ZeroRows& z, int block, int dim,
 
 // Three kinds of workgroups in one launch, so that the sums run beside the writing of the many rows without tokens (which
 // is most of the time at a large vocabulary): `pieces` slabs of sums of pieces, then `starts` slabs of rows that begin among
-// some entries, and, mixed in between, `zeros` of rows
-// without tokens.
-// Workgroups of pieces also list the rows that have them (`longs`: how many, then the first piece of each, in any order).
+// some entries, and, mixed in between, `zeros` of rows without tokens.  Workgroups of pieces also list the rows that have
+// them (`longs`: how many, then the first piece of each, in any order).
 template <typename T, typename O, bool ACC>
 __global__ __launch_bounds__(EB) void k_embedding_rows(const T* __restrict__ g, const int32_t* __restrict__ key,
                                                        const int32_t* __restrict__ pos, int n, int vocab, int dim,
@@ -644,7 +645,7 @@ __global__ __launch_bounds__(kLongThreads) void k_embedding_long_rows(const T* _
   }
 }
 
-size_t align16(size_t v) { return (v + 255) / 256 * 256; }
+size_t align256(size_t v) { return (v + 255) / 256 * 256; }
 
 // how the keys 0 .. vocab are sorted
 struct SortPlan {
@@ -670,7 +671,7 @@ Parts parts_of(int n, int vocab, int dim) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t o = off;
-    off = align16(off + bytes);
+    off = align256(off + bytes);
     return o;
   };
   for (int i = 0; i < 2; ++i) w.key[i] = take((size_t)n * 4), w.pos[i] = take((size_t)n * 4);
@@ -717,7 +718,8 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   int left = launches;
   const auto next_fill = [&] {
     const size_t bytes = (size_t)(fill_end - fill_at) / left-- / 16 * 16;
-    const Fill f = {fill_at, left ? bytes : (size_t)(fill_end - fill_at)};
+    Fill f = {fill_at, left ? bytes : (size_t)(fill_end - fill_at), kFill};
+    f.each = std::max(kFill, (f.bytes / kMaxFillBlocks + 16) / 16 * 16);
     fill_at += f.bytes;
     return f;
   };

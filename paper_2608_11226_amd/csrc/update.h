@@ -73,6 +73,8 @@ struct EmbeddingGradArgs {
   void* table;
 };
 constexpr int kMaxEmbeddingTokens = 1 << 28;
+// its launches have few enough workgroups
+inline bool embedding_backward_fits(int n, int dim) { return (int64_t)n * (((int64_t)dim + 1023) / 1024) <= (1 << 25); }
 size_t embedding_backward_workspace(int n, int vocab, int dim);
 hipError_t launch_embedding_backward(hipStream_t s, int grad_dtype, int table_dtype, const EmbeddingGradArgs& a, void* ws);
 

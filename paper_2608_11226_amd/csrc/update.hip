@@ -25,7 +25,7 @@ rollout_status fail(rollout_status st, const std::string& msg) {
   return st;
 }
 
-constexpr int32_t kMaxVocab = 1 << 30;
+constexpr int32_t kMaxVocab = 1 << 30, kMaxRows = 1 << 30;
 
 bool is_float_type(int32_t dtype) { return dtype == ROLLOUT_DTYPE_FP32 || dtype == ROLLOUT_DTYPE_BF16; }
 bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
@@ -65,7 +65,7 @@ rollout_status launched(hipError_t e, const char* what) {
 rollout_status check_rows(const void* z, int32_t dtype, int64_t stride, int32_t rows, int32_t vocab, float temperature) {
   if (!is_float_type(dtype)) return fail(ROLLOUT_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
   if (rows < 1 || vocab < 1) return fail(ROLLOUT_EINVAL, "n_rows and vocab must be >= 1");
-  if (vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab above 2^30");
+  if (rows > kMaxRows || vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "n_rows or vocab above 2^30");
   if (stride < vocab) return fail(ROLLOUT_EINVAL, "row_stride must be at least vocab");
   if (stride > INT64_MAX / 8 / rows) return fail(ROLLOUT_EINVAL, "row_stride too large");
   if (!z) return fail(ROLLOUT_EINVAL, "logits must be non-NULL");
@@ -92,7 +92,7 @@ extern "C" {
 rollout_status rollout_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top, uint64_t* h_bytes) {
   if (!h_bytes) return fail(ROLLOUT_EINVAL, "the result pointer is NULL");
   if (n_rows < 1 || vocab < 1) return fail(ROLLOUT_EINVAL, "n_rows and vocab must be >= 1");
-  if (vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "vocab above 2^30");
+  if (n_rows > kMaxRows || vocab > kMaxVocab) return fail(ROLLOUT_EUNSUPPORTED, "n_rows or vocab above 2^30");
   if (n_top < 0 || n_top > kMaxTop || n_top > vocab) return fail(ROLLOUT_EINVAL, "n_top must be in [0, 32] and at most vocab");
   if (n_top && vocab > kMaxTopVocab) return fail(ROLLOUT_EUNSUPPORTED, "alternatives of more than 327,680 ids");
   *h_bytes = logprobs_workspace(n_rows, vocab, n_top);
@@ -211,6 +211,8 @@ rollout_status rollout_embedding_backward_workspace(int32_t n_tokens, int32_t vo
   if (!h_bytes) return fail(ROLLOUT_EINVAL, "the result pointer is NULL");
   const rollout_status st = check_table(ROLLOUT_DTYPE_FP32, ROLLOUT_DTYPE_FP32, vocab, dim, n_tokens, 1.f);
   if (st != ROLLOUT_OK) return st;
+  if (!embedding_backward_fits(n_tokens, dim))
+    return fail(ROLLOUT_EUNSUPPORTED, "n_tokens times ceil(dim / 1024) above 2^25");
   *h_bytes = embedding_backward_workspace(n_tokens, vocab, dim);
   return ROLLOUT_OK;
 }
@@ -222,6 +224,9 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
   Range range("rollout_embedding_backward");
   rollout_status st = check_table(table_dtype, grad_dtype, vocab, dim, n_tokens, scale);
   if (st != ROLLOUT_OK) return st;
+  uint64_t need = 0;
+  st = rollout_embedding_backward_workspace(n_tokens, vocab, dim, &need);
+  if (st != ROLLOUT_OK) return st;
   if (accumulate != 0 && accumulate != 1) return fail(ROLLOUT_EINVAL, "accumulate must be 0 or 1");
   if (!d_grad || !d_tokens || !d_grad_table) return fail(ROLLOUT_EINVAL, "NULL buffer");
   if (!aligned_to(d_grad, elem_bytes(grad_dtype)) || !aligned_to(d_grad_table, elem_bytes(table_dtype)))
@@ -229,7 +234,7 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
   if (overlap(d_grad, (size_t)n_tokens * dim * elem_bytes(grad_dtype), d_grad_table,
               (size_t)vocab * dim * elem_bytes(table_dtype)))
     return fail(ROLLOUT_EINVAL, "the table's gradient overlaps the tokens' gradients");
-  st = check_workspace(d_workspace, workspace_bytes, embedding_backward_workspace(n_tokens, vocab, dim));
+  st = check_workspace(d_workspace, workspace_bytes, need);
   if (st != ROLLOUT_OK) return st;
   st = check_stream(hip_stream);
   if (st != ROLLOUT_OK) return st;

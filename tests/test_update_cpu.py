@@ -29,6 +29,7 @@ FORWARD = dict(z=A, dtype=0, stride=100, n=4, V=100, T=1.0, tokens=B, top=0, log
     (R.EINVAL, dict(n=0), "n_rows"), (R.EINVAL, dict(n=-3), "n_rows"), (R.EINVAL, dict(V=0), "vocab"),
     (R.EINVAL, dict(stride=99), "row_stride"), (R.EINVAL, dict(stride=1 << 62), "row_stride"),
     (R.EUNSUPPORTED, dict(V=(1 << 30) + 1, stride=1 << 31), "2^30"),
+    (R.EUNSUPPORTED, dict(n=(1 << 30) + 1), "2^30"),
     (R.EINVAL, dict(z=None), "logits"), (R.EINVAL, dict(z=A + 2), "aligned"), (R.EINVAL, dict(z=A + 1, dtype=1), "aligned"),
     (R.EINVAL, dict(T=0.0), "temperature"), (R.EINVAL, dict(T=-1.0), "temperature"), (R.EINVAL, dict(T=float("inf")), "temperature"),
     (R.EINVAL, dict(T=float("nan")), "temperature"), (R.EINVAL, dict(T=1e-40), "temperature"),
@@ -119,6 +120,7 @@ GRAD = dict(g=A, gdt=1, tokens=B, n=5, V=100, dim=8, scale=1.0, acc=0, table=C, 
 
 @pytest.mark.parametrize("code,change,text", [
     (R.EINVAL, dict(tdt=2), "dtype"), (R.EINVAL, dict(gdt=2), "dtype"), (R.EINVAL, dict(V=0), "vocab"), (R.EINVAL, dict(n=0), "n_tokens"),
+    (R.EUNSUPPORTED, dict(n=(1 << 25) + 1), "2^25"), (R.EUNSUPPORTED, dict(n=(1 << 23) + 1, dim=3585), "2^25"),
     (R.EINVAL, dict(acc=2), "accumulate"), (R.EINVAL, dict(scale=float("inf")), "scale"),
     (R.EINVAL, dict(g=None), "NULL"), (R.EINVAL, dict(tokens=None), "NULL"), (R.EINVAL, dict(table=None), "NULL"),
     (R.EINVAL, dict(g=A + 1), "aligned"), (R.EINVAL, dict(table=C + 2), "aligned"),
