@@ -173,6 +173,33 @@ def test_the_order_of_addition_follows_from_the_positions():
         assert torch.equal(first, again)
 
 
+@pytest.mark.parametrize("n", [300, 6000])
+def test_gradients_of_padding_are_not_used(n):
+    """NaN and infinities where the ids are padding or of no row; a token's own reach its row."""
+    rng = np.random.default_rng(17)
+    V, d = 70, 36
+    tok = ids("text", n, V, rng)
+    tok[::5] = -1
+    tok[1::50] = V
+    g = matrix(n, d, "fp32", rng)
+    td = to_dev(tok, torch)
+    want = torch.empty(V, d, device=DEV)
+    grad(g, "fp32", td, V, 1.0, 0, want, "fp32")
+    assert torch.isfinite(want).all()
+    outside = (td < 0) | (td >= V)
+    g[outside] = float("nan")
+    g[outside.nonzero().flatten()[::2]] = float("inf")
+    got = torch.empty(V, d, device=DEV)
+    grad(g, "fp32", td, V, 1.0, 0, got, "fp32")
+    assert torch.equal(want, got)
+    first = int(np.nonzero((tok >= 0) & (tok < V))[0][0])
+    g[first] = float("inf")
+    grad(g, "fp32", td, V, 1.0, 0, got, "fp32")
+    assert torch.all(got[tok[first]] == float("inf"))
+    others = torch.arange(V, device=DEV) != tok[first]
+    assert torch.equal(got[others], want[others])
+
+
 def test_a_large_table_passes_32_bit_offsets():
     """More than 2^31 elements of table and more than 2^31 bytes of gradients: rows at both ends."""
     V, d, n = 300000, 8192, 40

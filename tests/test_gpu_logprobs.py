@@ -146,6 +146,28 @@ def test_masks_infinities_and_invalid_tokens(dtype, V):
     assert want["logp"][1] == pytest.approx(-np.log(V)) and np.isneginf(want["logp"][6]) and np.isnan(want["logp"][7])
 
 
+@pytest.mark.parametrize("T", [0.01, 0.3, 7.5, 1000.0])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_temperatures(T, dtype):
+    """From almost certain to almost uniform: both directions."""
+    n, V = 6, 3001
+    z, seen, rng = rows(n, V, dtype, 31)
+    tok = rng.integers(0, V, n).astype(np.int32)
+    tok[:3] = seen[:3].argmax(1)
+    td = torch.from_numpy(tok).to(DEV)
+    T32 = float(np.float32(T))
+    log(f"temperature {T} {dtype}")
+    fw = forward(z, V, V, T, td, 5, dtype)
+    check_forward(fw, seen, T32, tok, 5)
+    g = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).to(DEV)
+    h = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).to(DEV)
+    out = torch.empty_like(z)
+    R.rollout_token_logprobs_backward(z, TYPE[dtype][1], V, n, V, T, td, fw["stats"], fw["entropy"], g, h, out, V)
+    num = [x.double().cpu().numpy() for x in (fw["stats"], fw["entropy"], g, h)]
+    want = U.token_logprobs_backward(seen, T32, tok, *num)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= backward_bound(seen, T32, tok, *num, want, dtype))
+
+
 def test_alternatives_of_values_that_stand_together():
     """All alternatives in one unit of a row, in every unit's first and last id, and equal everywhere."""
     V = 9000
