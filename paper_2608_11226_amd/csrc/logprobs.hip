@@ -280,6 +280,7 @@ __device__ __forceinline__ Soft scan_units(const T* zr, int V, float c, int lo, 
         raw[j] = u0 + j < hi ? load_row(zr, (u0 + j) * 64 * N + lane * N, V) : none;
     }
     float bm = -INFINITY;
+    uint32_t key = 0;  // lane j: of unit j's maximum
 #pragma unroll
     for (int j = 0; j < kUnits; ++j) {
       float v[N];
@@ -288,11 +289,12 @@ __device__ __forceinline__ Soft scan_units(const T* zr, int V, float c, int lo, 
 #pragma unroll
       for (int i = 1; i < N; ++i) um = fmaxf(um, v[i]);
       bm = fmaxf(bm, um);
-      if (KEYS && u0 + j < hi) {
+      if (KEYS) {
         const uint32_t k = wave_max_u32(key_of(um));
-        if (lane == 0) keys[u0 + j] = k;
+        key = lane == j ? k : key;
       }
     }
+    if (KEYS && lane < kUnits && u0 + lane < hi) keys[u0 + lane] = key;
     bm = fmaxf(a.m, bm);
     const float mm = finite_or_zero(bm);
     a = moved(a, bm, c);
