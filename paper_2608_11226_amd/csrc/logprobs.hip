@@ -188,6 +188,7 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
     if (wave == 0 && lane < nseg) lds.units[lane] = lane;
   }
   __syncthreads();
+  const float least = part ? of_key(part) : -INFINITY;
   constexpr int kAhead = 8;
   for (int r0 = wave; r0 < n; r0 += RW * kAhead) {
     u32x4 raw[kAhead];
@@ -204,10 +205,9 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
       unpack16(raw[j], v);
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const uint32_t k = key_of(v[i]);
-        if (k >= part && id0[j] + i < V) {
+        if (v[i] >= least && id0[j] + i < V) {
           const int at = atomicAdd(&lds.count, 1);
-          if (at < RB) lds.found[at] = make_uint2(k, (uint32_t)(id0[j] + i));
+          if (at < RB) lds.found[at] = make_uint2(key_of(v[i]), (uint32_t)(id0[j] + i));
         }
       }
     }
