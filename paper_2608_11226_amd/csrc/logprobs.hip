@@ -152,7 +152,8 @@ struct TopLds {
 // The same by a workgroup, where no more than RB values stand at or above a bound that at least `top` values reach.  Such
 // a bound is the top-th of 64 maxima of disjoint parts of the row: of the units' maxima, every 64th in a lane's part, or,
 // in rows of few units, of the threads' own values.  Only units whose maximum reaches the bound are read.  The values
-// found are ranked at once, every thread counting those before its own.
+// found are ranked at once, every thread counting those before its own.  (Twice the threads: 256 bf16 rows with 32 32.6 instead of
+// 35.2 us, but 300 rows of 1,024 ids 14.3 instead of 12.4.)
 template <typename T>
 __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int nseg, TopLds& lds, float m,
                          float temperature, float ln_s, int32_t* ids, float* logp, const uint32_t (&mine)[kMaxPer]) {
