@@ -355,7 +355,7 @@ __device__ __forceinline__ void note_run(const int32_t* key, int i, int n, int v
 
 // All passes by one workgroup, in LDS, for n up to kSmallSort, and the runs; the other workgroups zero the table.
 __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __restrict__ tokens, int n, int vocab, int passes,
-                                                              int bits, int32_t* key_out,
+                                                              int bits, int32_t* __restrict__ key_out,
                                                               int32_t* __restrict__ pos_out, int2* __restrict__ runs,
                                                               int32_t* __restrict__ longs, Fill fill) {
   __shared__ int32_t lds[4 * kSmallSort];  // keys and positions, of two buffers
@@ -397,24 +397,22 @@ __global__ __launch_bounds__(kSmallThreads) void k_sort_small(const int32_t* __r
       }
     }
     __syncthreads();
-    const bool done = pass == passes - 1;
     for (int i0 = lo; i0 < hi; i0 += 64) {
       const int i = i0 + lane;
       const bool valid = i < hi;
       const int k = valid ? key[i] : 0;
       const int to = take_place(place[wave], (k >> shift) & mask, valid, bits);
-      if (valid) {
-        (done ? key_out : key2)[to] = k;
-        (done ? pos_out : pos2)[to] = pos[i];
-      }
+      if (valid) key2[to] = k, pos2[to] = pos[i];
     }
     __syncthreads();
     int32_t* t = key;
     key = key2, key2 = t;
     t = pos, pos = pos2, pos2 = t;
   }
-  __syncthreads();  // the sorted keys are in memory, and this workgroup's own
-  for (int i = threadIdx.x; i < n; i += kSmallThreads) note_run(key_out, i, n, vocab, runs);
+  for (int i = threadIdx.x; i < n; i += kSmallThreads) {
+    key_out[i] = key[i], pos_out[i] = pos[i];
+    note_run(key, i, n, vocab, runs);
+  }
 }
 
 // ---------------------------------------------------------------------------
