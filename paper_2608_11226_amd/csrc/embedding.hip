@@ -9,8 +9,8 @@
 // sums once more.
 //
 // Both are bound by HBM where there is much to move: 49,152 rows of 3,584 looked up in 186 us (705 MB written beside some 150 MB
-// of scattered rows), their gradient into 152,064 fp32 rows in 494 us (2.18 GB, most of it zeros, beside 308 MB of gathered
-// rows: 5.0 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 9.5, rows 8.6, long rows 5.1 us).
+// of scattered rows), their gradient into 152,064 fp32 rows in 490 us (2.18 GB, most of it zeros, beside 308 MB of gathered
+// rows: 5.1 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 9.5, rows 8.6, long rows 5.1 us).
 #include "update.h"
 
 #include <type_traits>
@@ -21,8 +21,16 @@ namespace {
 constexpr int EB = 256;
 // Figures below are of the gradient of 49,152 tokens x 3,584 (bf16, text-like ids) into 152,064 fp32 rows, in all its launches,
 // and of 2,048 tokens x 128 (fp32) into 1,024 rows.
-// Entries of a piece, and pieces of a large piece: 16, 32 and 64 take 506, 493 and 503 us, and 21.9, 24.7 and 27.8.
-constexpr int kPiece = 32;
+// Entries of a piece (and pieces of a large piece): 1 << piece_shift(n, dim).  Pieces of 32 are best where there is much to add
+// (16, 32 and 64: 510, 488 and 484 us, 60,000 tokens x 640 88.8, 80.2 and 84.0), of 16 where the steps one after another count
+// (2,048 x 128 21.1, 23.5 and 25.7, 8,000 x 1,000 45.7, 48.8 and more, 16,000 x 1,000 49.1 and 52.6; 24,000 x 1,000 55.2 and
+// 56.4, 28,000 x 640 55.5 and 55.1, 16,000 x 2,048 59.3 and 58.3).  Few text-like tokens have no run of 32 (300 x 128 16.5 and
+// 13.8, 300 x 1,000 22.4 and 20.5; 500 x 128 17.7 and 18.1, 600 x 1,000 23.4 and 23.8).
+constexpr int kPieceShift = 5, kPiece = 1 << kPieceShift;
+constexpr int kFewTokens = 400, kSmallPieceTokens = 1 << 15, kSmallPieceValues = 1 << 24;
+inline int piece_shift(int n, int dim) {
+  return n >= kFewTokens && n < kSmallPieceTokens && (int64_t)n * dim <= kSmallPieceValues ? kPieceShift - 1 : kPieceShift;
+}
 constexpr int kAhead = 8;                // rows in flight
 constexpr int kEntries = 8;              // sorted entries whose rows a workgroup does (4, 8, 16: 490, 480, 488 us at the time)
 // Rows without tokens: about this many values a workgroup (4,096 491 us, 16,384 493, 65,536 501), if that leaves this many
@@ -433,10 +441,10 @@ __device__ __forceinline__ Shape shape_of(int width) {
   return {width, (int)blockDim.x / width, (int)threadIdx.x / width, ((int)threadIdx.x & (width - 1)) * 4};
 }
 
-// v += rows lo .. hi of g (those that pos names, or with pos NULL these themselves) at columns c .. c + 3, in order.  All lanes of
-// a group call it, also those behind the last column: half a wave (a group has whole ones) reads 32 positions at once, a lane each, so that a
-// batch of rows waits for itself alone (16,000 tokens into 2,064 x 640, bf16 into fp32, 56.0 -> 43.8 us; batches of 4 rows
-// 45.7, of 16 44.5).
+// v += rows lo .. hi of g (those that pos names, or with pos NULL these themselves) at columns c .. c + 3, in order.  All lanes
+// of a group call it, also those behind the last column: half a wave (a group has whole ones) reads 32 positions at once, a
+// lane each, so that a batch of rows waits for itself alone (16,000 tokens into 2,064 x 640, bf16 into fp32, 56.0 -> 43.8 us;
+// batches of 4 rows 45.7, of 16 44.5).
 template <typename T>
 __device__ __forceinline__ void add_rows(float (&v)[4], const T* g, const int32_t* pos, int lo, int hi, int dim, int c) {
   const int half = threadIdx.x & 32;
@@ -481,14 +489,14 @@ __device__ __forceinline__ void join_groups(float (&v)[4], const Shape& sh, floa
 struct Pieces {
   int p, q, P, Q;
 };
-__device__ __forceinline__ Pieces pieces_of(int2 run) {
+__device__ __forceinline__ Pieces pieces_of(int2 run, int shift) {
   Pieces r;
-  r.p = (run.x + kPiece - 1) / kPiece, r.q = max(run.y / kPiece, r.p);
+  r.p = (run.x + (1 << shift) - 1) >> shift, r.q = max(run.y >> shift, r.p);
   r.P = (r.p + kPiece - 1) / kPiece, r.Q = max(r.q / kPiece, r.P);
   return r;
 }
-__device__ __forceinline__ bool whole_piece(const int32_t* key, int p, int n, int vocab) {
-  return (int64_t)(p + 1) * kPiece <= n && key[p * kPiece] < vocab && key[p * kPiece] == key[p * kPiece + kPiece - 1];
+__device__ __forceinline__ bool whole_piece(const int32_t* key, int p, int shift, int n, int vocab) {
+  return p < n >> shift && key[p << shift] < vocab && key[p << shift] == key[((p + 1) << shift) - 1];
 }
 
 // dst row = scale * sum (+ dst row)
@@ -511,7 +519,7 @@ __device__ __forceinline__ void write_row(O* dst, int dim, int c, float scale, f
 // row is written where its run ends; the last run's entries behind these follow.
 template <typename T, typename O, bool ACC>
 __device__ __forceinline__ void do_entries(const T* g, const int32_t* key, const int32_t* pos, int n, int vocab, int dim,
-                                           float scale, const int2* runs, int first, int c, O* table) {
+                                           float scale, const int2* runs, int shift, int first, int c, O* table) {
   const int count = min(kEntries, n - first);
   int k[kEntries], at[kEntries];
 #pragma unroll
@@ -545,7 +553,7 @@ __device__ __forceinline__ void do_entries(const T* g, const int32_t* key, const
   }
   if (begin < 0) return;
   const int stop = row == final ? end : begin;  // a run before invalid ids has ended
-  const Pieces r = pieces_of(make_int2(begin, stop));
+  const Pieces r = pieces_of(make_int2(begin, stop), shift);
   if (r.p < r.q) return;
   add_rows(v, g, pos, first + count, max(stop, first + count), dim, c);
   if (c < dim) write_row<O, ACC>(table + (size_t)row * dim, dim, c, scale, v);
@@ -573,8 +581,8 @@ __device__ __forceinline__ void zero_rows(const ZeroRows& z, int block, int dim,
 template <typename T, typename O, bool ACC>
 __global__ __launch_bounds__(EB) void k_embedding_rows(const T* __restrict__ g, const int32_t* __restrict__ key,
                                                        const int32_t* __restrict__ pos, int n, int vocab, int dim,
-                                                       float scale, const int2* __restrict__ runs, int width, int slabs,
-                                                       int pieces, int starts, int zeros, ZeroRows z,
+                                                       float scale, const int2* __restrict__ runs, int shift, int width,
+                                                       int slabs, int pieces, int starts, int zeros, ZeroRows z,
                                                        float* __restrict__ sums, int32_t* __restrict__ longs,
                                                        O* __restrict__ table) {
   __shared__ float4 lds[EB];
@@ -584,12 +592,12 @@ __global__ __launch_bounds__(EB) void k_embedding_rows(const T* __restrict__ g, 
   if (b == (int)((blockIdx.x + 1) * busy / all)) return zero_rows(z, blockIdx.x - b, dim, sh, runs, table);
   if (b < pieces) {
     const int p = b / slabs, c = (b % slabs) * 4 * EB + sh.col;
-    if (!whole_piece(key, p, n, vocab)) return;
+    if (!whole_piece(key, p, shift, n, vocab)) return;
     // the first of its run: the run does not reach back over the whole piece before
-    if (threadIdx.x == 0 && b % slabs == 0 && (p == 0 || key[(p - 1) * kPiece] != key[p * kPiece]))
+    if (threadIdx.x == 0 && b % slabs == 0 && (p == 0 || key[(p - 1) << shift] != key[p << shift]))
       longs[1 + atomicAdd(longs, 1)] = p;
     float v[4] = {};
-    add_share(v, sh, g, pos, p * kPiece, p * kPiece + kPiece, dim, c);
+    add_share(v, sh, g, pos, p << shift, (p + 1) << shift, dim, c);
     join_groups(v, sh, lds);
     if (sh.group == 0 && c < dim) {
       float* dst = sums + (size_t)p * dim + c;  // read again soon
@@ -601,7 +609,7 @@ __global__ __launch_bounds__(EB) void k_embedding_rows(const T* __restrict__ g, 
     return;
   }
   const int first = ((b - pieces) / slabs * sh.groups + sh.group) * kEntries, c = ((b - pieces) % slabs) * 4 * EB + sh.col;
-  if (first < n) do_entries<T, O, ACC>(g, key, pos, n, vocab, dim, scale, runs, first, c, table);
+  if (first < n) do_entries<T, O, ACC>(g, key, pos, n, vocab, dim, scale, runs, shift, first, c, table);
 }
 
 // Large pieces (kPiece pieces) of one id, a slab of columns a workgroup.
@@ -624,7 +632,7 @@ __global__ __launch_bounds__(EB) void k_embedding_large(const int32_t* __restric
 template <typename T, typename O, bool ACC>
 __global__ __launch_bounds__(kLongThreads) void k_embedding_long_rows(const T* __restrict__ g, const int32_t* __restrict__ key,
                                                             const int32_t* __restrict__ pos, int dim, float scale,
-                                                            const int2* __restrict__ runs, int width, int slabs,
+                                                            const int2* __restrict__ runs, int shift, int width, int slabs,
                                                             const int32_t* __restrict__ longs, int busy, ZeroRows z,
                                                             const float* __restrict__ sums, const float* __restrict__ large,
                                                             O* __restrict__ table) {
@@ -633,11 +641,11 @@ __global__ __launch_bounds__(kLongThreads) void k_embedding_long_rows(const T* _
   if ((int)blockIdx.x >= busy) return zero_rows(z, blockIdx.x - busy, dim, sh, runs, table);
   const int64_t count = (int64_t)longs[0] * slabs;
   for (int64_t b = blockIdx.x; b < count; b += busy) {
-    const int c = (int)(b % slabs) * 4 * EB + sh.col, row = key[longs[1 + b / slabs] * kPiece];
+    const int c = (int)(b % slabs) * 4 * EB + sh.col, row = key[longs[1 + b / slabs] << shift];
     const int2 run = runs[row];
-    const Pieces r = pieces_of(run);
+    const Pieces r = pieces_of(run, shift);
     float v[4] = {};
-    add_share(v, sh, g, pos, run.x, r.p * kPiece, dim, c);
+    add_share(v, sh, g, pos, run.x, r.p << shift, dim, c);
     if (large && r.P < r.Q) {
       add_share(v, sh, sums, nullptr, r.p, r.P * kPiece, dim, c);
       add_share(v, sh, large, nullptr, r.P, r.Q, dim, c);
@@ -645,7 +653,7 @@ __global__ __launch_bounds__(kLongThreads) void k_embedding_long_rows(const T* _
     } else {
       add_share(v, sh, sums, nullptr, r.p, r.q, dim, c);
     }
-    add_share(v, sh, g, pos, r.q * kPiece, run.y, dim, c);
+    add_share(v, sh, g, pos, r.q << shift, run.y, dim, c);
     join_groups(v, sh, lds);
     if (sh.group == 0 && c < dim) write_row<O, ACC>(table + (size_t)row * dim, dim, c, scale, v);
   }
@@ -683,8 +691,11 @@ Parts parts_of(int n, int vocab, int dim) {
   for (int i = 0; i < 2; ++i) w.key[i] = take((size_t)n * 4), w.pos[i] = take((size_t)n * 4);
   w.hist = take((size_t)kMaxTiles * kDigits * 4);
   w.runs = take((size_t)vocab * sizeof(int2));
-  w.longs = take((size_t)(n / kPiece + 1) * 4);
-  w.sums = take((size_t)(n / kPiece) * dim * 4);
+  // sizes that no smaller n or dim exceeds, small pieces or not
+  const size_t small = std::min((size_t)n, (size_t)kSmallPieceTokens);
+  const size_t values = std::min((size_t)n * dim, (size_t)kSmallPieceValues);
+  w.longs = take((std::max((size_t)n / kPiece, small / (kPiece / 2)) + 1) * 4);
+  w.sums = take(std::max((size_t)(n / kPiece) * dim, values / (kPiece / 2)) * 4);
   w.large = take((size_t)(n / kPiece / kPiece) * dim * 4);
   w.bytes = off;
   return w;
@@ -715,7 +726,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   int32_t* longs = (int32_t*)(ws + w.longs);
   const SortPlan sp = sort_plan(a.n, a.vocab);
   const bool small = a.n <= kSmallSort;
-  const int launches = small ? 1 : 2 * sp.passes, pieces = a.n / kPiece;
+  const int launches = small ? 1 : 2 * sp.passes, shift = piece_shift(a.n, a.dim), pieces = a.n >> shift;
   const size_t row_bytes = (size_t)a.dim * sizeof(O);
   const ZeroPlan z = zero_plan(a, row_bytes, small, launches, pieces);
   // the sort's share of the zeros, launch by launch
@@ -757,8 +768,8 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   const int each = std::max(1, std::min(a.vocab / kRowWorkgroups, kRowValues / a.dim));
   const int zeros = (z.rows_end + each - 1) / each, long_zeros = (z.long_end - z.rows_end + each - 1) / each;
   hipLaunchKernelGGL((k_embedding_rows<T, O, ACC>), dim3((unsigned)((int64_t)pieces * slabs + starts + zeros)), dim3(EB), 0, s,
-                     (const T*)a.g, key, pos, a.n, a.vocab, a.dim, a.scale, runs, width, slabs, pieces * slabs, (int)starts,
-                     zeros, ZeroRows{0, z.rows_end, each}, sums, longs, (O*)a.table);
+                     (const T*)a.g, key, pos, a.n, a.vocab, a.dim, a.scale, runs, shift, width, slabs, pieces * slabs,
+                     (int)starts, zeros, ZeroRows{0, z.rows_end, each}, sums, longs, (O*)a.table);
   if (!pieces) return;
   // sums of sums where a run may have so many pieces that a workgroup would be long at them
   const int larges = pieces < kManyPieces ? 0 : pieces / kPiece;
@@ -768,7 +779,7 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   // at most as many as fit on the card beside each other; each does several rows if there are more
   const int busy = (int)std::min((int64_t)pieces * slabs, (int64_t)kLongWorkgroups);
   hipLaunchKernelGGL((k_embedding_long_rows<T, O, ACC>), dim3(busy + long_zeros), dim3(kLongThreads), 0, s, (const T*)a.g, key,
-                     pos, a.dim, a.scale, runs, width, slabs, longs, busy, ZeroRows{z.rows_end, z.long_end, each}, sums,
+                     pos, a.dim, a.scale, runs, shift, width, slabs, longs, busy, ZeroRows{z.rows_end, z.long_end, each}, sums,
                      larges ? large : nullptr, (O*)a.table);
 }
 

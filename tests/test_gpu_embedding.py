@@ -109,6 +109,28 @@ def test_gradient(n, V, d, kind):
 
 
 @pytest.mark.parametrize("kind", ["text", "same"])
+@pytest.mark.parametrize("n,V,d", [(32767, 3, 8), (32768, 3, 8), (32767, 40, 512), (16384, 5, 1024), (16385, 5, 1024), (15, 2, 4),
+                                   (16, 2, 4), (17, 2, 4), (31, 2, 4), (33, 2, 4), (399, 2, 4), (400, 2, 4)])
+def test_gradient_where_pieces_change_their_length(n, V, d, kind):
+    """Nothing behind the workspace is written, and the workspace of more tokens of more columns serves as well."""
+    rng = np.random.default_rng(n + d)
+    tok = ids(kind, n, V, rng)
+    td = to_dev(tok, torch)
+    log(f"{n} {kind} tokens, {V} x {d}")
+    g = matrix(n, d, "fp32", rng)
+    need, more = R.rollout_embedding_backward_workspace(n, V, d), R.rollout_embedding_backward_workspace(n + 1000, V, d + 100)
+    assert more >= need
+    ws = torch.full((more + 64,), 255, dtype=torch.uint8, device=DEV)
+    table = torch.empty(V, d, device=DEV)
+    R.rollout_embedding_backward(g, 0, td, n, V, d, 1.0, 0, table, 0, ws, need, None)
+    check_grad(table.double().cpu().numpy(), g, tok, V, 1.0, None, "fp32")
+    assert torch.all(ws[need:] == 255)
+    again = torch.empty(V, d, device=DEV)
+    R.rollout_embedding_backward(g, 0, td, n, V, d, 1.0, 0, again, 0, ws, more, None)
+    assert torch.equal(table, again)
+
+
+@pytest.mark.parametrize("kind", ["text", "same"])
 def test_gradient_of_more_than_a_million_tokens(kind):
     """Tiles longer than what a lane holds on to, more tokens than a lookup's grid has workgroups, and, all of one id, sums of
     sums of pieces."""

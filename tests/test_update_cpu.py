@@ -138,3 +138,12 @@ def test_workspaces_of_loss_and_embedding():
     refuse(R.EINVAL, R.rollout_embedding_backward_workspace, 0, 4, 4)
     assert R.lib.grpo_policy_loss_workspace(1, 1, None) == R.EINVAL
     assert R.lib.rollout_embedding_backward_workspace(1, 1, 1, None) == R.EINVAL
+
+
+@pytest.mark.parametrize("dim", [1, 500, 513, 1024, 3584])
+def test_the_embedding_workspace_of_more_serves_less(dim):
+    sizes = [R.rollout_embedding_backward_workspace(n, 1000, dim) for n in (1, 31, 4096, 4097, 16384, 16385, 32767, 32768, 70000)]
+    assert sizes == sorted(sizes)
+    for n in (100, 16000, 32767, 40000):
+        assert R.rollout_embedding_backward_workspace(n, 1000, dim) <= R.rollout_embedding_backward_workspace(n, 1000, dim + 1)
+        assert R.rollout_embedding_backward_workspace(n, 1000, dim) <= R.rollout_embedding_backward_workspace(n, 1001, dim)
