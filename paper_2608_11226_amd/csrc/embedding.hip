@@ -9,8 +9,8 @@
 // sums once more.
 //
 // Both are bound by HBM where there is much to move: 49,152 rows of 3,584 looked up in 186 us (705 MB written beside some 150 MB
-// of scattered rows), their gradient into 152,064 fp32 rows in 490 us (2.18 GB, most of it zeros, beside 308 MB of gathered
-// rows: 5.1 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 9.5, rows 8.6, long rows 5.1 us).
+// of scattered rows), their gradient into 152,064 fp32 rows in 491 us (2.18 GB, most of it zeros, beside 308 MB of gathered
+// rows: 5.1 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 8.6, rows 6.1, long rows 5.8 us).
 #include "update.h"
 
 #include <type_traits>
@@ -702,7 +702,7 @@ Parts parts_of(int n, int vocab, int dim) {
 }
 
 // Who zeroes the rows without tokens.  The small sort's launch zeroes the whole table beside it, for few rows are then written
-// twice (300 tokens into 152,064 x 3,584 fp32 414 -> 374 us).  The other sort and the long rows leave most of the card's memory
+// twice (300 tokens into 152,064 x 3,584 fp32 414 -> 374 us at the time).  The other sort and the long rows leave most of the card's memory
 // bandwidth unused for some microseconds a launch, so each of their launches zeroes about as much as fits there: first the
 // sort's, from the table's end (all rows, for no one knows yet which have tokens), then that of the long rows, then the one of
 // the other rows.
