@@ -292,9 +292,10 @@ rollout_status rollout_sample_noalloc(const float* d_logits, int32_t n_seqs, int
  * device (NULL = its default stream; a stream of another device: EINVAL), and
  * every buffer is the caller's, on that device.  A workspace is device memory
  * aligned to 16 bytes, at least as large as the call's _workspace query says
- * for the same sizes; nothing is kept in it from one call to the next, and
- * calls that may run at the same time (two streams, two captured graphs) need
- * one each.  Nothing is allocated or waited for, so every call can be captured
+ * for the same sizes (for larger ones it says no less, so the workspace of the
+ * largest call serves them all); nothing is kept in it from one call to the
+ * next, and calls that may run at the same time (two streams, two captured
+ * graphs) need one each.  Nothing is allocated or waited for, so every call can be captured
  * into a HIP graph.  Messages: rollout_last_error(NULL).
  *
  * dtype of a matrix: ROLLOUT_DTYPE_FP32 or ROLLOUT_DTYPE_BF16.  Arithmetic is

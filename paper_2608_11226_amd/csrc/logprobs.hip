@@ -477,9 +477,9 @@ struct Split {
 // Enough workgroups for the whole card where rows are few; a wave's share of a chunk is one batch of loads at least.
 // Short rows stay whole, whose second kernel would take longer than the loads it shares out (8,192 fp32 ids, 1 and 64 rows:
 // 5.2 and 5.4 us whole, 6.8 and 7.5 split; 32,003 ids 7.7 and 10.7 whole, 7.1 and 8.5 split).
+int most_chunks(int nseg) { return nseg <= kWhole ? 1 : std::min(kMaxChunks, nseg / (RW * kUnits)); }
 Split split_of(int rows, int nseg) {
-  const int most = nseg <= kWhole ? 1 : std::min(kMaxChunks, nseg / (RW * kUnits));
-  const int want = std::max(1, std::min(most, kWorkgroups / rows));
+  const int want = std::max(1, std::min(most_chunks(nseg), kWorkgroups / rows));
   const int units = (nseg + want - 1) / want;
   return {(nseg + units - 1) / units, units};
 }
@@ -521,12 +521,12 @@ void backward(hipStream_t s, const LogprobGradArgs& a) {
 
 }  // namespace
 
-// parts, and the keys of the units: for the type with more units
+// Parts, and the keys of the units, for the type with more units.  As many parts as any number of rows up to this one has, so
+// that the workspace of a large call serves small ones.
 size_t logprobs_workspace(int rows, int vocab, int top) {
-  size_t chunks = 0;
-  for (int N : {4, 8}) chunks = std::max(chunks, (size_t)split_of(rows, units_of(vocab, N)).chunks);
-  if (!top && chunks == 1) return 0;
-  return (size_t)rows * (chunks * sizeof(Soft) + (top ? (size_t)units_of(vocab, 4) * 4 : 0));
+  const size_t units = units_of(vocab, 4), most = most_chunks((int)units);
+  const size_t split = most > 1 ? std::min((size_t)rows * most, (size_t)kWorkgroups) : 0;
+  return (top ? std::max((size_t)rows, split) : split) * sizeof(Soft) + (top ? (size_t)rows * units * 4 : 0);
 }
 
 hipError_t launch_logprobs(hipStream_t s, int dtype, const LogprobArgs& a, void* ws) {

@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 
 import paper_2608_11226_amd as R
-from gpu_helpers import log
+from gpu_helpers import log, to_dev
 from oracle import update as U
 
 torch = pytest.importorskip("torch")
@@ -437,3 +437,21 @@ def test_tensors_of_rows():
         with pytest.raises(R.RolloutError) as e:
             bad()
         assert e.value.code == R.EINVAL
+
+
+@pytest.mark.parametrize("top", [0, 20])
+def test_the_workspace_of_a_large_call_serves_small_ones(top):
+    """The same bits as with a workspace of the call's own, and nothing behind what its size asks for is written."""
+    rng = np.random.default_rng(31)
+    V, most = 20000, 3000
+    big = torch.full((R.rollout_token_logprobs_workspace(most, V, top) + 64,), 255, dtype=torch.uint8, device=DEV)
+    for n in (1, 7, 130, 1024):
+        log(f"{n} rows of {V}, {top} alternatives")
+        z = to_dev(rng.standard_normal((n, V)).astype(np.float32), torch)
+        tokens = to_dev(rng.integers(0, V, n).astype(np.int32), torch)
+        want = forward(z, V, V, 1.0, tokens, top)
+        big.fill_(255)
+        got = forward(z, V, V, 1.0, tokens, top, ws=big)
+        for k in ("logp", "entropy", "stats", "ids", "top_logp"):
+            assert torch.equal(want[k], got[k]), k
+        assert torch.all(big[R.rollout_token_logprobs_workspace(n, V, top):] == 255)

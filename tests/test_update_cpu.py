@@ -147,3 +147,22 @@ def test_the_embedding_workspace_of_more_serves_less(dim):
     for n in (100, 16000, 32767, 40000):
         assert R.rollout_embedding_backward_workspace(n, 1000, dim) <= R.rollout_embedding_backward_workspace(n, 1000, dim + 1)
         assert R.rollout_embedding_backward_workspace(n, 1000, dim) <= R.rollout_embedding_backward_workspace(n, 1001, dim)
+
+
+@pytest.mark.parametrize("top", [0, 1, 32])
+def test_the_logprobs_workspace_of_more_serves_less(top):
+    rows, vocabs = (1, 2, 33, 64, 1000, 1025, 2048, 2049, 4096, 70000), (32, 4096, 16384, 16385, 32003, 152064, 327680)
+    for V in vocabs:
+        sizes = [R.rollout_token_logprobs_workspace(n, V, top) for n in rows]
+        assert sizes == sorted(sizes)
+    for n in rows:
+        sizes = [R.rollout_token_logprobs_workspace(n, V, top) for V in vocabs]
+        assert sizes == sorted(sizes)
+        assert sizes[0] >= R.rollout_token_logprobs_workspace(n, 32, 0)
+
+
+def test_the_loss_workspace_of_more_serves_less():
+    sizes = [R.grpo_policy_loss_workspace(n, 4096) for n in (1, 2, 7, 64, 700, 2048, 100000)]
+    assert sizes == sorted(sizes)
+    sizes = [R.grpo_policy_loss_workspace(64, n) for n in (1, 100, 511, 4096, 100000)]
+    assert sizes == sorted(sizes)
