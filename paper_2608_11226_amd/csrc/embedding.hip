@@ -244,6 +244,8 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, int block) {
 
 // A pass of the sort is two launches: the digits of every tile (a workgroup's keys) are counted, then every workgroup adds up
 // the other tiles' counts itself and places its keys.  49,152 tokens take 4.8 and 8.2 us a pass without the zeros beside them.
+// (The next pass's counts by atomics on memory while keys are placed, a launch less: 16,000 tokens x 640 48.0 instead of 41.4
+// us.)
 // The workgroups behind the tiles zero a share of the table: the sort leaves most of the card free.
 //
 // Digit counts into hist[tile][digit].  The first pass also empties the rows' runs and the list of long rows.
