@@ -41,16 +41,17 @@ constexpr int kLongThreads = 1024, kLongWorkgroups = 512;
 // From so many pieces on (65,536 tokens) pieces are summed to large ones first: one id's 2,047 pieces are 64 steps of a long
 // row's groups, and the kernel that sums them takes 7 us whether there is such an id or not.
 constexpr int kManyPieces = 2048;
-// Bytes of zeros that a launch of the sort writes beside it (none 526 us, 80 MB 497, 160 MB 493, 320 MB 496; 5,000 tokens into
-// a bf16 table 231, 203, 201 and 226), that of the long rows (none 535 us, 96 or 200 MB 530 at the time), and a workgroup.
+// Bytes of zeros that a launch of the sort writes beside it (none 526 us, 80 MB 497, 160 MB 493, 320 MB 496; 5,000 tokens by
+// tiles into a bf16 table 231, 203, 201 and 226), that of the long rows (none 535 us, 96 or 200 MB 530 at the time), and a workgroup.
 constexpr size_t kSortFill = 160u << 20, kLongFill = 96u << 20, kFill = 16384;
 constexpr int kMaxFillBlocks = 1 << 20;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortWaves = EB / 64;
 constexpr int kMaxTiles = 256;
 constexpr int kHeld = 4;                 // keys that a lane holds on to
-// Up to so many tokens (as many as the LDS holds twice) one workgroup sorts alone (4,000 tokens 34.8 us, by tiles 45.8).
-constexpr int kSmallSort = 4096, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+// Up to so many tokens one workgroup sorts alone, in LDS (6,000 x 640 34.3 us, by tiles 36.0, 5,000 x 1,000 33.6 and 41.1;
+// 7,900 x 640 would take 39.5 and by tiles 35.8).
+constexpr int kSmallSort = 6144, kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 
 // ---------------------------------------------------------------------------
 // pieces of rows: P values from any element on, of which n exist
@@ -245,7 +246,7 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, int block) {
 // A pass of the sort is two launches: the digits of every tile (a workgroup's keys) are counted, then every workgroup adds up
 // the other tiles' counts itself and places its keys.  49,152 tokens take 4.8 and 8.2 us a pass without the zeros beside them.
 // (The next pass's counts by atomics on memory while keys are placed, a launch less: 16,000 tokens x 640 48.0 instead of 41.4
-// us.)
+// us at the time.)
 // The workgroups behind the tiles zero a share of the table: the sort leaves most of the card free.
 //
 // Digit counts into hist[tile][digit].  The first pass also empties the rows' runs and the list of long rows.
@@ -673,8 +674,9 @@ SortPlan sort_plan(int n, int vocab) {
   SortPlan p;
   p.passes = (b + kDigitBits - 1) / kDigitBits;
   p.bits = (b + p.passes - 1) / p.passes;
-  // at most kMaxTiles tiles: every workgroup of a pass reads all of their counts
-  p.sub = std::max(256, (int)(((int64_t)n + kMaxTiles * kSortWaves - 1) / (kMaxTiles * kSortWaves) + 63) & ~63);
+  // at most kMaxTiles tiles: every workgroup of a pass reads all of their counts (at least 256 keys a wave: 8,000 x 1,000 45.9
+  // instead of 42.4 us, 44,112 x 1,000 66.7 instead of 65.5; at least 64: 42.2 and 69.3)
+  p.sub = std::max(128, (int)(((int64_t)n + kMaxTiles * kSortWaves - 1) / (kMaxTiles * kSortWaves) + 63) & ~63);
   p.tiles = (int)(((int64_t)n + (int64_t)p.sub * kSortWaves - 1) / ((int64_t)p.sub * kSortWaves));
   return p;
 }

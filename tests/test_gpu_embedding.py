@@ -85,7 +85,8 @@ def check_grad(got, g, tok, V, scale, base, tdt):
 @pytest.mark.parametrize("kind", ["uniform", "same", "text"])
 @pytest.mark.parametrize("n,V,d", [(1, 1, 1), (2, 5, 3), (63, 40, 8), (64, 40, 9), (65, 3, 128), (1000, 600, 100), (4096, 1024, 128),
                                    (4097, 1024, 128), (4200, 511, 40), (9000, 512, 24), (70000, 300, 16), (140000, 40, 33), (3000, 300000, 8),
-                                   (6000, 300000, 8), (200, 50, 3584), (5000, 2064, 2049)])
+                                   (6000, 300000, 8), (200, 50, 3584), (5000, 2064, 2049), (6144, 1024, 128), (6145, 1024, 128),
+                                   (6145, 300000, 8), (8000, 511, 40), (7000, 2064, 2049)])
 def test_gradient(n, V, d, kind):
     rng = np.random.default_rng(n + V)
     tok = ids(kind, n, V, rng)
