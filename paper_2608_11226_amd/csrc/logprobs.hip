@@ -151,7 +151,7 @@ struct TopLds {
 
 // The same by a workgroup, where no more than RB values stand at or above a bound that at least `top` values reach.  Such
 // a bound is the top-th of 64 maxima of disjoint parts of the row: of the units' maxima, every 64th in a lane's part, or,
-// in rows of few units, of the threads' own values.  Only units whose maximum reaches the bound are read.  The values
+// in rows of fewer units than alternatives, of the threads' own values.  Only units whose maximum reaches the bound are read.  The values
 // found are ranked at once, every thread counting those before its own.  (Twice the threads: 256 bf16 rows with 32 32.6 instead of
 // 35.2 us, but 300 rows of 1,024 ids 14.3 instead of 12.4.)
 template <typename T>
@@ -162,7 +162,7 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
   if (threadIdx.x == 0) lds.count = 0;
   uint32_t part = 0;
   int n = 0;  // units to read, the same in every wave
-  if (nseg >= 64) {
+  if (nseg >= top) {
 #pragma unroll
     for (int i = 0; i < kMaxPer; ++i) part = max(part, mine[i]);
     part = kth_key(part, top);
@@ -475,12 +475,18 @@ struct Split {
   int chunks, units;  // of a row; units of a chunk
 };
 // Enough workgroups for the whole card where rows are few; a wave's share of a chunk is one batch of loads at least.
+// Chunks are whole batches of a workgroup's loads, the nearest number of them, so that no wave does a rest alone (64 rows of
+// 152,064 fp32 ids with 8 alternatives 19.3 us with chunks of 19 units, 18.0 with 16; bf16 17.6 and 16.3).
 // Short rows stay whole, whose second kernel would take longer than the loads it shares out (8,192 fp32 ids, 1 and 64 rows:
 // 5.2 and 5.4 us whole, 6.8 and 7.5 split; 32,003 ids 7.7 and 10.7 whole, 7.1 and 8.5 split).
-int most_chunks(int nseg) { return nseg <= kWhole ? 1 : std::min(kMaxChunks, nseg / (RW * kUnits)); }
-Split split_of(int rows, int nseg) {
-  const int want = std::max(1, std::min(most_chunks(nseg), kWorkgroups / rows));
-  const int units = (nseg + want - 1) / want;
+constexpr int kBatchUnits = RW * kUnits;
+int most_chunks(int nseg, bool join) { return nseg <= kWhole && !join ? 1 : std::min(kMaxChunks, nseg / kBatchUnits); }
+Split split_of(int rows, int nseg, bool join) {
+  const int want = std::max(1, std::min(most_chunks(nseg, join), kWorkgroups / rows));
+  if (want == 1) return {1, nseg};
+  int units = (nseg + want - 1) / want;
+  const int whole = std::max(kBatchUnits, (units + kBatchUnits / 2) / kBatchUnits * kBatchUnits);
+  units = (nseg + whole - 1) / whole <= kMaxChunks ? whole : (units + kBatchUnits - 1) / kBatchUnits * kBatchUnits;
   return {(nseg + units - 1) / units, units};
 }
 
@@ -489,13 +495,14 @@ void forward(hipStream_t s, const LogprobArgs& a, char* ws) {
   constexpr int N = Chunk16<T>::N;
   const float c = (float)(1.4426950408889634 / (double)a.temperature);
   const int nseg = units_of(a.vocab, N);
-  const Split p = split_of(a.rows, nseg);
+  // A wave a row where rows are short and many, so that no wave waits for others over a few loads (fp32, 20,000 rows of 2,064
+  // ids 30 us, 41 by workgroups; 2,000 of 4,099 bf16 8.7 and 9.5; 300 rows of 4,099 fp32 are faster by workgroups).
+  const bool waves = nseg <= kUnits || (nseg <= kWhole && a.rows >= kWaveRows);
+  const Split p = waves ? Split{1, nseg} : split_of(a.rows, nseg, KEYS);
   const bool join = KEYS || p.chunks > 1;
   Soft* part = join ? (Soft*)ws : nullptr;
   uint32_t* keys = KEYS ? (uint32_t*)(part + (size_t)a.rows * p.chunks) : nullptr;
-  // A wave a row where rows are short and many, so that no wave waits for others over a few loads (fp32, 20,000 rows of 2,064
-  // ids 30 us, 41 by workgroups; 2,000 of 4,099 bf16 8.7 and 9.5; 300 rows of 4,099 fp32 are faster by workgroups).
-  if (nseg <= kUnits || (nseg <= kWhole && a.rows >= kWaveRows))
+  if (waves)
     hipLaunchKernelGGL((k_logprobs<T, 1, KEYS>), dim3(std::min((a.rows + RW - 1) / RW, kMaxGrid)), dim3(RB), 0, s, a, c, nseg,
                        part, keys);
   else
@@ -524,8 +531,10 @@ void backward(hipStream_t s, const LogprobGradArgs& a) {
 // Parts, and the keys of the units, for the type with more units.  As many parts as any number of rows up to this one has, so
 // that the workspace of a large call serves small ones.
 size_t logprobs_workspace(int rows, int vocab, int top) {
-  const size_t units = units_of(vocab, 4), most = most_chunks((int)units);
-  const size_t split = most > 1 ? std::min((size_t)rows * most, (size_t)kWorkgroups) : 0;
+  const size_t units = units_of(vocab, 4);
+  // r rows have at most kWorkgroups / r chunks each and half as many again where these are rounded to whole batches, and at
+  // most kWorkgroups / 2 rows have more than one
+  const size_t split = most_chunks((int)units, top > 0) > 1 ? std::min((size_t)rows * kMaxChunks, 2 * (size_t)kWorkgroups) : 0;
   return (top ? std::max((size_t)rows, split) : split) * sizeof(Soft) + (top ? (size_t)rows * units * 4 : 0);
 }
 
