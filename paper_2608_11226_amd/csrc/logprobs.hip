@@ -26,7 +26,7 @@ constexpr int kMaxChunks = 64;     // a lane each when parts are joined
 // 8,192; 256 fp32 rows with alternatives 44.4, 41.9 and 46.9 at the time.
 constexpr int kWorkgroups = 2048;
 constexpr int kWhole = 64;         // units of a row that is not split
-constexpr int kWaveRows = 1024;    // rows from which such a row is one wave's
+constexpr int kWaveRows = 2048;    // rows from which such a row is one wave's
 constexpr int kMaxGrid = 1 << 20;
 constexpr int kBatch = 4;          // 16-byte loads in flight a thread in the gradient
 constexpr size_t kLastLevelBytes = 256u << 20;
@@ -151,9 +151,10 @@ struct TopLds {
 
 // The same by a workgroup, where no more than RB values stand at or above a bound that at least `top` values reach.  Such
 // a bound is the top-th of 64 maxima of disjoint parts of the row: of the units' maxima, every 64th in a lane's part, or,
-// in rows of fewer units than alternatives, of the threads' own values.  Only units whose maximum reaches the bound are read.  The values
-// found are ranked at once, every thread counting those before its own.  (Twice the threads: 256 bf16 rows with 32 32.6 instead of
-// 35.2 us, but 300 rows of 1,024 ids 14.3 instead of 12.4.)
+// in rows of fewer units than alternatives, of the threads' own values (128 rows of 32,003 bf16 ids, 63 units, with 5: 25.9
+// us so, 19.1 by units).  Only units whose maximum reaches the bound are read.  The values found are ranked at once, every
+// thread counting those before its own.  (Twice the threads: 256 bf16 rows with 32 32.6 instead of 35.2 us, but 300 rows of
+// 1,024 ids 14.3 instead of 12.4.)
 template <typename T>
 __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int nseg, TopLds& lds, float m,
                          float temperature, float ln_s, int32_t* ids, float* logp, const uint32_t (&mine)[kMaxPer]) {
@@ -478,7 +479,8 @@ struct Split {
 // Chunks are whole batches of a workgroup's loads, the nearest number of them, so that no wave does a rest alone (64 rows of
 // 152,064 fp32 ids with 8 alternatives 19.3 us with chunks of 19 units, 18.0 with 16; bf16 17.6 and 16.3).
 // Short rows stay whole, whose second kernel would take longer than the loads it shares out (8,192 fp32 ids, 1 and 64 rows:
-// 5.2 and 5.4 us whole, 6.8 and 7.5 split; 32,003 ids 7.7 and 10.7 whole, 7.1 and 8.5 split).
+// 5.2 and 5.4 us whole, 6.8 and 7.5 split; 32,003 ids 7.7 and 10.7 whole, 7.1 and 8.5 split); with alternatives there is a
+// second kernel anyway (128 rows of 32,003 bf16 ids with 5 19.1 us whole, 15.7 split; 300 of 8,192 fp32 15.1 and 14.3).
 constexpr int kBatchUnits = RW * kUnits;
 int most_chunks(int nseg, bool join) { return nseg <= kWhole && !join ? 1 : std::min(kMaxChunks, nseg / kBatchUnits); }
 Split split_of(int rows, int nseg, bool join) {
@@ -496,7 +498,9 @@ void forward(hipStream_t s, const LogprobArgs& a, char* ws) {
   const float c = (float)(1.4426950408889634 / (double)a.temperature);
   const int nseg = units_of(a.vocab, N);
   // A wave a row where rows are short and many, so that no wave waits for others over a few loads (fp32, 20,000 rows of 2,064
-  // ids 30 us, 41 by workgroups; 2,000 of 4,099 bf16 8.7 and 9.5; 300 rows of 4,099 fp32 are faster by workgroups).
+  // ids 29 us, 37 by workgroups; bf16, 4,000 of 4,099 12.2 and 15.5, 12,000 of 32,003 128 and 153, of 32,000 125 and 120).
+  // Fewer rows are too few waves (bf16, 1,500 of 4,099 8.1 and 7.3, of 32,003 26.8 and 24.8; 1,100 of 16,000 fp32 21.4 and
+  // 16.1).
   const bool waves = nseg <= kUnits || (nseg <= kWhole && a.rows >= kWaveRows);
   const Split p = waves ? Split{1, nseg} : split_of(a.rows, nseg, KEYS);
   const bool join = KEYS || p.chunks > 1;

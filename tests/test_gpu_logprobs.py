@@ -455,3 +455,21 @@ def test_the_workspace_of_a_large_call_serves_small_ones(top):
         for k in ("logp", "entropy", "stats", "ids", "top_logp"):
             assert torch.equal(want[k], got[k]), k
         assert torch.all(big[R.rollout_token_logprobs_workspace(n, V, top):] == 255)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,units", [(2, 19), (2, 20), (3, 21), (2, 31), (40, 32), (2, 33), (3, 47), (2, 48), (150, 63), (2, 64),
+                                     (2, 65), (1024, 17), (2047, 5), (2048, 5), (2049, 17), (700, 40)])
+def test_alternatives_of_rows_of_any_number_of_units(n, units, dtype):
+    """Around as many units (1 KB) as alternatives, a split row or not, a wave or a workgroup a row; rows that end in a unit and
+    with it, some with many equal values."""
+    N = 4 if dtype == "fp32" else 8
+    for V in (units * 64 * N, units * 64 * N - 3):
+        log(f"alternatives {dtype} {n} x {V}")
+        z, seen, rng = rows(n, V, dtype, V, 0, 0, n > 1)
+        tok = rng.integers(0, V, n).astype(np.int32)
+        tok[::7] = -1
+        tok[0] = V - 1
+        td = torch.from_numpy(tok).to(DEV)
+        check_forward(forward(z, V, V, 1.0, td, 20, dtype), seen, 1.0, tok, 20)
+        check_forward(forward(z, V, V, 1.0, td, 0, dtype), seen, 1.0, tok)
