@@ -10,7 +10,7 @@
 //
 // Both are bound by HBM where there is much to move: 49,152 rows of 3,584 looked up in 186 us (705 MB written beside some 150 MB
 // of scattered rows), their gradient into 152,064 fp32 rows in 491 us (2.18 GB, most of it zeros, beside 308 MB of gathered
-// rows: 5.1 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 8.6, rows 6.1, long rows 5.8 us).
+// rows: 5.1 TB/s).  Small gradients are three launches (2,048 tokens x 128: sort 8.8, rows 6.2, long rows 5.8 us).
 #include "update.h"
 
 #include <type_traits>
@@ -42,7 +42,8 @@ constexpr int kLongThreads = 1024, kLongWorkgroups = 512;
 // row's groups, and the kernel that sums them takes 7 us whether there is such an id or not.
 constexpr int kManyPieces = 2048;
 // Bytes of zeros that a launch of the sort writes beside it (none 526 us, 80 MB 497, 160 MB 493, 320 MB 496; 5,000 tokens by
-// tiles into a bf16 table 231, 203, 201 and 226), that of the long rows (none 535 us, 96 or 200 MB 530 at the time), and a workgroup.
+// tiles into a bf16 table 231, 203, 201 and 226), that of the long rows (none 535 us, 96 or 200 MB 530 at the
+// time), and a workgroup (300 tokens into 152,064 x 3,584 fp32: 16 KB 362 us, 64 KB 433, 256 KB 382).
 constexpr size_t kSortFill = 160u << 20, kLongFill = 96u << 20, kFill = 16384;
 constexpr int kMaxFillBlocks = 1 << 20;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
@@ -706,9 +707,9 @@ Parts parts_of(int n, int vocab, int dim) {
 }
 
 // Who zeroes the rows without tokens.  The small sort's launch zeroes the whole table beside it, for few rows are then written
-// twice (300 tokens into 152,064 x 3,584 fp32 414 -> 374 us at the time).  The other sort and the long rows leave most of the card's memory
-// bandwidth unused for some microseconds a launch, so each of their launches zeroes about as much as fits there: first the
-// sort's, from the table's end (all rows, for no one knows yet which have tokens), then that of the long rows, then the one of
+// twice (300 tokens into 152,064 x 3,584 fp32 414 -> 374 us at the time).  The other sort and the long rows leave most of the
+// card's memory bandwidth unused for some microseconds a launch, so each of their launches zeroes about as much as fits there:
+// first the sort's, from the table's end (all rows, for no one knows yet which have tokens), then that of the long rows, then the one of
 // the other rows.
 struct ZeroPlan {
   int rows_end, long_end;  // [0, rows_end), [rows_end, long_end), and the sort's [long_end, vocab)

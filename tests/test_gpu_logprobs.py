@@ -459,10 +459,11 @@ def test_the_workspace_of_a_large_call_serves_small_ones(top):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("n,units", [(2, 19), (2, 20), (3, 21), (2, 31), (40, 32), (2, 33), (3, 47), (2, 48), (150, 63), (2, 64),
-                                     (2, 65), (1024, 17), (2047, 5), (2048, 5), (2049, 17), (700, 40)])
+                                     (2, 65), (1024, 17), (2047, 5), (2048, 5), (2049, 17), (700, 40), (682, 69), (1024, 66),
+                                     (409, 115), (1, 1100)])
 def test_alternatives_of_rows_of_any_number_of_units(n, units, dtype):
     """Around as many units (1 KB) as alternatives, a split row or not, a wave or a workgroup a row; rows that end in a unit and
-    with it, some with many equal values."""
+    with it, some with many equal values.  Nothing behind the workspace is written."""
     N = 4 if dtype == "fp32" else 8
     for V in (units * 64 * N, units * 64 * N - 3):
         log(f"alternatives {dtype} {n} x {V}")
@@ -471,5 +472,8 @@ def test_alternatives_of_rows_of_any_number_of_units(n, units, dtype):
         tok[::7] = -1
         tok[0] = V - 1
         td = torch.from_numpy(tok).to(DEV)
-        check_forward(forward(z, V, V, 1.0, td, 20, dtype), seen, 1.0, tok, 20)
-        check_forward(forward(z, V, V, 1.0, td, 0, dtype), seen, 1.0, tok)
+        for top in (20, 0) if V <= 327680 else (0,):
+            need = R.rollout_token_logprobs_workspace(n, V, top)
+            ws = torch.full((need + 64,), 255, dtype=torch.uint8, device=DEV)
+            check_forward(forward(z, V, V, 1.0, td, top, dtype, ws=ws), seen, 1.0, tok, top)
+            assert torch.all(ws[need:] == 255)
