@@ -195,6 +195,7 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
 #pragma unroll
     for (int i = 0; i < kMaxPer; ++i) {
       const unsigned long long b = __ballot(mine[i] >= part);
+      if (!b) continue;
       if (wave == 0 && mine[i] >= part) lds.units[n + __popcll(b & ((1ull << lane) - 1))] = i * 64 + lane;
       n += __popcll(b);
     }
@@ -222,8 +223,10 @@ __device__ void take_top(const T* row, int V, int top, const uint32_t* keys, int
     int id0[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
-      id0[j] = (lds.units[min(r0 + j * RW, n - 1)] * 64 + lane) * N;
-      raw[j] = load_row(row, id0[j], V);
+      if (r0 + j * RW < n) {
+        id0[j] = (__builtin_amdgcn_readfirstlane(lds.units[r0 + j * RW]) * 64 + lane) * N;
+        raw[j] = load_row(row, id0[j], V);
+      }
     }
 #pragma unroll
     for (int j = 0; j < kAhead; ++j) {
