@@ -395,7 +395,7 @@ __global__ __launch_bounds__(RB) void k_logprobs(LogprobArgs a, float c, int uni
 }
 
 // A row's parts joined, and its alternatives: one workgroup a row with alternatives, otherwise one wave.  Bound by its chain
-// of reads (parts and keys, units, the token's logit) and by the ranking: 64 rows with 8 alternatives 7.7 us, 256 with 20 9.8,
+// of reads (parts and keys, units, the token's logit) and by the ranking: 64 rows with 8 alternatives 6.0 us, 256 with 20 8.3,
 // of which 4 are the launch and the first reads.
 template <typename T, bool TOP>
 __global__ __launch_bounds__(RB) void k_logprobs_join(LogprobArgs a, float c, int chunks, const Soft* __restrict__ part,
