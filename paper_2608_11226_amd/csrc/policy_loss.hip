@@ -21,6 +21,9 @@ constexpr int kTile = LB * 4;     // tokens of a workgroup's step
 // Odd: the steps of a workgroup are kMaxBlocks tiles apart and shall not all fall on the same part of completions, whose ends
 // have nothing to do (of 8.4 M tokens: 28.7 us, 30.2 with 1,536; 29.1 and 32.2 with 1,023 and 1,791).
 constexpr int kMaxBlocks = 1279;
+// Up to one step of as many threads one workgroup does all, and there is no join (8 sequences of 256 in a graph and eager 6.7
+// and 10.7 us, in four workgroups and a join 7.8 and 13.3; two steps, 16 of 512, 9.8 and 10.7, 8.1 and 13.3).
+constexpr int kOneThreads = 1024;
 constexpr int kJoin = 512;         // threads that join their sums, at most (256 to 512 4.0 us, 1,024 5.5)
 constexpr int kSums = 7;          // loss, r, kl, clipped low, clipped high, H, tokens
 // Every workgroup adds up to this many lengths itself to know how many tokens there are; more are first added up in
@@ -57,18 +60,19 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int s, int N) {
   return lengths ? max(0, min(lengths[s], N)) : N;
 }
 
-// Sum of n lengths, in every thread (less than 2^31: exact in any order).
+// Sum of n lengths, in every one of T threads (less than 2^31: exact in any order).
+template <int T>
 __device__ __forceinline__ int add_lengths(const int32_t* lengths, int lo, int hi, int N, int32_t* red) {
   int v = 0;
 #pragma unroll 4
-  for (int s = lo + threadIdx.x; s < hi; s += LB) v += length_of(lengths, s, N);
+  for (int s = lo + threadIdx.x; s < hi; s += T) v += length_of(lengths, s, N);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   v = 0;
 #pragma unroll
-  for (int i = 0; i < LB / 64; ++i) v += red[i];
+  for (int i = 0; i < T / 64; ++i) v += red[i];
   return v;
 }
 
@@ -76,7 +80,7 @@ __global__ __launch_bounds__(LB) void k_policy_count(const int32_t* __restrict__
                                                      int32_t* __restrict__ counts) {
   __shared__ int32_t red[LB / 64];
   const int lo = min((int64_t)blockIdx.x * each, (int64_t)S), hi = (int)min((int64_t)lo + each, (int64_t)S);
-  const int v = add_lengths(lengths, lo, hi, N, red);
+  const int v = add_lengths<LB>(lengths, lo, hi, N, red);
   if (threadIdx.x == 0) counts[blockIdx.x] = v;
 }
 
@@ -188,18 +192,19 @@ __device__ __forceinline__ void write_sums(double v, float* loss, float* stats) 
 }
 
 // A thread does four tokens at a time.  counts: n_counts numbers that add up to the tokens (the lengths, or sums of them).
-__global__ __launch_bounds__(LB) void k_policy_loss(PolicyLossArgs a, Borders border, const int32_t* __restrict__ counts,
-                                                    int n_counts, double* __restrict__ part) {
-  __shared__ int32_t red[LB / 64];
-  __shared__ double sums[LB / 64 * kSums];
+template <int T>
+__global__ __launch_bounds__(T) void k_policy_loss(PolicyLossArgs a, Borders border, const int32_t* __restrict__ counts,
+                                                   int n_counts, double* __restrict__ part) {
+  __shared__ int32_t red[T / 64];
+  __shared__ double sums[T / 64 * kSums];
   const int S = a.seqs, N = a.max_len;
-  const int64_t total = (int64_t)S * N, stride = (int64_t)gridDim.x * kTile;
+  const int64_t total = (int64_t)S * N, stride = (int64_t)gridDim.x * T * 4;
   Sums sum;
   double all = (double)total;
   if (a.mean == ROLLOUT_MEAN_TOKEN && a.lengths)
-    all = max(add_lengths(counts, 0, n_counts, counts == a.lengths ? N : 0x7FFFFFFF, red), 1);
+    all = max(add_lengths<T>(counts, 0, n_counts, counts == a.lengths ? N : 0x7FFFFFFF, red), 1);
   const float w_all = (float)(1.0 / all);
-  for (int64_t i0 = (int64_t)blockIdx.x * kTile + threadIdx.x * 4; i0 < total; i0 += stride)
+  for (int64_t i0 = (int64_t)blockIdx.x * T * 4 + threadIdx.x * 4; i0 < total; i0 += stride)
     use_step(a, border, w_all, load_step(a, i0, total), sum);
   const double each[kSums] = {sum.loss, sum.r, sum.kl, (double)sum.low, (double)sum.high, sum.H, (double)sum.tokens};
   const double v = block_sums(each, sums);
@@ -243,7 +248,12 @@ hipError_t launch_policy_loss(hipStream_t s, const PolicyLossArgs& a, void* ws) 
     hipLaunchKernelGGL(k_policy_count, dim3(n_counts), dim3(LB), 0, s, a.lengths, a.seqs, a.max_len, each, sums);
     counts = sums;
   }
-  hipLaunchKernelGGL(k_policy_loss, dim3(blocks), dim3(LB), 0, s, a, b, counts, n_counts, part);
+  const int64_t total = (int64_t)a.seqs * a.max_len;
+  if (total > kTile && total <= 4 * kOneThreads) {
+    hipLaunchKernelGGL(k_policy_loss<kOneThreads>, dim3(1), dim3(kOneThreads), 0, s, a, b, counts, n_counts, part);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(k_policy_loss<LB>, dim3(blocks), dim3(LB), 0, s, a, b, counts, n_counts, part);
   if (blocks > 1 && (a.loss || a.stats))
     hipLaunchKernelGGL(k_policy_join, dim3(1), dim3((std::min(blocks, kJoin) + 63) / 64 * 64), 0, s, part, blocks, a.loss,
                        a.stats);

@@ -82,6 +82,24 @@ def test_sizes_and_means(S, N):
         check(run(*dev, *k), *data, *k)
 
 
+@pytest.mark.parametrize("S,N", [(1, 1024), (5, 205), (2, 2048), (1, 4095), (17, 241), (4096, 1), (4097, 1), (683, 6), (2, 2049)])
+def test_as_many_places_as_one_workgroup_does_and_more(S, N):
+    """All inputs, and without lengths, statistics and loss: gradients are the same bits."""
+    data = inputs(S, N, S + N)
+    dev = [to_dev(x, torch) for x in data]
+    for mean in (0, 1, 2):
+        log(f"policy loss {S} x {N} mean {mean}")
+        k = (0.2, 0.28, 0.04, 0.01, mean)
+        out = run(*dev, *k)
+        check(out, *data, *k)
+        none = run(*dev[:5], None, *k)
+        check(none, *data[:5], None, *k)
+        need = R.grpo_policy_loss_workspace(S, N)
+        ws, grad = torch.empty(need, dtype=torch.uint8, device=DEV), torch.empty(S, N, device=DEV)
+        R.grpo_policy_loss(*dev, S, N, *k, None, None, grad, None, ws, need)
+        assert torch.equal(grad, out[2])
+
+
 def test_absent_inputs_and_outputs():
     data = inputs(6, 77, 4)
     dev = [to_dev(x, torch) for x in data]
