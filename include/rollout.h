@@ -370,6 +370,11 @@ rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dty
  * with A = 0 the first term is 0 whatever the ratio.  d_old_logp NULL: the
  * log probabilities themselves, held constant (r = 1).  d_ref_logp NULL: no penalty
  * (kl_coef must be 0).  d_entropy NULL: no entropy term (entropy_coef must be 0).
+ * A coefficient of 0 leaves its term out of loss and gradients (the statistics stay), so
+ * that a term which overflows can still be watched.  Terms are fp32: an exponential of
+ * more than 88.7 is infinite.  A log probability of -inf (a masked id) has ratio 0 and
+ * exp(x) - 1 - x = inf; where lp and old (or lp and ref) are both infinite their
+ * difference, and what follows from it, is NaN.
  * Outputs, each NULL if not wanted: d_loss fp32 [1]; d_stats fp32 [5], means over the counted
  * tokens of r, of exp(x) - 1 - x, of tokens clipped below, clipped above, of H; d_grad_logp,
  * d_grad_entropy fp32 [n_seqs, max_len], that must not overlap an input.  Sums are fp64.

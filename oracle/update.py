@@ -105,11 +105,11 @@ def policy_loss(logp, old, ref, entropy, adv, lengths, clip_low, clip_high, kl_c
             low, high = A < 0 and r < 1.0 - lo, A > 0 and r > 1.0 + hi
             surr = (1.0 + hi) * A if high else (1.0 - lo) * A if low else r * A
             x = float(ref[s, t]) - logp[s, t] if ref is not None else 0.0
-            kl = np.expm1(x) - x
+            kl = np.expm1(x) - x if x < np.inf else np.inf
             H = float(entropy[s, t]) if entropy is not None else 0.0
-            loss += w * (-surr + b * kl - c * H)
+            loss += w * (-surr + (b * kl if b else 0.0) - (c * H if c else 0.0))
             sums += r, kl, low, high, H
-            dlogp[s, t] = w * ((0.0 if low or high else -A * r) - b * np.expm1(x))
+            dlogp[s, t] = w * ((0.0 if low or high else -A * r) - (b * np.expm1(x) if b else 0.0))
             dent[s, t] = -c * w
     return loss, sums / max(1, total), dlogp, dent
 

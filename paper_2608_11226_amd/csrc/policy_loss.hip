@@ -131,6 +131,9 @@ __device__ __forceinline__ Step load_step(const PolicyLossArgs& a, int64_t i0, i
   return q;
 }
 
+// e^x - 1 - x from x and e^x - 1; infinite at both ends.
+__device__ __forceinline__ float penalty(float x, float ex) { return ex == INFINITY ? ex : ex - x; }
+
 struct Sums {
   double loss = 0.0, r = 0.0, kl = 0.0, H = 0.0;
   int low = 0, high = 0, tokens = 0;
@@ -154,13 +157,16 @@ __device__ __forceinline__ void use_step(const PolicyLossArgs& a, const Borders&
         float tok = high ? -(1.f + a.clip_high) * A : low ? -(1.f - a.clip_low) * A : -rA;
         float g = high || low ? 0.f : -rA;
         if (a.ref) {
-          const float x = q.ref[j] - q.lp[j], ex = expm1f(x), kl = ex - x;
-          tok = fmaf(a.kl_coef, kl, tok);
-          g = fmaf(-a.kl_coef, ex, g);
+          const float x = q.ref[j] - q.lp[j], ex = expm1f(x), kl = penalty(x, ex);
+          // no coefficient, no term: 0 times an overflowed exponential is not a number
+          if (a.kl_coef != 0.f) {
+            tok = fmaf(a.kl_coef, kl, tok);
+            g = fmaf(-a.kl_coef, ex, g);
+          }
           sum.kl += (double)kl;
         }
         if (a.entropy) {
-          tok = fmaf(-a.entropy_coef, q.H[j], tok);
+          if (a.entropy_coef != 0.f) tok = fmaf(-a.entropy_coef, q.H[j], tok);
           sum.H += (double)q.H[j];
         }
         sum.loss += (double)(tok * w);

@@ -213,3 +213,40 @@ def test_repeats_and_graphs():
         torch.cuda.synchronize()
         for graph, out in made:
             assert all(torch.equal(x, y) for x, y in zip(want, out)), replay
+
+
+@pytest.mark.parametrize("mean", [0, 1, 2])
+def test_terms_without_a_coefficient_are_left_out(mean):
+    """Penalties that overflow, masked ids (log p -inf) and entropies that are not finite, with coefficients of 0: loss and
+    gradients are those of the call without them, the statistics are still theirs."""
+    S, N = 4, 6
+    lp, old, ref, H, adv, _ = inputs(S, N, 33)
+    lp[0, 1], lp[2, 3] = -np.inf, -np.inf        # x = inf
+    ref[1, 2] = lp[1, 2] + 90                    # e^x is past fp32
+    ref[3, 0] = -np.inf                          # x = -inf
+    dev = [to_dev(x, torch) for x in (lp, old, ref, H, adv)] + [None]
+    want = run(dev[0], dev[1], None, None, dev[4], None, 0.2, 0.28, 0.0, 0.0, mean)
+    assert torch.isfinite(want[0]).all() and torch.isfinite(want[2]).all()
+    got = run(dev[0], dev[1], dev[2], dev[3], dev[4], None, 0.2, 0.28, 0.0, 0.0, mean)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]) and not got[3].any()
+    assert torch.equal(got[1][[0, 2, 3]], want[1][[0, 2, 3]])
+    assert got[1][1].item() == float("inf")      # every one of these penalties is infinite in fp32
+    for bad in (float("inf"), float("nan")):
+        dev[3][2, 2] = bad
+        got = run(dev[0], dev[1], dev[2], dev[3], dev[4], None, 0.2, 0.28, 0.0, 0.0, mean)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+        assert not torch.isfinite(got[1][4])
+
+
+def test_penalty_of_a_masked_id():
+    """log p = -inf under a reference that allows the id: the penalty's limit, and its gradient's."""
+    lp = np.array([[-np.inf, -1.0]], dtype=np.float32)
+    ref = np.array([[-2.0, -1.5]], dtype=np.float32)
+    adv = np.array([0.5], dtype=np.float32)
+    out = run(*(to_dev(x, torch) if x is not None else None for x in (lp, lp + 0, ref, None, adv, None)), 0.2, 0.28, 0.1, 0.0, 1)
+    assert np.isnan(out[0].item())               # lp and old are both infinite: no ratio
+    old = np.array([[-3.0, -1.0]], dtype=np.float32)
+    out = run(*(to_dev(x, torch) if x is not None else None for x in (lp, old, ref, None, adv, None)), 0.2, 0.28, 0.1, 0.0, 1)
+    loss, stats, dlp, _ = U.policy_loss(lp, old, ref, None, adv, None, 0.2, 0.28, 0.1, 0.0, 1)
+    assert out[0].item() == loss == np.inf and out[1][1].item() == stats[1] == np.inf
+    assert out[2][0, 0].item() == dlp[0, 0] == -np.inf and abs(out[2][0, 1].item() - dlp[0, 1]) <= 32 * EPS * abs(dlp[0, 1])

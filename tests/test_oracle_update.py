@@ -113,3 +113,14 @@ def test_embedding_and_gradient_match_autograd():
     np.testing.assert_allclose(U.embedding_backward(g, tok, 11, 1.5), w.grad, atol=1e-14)
     np.testing.assert_allclose(U.embedding_backward(g, tok, 11, 1.5, E), w.grad.numpy() + E, atol=1e-14)
     assert np.isnan(U.embedding(E, [11], 1.0)).all() and not U.embedding_backward(g[:1], [11], 11, 1.0).any()
+
+
+@pytest.mark.filterwarnings("ignore:overflow")
+def test_policy_loss_terms_without_a_coefficient():
+    lp, ref = np.array([[-np.inf, -1.0, -2.0]]), np.array([[-1.0, -np.inf, 800.0]])
+    f = lambda r, b, e: U.policy_loss(lp, np.full((1, 3), -1.0), r, e, [0.5], None, 0.2, 0.2, b, 0.0, 0)
+    want, (got, stats, dlp, _) = f(None, 0.0, None), f(ref, 0.0, np.full((1, 3), np.inf))
+    assert got == want[0] and np.isfinite(got) and np.array_equal(dlp, want[2])
+    assert np.isposinf(stats[1]) and np.isposinf(stats[4])
+    loss, _, dlp, _ = f(ref, 0.1, None)
+    assert np.isposinf(loss) and np.isneginf(dlp[0, 0])
