@@ -250,3 +250,26 @@ def test_penalty_of_a_masked_id():
     loss, stats, dlp, _ = U.policy_loss(lp, old, ref, None, adv, None, 0.2, 0.28, 0.1, 0.0, 1)
     assert out[0].item() == loss == np.inf and out[1][1].item() == stats[1] == np.inf
     assert out[2][0, 0].item() == dlp[0, 0] == -np.inf and abs(out[2][0, 1].item() - dlp[0, 1]) <= 32 * EPS * abs(dlp[0, 1])
+
+
+@pytest.mark.parametrize("spread", [1e-7, 1e-6, 1e-5, 1e-4, 1e-3, 1e-2, 0.1, 0.25, 0.49999, 0.5, 0.75, 1.0, 3.0])
+@pytest.mark.parametrize("random", [True, False])
+def test_penalty_of_a_policy_near_its_reference(spread, random):
+    """The penalty relative to itself, as the statistic and as all of the loss.  It is about x^2 / 2.  x = ref - lp is rounded
+    once (eps, no more than (2 + |x|) eps of the penalty); near zero a polynomial of which each step's rounding counts a third
+    at most of the one after it and the coefficients' as much (3 eps), x^2 and the product (2 eps); further out e^x - 1 is off by
+    2 eps, which is up to 4.4 times its size (9 eps), and the difference by 1.  The sum and the means: 2 eps.  In all under
+    (16 + |x|) eps."""
+    rng = np.random.default_rng(int(spread * 1e7))
+    S, N = 3, 257
+    lp = -rng.exponential(1.0, (S, N)).astype(np.float32) - 0.25
+    x = rng.standard_normal((S, N)) if random else rng.choice([-1.0, 1.0], (S, N))
+    ref = (lp + spread * x).astype(np.float32)
+    x = ref.astype(np.float64) - lp
+    exact = np.where(np.abs(x) < 0.01, x ** 2 * (1 / 2 + x / 6 + x ** 2 / 24 + x ** 3 / 120 + x ** 4 / 720), np.expm1(x) - x).mean()
+    out = run(*(to_dev(v, torch) if v is not None else None
+                for v in (lp, lp + 0, ref, None, np.zeros(S, dtype=np.float32), None)), 0.2, 0.28, 1.0, 0.0, 1)
+    bound = (16 + np.abs(x).max()) * EPS * exact
+    log(f"penalty near {spread}: {exact:.9g}, off by {abs(out[1][1].item() - exact) / exact / EPS:.2f} eps")
+    assert abs(out[1][1].item() - exact) <= bound
+    assert abs(out[0].item() - exact) <= bound
