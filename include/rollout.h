@@ -295,8 +295,11 @@ rollout_status rollout_sample_noalloc(const float* d_logits, int32_t n_seqs, int
  * for the same sizes (for larger ones it says no less, so the workspace of the
  * largest call serves them all); nothing is kept in it from one call to the
  * next, and calls that may run at the same time (two streams, two captured
- * graphs) need one each.  Nothing is allocated or waited for, so every call can be captured
- * into a HIP graph.  Messages: rollout_last_error(NULL).
+ * graphs) need one each.  Buffers are aligned to their element's size, and no output and no
+ * workspace shares a byte with another one or with an input, but for the one case named
+ * below (EINVAL; the space between the rows of logits belongs to no one).  Nothing is
+ * allocated or waited for, so every call can be captured into a HIP graph.  Messages:
+ * rollout_last_error(NULL).
  *
  * dtype of a matrix: ROLLOUT_DTYPE_FP32 or ROLLOUT_DTYPE_BF16.  Arithmetic is
  * fp32 or wider, outputs are rounded once (to nearest, ties to even).  Results
@@ -340,8 +343,8 @@ rollout_status rollout_token_logprobs(const void* d_logits, int32_t dtype, int64
  * its entropy, g = d_grad_logp and h = d_grad_entropy (fp32 [n_rows]; h NULL: 0):
  *   dz_i = (g (1[i = token] - p_i) - h p_i (log p_i + H)) / T
  * into d_grad_logits, n_rows rows of vocab values of dtype, grad_stride elements
- * apart; it may be d_logits itself at the same stride (any other overlap:
- * EINVAL).  d_stats and d_entropy (needed only with h) are the forward call's.
+ * apart; it may be d_logits itself at the same stride (any other overlap of the
+ * two, from first to last row: EINVAL).  d_stats and d_entropy (needed only with h) are the forward call's.
  * What lies between the rows is left alone.  Rows that are padding, have g = h = 0
  * or hold nothing but -inf get zeros and are not read; a token >= vocab makes
  * its row NaN.  Errors: EINVAL, EUNSUPPORTED (n_rows or vocab above 2^30), EDEVICE.
@@ -377,7 +380,7 @@ rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dty
  * difference, and what follows from it, is NaN.
  * Outputs, each NULL if not wanted: d_loss fp32 [1]; d_stats fp32 [5], means over the counted
  * tokens of r, of exp(x) - 1 - x, of tokens clipped below, clipped above, of H; d_grad_logp,
- * d_grad_entropy fp32 [n_seqs, max_len], that must not overlap an input.  Sums are fp64.
+ * d_grad_entropy fp32 [n_seqs, max_len].  Sums are fp64.
  * Errors: EINVAL (sizes, clip_low outside [0, 1], clip_high < 0, coefficients, mean,
  * NULL buffers, overlap, no output), EUNSUPPORTED (2^31 tokens or more), ENOMEM
  * (workspace too small), EDEVICE.

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include <rocprofiler-sdk-roctx/roctx.h>
@@ -34,6 +35,47 @@ bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0;
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
   return x < y + b_bytes && y < x + a_bytes;
+}
+
+// [p, p + bytes) shares a byte with one of `rows` rows of row_bytes that are stride bytes apart (at least row_bytes): what lies
+// between the rows is not theirs
+bool overlap_rows(const void* base, size_t rows, size_t stride, size_t row_bytes, const void* p, size_t bytes) {
+  const int64_t lo = (int64_t)((uintptr_t)p - (uintptr_t)base), hi = lo + (int64_t)bytes;
+  const int64_t r = lo < (int64_t)row_bytes ? 0 : (lo - (int64_t)row_bytes) / (int64_t)stride + 1;  // the first that ends behind lo
+  return r < (int64_t)rows && r * (int64_t)stride < hi;
+}
+
+// A buffer of a call, or (rows > 1) a matrix of rows that are stride bytes apart; NULL: absent.
+struct Span {
+  const char* name;
+  const void* p;
+  size_t bytes, rows = 1, stride = 0;
+};
+
+bool overlap(const Span& a, const Span& b) {
+  if (!a.p || !b.p || !a.bytes || !b.bytes) return false;
+  if (a.rows > 1) return overlap_rows(a.p, a.rows, a.stride, a.bytes, b.p, b.bytes);
+  if (b.rows > 1) return overlap_rows(b.p, b.rows, b.stride, b.bytes, a.p, a.bytes);
+  return overlap(a.p, a.bytes, b.p, b.bytes);
+}
+
+// Kernels read a call's inputs while other workgroups write its outputs and the workspace: all of them stand apart.  (A pair of
+// matrices with rows apart is the caller's to check.)
+rollout_status check_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span* o = outs.begin(); o != outs.end(); ++o) {
+    for (const Span& i : ins)
+      if (overlap(*o, i)) return fail(ROLLOUT_EINVAL, std::string(o->name) + " overlaps an input, " + i.name);
+    for (const Span* q = outs.begin(); q != o; ++q)
+      if (overlap(*o, *q)) return fail(ROLLOUT_EINVAL, std::string(o->name) + " overlaps " + q->name);
+  }
+  return ROLLOUT_OK;
+}
+
+// fp32 and int32 buffers
+rollout_status check_words(std::initializer_list<const void*> buffers) {
+  for (const void* p : buffers)
+    if (!aligned_to(p, 4)) return fail(ROLLOUT_EINVAL, "an fp32 or int32 buffer is not aligned to 4 bytes");
+  return ROLLOUT_OK;
 }
 
 // the stream (NULL: the default one) belongs to the current device
@@ -115,6 +157,14 @@ rollout_status rollout_token_logprobs(const void* d_logits, int32_t dtype, int64
   if (!d_logp && !d_entropy && !d_stats && !n_top) return fail(ROLLOUT_EINVAL, "no output asked for");
   st = check_workspace(d_workspace, workspace_bytes, need);
   if (st != ROLLOUT_OK) return st;
+  st = check_words({d_tokens, d_logp, d_entropy, d_stats, n_top ? d_top_ids : nullptr, n_top ? d_top_logp : nullptr});
+  if (st != ROLLOUT_OK) return st;
+  const size_t es = elem_bytes(dtype), n = n_rows;
+  st = check_apart({{"d_logp", d_logp, 4 * n}, {"d_entropy", d_entropy, 4 * n}, {"d_stats", d_stats, 8 * n},
+                    {"d_top_ids", d_top_ids, 4 * n * n_top}, {"d_top_logp", d_top_logp, 4 * n * n_top},
+                    {"the workspace", d_workspace, need}},
+                   {{"the logits", d_logits, vocab * es, n, row_stride * es}, {"d_tokens", d_tokens, 4 * n}});
+  if (st != ROLLOUT_OK) return st;
   st = check_stream(hip_stream);
   if (st != ROLLOUT_OK) return st;
   const LogprobArgs a = {d_logits, row_stride, n_rows, vocab, temperature, d_tokens, n_top,
@@ -140,6 +190,14 @@ rollout_status rollout_token_logprobs_backward(const void* d_logits, int32_t dty
   if (!in_place && overlap(d_logits, ((size_t)(n_rows - 1) * row_stride + vocab) * es, d_grad_logits,
                            ((size_t)(n_rows - 1) * grad_stride + vocab) * es))
     return fail(ROLLOUT_EINVAL, "the gradients overlap the logits without being in their place");
+  const size_t n = n_rows;
+  const float* entropy = d_grad_entropy ? d_entropy : nullptr;  // not read otherwise
+  st = check_words({d_tokens, d_stats, entropy, d_grad_logp, d_grad_entropy});
+  if (st != ROLLOUT_OK) return st;
+  st = check_apart({{"d_grad_logits", d_grad_logits, vocab * es, n, grad_stride * es}},
+                   {{"d_tokens", d_tokens, 4 * n}, {"d_stats", d_stats, 8 * n}, {"d_entropy", entropy, 4 * n},
+                    {"d_grad_logp", d_grad_logp, 4 * n}, {"d_grad_entropy", d_grad_entropy, 4 * n}});
+  if (st != ROLLOUT_OK) return st;
   st = check_stream(hip_stream);
   if (st != ROLLOUT_OK) return st;
   const LogprobGradArgs a = {d_logits, row_stride, n_rows, vocab, temperature, d_tokens, d_stats,
@@ -174,14 +232,17 @@ rollout_status grpo_policy_loss(const float* d_logp, const float* d_old_logp, co
     return fail(ROLLOUT_EINVAL, "mean must be 0 (sequence), 1 (token) or 2 (fixed)");
   if (!d_loss && !d_stats && !d_grad_logp && !d_grad_entropy) return fail(ROLLOUT_EINVAL, "no output asked for");
   const size_t whole = (size_t)n_seqs * max_len * 4;
-  float* outs[] = {d_grad_logp, d_grad_entropy};
-  const float* ins[] = {d_logp, d_old_logp, d_ref_logp, d_entropy};
-  for (float* o : outs)
-    for (const float* i : ins)
-      if (o && i && overlap(o, whole, i, whole)) return fail(ROLLOUT_EINVAL, "a gradient overlaps an input");
   if (d_grad_logp && d_grad_entropy && overlap(d_grad_logp, whole, d_grad_entropy, whole))
     return fail(ROLLOUT_EINVAL, "the gradients overlap");
   st = check_workspace(d_workspace, workspace_bytes, need);
+  if (st != ROLLOUT_OK) return st;
+  st = check_words({d_logp, d_old_logp, d_ref_logp, d_entropy, d_adv, d_lengths, d_loss, d_stats, d_grad_logp, d_grad_entropy});
+  if (st != ROLLOUT_OK) return st;
+  const size_t n = n_seqs;
+  st = check_apart({{"d_loss", d_loss, 4}, {"d_stats", d_stats, 20}, {"d_grad_logp", d_grad_logp, whole},
+                    {"d_grad_entropy", d_grad_entropy, whole}, {"the workspace", d_workspace, need}},
+                   {{"d_logp", d_logp, whole}, {"d_old_logp", d_old_logp, whole}, {"d_ref_logp", d_ref_logp, whole},
+                    {"d_entropy", d_entropy, whole}, {"d_adv", d_adv, 4 * n}, {"d_lengths", d_lengths, 4 * n}});
   if (st != ROLLOUT_OK) return st;
   st = check_stream(hip_stream);
   if (st != ROLLOUT_OK) return st;
@@ -199,8 +260,11 @@ rollout_status rollout_embedding(const void* d_table, int32_t table_dtype, int32
   if (!d_table || !d_tokens || !d_out) return fail(ROLLOUT_EINVAL, "NULL buffer");
   if (!aligned_to(d_table, elem_bytes(table_dtype)) || !aligned_to(d_out, elem_bytes(out_dtype)))
     return fail(ROLLOUT_EINVAL, "a matrix is not aligned to its type");
-  if (overlap(d_table, (size_t)vocab * dim * elem_bytes(table_dtype), d_out, (size_t)n_tokens * dim * elem_bytes(out_dtype)))
-    return fail(ROLLOUT_EINVAL, "the output overlaps the table");
+  st = check_words({d_tokens});
+  if (st != ROLLOUT_OK) return st;
+  st = check_apart({{"d_out", d_out, (size_t)n_tokens * dim * elem_bytes(out_dtype)}},
+                   {{"d_table", d_table, (size_t)vocab * dim * elem_bytes(table_dtype)}, {"d_tokens", d_tokens, 4 * (size_t)n_tokens}});
+  if (st != ROLLOUT_OK) return st;
   st = check_stream(hip_stream);
   if (st != ROLLOUT_OK) return st;
   const EmbeddingArgs a = {d_table, vocab, dim, d_tokens, n_tokens, scale, d_out};
@@ -231,10 +295,12 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
   if (!d_grad || !d_tokens || !d_grad_table) return fail(ROLLOUT_EINVAL, "NULL buffer");
   if (!aligned_to(d_grad, elem_bytes(grad_dtype)) || !aligned_to(d_grad_table, elem_bytes(table_dtype)))
     return fail(ROLLOUT_EINVAL, "a matrix is not aligned to its type");
-  if (overlap(d_grad, (size_t)n_tokens * dim * elem_bytes(grad_dtype), d_grad_table,
-              (size_t)vocab * dim * elem_bytes(table_dtype)))
-    return fail(ROLLOUT_EINVAL, "the table's gradient overlaps the tokens' gradients");
   st = check_workspace(d_workspace, workspace_bytes, need);
+  if (st != ROLLOUT_OK) return st;
+  st = check_words({d_tokens});
+  if (st != ROLLOUT_OK) return st;
+  st = check_apart({{"d_grad_table", d_grad_table, (size_t)vocab * dim * elem_bytes(table_dtype)}, {"the workspace", d_workspace, need}},
+                   {{"d_grad", d_grad, (size_t)n_tokens * dim * elem_bytes(grad_dtype)}, {"d_tokens", d_tokens, 4 * (size_t)n_tokens}});
   if (st != ROLLOUT_OK) return st;
   st = check_stream(hip_stream);
   if (st != ROLLOUT_OK) return st;

@@ -166,3 +166,96 @@ def test_the_loss_workspace_of_more_serves_less():
     assert sizes == sorted(sizes)
     sizes = [R.grpo_policy_loss_workspace(64, n) for n in (1, 100, 511, 4096, 100000)]
     assert sizes == sorted(sizes)
+
+
+# Matrices of 4 rows of 100 values, 128 apart, and small buffers beside them (as FORWARD, with room between the rows).
+WIDE = dict(FORWARD, stride=128, top=3, ids=G, tops=H)
+
+
+@pytest.mark.parametrize("change,text", [
+    # outputs over inputs: logits (first and last element of a row), tokens
+    (dict(logp=A), "overlaps an input, the logits"), (dict(entropy=A + 4 * (3 * 128 + 99)), "the logits"),
+    (dict(stats=A + 4 * 128 - 28), "the logits"), (dict(logp=A - 12), "the logits"), (dict(ids=A + 4 * 128 - 44), "the logits"),
+    (dict(tops=A + 4 * (128 + 99)), "the logits"), (dict(logp=A - (1 << 20) + 4, top=0, n=1 << 18), "the logits"),
+    (dict(logp=B), "d_tokens"), (dict(stats=B - 28), "d_tokens"), (dict(ids=B + 12), "d_tokens"), (dict(tops=B), "d_tokens"),
+    # outputs over each other
+    (dict(entropy=C), "d_entropy overlaps d_logp"), (dict(stats=C + 12), "d_stats overlaps d_logp"),
+    (dict(stats=D - 28), "d_stats overlaps d_entropy"), (dict(tops=G + 44), "d_top_logp overlaps d_top_ids"),
+    # the workspace
+    (dict(ws=A), "workspace overlaps an input, the logits"), (dict(ws=B - 16), "workspace overlaps an input, d_tokens"),
+    (dict(ws=C), "workspace overlaps d_logp"), (dict(ws=H), "workspace overlaps d_top_logp"),
+    # alignment of everything that is not a matrix
+    (dict(tokens=B + 2), "aligned to 4"), (dict(logp=C + 1), "aligned to 4"), (dict(entropy=D + 2), "aligned to 4"),
+    (dict(stats=E + 3), "aligned to 4"), (dict(ids=G + 2), "aligned to 4"), (dict(tops=H + 1), "aligned to 4"),
+])
+def test_logprobs_buffers_stand_apart(change, text):
+    refuse(R.EINVAL, R.rollout_token_logprobs, *call(WIDE, **change), text=text)
+
+
+BACK = dict(BACKWARD, stride=128, dz_stride=120)
+
+
+@pytest.mark.parametrize("change,text", [
+    (dict(dz=B), "d_tokens"), (dict(dz=C - 4 * (3 * 120 + 99)), "d_stats"), (dict(dz=C + 28), "d_stats"),
+    (dict(dz=D + 12), "d_entropy"), (dict(dz=E), "d_grad_logp"), (dict(dz=F - 4 * 99), "d_grad_entropy"),
+    (dict(tokens=B + 1), "aligned to 4"), (dict(stats=C + 2), "aligned to 4"), (dict(entropy=D + 2), "aligned to 4"),
+    (dict(g=E + 2), "aligned to 4"), (dict(h=F + 3), "aligned to 4"),
+])
+def test_logprobs_backward_buffers_stand_apart(change, text):
+    refuse(R.EINVAL, R.rollout_token_logprobs_backward, *call(BACK, **change), text=text)
+
+
+@pytest.mark.parametrize("change,text", [
+    (dict(dlp=E - 252), "d_adv"), (dict(dlp=F + 12), "d_lengths"), (dict(dH=E), "d_adv"), (dict(dH=F), "d_lengths"),
+    (dict(loss=A + 252), "d_loss overlaps an input, d_logp"), (dict(loss=E), "d_adv"), (dict(stats=F - 16), "d_lengths"),
+    (dict(stats=C), "d_ref_logp"), (dict(loss=G + 64 + 16), "overlaps d_loss"), (dict(loss=H + 252), "d_grad_logp overlaps d_loss"),
+    (dict(stats=H + (1 << 20)), "d_grad_entropy overlaps d_stats"),
+    (dict(ws=A - 16), "workspace overlaps an input, d_logp"), (dict(ws=E), "d_adv"), (dict(ws=F), "d_lengths"),
+    (dict(ws=G), "workspace overlaps d_loss"), (dict(ws=H + 240), "workspace overlaps d_grad_logp"),
+    (dict(lp=A + 2), "aligned to 4"), (dict(old=B + 1), "aligned to 4"), (dict(ref=C + 2), "aligned to 4"),
+    (dict(H=D + 2), "aligned to 4"), (dict(adv=E + 2), "aligned to 4"), (dict(lengths=F + 2), "aligned to 4"),
+    (dict(loss=G + 2), "aligned to 4"), (dict(stats=G + 66), "aligned to 4"), (dict(dlp=H + 1), "aligned to 4"),
+    (dict(dH=H + (1 << 20) + 2), "aligned to 4"),
+])
+def test_policy_loss_buffers_stand_apart(change, text):
+    refuse(R.EINVAL, R.grpo_policy_loss, *call(LOSS, **change), text=text)
+
+
+@pytest.mark.parametrize("change,text", [(dict(out=B), "d_tokens"), (dict(out=B - 78), "d_tokens"), (dict(out=B + 18), "d_tokens"),
+                                         (dict(tokens=B + 2), "aligned to 4")])
+def test_embedding_buffers_stand_apart(change, text):
+    refuse(R.EINVAL, R.rollout_embedding, *call(LOOKUP, **change), text=text)
+
+
+@pytest.mark.parametrize("change,text", [
+    (dict(table=B - 3196), "d_tokens"), (dict(table=B + 16), "d_tokens"), (dict(ws=A), "workspace overlaps an input, d_grad"),
+    (dict(ws=B), "workspace overlaps an input, d_tokens"), (dict(ws=C), "workspace overlaps d_grad_table"),
+    (dict(ws=C + 3184), "workspace overlaps d_grad_table"), (dict(tokens=B + 2), "aligned to 4"),
+])
+def test_embedding_backward_buffers_stand_apart(change, text):
+    refuse(R.EINVAL, R.rollout_embedding_backward, *call(GRAD, **change), text=text)
+
+
+def accepted(fn, *args):
+    """The call passes every check of its buffers: without a device it is refused for that alone."""
+    if R._torch.cuda.is_available():
+        pytest.skip("addresses that are never dereferenced would be")
+    refuse(R.EDEVICE, fn, *args)
+
+
+def test_buffers_beside_each_other_are_taken():
+    """Right before and behind one another, and between the rows of logits."""
+    accepted(R.rollout_token_logprobs, *call(WIDE))
+    accepted(R.rollout_token_logprobs, *call(WIDE, logp=A - 16, entropy=A + 4 * (3 * 128 + 100), stats=C, ids=A + 4 * 100,
+                                             tops=A + 4 * (128 + 100)))
+    accepted(R.rollout_token_logprobs, *call(WIDE, logp=A + 4 * (2 * 128 + 100), entropy=A + 4 * (2 * 128 + 104), tokens=A + 4 * 508))
+    accepted(R.rollout_token_logprobs, *call(WIDE, ids=B, tops=B, top=0, entropy=C + 16, stats=C + 32))  # ids: not asked for
+    accepted(R.rollout_token_logprobs_backward, *call(BACK))
+    accepted(R.rollout_token_logprobs_backward, *call(BACK, dz=A, dz_stride=128))
+    accepted(R.rollout_token_logprobs_backward, *call(BACK, dz=C - 400))
+    accepted(R.rollout_token_logprobs_backward, *call(BACK, g=G + 4 * 100, tokens=G + 4 * (120 + 104), stats=G + 4 * (240 + 100)))
+    accepted(R.rollout_token_logprobs_backward, *call(BACK, entropy=G + 2, h=None))  # not read
+    accepted(R.grpo_policy_loss, *call(LOSS))
+    accepted(R.grpo_policy_loss, *call(LOSS, loss=E + 16, stats=E + 20, dlp=A + 256, dH=A + 512))
+    accepted(R.rollout_embedding, *call(LOOKUP, out=B + 20))
+    accepted(R.rollout_embedding_backward, *call(GRAD, table=B + 20))
