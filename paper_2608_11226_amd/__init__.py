@@ -227,10 +227,12 @@ def rollout_length_rewards(lengths, n: int, target: int, rewards, total_tokens=N
 
 
 # The update side of a GRPO step: no context, caller-owned workspaces.  A tensor passed for a buffer has to be on the
-# current device, of the buffer's type, contiguous (the rows of logits may be strided) and large enough; an integer
-# address is passed on as it is.  Workspaces are uint8 tensors.
-def _buf(name: str, x, kind, n: int, device: int) -> int | None:
-    """Device pointer of a buffer of n elements of a torch type."""
+# current device, of the buffer's type, contiguous (the rows of logits may be strided, by the row stride of the call) and
+# large enough; a contiguous one is taken as so many elements in a row, whatever its shape, and an integer address is
+# passed on as it is.  Workspaces are uint8 tensors.
+def _buf(name: str, x, kind, n: int, device: int, rows=None) -> int | None:
+    """Device pointer of a buffer of n elements of a torch type.  rows: (rows, stride, width) of a matrix whose rows may
+    be apart."""
     if x is None or type(x) is int:
         return x
     if not hasattr(x, "is_contiguous"):
@@ -241,14 +243,27 @@ def _buf(name: str, x, kind, n: int, device: int) -> int | None:
         raise RolloutError(EINVAL, f"{name} must be {kind}, not {x.dtype}")
     if x.get_device() != device:
         raise RolloutError(EINVAL, f"{name} is on {x.device}, not on the current device")
-    have = x.numel()
     if not x.is_contiguous():
-        if not name.endswith("logits") or x.stride(-1) != 1:
+        if rows is None or x.stride(-1) != 1:
             raise RolloutError(EINVAL, f"{name} is not contiguous")
-        have = sum((k - 1) * s for k, s in zip(x.shape, x.stride())) + 1 if have else 0
-    if have < n:
-        raise RolloutError(EINVAL, f"{name} holds {have} elements, the call needs {n}")
+        _strided_rows(name, x, *rows)
+    elif x.numel() < n:
+        raise RolloutError(EINVAL, f"{name} holds {x.numel()} elements, the call needs {n}")
     return x.data_ptr()
+
+
+def _strided_rows(name: str, x, n: int, stride: int, width: int):
+    """Row r of the call is row r of x, for all n of them (dimensions before the last count rows)."""
+    if x.shape[-1] < width:
+        raise RolloutError(EINVAL, f"{name} has rows of {x.shape[-1]} elements, the call needs {width}")
+    have = 1
+    for size, step in zip(reversed(x.shape[:-1]), reversed(x.stride()[:-1])):
+        if size > 1 and have < n:
+            if step != stride * have:
+                raise RolloutError(EINVAL, f"{name} has rows {step} elements apart, not {stride * have}")
+            have *= size
+    if have < n:
+        raise RolloutError(EINVAL, f"{name} holds {have} rows, the call needs {n}")
 
 
 def _kind(dtype: int):
@@ -273,8 +288,8 @@ def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, voc
                            workspace=None, workspace_bytes: int = 0, stream=None):
     dev = _device()
     _check(lib.rollout_token_logprobs(
-        _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev), dtype, row_stride, n_rows, vocab,
-        temperature,
+        _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev, (n_rows, row_stride, vocab)),
+        dtype, row_stride, n_rows, vocab, temperature,
         _buf("tokens", tokens, _I, n_rows, dev), n_top, _buf("logp", logp, _F, n_rows, dev),
         _buf("entropy", entropy, _F, n_rows, dev),
         _buf("stats", stats, _F, 2 * n_rows, dev), _buf("top_ids", top_ids, _I, n_rows * n_top, dev),
@@ -287,13 +302,13 @@ def rollout_token_logprobs_backward(logits, dtype: int, row_stride: int, n_rows:
                                     stream=None):
     dev = _device()
     _check(lib.rollout_token_logprobs_backward(
-        _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev), dtype, row_stride, n_rows, vocab,
-        temperature,
+        _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev, (n_rows, row_stride, vocab)),
+        dtype, row_stride, n_rows, vocab, temperature,
         _buf("tokens", tokens, _I, n_rows, dev), _buf("stats", stats, _F, 2 * n_rows, dev),
         _buf("entropy", entropy, _F, n_rows, dev),
         _buf("grad_logp", grad_logp, _F, n_rows, dev), _buf("grad_entropy", grad_entropy, _F, n_rows, dev),
-        _buf("grad_logits", grad_logits, _kind(dtype), (n_rows - 1) * grad_stride + vocab, dev), grad_stride,
-        _ptr(stream)))
+        _buf("grad_logits", grad_logits, _kind(dtype), (n_rows - 1) * grad_stride + vocab, dev, (n_rows, grad_stride, vocab)),
+        grad_stride, _ptr(stream)))
 
 
 def grpo_policy_loss_workspace(n_seqs: int, max_len: int) -> int:

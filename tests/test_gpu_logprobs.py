@@ -477,3 +477,24 @@ def test_alternatives_of_rows_of_any_number_of_units(n, units, dtype):
             ws = torch.full((need + 64,), 255, dtype=torch.uint8, device=DEV)
             check_forward(forward(z, V, V, 1.0, td, top, dtype, ws=ws), seen, 1.0, tok, top)
             assert torch.all(ws[need:] == 255)
+
+
+def test_views_are_read_and_written_at_their_own_stride():
+    """The stride of a view has to be the call's: a smaller one would read, and write, what lies between its rows."""
+    n, V = 5, 40
+    wide = torch.randn(n, V + 24, device=DEV)
+    part, tok = wide[:, 9:9 + V], torch.arange(n, dtype=torch.int32, device=DEV)
+    for stride in (V, V + 1, V + 25, 2 * (V + 24)):
+        for call in (lambda: forward(part, stride, V, 1.0, tok),
+                     lambda: R.rollout_token_logprobs_backward(wide.clone(), 0, V + 24, n, V, 1.0, tok, torch.zeros(n, 2, device=DEV),
+                                                               None, torch.ones(n, device=DEV), None, part, stride)):
+            with pytest.raises(R.RolloutError) as e:
+                call()
+            assert e.value.code == R.EINVAL and "apart" in str(e.value)
+    z, before = part.contiguous(), wide.clone()
+    fw = forward(part, V + 24, V, 1.0, tok)
+    R.rollout_token_logprobs_backward(part, 0, V + 24, n, V, 1.0, tok, fw["stats"], None, torch.ones(n, device=DEV), None, part, V + 24)
+    want = torch.empty_like(z)
+    R.rollout_token_logprobs_backward(z, 0, V, n, V, 1.0, tok, fw["stats"], None, torch.ones(n, device=DEV), None, want, V)
+    assert torch.equal(part, want)
+    assert torch.equal(wide[:, :9], before[:, :9]) and torch.equal(wide[:, 9 + V:], before[:, 9 + V:])

@@ -259,3 +259,36 @@ def test_buffers_beside_each_other_are_taken():
     accepted(R.grpo_policy_loss, *call(LOSS, loss=E + 16, stats=E + 20, dlp=A + 256, dH=A + 512))
     accepted(R.rollout_embedding, *call(LOOKUP, out=B + 20))
     accepted(R.rollout_embedding_backward, *call(GRAD, table=B + 20))
+
+
+def _view_calls(monkeypatch):
+    """Both directions on views of a host matrix that the binding takes for the device's: EDEVICE is what a call comes to that
+    passes all checks."""
+    if R._torch.cuda.is_available():
+        pytest.skip("host tensors would reach the device")
+    monkeypatch.setattr(R, "_device", lambda: -1)
+    z, f = R._torch.zeros, lambda k, n, stride, V, **w: R.rollout_token_logprobs(k, 0, stride, n, V, 1.0, R._torch.zeros(64, dtype=R._torch.int32),
+                                                                               0, R._torch.zeros(64))
+    back = lambda k, n, stride, V: R.rollout_token_logprobs_backward(
+        R._torch.zeros(64, 64), 0, 64, n, V, 1.0, R._torch.zeros(64, dtype=R._torch.int32), R._torch.zeros(128), None,
+        R._torch.zeros(64), None, k, stride)
+    return z, (f, back)
+
+
+def test_rows_of_views_have_the_stride_of_the_call(monkeypatch):
+    zeros, fns = _view_calls(monkeypatch)
+    wide, deep = zeros(12, 50), zeros(4, 6, 50)
+    for fn in fns:
+        for x, n, stride, V in ((wide[:, 7:37], 12, 50, 30), (wide[:, 7:37], 5, 50, 30), (wide[:, 7:37], 12, 50, 20),
+                                (wide[::2, :30], 6, 100, 30), (deep[:, :, :30], 24, 50, 30), (deep[:, :3, :30], 3, 50, 30),
+                                (deep[:, 2:3, :30], 4, 300, 30), (wide[3:4, :30], 1, 30, 30), (wide[:, 7:37], 1, 30, 30),
+                                (deep[:, :1, :30], 4, 300, 30), (wide, 20, 30, 30)):
+            refuse(R.EDEVICE, fn, x, n, stride, V)
+        for x, n, stride, V, text in ((wide[:, 7:37], 12, 30, 30, "apart"), (wide[:, 7:37], 12, 49, 30, "apart"),
+                                      (wide[:, 7:37], 12, 51, 30, "apart"), (wide[:, 7:37], 13, 50, 30, "12 rows"),
+                                      (wide[:, 7:37], 2, 30, 30, "apart"), (wide[::2, :30], 6, 50, 30, "apart"),
+                                      (deep[:, :3, :30], 12, 50, 30, "apart"), (deep[:, :3, :30], 4, 50, 30, "apart"),
+                                      (deep[::2, :, :30], 12, 50, 30, "apart"), (wide[:, :20], 11, 50, 30, "rows of 20"),
+                                      (wide.t(), 50, 12, 12, "contiguous"), (wide[:1].expand(12, 50), 12, 50, 50, "apart"),
+                                      (wide[:, 7:37], 12, 30, 31, "30 elements")):
+            refuse(R.EINVAL, fn, x, n, stride, V, text=text)
