@@ -266,6 +266,16 @@ def _strided_rows(name: str, x, n: int, stride: int, width: int):
         raise RolloutError(EINVAL, f"{name} holds {have} rows, the call needs {n}")
 
 
+def _sizes(ints, longs=(), size: int = 0):
+    """Numbers that the library's int32, int64 and uint64 arguments hold.  ctypes would pass on the low bits of others.
+    Called where one of them is negative or above 2^31 - 1, which is rare."""
+    for x, bits in [(x, 31) for x in ints] + [(x, 63) for x in longs]:
+        if not -(1 << bits) <= x < 1 << bits:
+            raise RolloutError(EINVAL if x < 0 else EUNSUPPORTED, f"{x} does not fit an int{bits + 1}")
+    if not 0 <= size < 1 << 64:
+        raise RolloutError(EINVAL, f"a workspace of {size} bytes")
+
+
 def _kind(dtype: int):
     kind = _TYPES.get(dtype)
     if kind is None:
@@ -278,6 +288,8 @@ def _device() -> int:
 
 
 def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) -> int:
+    if (n_rows | vocab | n_top) >> 31:
+        _sizes((n_rows, vocab, n_top))
     out = ctypes.c_uint64(0)
     _check(lib.rollout_token_logprobs_workspace(n_rows, vocab, n_top, ctypes.byref(out)))
     return out.value
@@ -286,6 +298,8 @@ def rollout_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int = 0) ->
 def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float, tokens,
                            n_top: int = 0, logp=None, entropy=None, stats=None, top_ids=None, top_logp=None,
                            workspace=None, workspace_bytes: int = 0, stream=None):
+    if (n_rows | vocab | n_top | row_stride | workspace_bytes) >> 31:
+        _sizes((n_rows, vocab, n_top), (row_stride,), workspace_bytes)
     dev = _device()
     _check(lib.rollout_token_logprobs(
         _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev, (n_rows, row_stride, vocab)),
@@ -300,6 +314,8 @@ def rollout_token_logprobs(logits, dtype: int, row_stride: int, n_rows: int, voc
 def rollout_token_logprobs_backward(logits, dtype: int, row_stride: int, n_rows: int, vocab: int, temperature: float,
                                     tokens, stats, entropy, grad_logp, grad_entropy, grad_logits, grad_stride: int,
                                     stream=None):
+    if (n_rows | vocab | row_stride | grad_stride) >> 31:
+        _sizes((n_rows, vocab), (row_stride, grad_stride))
     dev = _device()
     _check(lib.rollout_token_logprobs_backward(
         _buf("logits", logits, _kind(dtype), (n_rows - 1) * row_stride + vocab, dev, (n_rows, row_stride, vocab)),
@@ -312,6 +328,8 @@ def rollout_token_logprobs_backward(logits, dtype: int, row_stride: int, n_rows:
 
 
 def grpo_policy_loss_workspace(n_seqs: int, max_len: int) -> int:
+    if (n_seqs | max_len) >> 31:
+        _sizes((n_seqs, max_len))
     out = ctypes.c_uint64(0)
     _check(lib.grpo_policy_loss_workspace(n_seqs, max_len, ctypes.byref(out)))
     return out.value
@@ -320,6 +338,8 @@ def grpo_policy_loss_workspace(n_seqs: int, max_len: int) -> int:
 def grpo_policy_loss(logp, old_logp, ref_logp, entropy, adv, lengths, n_seqs: int, max_len: int, clip_low: float,
                      clip_high: float, kl_coef: float, entropy_coef: float, mean: int, loss=None, stats=None,
                      grad_logp=None, grad_entropy=None, workspace=None, workspace_bytes: int = 0, stream=None):
+    if (n_seqs | max_len | mean | workspace_bytes) >> 31:
+        _sizes((n_seqs, max_len, mean), (), workspace_bytes)
     dev = _device()
     n = n_seqs * max_len
     _check(lib.grpo_policy_loss(
@@ -334,6 +354,8 @@ def grpo_policy_loss(logp, old_logp, ref_logp, entropy, adv, lengths, n_seqs: in
 
 def rollout_embedding(table, table_dtype: int, vocab: int, dim: int, tokens, n_tokens: int, scale: float, out,
                       out_dtype: int, stream=None):
+    if (n_tokens | vocab | dim) >> 31:
+        _sizes((n_tokens, vocab, dim))
     dev = _device()
     _check(lib.rollout_embedding(
         _buf("table", table, _kind(table_dtype), vocab * dim, dev), table_dtype, vocab, dim,
@@ -342,6 +364,8 @@ def rollout_embedding(table, table_dtype: int, vocab: int, dim: int, tokens, n_t
 
 
 def rollout_embedding_backward_workspace(n_tokens: int, vocab: int, dim: int) -> int:
+    if (n_tokens | vocab | dim) >> 31:
+        _sizes((n_tokens, vocab, dim))
     out = ctypes.c_uint64(0)
     _check(lib.rollout_embedding_backward_workspace(n_tokens, vocab, dim, ctypes.byref(out)))
     return out.value
@@ -350,6 +374,8 @@ def rollout_embedding_backward_workspace(n_tokens: int, vocab: int, dim: int) ->
 def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, vocab: int, dim: int, scale: float,
                                accumulate: int, grad_table, table_dtype: int, workspace=None, workspace_bytes: int = 0,
                                stream=None):
+    if (n_tokens | vocab | dim | accumulate | workspace_bytes) >> 31:
+        _sizes((n_tokens, vocab, dim, accumulate), (), workspace_bytes)
     dev = _device()
     _check(lib.rollout_embedding_backward(
         _buf("grad", grad, _kind(grad_dtype), n_tokens * dim, dev), grad_dtype,

@@ -292,3 +292,49 @@ def test_rows_of_views_have_the_stride_of_the_call(monkeypatch):
                                       (wide.t(), 50, 12, 12, "contiguous"), (wide[:1].expand(12, 50), 12, 50, 50, "apart"),
                                       (wide[:, 7:37], 12, 30, 31, "30 elements")):
             refuse(R.EINVAL, fn, x, n, stride, V, text=text)
+
+
+BIG = 1 << 32  # its low 32 bits are 0
+
+
+@pytest.mark.parametrize("code,fn,base,change", [
+    (R.EUNSUPPORTED, R.rollout_token_logprobs, FORWARD, dict(n=BIG + 4)),
+    (R.EUNSUPPORTED, R.rollout_token_logprobs, FORWARD, dict(V=BIG + 100, stride=BIG + 100)),
+    (R.EUNSUPPORTED, R.rollout_token_logprobs, FORWARD, dict(stride=(1 << 64) + 100)),
+    (R.EUNSUPPORTED, R.rollout_token_logprobs, FORWARD, dict(top=BIG)),
+    (R.EINVAL, R.rollout_token_logprobs, FORWARD, dict(n=4 - BIG)),
+    (R.EINVAL, R.rollout_token_logprobs, FORWARD, dict(ws_bytes=-1)),
+    (R.EINVAL, R.rollout_token_logprobs, FORWARD, dict(ws_bytes=1 << 64)),
+    (R.EUNSUPPORTED, R.rollout_token_logprobs_backward, BACKWARD, dict(n=BIG + 4)),
+    (R.EUNSUPPORTED, R.rollout_token_logprobs_backward, BACKWARD, dict(V=BIG + 100, stride=BIG + 100, dz_stride=BIG + 100)),
+    (R.EINVAL, R.rollout_token_logprobs_backward, BACKWARD, dict(stride=100 - (1 << 64))),
+    (R.EUNSUPPORTED, R.rollout_token_logprobs_backward, BACKWARD, dict(dz_stride=(1 << 64) + 100)),
+    (R.EUNSUPPORTED, R.grpo_policy_loss, LOSS, dict(S=BIG + 4)), (R.EUNSUPPORTED, R.grpo_policy_loss, LOSS, dict(N=BIG + 16)),
+    (R.EUNSUPPORTED, R.grpo_policy_loss, LOSS, dict(mean=BIG + 1)), (R.EINVAL, R.grpo_policy_loss, LOSS, dict(ws_bytes=-1)),
+    (R.EUNSUPPORTED, R.rollout_embedding, LOOKUP, dict(V=BIG + 100)), (R.EUNSUPPORTED, R.rollout_embedding, LOOKUP, dict(dim=BIG + 8)),
+    (R.EUNSUPPORTED, R.rollout_embedding, LOOKUP, dict(n=BIG + 5)), (R.EINVAL, R.rollout_embedding, LOOKUP, dict(n=5 - BIG)),
+    (R.EUNSUPPORTED, R.rollout_embedding_backward, GRAD, dict(n=BIG + 5)),
+    (R.EUNSUPPORTED, R.rollout_embedding_backward, GRAD, dict(V=BIG + 100)),
+    (R.EUNSUPPORTED, R.rollout_embedding_backward, GRAD, dict(dim=BIG + 8)),
+    (R.EUNSUPPORTED, R.rollout_embedding_backward, GRAD, dict(acc=BIG)),
+    (R.EINVAL, R.rollout_embedding_backward, GRAD, dict(ws_bytes=-1)),
+    (R.EINVAL, R.rollout_embedding_backward, GRAD, dict(ws_bytes=1 << 64)),
+])
+def test_numbers_that_c_does_not_hold(code, fn, base, change):
+    refuse(code, fn, *call(base, **change))
+
+
+def test_sizes_of_workspaces_that_c_does_not_hold():
+    for fn, args in ((R.rollout_token_logprobs_workspace, (4, 100, 2)), (R.grpo_policy_loss_workspace, (4, 16)),
+                     (R.rollout_embedding_backward_workspace, (5, 100, 8))):
+        for i in range(len(args)):
+            refuse(R.EUNSUPPORTED, fn, *(x + BIG if j == i else x for j, x in enumerate(args)))
+            refuse(R.EINVAL, fn, *(x - BIG if j == i else x for j, x in enumerate(args)))
+
+
+def test_a_negative_workspace_size_does_not_pass_for_a_large_one(monkeypatch):
+    """As a tensor's size every length is enough for -1, as an unsigned number -1 is enough for every call."""
+    if R._torch.cuda.is_available():
+        pytest.skip("host tensors would reach the device")
+    monkeypatch.setattr(R, "_device", lambda: -1)
+    refuse(R.EINVAL, R.rollout_embedding_backward, *call(GRAD, ws=R._torch.zeros(16, dtype=R._torch.uint8), ws_bytes=-1))
