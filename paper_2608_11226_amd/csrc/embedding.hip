@@ -35,7 +35,7 @@ constexpr int kAhead = 8;                // rows in flight
 constexpr int kEntries = 8;              // sorted entries whose rows a workgroup does (4, 8, 16: 490, 480, 488 us at the time)
 // Rows without tokens: about this many values a workgroup (4,096 491 us, 16,384 493, 65,536 501), if that leaves this many
 // workgroups.
-constexpr int kRowValues = 16384, kRowWorkgroups = 8192;
+constexpr int kRowValues = 16384, kRowWorkgroups = 8192, kMaxRowWorkgroups = 1 << 23;
 // Threads and most workgroups of the long rows (256 threads 515 us instead of 493, 128 workgroups 505).
 constexpr int kLongThreads = 1024, kLongWorkgroups = 512;
 // From so many pieces on (65,536 tokens) pieces are summed to large ones first: one id's 2,047 pieces are 64 steps of a long
@@ -769,8 +769,9 @@ void backward(hipStream_t s, const EmbeddingGradArgs& a, char* ws) {
   if (!small) hipLaunchKernelGGL(k_embedding_runs, dim3((a.n + EB - 1) / EB), dim3(EB), 0, s, key, a.n, a.vocab, runs);
   const int entries = EB / width * kEntries;  // of a workgroup
   const int64_t starts = ((int64_t)a.n + entries - 1) / entries * slabs;
-  // rows without tokens: some kRowValues values a workgroup where there are many of them
-  const int each = std::max(1, std::min(a.vocab / kRowWorkgroups, kRowValues / a.dim));
+  // rows without tokens: some kRowValues values a workgroup where there are many of them, and never more than kMaxRowWorkgroups,
+  // with which the launch stays below 2^32 threads
+  const int each = std::max({1, std::min(a.vocab / kRowWorkgroups, kRowValues / a.dim), a.vocab / kMaxRowWorkgroups + 1});
   const int zeros = (z.rows_end + each - 1) / each, long_zeros = (z.long_end - z.rows_end + each - 1) / each;
   hipLaunchKernelGGL((k_embedding_rows<T, O, ACC>), dim3((unsigned)((int64_t)pieces * slabs + starts + zeros)), dim3(EB), 0, s,
                      (const T*)a.g, key, pos, a.n, a.vocab, a.dim, a.scale, runs, shift, width, slabs, pieces * slabs,
