@@ -412,7 +412,8 @@ rollout_status rollout_embedding(const void* d_table, int32_t table_dtype, int32
  * 0 every row is written (rows without tokens with zeros); with 1 the sum is added
  * to what the row holds, rounded once, and rows without tokens are left alone.
  * Ids outside [0, vocab) contribute nothing.  Tokens are sorted by id and a row's are
- * added in fp32 in an order that their positions fix.  Errors as above, EUNSUPPORTED also where
+ * added in fp32 in an order that the call's sizes and tokens fix: the same call gives the
+ * same bits, but other ids in the batch may move a row's sum by roundings.  Errors as above, EUNSUPPORTED also where
  * n_tokens ceil(dim / 1024) is above 2^25, and ENOMEM (workspace too small).
  */
 rollout_status rollout_embedding_backward_workspace(int32_t n_tokens, int32_t vocab, int32_t dim, uint64_t* h_bytes);

@@ -286,3 +286,22 @@ def test_repeats_and_graphs(n):
         torch.cuda.synchronize()
         for graph, table, ws in made:
             assert torch.equal(first, table), replay
+
+
+def test_other_ids_in_the_batch_move_a_sum_by_roundings_only():
+    """Where a run lies among the sorted ids decides where it is cut into pieces, and the batch's size how long they are: a
+    row's sum is the same bits for the same batch, and within its bound whatever else is there."""
+    rng = np.random.default_rng(13)
+    n, d, V = 100, 4, 3
+    vals = (rng.standard_normal((n, d)) * 2.0 ** rng.integers(-20, 20, (n, 1))).astype(np.float32)
+    for before, behind in ((0, 0), (1, 0), (7, 0), (16, 3), (31, 500), (33, 33), (500, 5000), (9000, 1)):
+        tok = np.repeat(np.array([0, 1, 2], dtype=np.int32), (before, n, behind))
+        g = np.concatenate([rng.standard_normal((before, d)), vals, rng.standard_normal((behind, d))]).astype(np.float32)
+        order = rng.permutation(len(tok))
+        order[np.flatnonzero(tok[order] == 1)] = np.flatnonzero(tok == 1)  # this row's tokens in the same order
+        tok, g = np.ascontiguousarray(tok[order]), np.ascontiguousarray(g[order])
+        gd, td, table, again = to_dev(g, torch), to_dev(tok, torch), torch.empty(V, d, device=DEV), torch.empty(V, d, device=DEV)
+        grad(gd, "fp32", td, V, 1.0, 0, table, "fp32")
+        grad(gd, "fp32", td, V, 1.0, 0, again, "fp32")
+        assert torch.equal(table, again)
+        check_grad(table.double().cpu().numpy(), gd, tok, V, 1.0, None, "fp32")

@@ -498,3 +498,41 @@ def test_views_are_read_and_written_at_their_own_stride():
     R.rollout_token_logprobs_backward(z, 0, V, n, V, 1.0, tok, fw["stats"], None, torch.ones(n, device=DEV), None, want, V)
     assert torch.equal(part, want)
     assert torch.equal(wide[:, :9], before[:, :9]) and torch.equal(wide[:, 9 + V:], before[:, 9 + V:])
+
+
+def test_waves_go_on_to_further_rows():
+    """More rows than 2^20 workgroups of four waves take at once, without alternatives."""
+    n, V = 4 * (1 << 20) + 4099, 5
+    z = torch.randn(n, V, device=DEV, dtype=torch.bfloat16) * 3
+    tok = torch.randint(-1, V, (n,), device=DEV, dtype=torch.int32)
+    log(f"{n} x {V}")
+    got = forward(z, V, V, 1.0, tok, 0, "bf16")
+    lp = torch.log_softmax(z.double(), 1)
+    live = tok >= 0
+    want = lp.gather(1, tok.clamp(min=0).long()[:, None])[:, 0] * live
+    assert (got["logp"] - want).abs().max().item() <= 200 * EPS  # distances of at most 27
+    H = -(lp.exp() * lp).sum(1) * live
+    assert (got["entropy"] - H).abs().max().item() <= 200 * EPS
+    assert torch.equal(got["stats"][:, 0], torch.where(live, z.amax(1).float(), 0.0))
+
+
+def test_workgroups_go_on_to_further_rows():
+    """More than 2^20 rows that take a workgroup each (of 69 GB; nearly all are padding, which is not read, so only rows at both
+    ends hold anything): a workgroup's second row follows a first one of its own, or a padded one, in the same LDS."""
+    n, V, dtype = (1 << 20) + 24, 32769, "bf16"
+    if torch.cuda.mem_get_info()[0] < 2 * n * V + (4 << 30):
+        torch.cuda.empty_cache()
+    z = torch.empty(n, V, dtype=torch.bfloat16, device=DEV)
+    rows = torch.cat([torch.arange(16), (1 << 20) + torch.arange(24)]).to(DEV)
+    z[rows] = (torch.randn(rows.numel(), V, device=DEV) * 3).to(z.dtype)
+    tok = torch.full((n,), -1, dtype=torch.int32, device=DEV)
+    tok[rows] = torch.randint(0, V, (rows.numel(),), device=DEV, dtype=torch.int32)
+    tok[rows[3::8]] = -1
+    log(f"{n} x {V}")
+    got = forward(z, V, V, 0.9, tok, 0, dtype)
+    check_forward({k: got[k][rows] for k in ("logp", "entropy", "stats")}, z[rows].double().cpu().numpy(), float(np.float32(0.9)),
+                  tok[rows].cpu().numpy())
+    for k in ("logp", "entropy", "stats"):
+        assert not got[k][tok < 0].any()
+    del z
+    torch.cuda.empty_cache()
