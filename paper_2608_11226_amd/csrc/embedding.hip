@@ -3,10 +3,10 @@
 //   out_n = scale E[id_n];     dE_v = scale sum over n with id_n = v of g_n   (+ the old dE_v)
 //
 // The gradient sorts (id, position) pairs by id with a stable radix sort, so that a row's tokens stand together in
-// token order, and adds up each run in an order that follows from its place alone: no atomics on floats, the same bits on every
-// call.  A run's length is anything from one to all of the tokens (text repeats its frequent ids), so runs are cut at fixed
-// places of the sorted order: every 32 entries that belong to one id are summed beforehand, and in long batches every 32 such
-// sums once more.
+// token order, and adds up each run in an order that follows from its place among them: no atomics on floats, the same bits on
+// every such call.  A run's length is anything from one to all of the tokens (text repeats its frequent ids), so runs are cut at
+// fixed places of the sorted order: every 32 entries (16 in batches of some hundreds to some ten thousand tokens) that belong to
+// one id are summed beforehand, and in long batches every 32 such sums once more.
 //
 // Both are bound by HBM where there is much to move: 49,152 rows of 3,584 looked up in 186 us (705 MB written beside some 150 MB
 // of scattered rows), their gradient into 152,064 fp32 rows in 491 us (2.18 GB, most of it zeros, beside 308 MB of gathered
@@ -23,16 +23,17 @@ constexpr int EB = 256;
 // and of 2,048 tokens x 128 (fp32) into 1,024 rows.
 // Entries of a piece (and pieces of a large piece): 1 << piece_shift(n, dim).  Pieces of 32 are best where there is much to add
 // (16, 32 and 64: 510, 488 and 484 us, 60,000 tokens x 640 88.8, 80.2 and 84.0), of 16 where the steps one after another count
-// (2,048 x 128 21.1, 23.5 and 25.7, 8,000 x 1,000 45.7, 48.8 and more, 16,000 x 1,000 49.1 and 52.6; 24,000 x 1,000 55.2 and
-// 56.4, 28,000 x 640 55.5 and 55.1, 16,000 x 2,048 59.3 and 58.3).  Few text-like tokens have no run of 32 (300 x 128 16.5 and
-// 13.8, 300 x 1,000 22.4 and 20.5; 500 x 128 17.7 and 18.1, 600 x 1,000 23.4 and 23.8).
+// (2,048 x 128 21.1, 23.5 and 25.7, 8,000 x 1,000 45.7, 48.8 and more, 16,000 x 1,000 49.1 and 52.6), and neither in
+// between (24,000 x 1,000 63.8 and 63.3, 28,000 x 640 55.5 and 55.1, 16,000 x 2,048 59.3 and 58.3).  Few text-like tokens have
+// no run of 32 (300 x 128 16.5 and 13.8, 300 x 1,000 22.4 and 20.5; 500 x 128 17.7 and 18.1, 600 x 1,000 23.4 and 23.8).
 constexpr int kPieceShift = 5, kPiece = 1 << kPieceShift;
 constexpr int kFewTokens = 400, kSmallPieceTokens = 1 << 15, kSmallPieceValues = 1 << 24;
 inline int piece_shift(int n, int dim) {
   return n >= kFewTokens && n < kSmallPieceTokens && (int64_t)n * dim <= kSmallPieceValues ? kPieceShift - 1 : kPieceShift;
 }
 constexpr int kAhead = 8;                // rows in flight
-constexpr int kEntries = 8;              // sorted entries whose rows a workgroup does (4, 8, 16: 490, 480, 488 us at the time)
+constexpr int kEntries = 8;              // sorted entries whose rows a workgroup does (4, 8, 16: 483, 494, 498 us; 60,000 x
+                                         // 640 67, 62 and 62; 2,048 x 128 20.2, 19.5 and 20.7)
 // Rows without tokens: about this many values a workgroup (4,096 491 us, 16,384 493, 65,536 501), if that leaves this many
 // workgroups.
 constexpr int kRowValues = 16384, kRowWorkgroups = 8192, kMaxRowWorkgroups = 1 << 23;
@@ -42,8 +43,8 @@ constexpr int kLongThreads = 1024, kLongWorkgroups = 512;
 // row's groups, and the kernel that sums them takes 7 us whether there is such an id or not.
 constexpr int kManyPieces = 2048;
 // Bytes of zeros that a launch of the sort writes beside it (none 526 us, 80 MB 497, 160 MB 493, 320 MB 496; 5,000 tokens by
-// tiles into a bf16 table 231, 203, 201 and 226), that of the long rows (none 535 us, 96 or 200 MB 530 at the
-// time), and a workgroup (300 tokens into 152,064 x 3,584 fp32: 16 KB 362 us, 64 KB 433, 256 KB 382).
+// tiles into a bf16 table 231, 203, 201 and 226), that of the long rows (none 497 us, 96 MB 494, 200 MB 486),
+// and a workgroup (300 tokens into 152,064 x 3,584 fp32: 16 KB 362 us, 64 KB 433, 256 KB 382).
 constexpr size_t kSortFill = 160u << 20, kLongFill = 96u << 20, kFill = 16384;
 constexpr int kMaxFillBlocks = 1 << 20;
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;

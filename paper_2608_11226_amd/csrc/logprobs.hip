@@ -24,8 +24,8 @@ constexpr int RW = RB / 64;
 constexpr int kUnits = 4;  // 16-byte loads in flight a lane
 constexpr int kMaxUnits = kMaxTopVocab / 256, kMaxPer = kMaxUnits / 64;  // of a row, of a lane, where alternatives are taken
 constexpr int kMaxChunks = 64;     // a lane each when parts are joined
-// Workgroups that a launch of few rows is split into: 515 bf16 rows of 152,064 39.5 us with 1,024, 36.1 with 2,048, 36.4 with
-// 8,192; 256 fp32 rows with alternatives 44.4, 41.9 and 46.9 at the time.
+// Workgroups that a launch of few rows is split into: 515 bf16 rows of 152,064 38.5 us with 1,024, 32.7 with 2,048, 34.4 with
+// 8,192; 256 fp32 rows with 20 alternatives 37.0, 36.4 and 36.6.
 constexpr int kWorkgroups = 2048;
 constexpr int kWhole = 64;         // units of a row that is not split
 constexpr int kWaveRows = 2048;    // rows from which such a row is one wave's

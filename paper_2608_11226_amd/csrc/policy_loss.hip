@@ -9,8 +9,8 @@
 // per thread, per workgroup, and over the workgroups by a second kernel, always in the same order.
 //
 // Bound by HBM where there are many tokens (2,048 sequences of 4,096 places, half of them tokens, with reference and
-// entropies: 67 MB read and 67 written in 28.4 us, 4.7 TB/s, and 4 us for the join), by its two launches where there are few
-// (64 of 512: 5.3 and 2.0 us).
+// entropies: 67 MB read and 67 written in 30.7 us, 4.4 TB/s, and 4 us for the join), by its two launches where there are few
+// (64 of 512: 5.4 and 1.9 us).
 #include "update.h"
 
 namespace rollout {
@@ -19,7 +19,8 @@ namespace {
 constexpr int LB = 256;
 constexpr int kTile = LB * 4;     // tokens of a workgroup's step
 // Odd: the steps of a workgroup are kMaxBlocks tiles apart and shall not all fall on the same part of completions, whose ends
-// have nothing to do (of 8.4 M tokens: 28.7 us, 30.2 with 1,536; 29.1 and 32.2 with 1,023 and 1,791).
+// have nothing to do (of 8.4 M tokens, before the penalty's series: 28.7 us, 30.2 with
+// 1,536; 29.1 and 32.2 with 1,023 and 1,791).
 constexpr int kMaxBlocks = 1279;
 // Up to one step of as many threads one workgroup does all, and there is no join (8 sequences of 256 in a graph and eager 6.7
 // and 10.7 us, in four workgroups and a join 7.8 and 13.3; two steps, 16 of 512, 9.8 and 10.7, 8.1 and 13.3).

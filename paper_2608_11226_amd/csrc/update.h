@@ -1,5 +1,5 @@
 // The operators of a GRPO step's update side: token log probabilities and their gradient (logprobs.hip), the clipped
-// group loss (grpo.hip), embedding lookup and its gradient (embedding.hip).  Launchers called by the C entry points in
+// group loss (policy_loss.hip), embedding lookup and its gradient (embedding.hip).  Launchers called by the C entry points in
 // update.hip, and device helpers that these kernels share.
 #pragma once
 
