@@ -279,7 +279,8 @@ def _prepare_adamw(case, g, st):
 def _power(amax):
     """The smallest power of two that brings amax to at most 448 (2^-126 at least)."""
     f, e = torch.frexp(amax)
-    return torch.ldexp(torch.ones_like(amax), torch.clamp(e - 9 + (f > 0.875).to(e.dtype), min=-126))
+    e = torch.where(amax > 0, e - 9 + (f > 0.875).to(e.dtype), -126)
+    return torch.ldexp(torch.ones_like(amax), torch.clamp(e, min=-126))
 
 
 def _encode(x):
