@@ -54,6 +54,10 @@ typedef int32_t rollout_status;
                                     integer dot product in fp32.  Embedding and LM head stay bf16.  Needs
                                     d_model, n_heads*head_dim and d_ff to be multiples of 128. */
 
+#define ROLLOUT_DTYPE_E4M3 3     /* 8 bits: sign, 4 exponent bits (bias 7), 3 mantissa bits, largest value 448, no
+                                    infinity.  Outputs and optimiser states of the update side, always with a power of
+                                    two as fp32 scale: what is stored stands for code * scale.  No model's type. */
+
 typedef struct rollout_ctx rollout_ctx;
 
 /*
@@ -421,6 +425,136 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
                                           int32_t vocab, int32_t dim, float scale, int32_t accumulate, void* d_grad_table,
                                           int32_t table_dtype, void* d_workspace, uint64_t workspace_bytes,
                                           void* hip_stream);
+
+/*
+ * The update through the layers: attention over packed sequences and its gradient, the norm of the
+ * residual stream and its gradient, and the optimiser's step.  Matrix products are the caller's.
+ *
+ * Attention.  Sequences lie one behind the other in matrices of tokens, d_q [n_q, n_heads * head_dim] and
+ * d_k, d_v [n_k, n_kv_heads * head_dim], whose rows are a stride of elements apart (so that the three
+ * may be columns of one projection's output; n_heads / n_kv_heads query heads share a key's).  Sequence
+ * s has the rows from starts[s] on, lens[s] of them, at most up to starts[s + 1] (d_q_starts, d_k_starts
+ * int32 [n_seqs + 1], ascending; d_q_lens, d_k_lens int32 [n_seqs], NULL: all of them.  Values are taken
+ * into [0, rows]; with starts that descend it is not said which rows are written).  A padded batch has
+ * starts s * max_len and its lengths.  d_k_starts NULL: keys lie where the queries do (n_k = n_q).
+ *   s_ij = scale q_i k_j;  lse_i = log sum_j exp(s_ij);  out_i = sum_j exp(s_ij - lse_i) v_j
+ * over all keys of the sequence or, causal, over keys j <= i + len_k - len_q (the queries are the last
+ * of the keys' tokens).  A query without keys gets out 0 and lse -inf.  Rows of no sequence are neither
+ * read nor written, in the outputs either.  What is not finite in a sequence may reach all of its rows,
+ * and none of another one's.
+ * d_out as d_q, d_lse fp32 [n_heads, n_q].
+ * dtype FP32 (fp32 products) or BF16 (probabilities and their gradients enter products as bf16; sums
+ * and statistics are fp32).  Matrices and strides are multiples of 16 bytes, rows at most 2^25 bytes apart.
+ * Errors: EINVAL (shape, NULL buffers, alignment, strides, overlap), EUNSUPPORTED (head_dim not 32, 64 or
+ * 128, n_heads times tokens above 2^26, n_heads times sequences above 2^23, strides), ENOMEM
+ * (workspace too small), EDEVICE.
+ */
+typedef struct {
+  int32_t dtype;               /* ROLLOUT_DTYPE_FP32 or _BF16: of all matrices */
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t n_seqs;
+  int32_t n_q, n_k;            /* rows of the queries' and of the keys' matrices */
+  int32_t causal;              /* 0 or 1 */
+  float scale;                 /* of the products, > 0 */
+} rollout_attention_shape;
+
+rollout_status rollout_attention_workspace(const rollout_attention_shape* shape, uint64_t* h_bytes);
+rollout_status rollout_attention(const rollout_attention_shape* shape, const void* d_q, int64_t q_stride, const void* d_k,
+                                 int64_t k_stride, const void* d_v, int64_t v_stride, const int32_t* d_q_starts,
+                                 const int32_t* d_q_lens, const int32_t* d_k_starts, const int32_t* d_k_lens, void* d_out,
+                                 int64_t out_stride, float* d_lse, void* d_workspace, uint64_t workspace_bytes,
+                                 void* hip_stream);
+
+/*
+ * Its gradient: with p_ij = exp(s_ij - lse_i) and D_i = sum grad_out_i out_i, out and lse being the forward call's,
+ *   grad_v_j = sum_i p_ij grad_out_i;  ds_ij = p_ij (grad_out_i v_j - D_i)
+ *   grad_k_j = scale sum_i ds_ij q_i;  grad_q_i = scale sum_j ds_ij k_j
+ * each over the query heads that share the key's.  Every row of a sequence is written (keys that no query
+ * attends, and queries without keys, get 0).  The gradients' rows may be columns of one matrix.
+ * Errors as above.
+ */
+rollout_status rollout_attention_backward_workspace(const rollout_attention_shape* shape, uint64_t* h_bytes);
+rollout_status rollout_attention_backward(const rollout_attention_shape* shape, const void* d_q, int64_t q_stride,
+                                          const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                                          const int32_t* d_q_starts, const int32_t* d_q_lens, const int32_t* d_k_starts,
+                                          const int32_t* d_k_lens, const void* d_out, int64_t out_stride, const float* d_lse,
+                                          const void* d_grad_out, int64_t grad_out_stride, void* d_grad_q,
+                                          int64_t grad_q_stride, void* d_grad_k, int64_t grad_k_stride, void* d_grad_v,
+                                          int64_t grad_v_stride, void* d_workspace, uint64_t workspace_bytes,
+                                          void* hip_stream);
+
+/*
+ * Root-mean-square norm of rows of dim values, behind the addition to the residual stream:
+ *   h = x + delta (rounded to x_dtype);  rstd = 1 / sqrt(mean h^2 + eps);  y = h rstd gain
+ * d_x [n_rows, dim] of x_dtype, d_delta of delta_dtype with d_h of x_dtype (which may be d_x), or both NULL (h = x);
+ * d_gain fp32 [dim], NULL: 1; d_y of y_dtype; d_rstd fp32 [n_rows], NULL if not wanted (the gradient needs it).
+ * x and delta are FP32 or BF16.  y is FP32, BF16 or E4M3: then d_scales [n_rows] (otherwise NULL) receives
+ * the smallest power of two, 2^-126 at least, for which no |y| of the row, over it, is above 448, and d_y the codes of y over it, to
+ * nearest, ties to even (NaN where y is not finite).  Matrices are dense, and rows may start at any element.
+ * Errors: EINVAL (sizes, types, alignment, NULL buffers, overlap), EUNSUPPORTED (dim above 32,768,
+ * rows whose launch would have 2^32 threads: 2^26 up to dim 2,048, 2^24 up to 8,192, 2^22 above), EDEVICE.
+ */
+rollout_status rollout_rms_norm(const void* d_x, int32_t x_dtype, const void* d_delta, int32_t delta_dtype,
+                                const float* d_gain, int32_t n_rows, int32_t dim, float eps, void* d_h, void* d_y,
+                                int32_t y_dtype, float* d_scales, float* d_rstd, void* hip_stream);
+
+/*
+ * Its gradient.  d_h are the normed rows (d_h of the forward call, or d_x without an addition), d_rstd its statistics,
+ * d_grad_h of grad_x_dtype the gradient that reaches h by the residual stream (NULL: none; it may be d_grad_x):
+ *   t = grad_y gain;  xhat = h rstd;  grad_x = grad_h + rstd (t - xhat mean(t xhat));  grad_gain = sum over rows of grad_y xhat
+ * grad_x is the gradient of x and of delta alike.  d_grad_gain fp32 [dim], NULL: not wanted (and no workspace
+ * needed); accumulate 1 adds to what it holds.  Errors as above, and ENOMEM (workspace too small).
+ */
+rollout_status rollout_rms_norm_backward_workspace(int32_t n_rows, int32_t dim, uint64_t* h_bytes);
+rollout_status rollout_rms_norm_backward(const void* d_grad_y, int32_t grad_y_dtype, const void* d_h, int32_t h_dtype,
+                                         const float* d_gain, const float* d_rstd, int32_t n_rows, int32_t dim,
+                                         const void* d_grad_h, void* d_grad_x, int32_t grad_x_dtype, float* d_grad_gain,
+                                         int32_t accumulate, void* d_workspace, uint64_t workspace_bytes,
+                                         void* hip_stream);
+
+/*
+ * AdamW over many tensors in one launch.  A table names them: rollout_adamw_table writes it to host memory
+ * (rollout_adamw_table_bytes of it), the caller copies it to the device once, and it serves every step as long as
+ * the buffers stay where they are.  A tensor of n >= 0 elements:
+ *   d_param of param_dtype (FP32 or BF16), d_grad of grad_dtype (FP32 or BF16);
+ *   d_m, d_v: first and second moment, fp32 (state_dtype FP32), or E4M3 codes with d_m_scales, d_v_scales fp32
+ *     [ceil(n / 128)], one scale for 128 elements: m = code scale, sqrt(v) = code scale.  Zeros are a fresh state;
+ *   d_copy: bf16 copy of fp32 weights that the step writes (to nearest), or NULL.
+ * Buffers are aligned to their elements; one that is written shares no byte with any other of the table.
+ * The step, with g = grad_scale grad and t = step:
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   param = param (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32, with the new moments before they are rounded.  BF16 weights and E4M3 states are rounded up or down with
+ * the probability that keeps their expectation (to nearest they would not move by steps that are small beside them), by 16 bits r
+ * of a counter hash of (seed, t, the tensor's place in the table, the element): bf16 drops 16 bits of
+ * the fp32 value's magnitude after adding r, e4m3 drops 20 after adding 16 r + 8 (below 2^-6, where values are 2^-9 apart,
+ * from the magnitude plus 2^-6).  A scale is the smallest power of two, 2^-126 at least, that leaves no magnitude of
+ * its 128 above 448; a second moment above 0 keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the
+ * low 16 bits and v the high ones; a weight the low ones of f(h + (k >> 32)).  f is MurmurHash3's 32-bit
+ * finaliser, k = F(F(seed + G t) + G (1 + tensor + 2^20 floor(i / 2^32))) with SplitMix64's finaliser F and constant G.
+ * d_grad_scale fp32 [1] (a clipping factor, say; NULL: 1): where it is not finite nothing changes.  d_lr fp32 [1] and d_step
+ * int64 [1] replace lr and step if not NULL (a captured call reads them at every replay; a step below 1 counts as 1).
+ * n_chunks is what rollout_adamw_table said; d_table has to hold what it wrote.
+ * Errors: EINVAL (types, alignment, NULL buffers, overlap, factors), EUNSUPPORTED (more than 2^20 tensors,
+ * 2^36 elements or 2^24 - 8 chunks of them), ENOMEM (table too small), EDEVICE.
+ */
+typedef struct {
+  void* d_param;
+  const void* d_grad;
+  void *d_m, *d_v;
+  float *d_m_scales, *d_v_scales;   /* E4M3 states only */
+  void* d_copy;
+  int64_t n;
+  int32_t param_dtype, grad_dtype, state_dtype;
+  float weight_decay;
+} rollout_adamw_tensor;
+
+rollout_status rollout_adamw_table_bytes(int32_t n_tensors, uint64_t* h_bytes);
+rollout_status rollout_adamw_table(const rollout_adamw_tensor* h_tensors, int32_t n_tensors, void* h_table,
+                                   uint64_t table_bytes, int64_t* h_chunks);
+rollout_status rollout_adamw(const void* d_table, int32_t n_tensors, int64_t n_chunks, double lr, double beta1, double beta2,
+                             double eps, int64_t step, uint64_t seed, const float* d_grad_scale, const float* d_lr,
+                             const int64_t* d_step, void* hip_stream);
 
 /* ------------------------------------------------------------------------ */
 /* Inspection and measurement                                                */

@@ -19,7 +19,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("ROLLOUT_LIBRARY") or os.path.join(_PKG, "librollout.so")
 
 OK, EINVAL, ENOMEM, EDEVICE, ESTATE, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
-DTYPE_FP32, DTYPE_BF16, DTYPE_INT4 = 0, 1, 2
+DTYPE_FP32, DTYPE_BF16, DTYPE_INT4, DTYPE_E4M3 = 0, 1, 2, 3
 _NAMES = {EINVAL: "EINVAL", ENOMEM: "ENOMEM", EDEVICE: "EDEVICE", ESTATE: "ESTATE", EUNSUPPORTED: "EUNSUPPORTED"}
 
 EXPORTED = (
@@ -30,6 +30,9 @@ EXPORTED = (
     "rollout_token_logprobs_workspace", "rollout_token_logprobs", "rollout_token_logprobs_backward",
     "grpo_policy_loss_workspace", "grpo_policy_loss",
     "rollout_embedding", "rollout_embedding_backward_workspace", "rollout_embedding_backward",
+    "rollout_attention_workspace", "rollout_attention", "rollout_attention_backward_workspace", "rollout_attention_backward",
+    "rollout_rms_norm", "rollout_rms_norm_backward_workspace", "rollout_rms_norm_backward",
+    "rollout_adamw_table_bytes", "rollout_adamw_table", "rollout_adamw",
 )
 MEAN_SEQUENCE, MEAN_TOKEN, MEAN_FIXED = 0, 1, 2  # ROLLOUT_MEAN_*
 NOALLOC_SCRATCH_BYTES = 64 << 20  # ROLLOUT_SAMPLE_NOALLOC_SCRATCH_BYTES
@@ -88,6 +91,23 @@ class StepProfile(ctypes.Structure):
     ]
 
 
+class AttentionShape(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32), ("n_q", ctypes.c_int32), ("n_k", ctypes.c_int32), ("causal", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [
+        ("d_param", ctypes.c_void_p), ("d_grad", ctypes.c_void_p), ("d_m", ctypes.c_void_p), ("d_v", ctypes.c_void_p),
+        ("d_m_scales", ctypes.c_void_p), ("d_v_scales", ctypes.c_void_p), ("d_copy", ctypes.c_void_p), ("n", ctypes.c_int64),
+        ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32), ("state_dtype", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float),
+    ]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2608_11226_amd/build.py`")
@@ -99,6 +119,7 @@ def _load():
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, f32, u64, f64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_float, ctypes.c_uint64, ctypes.c_double
     i64, pu64 = ctypes.c_int64, ctypes.POINTER(u64)
+    shape = ctypes.POINTER(AttentionShape)
     sig = {
         "rollout_plan": ([ctypes.POINTER(ModelConfig), i32, ctypes.POINTER(Plan)], i32),
         "rollout_init": ([ctypes.POINTER(ModelConfig), vp, u64, vp, ctypes.POINTER(vp)], i32),
@@ -125,6 +146,17 @@ def _load():
         "rollout_embedding": ([vp, i32, i32, i32, vp, i32, f32, vp, i32, vp], i32),
         "rollout_embedding_backward_workspace": ([i32, i32, i32, pu64], i32),
         "rollout_embedding_backward": ([vp, i32, vp, i32, i32, i32, f32, i32, vp, i32, vp, u64, vp], i32),
+        "rollout_attention_workspace": ([shape, pu64], i32),
+        "rollout_attention": ([shape, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, u64, vp], i32),
+        "rollout_attention_backward_workspace": ([shape, pu64], i32),
+        "rollout_attention_backward": ([shape, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64,
+                                        vp, i64, vp, u64, vp], i32),
+        "rollout_rms_norm": ([vp, i32, vp, i32, vp, i32, i32, f32, vp, vp, i32, vp, vp, vp], i32),
+        "rollout_rms_norm_backward_workspace": ([i32, i32, pu64], i32),
+        "rollout_rms_norm_backward": ([vp, i32, vp, i32, vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, u64, vp], i32),
+        "rollout_adamw_table_bytes": ([i32, pu64], i32),
+        "rollout_adamw_table": ([ctypes.POINTER(AdamwTensor), i32, vp, u64, ctypes.POINTER(i64)], i32),
+        "rollout_adamw": ([vp, i32, i64, f64, f64, f64, f64, i64, u64, vp, vp, vp, vp], i32),
         "occ_rolling_mean": ([vp, ctypes.c_int64, f64, f64, vp], i32),
         "occ_violation": ([vp, ctypes.c_int64, f64, f64, ctypes.POINTER(f64), ctypes.POINTER(f64)], i32),
         "occ_normalize_budget": ([f64, f64, f64], f64),
@@ -382,6 +414,144 @@ def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, voc
         _buf("tokens", tokens, _I, n_tokens, dev), n_tokens, vocab,
         dim, scale, accumulate, _buf("grad_table", grad_table, _kind(table_dtype), vocab * dim, dev), table_dtype,
         _buf("workspace", workspace, _U8, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
+
+
+def _matrix(name: str, x, kind, n: int, stride: int, width: int, device: int):
+    """A matrix of n rows of width elements, stride apart."""
+    return _buf(name, x, kind, (n - 1) * stride + width, device, (n, stride, width))
+
+
+def rollout_attention_workspace(shape: AttentionShape) -> int:
+    out = ctypes.c_uint64(0)
+    _check(lib.rollout_attention_workspace(ctypes.byref(shape), ctypes.byref(out)))
+    return out.value
+
+
+def rollout_attention(shape: AttentionShape, q, q_stride: int, k, k_stride: int, v, v_stride: int, q_starts, q_lens, k_starts,
+                      k_lens, out, out_stride: int, lse, workspace=None, workspace_bytes: int = 0, stream=None):
+    if (q_stride | k_stride | v_stride | out_stride | workspace_bytes) >> 31:
+        _sizes((), (q_stride, k_stride, v_stride, out_stride), workspace_bytes)
+    dev, kind = _device(), _kind(shape.dtype)
+    nq, nk, wq, wk, S = shape.n_q, shape.n_k, shape.n_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim, shape.n_seqs
+    _check(lib.rollout_attention(
+        ctypes.byref(shape), _matrix("q", q, kind, nq, q_stride, wq, dev), q_stride, _matrix("k", k, kind, nk, k_stride, wk, dev),
+        k_stride, _matrix("v", v, kind, nk, v_stride, wk, dev), v_stride, _buf("q_starts", q_starts, _I, S + 1, dev),
+        _buf("q_lens", q_lens, _I, S, dev), _buf("k_starts", k_starts, _I, S + 1, dev), _buf("k_lens", k_lens, _I, S, dev),
+        _matrix("out", out, kind, nq, out_stride, wq, dev), out_stride, _buf("lse", lse, _F, shape.n_heads * nq, dev),
+        _buf("workspace", workspace, _U8, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
+
+
+def rollout_attention_backward_workspace(shape: AttentionShape) -> int:
+    out = ctypes.c_uint64(0)
+    _check(lib.rollout_attention_backward_workspace(ctypes.byref(shape), ctypes.byref(out)))
+    return out.value
+
+
+def rollout_attention_backward(shape: AttentionShape, q, q_stride: int, k, k_stride: int, v, v_stride: int, q_starts, q_lens,
+                               k_starts, k_lens, out, out_stride: int, lse, grad_out, grad_out_stride: int, grad_q,
+                               grad_q_stride: int, grad_k, grad_k_stride: int, grad_v, grad_v_stride: int, workspace=None,
+                               workspace_bytes: int = 0, stream=None):
+    strides = (q_stride, k_stride, v_stride, out_stride, grad_out_stride, grad_q_stride, grad_k_stride, grad_v_stride)
+    if any(s >> 31 for s in strides) or workspace_bytes >> 31:
+        _sizes((), strides, workspace_bytes)
+    dev, kind = _device(), _kind(shape.dtype)
+    nq, nk, wq, wk, S = shape.n_q, shape.n_k, shape.n_heads * shape.head_dim, shape.n_kv_heads * shape.head_dim, shape.n_seqs
+    _check(lib.rollout_attention_backward(
+        ctypes.byref(shape), _matrix("q", q, kind, nq, q_stride, wq, dev), q_stride, _matrix("k", k, kind, nk, k_stride, wk, dev),
+        k_stride, _matrix("v", v, kind, nk, v_stride, wk, dev), v_stride, _buf("q_starts", q_starts, _I, S + 1, dev),
+        _buf("q_lens", q_lens, _I, S, dev), _buf("k_starts", k_starts, _I, S + 1, dev), _buf("k_lens", k_lens, _I, S, dev),
+        _matrix("out", out, kind, nq, out_stride, wq, dev), out_stride, _buf("lse", lse, _F, shape.n_heads * nq, dev),
+        _matrix("grad_out", grad_out, kind, nq, grad_out_stride, wq, dev), grad_out_stride,
+        _matrix("grad_q", grad_q, kind, nq, grad_q_stride, wq, dev), grad_q_stride,
+        _matrix("grad_k", grad_k, kind, nk, grad_k_stride, wk, dev), grad_k_stride,
+        _matrix("grad_v", grad_v, kind, nk, grad_v_stride, wk, dev), grad_v_stride,
+        _buf("workspace", workspace, _U8, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
+
+
+def rollout_rms_norm(x, x_dtype: int, delta, delta_dtype: int, gain, n_rows: int, dim: int, eps: float, h, y, y_dtype: int,
+                     scales=None, rstd=None, stream=None):
+    if (n_rows | dim) >> 31:
+        _sizes((n_rows, dim))
+    dev, n = _device(), n_rows * dim
+    _check(lib.rollout_rms_norm(
+        _buf("x", x, _kind(x_dtype), n, dev), x_dtype, _buf("delta", delta, None if delta is None else _kind(delta_dtype), n, dev),
+        delta_dtype, _buf("gain", gain, _F, dim, dev), n_rows, dim, eps, _buf("h", h, _kind(x_dtype), n, dev),
+        _code_buf("y", y, n, dev) if y_dtype == DTYPE_E4M3 else _buf("y", y, _kind(y_dtype), n, dev), y_dtype,
+        _buf("scales", scales, _F, n_rows, dev), _buf("rstd", rstd, _F, n_rows, dev), _ptr(stream)))
+
+
+def rollout_rms_norm_backward_workspace(n_rows: int, dim: int) -> int:
+    if (n_rows | dim) >> 31:
+        _sizes((n_rows, dim))
+    out = ctypes.c_uint64(0)
+    _check(lib.rollout_rms_norm_backward_workspace(n_rows, dim, ctypes.byref(out)))
+    return out.value
+
+
+def rollout_rms_norm_backward(grad_y, grad_y_dtype: int, h, h_dtype: int, gain, rstd, n_rows: int, dim: int, grad_h, grad_x,
+                              grad_x_dtype: int, grad_gain=None, accumulate: int = 0, workspace=None, workspace_bytes: int = 0,
+                              stream=None):
+    if (n_rows | dim | accumulate | workspace_bytes) >> 31:
+        _sizes((n_rows, dim, accumulate), (), workspace_bytes)
+    dev, n, kind = _device(), n_rows * dim, _kind(grad_x_dtype)
+    _check(lib.rollout_rms_norm_backward(
+        _buf("grad_y", grad_y, _kind(grad_y_dtype), n, dev), grad_y_dtype, _buf("h", h, _kind(h_dtype), n, dev), h_dtype,
+        _buf("gain", gain, _F, dim, dev), _buf("rstd", rstd, _F, n_rows, dev), n_rows, dim, _buf("grad_h", grad_h, kind, n, dev),
+        _buf("grad_x", grad_x, kind, n, dev), grad_x_dtype, _buf("grad_gain", grad_gain, _F, dim, dev), accumulate,
+        _buf("workspace", workspace, _U8, workspace_bytes, dev), workspace_bytes, _ptr(stream)))
+
+
+def _code_buf(name: str, x, n: int, device: int) -> int | None:
+    """A buffer of e4m3 codes: torch's type of that name, or plain bytes."""
+    return _buf(name, x, _U8 if getattr(x, "dtype", None) is _U8 else _torch.float8_e4m3fn, n, device)
+
+
+def adamw_tensor(param, grad, m, v, weight_decay: float, m_scales=None, v_scales=None, copy=None) -> AdamwTensor:
+    """A table entry from tensors on the current device: contiguous, as many elements each as param (scales: one for 128).
+    Moments of torch.float8_e4m3fn or torch.uint8 are codes.  The entry keeps addresses only: the tensors have to live as
+    long as the table is used."""
+    dev, n = _device(), param.numel()
+    codes = {t: c for c, t in _TYPES.items()}
+    for name, x in (("param", param), ("grad", grad)):
+        if x.dtype not in codes:
+            raise RolloutError(EINVAL, f"{name} must be torch.float32 or torch.bfloat16, not {x.dtype}")
+        if not x.is_contiguous():
+            raise RolloutError(EINVAL, f"{name} is not contiguous")
+    eight = m.dtype in (_U8, _torch.float8_e4m3fn)
+    state = (lambda name, x: _code_buf(name, x, n, dev)) if eight else (lambda name, x: _buf(name, x, _F, n, dev))
+    blocks = (n + 127) // 128
+    for name, x in (("grad", grad), ("m", m), ("v", v), ("copy", copy)):
+        if x is not None and x.numel() != n:
+            raise RolloutError(EINVAL, f"{name} holds {x.numel()} elements, not {n}")
+    return AdamwTensor(
+        _buf("param", param, param.dtype, n, dev), _buf("grad", grad, grad.dtype, n, dev), state("m", m), state("v", v),
+        _buf("m_scales", m_scales, _F, blocks, dev), _buf("v_scales", v_scales, _F, blocks, dev),
+        _buf("copy", copy, _torch.bfloat16, n, dev), n, codes[param.dtype], codes[grad.dtype],
+        DTYPE_E4M3 if eight else DTYPE_FP32, weight_decay)
+
+
+def rollout_adamw_table(tensors):
+    """(the table as a uint8 tensor in host memory, its number of chunks) of a list of AdamwTensor.  Copy the table to the
+    device and pass that to rollout_adamw."""
+    n, need, chunks = len(tensors), ctypes.c_uint64(0), ctypes.c_int64(0)
+    _check(lib.rollout_adamw_table_bytes(n, ctypes.byref(need)))
+    table = _torch.zeros(need.value, dtype=_U8)
+    _check(lib.rollout_adamw_table((AdamwTensor * n)(*tensors), n, table.data_ptr(), need.value, ctypes.byref(chunks)))
+    return table, chunks.value
+
+
+def rollout_adamw(table, n_tensors: int, n_chunks: int, lr: float, beta1: float, beta2: float, eps: float, step: int, seed: int = 0,
+                  grad_scale=None, lr_now=None, step_now=None, stream=None):
+    """lr_now fp32 [1] and step_now int64 [1], on the device, replace lr and step."""
+    if (n_tensors | n_chunks | step | seed) >> 31:
+        _sizes((n_tensors,), (n_chunks, step), seed)
+    dev = _device()
+    need = ctypes.c_uint64(0)
+    _check(lib.rollout_adamw_table_bytes(n_tensors, ctypes.byref(need)))
+    _check(lib.rollout_adamw(
+        _buf("table", table, _U8, need.value, dev), n_tensors, n_chunks, lr, beta1, beta2, eps, step, seed,
+        _buf("grad_scale", grad_scale, _F, 1, dev), _buf("lr_now", lr_now, _F, 1, dev),
+        _buf("step_now", step_now, _torch.int64, 1, dev), _ptr(stream)))
 
 
 def rollout_sync(ctx):

@@ -1,0 +1,303 @@
+// Root-mean-square norm of the residual stream, with the addition that comes before it, and its gradient.
+//
+//   h = x + delta (rounded to x's type),  r = 1 / sqrt(mean h^2 + eps),  y = h r gain
+//   dx_i = r (t_i - xhat_i mean_k(t_k xhat_k)) + inner_i,  t = dy gain, xhat = h r;   dgain_i = sum over rows of dy_i xhat_i
+//
+// A row is read once and stays in registers, 8 neighbours of it per thread and step: of one wave up to 2,048 values, of four
+// up to 8,192, of sixteen up to 32,768.  An output in 8 bits (e4m3) takes a second reduction, the largest |y|, and has the
+// smallest power of two as scale that brings it to at most 448: a power of two takes nothing from the 4 bits of a value.
+#include "update.h"
+
+namespace rollout {
+namespace {
+
+constexpr int kSteps = 4;  // of 8 values that a thread holds
+
+struct None {};
+
+template <typename T>
+__device__ __forceinline__ void read8(const T* p, int n, float (&v)[8]) {
+  if (n >= 8) {
+    if constexpr (sizeof(T) == 2) {
+      unpack16(load16(p), v);
+    } else {
+      float a[4], b[4];
+      unpack16(load16(p), a);
+      unpack16(load16(p + 4), b);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? ldf(p, i) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void write8(T* p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    if constexpr (sizeof(T) == 2) {
+      store16(p, pack16(v));
+    } else {
+      const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+      store16(p, pack16(a));
+      store16(p + 4, pack16(b));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) put(p + i, v[i]);
+  }
+}
+// e4m3, to nearest, ties to even; what is not a number, or infinite, becomes NaN
+__device__ __forceinline__ void write8(uint8_t* p, int n, const float (&v)[8]) {
+  uint32_t w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int t = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i], v[4 * i + 1], 0, false);
+    w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * i + 2], v[4 * i + 3], t, true);
+  }
+  typedef uint32_t Raw __attribute__((ext_vector_type(2), aligned(1), may_alias));
+  if (n >= 8) {
+    *reinterpret_cast<Raw*>(p) = Raw{w[0], w[1]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+// Sum (or maximum) over the W threads of a row, the same in all of them; red: 2 W / 64 values, used in turn.
+template <int W, typename F>
+__device__ __forceinline__ float row_reduce(float v, float* red, F f) {
+  if constexpr (W > 64) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int i = 1; i < W / 64; ++i) v = f(v, red[i]);
+  }
+  return v;
+}
+
+// W threads a row (64: four rows in a workgroup).  D: type of what is added, or None.
+template <typename X, typename D, typename Y, int W>
+__global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
+  constexpr bool kAdds = !std::is_same<D, None>::value;
+  __shared__ float red[2][W / 64];
+  const int t = threadIdx.x % W;
+  const int64_t row = (int64_t)blockIdx.x * (W < 256 ? 256 / W : 1) + threadIdx.x / W;
+  if (row >= A.rows) return;  // (a whole wave)
+  const X* x = (const X*)A.x + row * A.dim;
+  float h[kSteps][8];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = 8 * (t + s * W);
+    if (i < A.dim) read8(x + i, A.dim - i, h[s]);
+  }
+  if constexpr (kAdds) {
+    const D* d = (const D*)A.delta + row * A.dim;
+    X* to = (X*)A.h + row * A.dim;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int i = 8 * (t + s * W);
+      if (i >= A.dim) continue;
+      float v[8];
+      read8(d + i, A.dim - i, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        h[s][e] += v[e];
+        if constexpr (sizeof(X) == 2) h[s][e] = bf16_to_f32(round_bf16(h[s][e]));  // the norm is of what is stored
+      }
+      write8(to + i, A.dim - i, h[s]);
+    }
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s)
+    if (8 * (t + s * W) < A.dim)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(h[s][e], h[s][e], sum);
+  sum = row_reduce<W>(wave_sum_f32(sum), red[0], [](float a, float b) { return a + b; });
+  const float r = 1.f / sqrtf(sum / (float)A.dim + A.eps);
+  if (A.rstd && t == 0) A.rstd[row] = r;
+  float most = 0.f;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = 8 * (t + s * W);
+    if (i >= A.dim) continue;
+    float g[8];
+    if (A.gain) read8(A.gain + i, A.dim - i, g);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      h[s][e] *= r;
+      if (A.gain) h[s][e] *= g[e];
+      if constexpr (sizeof(Y) == 1) most = fmaxf(most, fabsf(h[s][e]));
+    }
+  }
+  float by = 1.f;
+  if constexpr (sizeof(Y) == 1) {
+    most = row_reduce<W>(wave_max_f32(most), red[1], [](float a, float b) { return fmaxf(a, b); });
+    const float scale = e4m3_scale(most);
+    by = 1.f / scale;  // exact
+    if (t == 0) A.scales[row] = scale;
+  }
+  Y* y = (Y*)A.y + row * A.dim;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = 8 * (t + s * W);
+    if (i >= A.dim) continue;
+    if constexpr (sizeof(Y) == 1)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[s][e] *= by;
+    write8(y + i, A.dim - i, h[s]);
+  }
+}
+
+// Rows `worker`, `worker` + workers, ... of the gradient; the worker's sum of dy xhat stays in registers and ends in
+// partial[worker].
+template <typename X, typename G, typename O, int W>
+__global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm_backward(NormGradArgs A, int workers, float* __restrict__ partial) {
+  __shared__ float red[2][W / 64];
+  const int t = threadIdx.x % W;
+  const int worker = (int)blockIdx.x * (W < 256 ? 256 / W : 1) + threadIdx.x / W;
+  if (worker >= workers) return;  // (a whole wave)
+  float sum[kSteps][8] = {};
+  float* turn = red[0];
+  float* other = red[1];
+  for (int64_t row = worker; row < A.rows; row += workers) {
+    const X* hp = (const X*)A.h + row * A.dim;
+    const G* dyp = (const G*)A.dy + row * A.dim;
+    const float r = A.rstd[row];
+    float xhat[kSteps][8], g[kSteps][8];
+    float dot = 0.f;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int i = 8 * (t + s * W);
+      if (i >= A.dim) continue;
+      read8(hp + i, A.dim - i, xhat[s]);
+      read8(dyp + i, A.dim - i, g[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int i = 8 * (t + s * W);
+      if (i >= A.dim) continue;
+      float gain[8];
+      if (A.gain) read8(A.gain + i, A.dim - i, gain);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        xhat[s][e] *= r;
+        sum[s][e] = fmaf(g[s][e], xhat[s][e], sum[s][e]);
+        if (A.gain) g[s][e] *= gain[e];
+        dot = fmaf(g[s][e], xhat[s][e], dot);
+      }
+    }
+    dot = row_reduce<W>(wave_sum_f32(dot), turn, [](float a, float b) { return a + b; }) / (float)A.dim;
+    float* swap = turn;
+    turn = other;
+    other = swap;
+    O* to = (O*)A.dx + row * A.dim;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int i = 8 * (t + s * W);
+      if (i >= A.dim) continue;
+      float v[8] = {};
+      if (A.inner) read8((const O*)A.inner + row * A.dim + i, A.dim - i, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = fmaf(r, g[s][e] - xhat[s][e] * dot, v[e]);
+      write8(to + i, A.dim - i, v);
+    }
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = 8 * (t + s * W);
+    if (i < A.dim) write8(partial + (int64_t)worker * A.dim + i, A.dim - i, sum[s]);
+  }
+}
+
+// Sums of the workers' columns in a fixed order: 32 columns a workgroup, every 8th worker a thread row.
+__global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ partial, int workers, int dim, int accumulate,
+                                                   float* __restrict__ dgain) {
+  __shared__ float red[8][32];
+  const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c;
+  float sum = 0.f;
+  if (col < dim)
+#pragma unroll 8
+    for (int w = k; w < workers; w += 8) sum += partial[(int64_t)w * dim + col];
+  red[k][c] = sum;
+  __syncthreads();
+  if (k || col >= dim) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) sum += red[i][c];
+  dgain[col] = accumulate ? dgain[col] + sum : sum;
+}
+
+}  // namespace
+
+int norm_threads(int dim) { return dim <= 64 * 8 * kSteps ? 64 : dim <= 256 * 8 * kSteps ? 256 : 1024; }
+
+namespace {
+
+template <typename X, typename D, typename Y>
+hipError_t forward(hipStream_t s, const NormArgs& a) {
+  const int w = norm_threads(a.dim);
+  if (w == 64)
+    k_rms_norm<X, D, Y, 64><<<(a.rows + 3) / 4, 256, 0, s>>>(a);
+  else if (w == 256)
+    k_rms_norm<X, D, Y, 256><<<a.rows, 256, 0, s>>>(a);
+  else
+    k_rms_norm<X, D, Y, 1024><<<a.rows, 1024, 0, s>>>(a);
+  return hipGetLastError();
+}
+template <typename X, typename D>
+hipError_t forward_to(hipStream_t s, int y_dtype, const NormArgs& a) {
+  return y_dtype == ROLLOUT_DTYPE_FP32   ? forward<X, D, float>(s, a)
+         : y_dtype == ROLLOUT_DTYPE_BF16 ? forward<X, D, uint16_t>(s, a)
+                                         : forward<X, D, uint8_t>(s, a);
+}
+template <typename X>
+hipError_t forward_from(hipStream_t s, int delta_dtype, int y_dtype, const NormArgs& a) {
+  return !a.delta                            ? forward_to<X, None>(s, y_dtype, a)
+         : delta_dtype == ROLLOUT_DTYPE_FP32 ? forward_to<X, float>(s, y_dtype, a)
+                                             : forward_to<X, uint16_t>(s, y_dtype, a);
+}
+
+int workers_of(int rows, int dim) { return std::min(rows, norm_threads(dim) == 64 ? 4096 : 1024); }
+
+template <typename X, typename G, typename O>
+hipError_t backward(hipStream_t s, const NormGradArgs& a, float* partial) {
+  const int w = norm_threads(a.dim), n = workers_of(a.rows, a.dim);
+  float* p = a.dgain ? partial : nullptr;
+  if (w == 64)
+    k_rms_norm_backward<X, G, O, 64><<<(n + 3) / 4, 256, 0, s>>>(a, n, p);
+  else if (w == 256)
+    k_rms_norm_backward<X, G, O, 256><<<n, 256, 0, s>>>(a, n, p);
+  else
+    k_rms_norm_backward<X, G, O, 1024><<<n, 1024, 0, s>>>(a, n, p);
+  if (a.dgain) k_norm_join<<<(a.dim + 31) / 32, 256, 0, s>>>(partial, n, a.dim, a.accumulate, a.dgain);
+  return hipGetLastError();
+}
+template <typename X, typename G>
+hipError_t backward_to(hipStream_t s, int dx_dtype, const NormGradArgs& a, float* p) {
+  return dx_dtype == ROLLOUT_DTYPE_FP32 ? backward<X, G, float>(s, a, p) : backward<X, G, uint16_t>(s, a, p);
+}
+template <typename X>
+hipError_t backward_from(hipStream_t s, int dy_dtype, int dx_dtype, const NormGradArgs& a, float* p) {
+  return dy_dtype == ROLLOUT_DTYPE_FP32 ? backward_to<X, float>(s, dx_dtype, a, p) : backward_to<X, uint16_t>(s, dx_dtype, a, p);
+}
+
+}  // namespace
+
+hipError_t launch_rms_norm(hipStream_t s, int x_dtype, int delta_dtype, int y_dtype, const NormArgs& a) {
+  return x_dtype == ROLLOUT_DTYPE_FP32 ? forward_from<float>(s, delta_dtype, y_dtype, a)
+                                       : forward_from<uint16_t>(s, delta_dtype, y_dtype, a);
+}
+
+size_t rms_norm_backward_workspace(int rows, int dim) { return (size_t)workers_of(rows, dim) * dim * 4; }
+
+hipError_t launch_rms_norm_backward(hipStream_t s, int h_dtype, int dy_dtype, int dx_dtype, const NormGradArgs& a, void* ws) {
+  return h_dtype == ROLLOUT_DTYPE_FP32 ? backward_from<float>(s, dy_dtype, dx_dtype, a, (float*)ws)
+                                       : backward_from<uint16_t>(s, dy_dtype, dx_dtype, a, (float*)ws);
+}
+
+}  // namespace rollout

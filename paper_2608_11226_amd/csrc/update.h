@@ -6,6 +6,7 @@
 #include "internal.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace rollout {
 
@@ -78,6 +79,81 @@ inline bool embedding_backward_fits(int n, int dim) { return (int64_t)n * (((int
 size_t embedding_backward_workspace(int n, int vocab, int dim);
 hipError_t launch_embedding_backward(hipStream_t s, int grad_dtype, int table_dtype, const EmbeddingGradArgs& a, void* ws);
 
+// Strides are in elements.  k_starts and k_lens are never NULL: the queries' where the sequences' keys are their own.
+struct AttentionArgs {
+  int heads, kv_heads, head_dim, n_seqs, n_q, n_k;
+  bool causal;
+  float scale;
+  const void *q, *k, *v;
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t *q_starts, *q_lens, *k_starts, *k_lens;  // lens may be NULL: whole
+  void* out;
+  int64_t out_stride;
+  float* lse;  // [heads][n_q]
+};
+size_t packed_attention_workspace(const AttentionArgs& a);
+hipError_t launch_packed_attention(hipStream_t s, int dtype, const AttentionArgs& a, void* ws);
+
+struct AttentionGradArgs : AttentionArgs {
+  const void* dout;
+  int64_t dout_stride;
+  void *dq, *dk, *dv;
+  int64_t dq_stride, dk_stride, dv_stride;
+};
+size_t packed_attention_backward_workspace(const AttentionArgs& a);
+hipError_t launch_packed_attention_backward(hipStream_t s, int dtype, const AttentionGradArgs& a, void* ws);
+
+constexpr int kMaxNormDim = 32768;
+int norm_threads(int dim);  // of a row
+inline bool norm_fits(int rows, int dim) { return (int64_t)rows * norm_threads(dim) < (int64_t)1 << 32; }
+struct NormArgs {
+  const void *x, *delta;  // delta may be NULL
+  const float* gain;      // may be NULL
+  int rows, dim;
+  float eps;
+  void *h, *y;
+  float *scales, *rstd;
+};
+hipError_t launch_rms_norm(hipStream_t s, int x_dtype, int delta_dtype, int y_dtype, const NormArgs& a);
+
+struct NormGradArgs {
+  const void *dy, *h;
+  const float *gain, *rstd;
+  int rows, dim;
+  const void* inner;  // of dx's type; may be NULL, or dx
+  void* dx;
+  float* dgain;  // may be NULL
+  int accumulate;
+};
+size_t rms_norm_backward_workspace(int rows, int dim);
+hipError_t launch_rms_norm_backward(hipStream_t s, int h_dtype, int dy_dtype, int dx_dtype, const NormGradArgs& a, void* ws);
+
+// A tensor in the table that the kernel reads; its chunks are first, first + 1, ...
+struct AdamwEntry {
+  void* param;
+  const void* grad;
+  void *m, *v;
+  float *m_scales, *v_scales;
+  void* copy;
+  int64_t n, first, chunk;
+  float decay;
+  int32_t kind;  // 1: bf16 weights, 2: bf16 gradients, 4: states in 8 bits
+};
+constexpr int kMaxAdamwTensors = 1 << 20;
+constexpr int64_t kMaxAdamwElements = (int64_t)1 << 36;
+// elements that a workgroup takes of a tensor, by the number of all
+int64_t adamw_chunk(int64_t all);
+struct AdamwArgs {
+  float b1, c1, b2, c2, eps, lr;
+  double log_b1, log_b2, unbias1;  // 1 / (1 - b1^step)
+  float unbias2;                   // 1 / sqrt(1 - b2^step)
+  int64_t step;
+  uint64_t seed;
+  const float *grad_scale, *d_lr;
+  const int64_t* d_step;
+};
+hipError_t launch_adamw(hipStream_t s, const void* table, int tensors, int64_t chunks, const AdamwArgs& a);
+
 }  // namespace rollout
 
 #ifdef __HIPCC__
@@ -147,6 +223,13 @@ __device__ __forceinline__ u32x4 pack16(const float (&v)[8]) {
 }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t* p, float v) { *p = round_bf16(v); }
+
+// Smallest power of two that brings `most` (>= 0) to at most 448, the largest e4m3 value; 2^-126 at least.  448 is 1.75 2^8.
+__device__ __forceinline__ float e4m3_scale(float most) {
+  const uint32_t u = __float_as_uint(most);
+  const int e = min((int)(u >> 23), 254) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return __uint_as_float((uint32_t)max(e, 1) << 23);
+}
 
 // Reductions of one value per lane by lane moves, without LDS, the result the same in every lane: shifts of 1, 2, 4 and 8
 // lanes within each row of 16, then row 0's result into row 1 and row 2's into row 3, then the first two rows' into the

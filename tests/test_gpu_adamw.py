@@ -1,0 +1,243 @@
+"""AdamW over many tensors against the definition in float64: sizes, types, rounding by the counter hash, replays."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2608_11226_amd as R
+from layer_cases import DEV, U, wide
+from oracle import layers as L
+
+pytestmark = pytest.mark.gpu
+
+LR, B1, B2, EPS = 3e-3, 0.9, 0.97, 1e-8
+E4M3 = torch.float8_e4m3fn
+SIZES = [1, 7, 8, 127, 128, 129, 2047, 2048, 2049, 5000, 0, 70001]
+
+
+class Tensor:
+    def __init__(self, g, n, param="fp32", grad="fp32", state="fp32", copy=False, decay=0.1, offset=0, fresh=False):
+        rand = lambda by: torch.randn(n, generator=g, device=DEV) * by  # noqa: E731
+        at = lambda x: torch.cat([torch.zeros(offset, device=DEV, dtype=x.dtype), x])[offset:]  # noqa: E731
+        T = {"fp32": torch.float32, "bf16": torch.bfloat16}
+        self.n, self.param, self.state, self.decay = n, param, state, decay
+        size = torch.exp(2.0 * rand(1.0)) * 1e-3
+        self.p, self.g = at((0.05 * rand(1.0)).to(T[param])), at((rand(1.0) * size).to(T[grad]))
+        m, v = (rand(0.4) * size, (0.3 + torch.rand(n, generator=g, device=DEV)) * size ** 2) if not fresh else (rand(0.0), rand(0.0))
+        self.ms = self.vs = None
+        if state == "e4m3":
+            self.m, self.ms = self.encode(m)
+            self.v, self.vs = self.encode(v.sqrt())
+            self.m, self.v = at(self.m.view(torch.uint8)).view(E4M3), at(self.v.view(torch.uint8)).view(E4M3)
+        else:
+            self.m, self.v = at(m), at(v)
+        self.copy = at(torch.zeros(n, dtype=torch.bfloat16, device=DEV)) if copy else None
+
+    @staticmethod
+    def encode(x):
+        n = x.numel()
+        y = torch.cat([x, torch.zeros(-n % 128, device=DEV)]).view(-1, 128)
+        s = torch.tensor(L.power_scale(wide(y.abs().amax(1))), dtype=torch.float32, device=DEV) if n else torch.zeros(0, device=DEV)
+        return (y / s[:, None]).to(E4M3).view(-1)[:n].clone(), s
+
+    def entry(self):
+        return R.adamw_tensor(self.p, self.g, self.m, self.v, self.decay, self.ms, self.vs, self.copy)
+
+    def all(self):
+        return [x for x in (self.p, self.m, self.v, self.ms, self.vs, self.copy) if x is not None]
+
+    def moments(self):
+        m, v = wide(self.m), wide(self.v)
+        if self.state == "e4m3":
+            b = np.arange(self.n) // 128
+            m, v = m * wide(self.ms)[b], (v * wide(self.vs)[b]) ** 2
+        return m, v
+
+
+def table_of(tensors):
+    table, chunks = R.rollout_adamw_table([t.entry() for t in tensors])
+    return table.to(DEV), len(tensors), chunks
+
+
+def check_step(tensors, step, seed, before, grad_scale=1.0, lr=LR):
+    for i, (t, (p, m, v)) in enumerate(zip(tensors, before)):
+        if not t.n:
+            continue
+        g = wide(t.g) * grad_scale
+        # moments as fp32 holds them before the step (a product with a power of two, and its square)
+        wp, wm, wv = L.adamw(p, g, m, v, lr, B1, B2, EPS, step, t.decay)
+        # 4 roundings: factors, products, sum, the scaled gradient (twice in its square)
+        em, ev = 5 * U * (np.abs(B1 * m) + np.abs((1 - B1) * g)), 7 * U * (B2 * v + (1 - B2) * g * g)
+        root = np.sqrt(wv / (1 - B2 ** step)) + EPS
+        eu = lr / (1 - B1 ** step) * (em / root + np.abs(wm) / root * (6 * U + ev / np.maximum(2 * wv, 1e-300) + 4 * U))
+        ep = 4 * U * np.abs(wp) + 3 * U * np.abs(p) + 1.1 * eu
+        rm, rv, rp = L.adamw_bits(seed, step, i, np.arange(t.n))
+        if t.param == "fp32":
+            assert (np.abs(wide(t.p) - wp) <= ep).all(), i
+            if t.copy is not None:
+                assert torch.equal(t.copy, t.p.to(torch.bfloat16))
+        else:
+            e = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(wp), 2.0 ** -126))) - 7)
+            at = np.abs(wp) / e + rp / 2.0 ** 16
+            settled = np.abs(at - np.round(at)) > ep / e * 2 + 2.0 ** -15
+            got = np.abs(wide(t.p)) / e
+            assert (got[settled] == np.floor(at)[settled]).all() and (np.abs(got - at) <= 1 + 2.0 ** -14 + ep / e).all(), i
+            assert settled.mean() > 0.99 or t.n < 1000
+        if t.state == "fp32":
+            assert (np.abs(wide(t.m) - wm) <= em).all() and (np.abs(wide(t.v) - wv) <= ev + 1e-45).all(), i
+            continue
+        nb = (t.n + 127) // 128
+        for got, scales, want, err, bits, root in ((t.m, t.ms, wm, em, rm, False), (t.v, t.vs, np.sqrt(wv), ev / np.maximum(2 * np.sqrt(wv), 1e-300), rv, True)):
+            a = np.abs(want)
+            pad = np.zeros(nb * 128)
+            pad[:t.n] = a
+            most = pad.reshape(nb, 128).max(1)
+            s = wide(scales)
+            assert ((s == L.power_scale(most * (1 - 2.0 ** -20))) | (s == L.power_scale(most * (1 + 2.0 ** -20)))).all(), i
+            s = s[np.arange(t.n) // 128]
+            e = L.spacing(a / s)
+            at = a / s / e + (16 * bits + 8) / 2.0 ** 20
+            slack = err / s / e * 2 + 2.0 ** -18
+            settled = np.abs(at - np.round(at)) > slack
+            code = np.abs(wide(got)) / e
+            expect = np.floor(at)
+            if root:
+                expect = np.where((expect == 0) & (a > 0), 2.0 ** -9 / e, expect)
+                assert (wide(got)[a > 0] > 0).all()
+            assert (code[settled] == expect[settled]).all(), i
+            assert (np.abs(code - at)[~settled] <= 1 + 2 * slack[~settled]).all(), i
+            assert settled.mean() > 0.99 or t.n < 1000
+            assert ((wide(got) == 0) | (np.sign(wide(got)) == np.sign(want))).all()
+
+
+def step_of(handle, step, seed, stream=None, **kw):
+    R.rollout_adamw(*handle, LR, B1, B2, EPS, step, seed, stream=stream or torch.cuda.current_stream().cuda_stream, **kw)
+
+
+@pytest.mark.parametrize("param,grad,state,copy", [
+    ("fp32", "fp32", "fp32", False), ("fp32", "bf16", "fp32", True), ("bf16", "bf16", "fp32", False), ("bf16", "fp32", "fp32", False),
+    ("fp32", "fp32", "e4m3", True), ("fp32", "bf16", "e4m3", False), ("bf16", "bf16", "e4m3", False), ("bf16", "fp32", "e4m3", False)])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_adamw(param, grad, state, copy, offset):
+    g = torch.Generator(device=DEV).manual_seed(offset)
+    tensors = [Tensor(g, n, param, grad, state, copy, 0.1 * (i % 2), offset) for i, n in enumerate(SIZES)]
+    handle = table_of(tensors)
+    for step in (1, 2, 9):
+        before = [(wide(t.p), *t.moments()) for t in tensors]
+        step_of(handle, step, 1234567890123, grad_scale=torch.full((1,), 0.5, device=DEV) if step == 2 else None)
+        torch.cuda.synchronize()
+        check_step(tensors, step, 1234567890123, before, 0.5 if step == 2 else 1.0)
+
+
+def test_kinds_in_one_table_and_many_tensors():
+    g = torch.Generator(device=DEV).manual_seed(3)
+    kinds = [("fp32", "fp32", "fp32", False), ("bf16", "bf16", "e4m3", False), ("fp32", "bf16", "e4m3", True), ("bf16", "fp32", "fp32", False)]
+    tensors = [Tensor(g, (37 * i) % 401 if i % 50 else 9000, *kinds[i % 4], decay=0.0) for i in range(700)]
+    before = [(wide(t.p), *t.moments()) for t in tensors]
+    step_of(table_of(tensors), 3, 5)
+    torch.cuda.synchronize()
+    check_step(tensors, 3, 5, before)
+
+
+def test_large_table_takes_larger_chunks():
+    g = torch.Generator(device=DEV).manual_seed(4)
+    tensors = [Tensor(g, n, "fp32", "bf16", "e4m3", True) for n in (3000001, 128, 2000003)]
+    handle = table_of(tensors)
+    assert handle[2] < 1000  # larger ones than the 2,048 elements of small tables
+    before = [(wide(t.p), *t.moments()) for t in tensors]
+    step_of(handle, 2, 9)
+    torch.cuda.synchronize()
+    check_step(tensors, 2, 9, before)
+
+
+def test_from_fresh_states():
+    g = torch.Generator(device=DEV).manual_seed(5)
+    for state in ("fp32", "e4m3"):
+        t = Tensor(g, 1000, state=state, fresh=True)
+        t.g[100:300] = 0.0  # a whole block without gradients among them
+        before = [(wide(t.p), *t.moments())]
+        step_of(table_of([t]), 1, 0)
+        torch.cuda.synchronize()
+        check_step([t], 1, 0, before)
+        assert (t.m[100:300].float() == 0).all() and (t.v[100:300].float() == 0).all()
+
+
+def test_expectation_of_rounded_states():
+    """Over many seeds an 8-bit moment is on average what fp32 would hold."""
+    g = torch.Generator(device=DEV).manual_seed(6)
+    t = Tensor(g, 128, state="e4m3")
+    first = [x.clone() for x in t.all()]
+    _, m, v = L.adamw(wide(t.p), wide(t.g), *t.moments(), LR, B1, B2, EPS, 4, 0.1)
+    handle, sums, n = table_of([t]), [0.0, 0.0], 4000
+    for seed in range(n):
+        for x, y in zip(t.all(), first):
+            x.copy_(y)
+        step_of(handle, 4, seed)
+        sums[0] = sums[0] + t.m.double() * t.ms.double()
+        sums[1] = sums[1] + t.v.double() * t.vs.double()
+    for s, want, scale in zip(sums, (m, np.sqrt(v)), (t.ms, t.vs)):
+        e = L.spacing(np.abs(want) / wide(scale)) * wide(scale)
+        # a draw is off by at most one spacing with variance of at most a quarter of its square: six deviations of the mean
+        assert (np.abs(wide(s) / n - want) <= 6 * 0.5 * e / np.sqrt(n) + 2.0 ** -16 * e).all()
+
+
+def test_gradients_that_are_not_finite():
+    g = torch.Generator(device=DEV).manual_seed(7)
+    for state, param in (("fp32", "fp32"), ("e4m3", "bf16")):
+        t = Tensor(g, 500, param, state=state)
+        handle, first = table_of([t]), [x.clone() for x in t.all()]
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            step_of(handle, 2, 0, grad_scale=torch.full((1,), bad, device=DEV))
+            assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(t.all(), first))
+        t.g[3], t.g[200] = float("nan"), float("inf")
+        step_of(handle, 2, 0)
+        # they stay where they are
+        bad = torch.zeros(500, dtype=torch.bool, device=DEV)
+        bad[3] = bad[200] = True
+        assert t.p[bad].isnan().all() and t.p[~bad].isfinite().all()
+        m = t.m.float()
+        assert m[3].isnan() and not m[200].isfinite() and m[~bad].isfinite().all() and t.v.float()[~bad].isfinite().all()
+
+
+def test_a_step_that_changes_nothing():
+    g = torch.Generator(device=DEV).manual_seed(8)
+    t = Tensor(g, 300, decay=0.0)
+    p = t.p.clone()
+    R.rollout_adamw(*table_of([t]), 0.0, B1, B2, EPS, 1, 0, stream=torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(t.p, p)
+    handle = table_of([Tensor(g, 0)])
+    assert handle[2] == 0
+    step_of(handle, 1, 0)
+
+
+def test_rate_and_step_from_the_device_in_a_graph():
+    g = torch.Generator(device=DEV).manual_seed(9)
+    tensors = [Tensor(g, n, "fp32", "bf16", s, True) for n, s in ((5000, "e4m3"), (300, "fp32"))]
+    handle, first = table_of(tensors), None
+    lr, step = torch.full((1,), 1e-3, device=DEV), torch.ones(1, dtype=torch.int64, device=DEV)
+    scale = torch.ones(1, device=DEV)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            R.rollout_adamw(*handle, 0.5, B1, B2, EPS, 99, 42, scale, lr, step, s.cuda_stream)
+    for k in range(1, 5):
+        step.fill_(k)
+        lr.fill_(float(np.float32(LR / k)))
+        scale.fill_(1.0 / k)
+        torch.cuda.synchronize()
+        before = [(wide(t.p), *t.moments()) for t in tensors]
+        graph.replay()
+        torch.cuda.synchronize()
+        check_step(tensors, k, 42, before, float(np.float32(1.0 / k)), float(np.float32(LR / k)))
+
+
+def test_on_another_stream():
+    g = torch.Generator(device=DEV).manual_seed(10)
+    t = Tensor(g, 40000, state="e4m3")
+    before = [(wide(t.p), *t.moments())]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    step_of(table_of([t]), 5, 1, stream=s.cuda_stream)
+    s.synchronize()
+    check_step([t], 5, 1, before)
