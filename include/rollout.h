@@ -446,7 +446,7 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
  * dtype FP32 (fp32 products) or BF16 (probabilities and their gradients enter products as bf16; sums
  * and statistics are fp32).  Matrices and strides are multiples of 16 bytes, rows at most 2^25 bytes apart.
  * Errors: EINVAL (shape, NULL buffers, alignment, strides, overlap), EUNSUPPORTED (head_dim not 32, 64 or
- * 128, n_heads times tokens above 2^26, n_heads times sequences above 2^23, strides), ENOMEM
+ * 128, n_heads / n_kv_heads above 64, n_heads times tokens above 2^26, n_heads times sequences above 2^23, strides), ENOMEM
  * (workspace too small), EDEVICE.
  */
 typedef struct {

@@ -265,11 +265,14 @@ def rollout_length_rewards(lengths, n: int, target: int, rewards, total_tokens=N
 def _buf(name: str, x, kind, n: int, device: int, rows=None) -> int | None:
     """Device pointer of a buffer of n elements of a torch type.  rows: (rows, stride, width) of a matrix whose rows may
     be apart."""
-    if x is None or type(x) is int:
+    if type(x) is _torch.Tensor:
+        if x.dtype is kind and x.is_contiguous() and x.numel() >= n and x.get_device() == device:
+            return x.data_ptr()
+    elif x is None or type(x) is int:
         return x
-    if not hasattr(x, "is_contiguous"):
+    elif not hasattr(x, "is_contiguous"):
         return _ptr(x)
-    if x.dtype is kind and x.is_contiguous() and x.numel() >= n and x.get_device() == device:
+    elif x.dtype is kind and x.is_contiguous() and x.numel() >= n and x.get_device() == device:
         return x.data_ptr()
     if x.dtype is not kind:
         raise RolloutError(EINVAL, f"{name} must be {kind}, not {x.dtype}")
@@ -418,6 +421,10 @@ def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, voc
 
 def _matrix(name: str, x, kind, n: int, stride: int, width: int, device: int):
     """A matrix of n rows of width elements, stride apart."""
+    if type(x) is _torch.Tensor and x.dtype is kind and x.dim() == 2 and x.get_device() == device:
+        have, wide = x.shape
+        if have >= n and wide >= width and x.stride() == (stride, 1):
+            return x.data_ptr()
     return _buf(name, x, kind, (n - 1) * stride + width, device, (n, stride, width))
 
 

@@ -317,6 +317,12 @@ __device__ __forceinline__ void dma_lds16_at(const void* src, uint32_t offset, v
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(src), "{m0}"(lds) : "memory");
 }
 
+// The same with 4 bytes per lane.
+__device__ __forceinline__ void dma_lds4_at(const void* src, uint32_t offset, void* dst) {
+  const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)dst);
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(offset), "s"(src), "{m0}"(lds) : "memory");
+}
+
 // All but the wave's latest N transfers into LDS and all its LDS accesses are complete, then every wave has arrived.
 template <int N = 0>
 __device__ __forceinline__ void dma_wait_barrier() {

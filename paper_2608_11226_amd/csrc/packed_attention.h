@@ -79,18 +79,21 @@ struct Rows {
   static constexpr int kChunks = kBytes / 16;
   typedef typename Operand<T>::Frag Frag;
 
-  static __device__ __forceinline__ int swizzle(int row) {
+  static __host__ __device__ constexpr int swizzle(int row) {
     if constexpr (kChunks >= 16) return ((row & 7) << 1) | ((row >> 3) & 1);
-    if constexpr (kChunks == 8) return ((row & 6)) | ((row >> 3) & 1);
+    if constexpr (kChunks == 8) return (row & 6) | ((row >> 3) & 1);
     return (row >> 2) & 3;
   }
   // byte offset of chunk c of a row
   static __device__ __forceinline__ int at(int row, int c) { return row * kBytes + ((c ^ swizzle(row)) << 4); }
 
-  // N rows from global memory straight into LDS, by NW waves.  src: the first row,
-  // the same for the whole wave; stride in bytes; rows behind `last` (>= 0) are copies of it.
-  template <int N, int NW>
-  static __device__ __forceinline__ void load(char* lds, const char* src, uint32_t stride, int last, int wave, int lane) {
+  // loads of a wave for N rows by NW waves (some waves have none where there are fewer than waves)
+  static constexpr int loads(int N, int NW) { return N * kChunks / 64 >= NW ? N * kChunks / 64 / NW : 1; }
+
+  // Loads N rows from global memory straight into LDS, by NW waves.  issue(row, offset, place): what lane has to load of row
+  // `row`, 16 bytes at `offset` of it, and the bytes behind the tile's beginning where the wave's lands.
+  template <int N, int NW, typename F>
+  static __device__ __forceinline__ void load_with(int wave, int lane, F issue) {
     constexpr int kPer = 64 / kChunks;  // rows of an instruction
     constexpr int kInstr = N * kChunks / 64;
     static_assert(N * kChunks % 64 == 0 && kChunks <= 64, "whole loads");
@@ -99,30 +102,37 @@ struct Rows {
       if (kInstr % NW != 0 && i * NW + wave >= kInstr) break;
       const int first = (i * NW + wave) * kPer;
       const int row = first + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
-      dma_lds16_at(src, (uint32_t)min(row, last) * stride + (uint32_t)(c << 4), lds + first * kBytes);
+      issue(row, (uint32_t)(c << 4), first * kBytes);
     }
+  }
+  // src: the first row, the same for the whole wave; stride in bytes; rows behind `last` (>= 0) are copies of it.
+  template <int N, int NW>
+  static __device__ __forceinline__ void load(char* lds, const char* src, uint32_t stride, int last, int wave, int lane) {
+    load_with<N, NW>(wave, lane, [&](int row, uint32_t offset, int place) {
+      dma_lds16_at(src, (uint32_t)min(row, last) * stride + offset, lds + place);
+    });
   }
 };
 
 // Reading a tile as an operand: block (32 rows from row0) as it lies (contraction over the row's values), or transposed
-// (contraction over 16 of its rows).  The lane's part of the addresses is worked out once.
+// (contraction over 16 of its rows).  The swizzle makes an address the lane's own part with constants exclusive-ored into it:
+// one instruction for each of them and no register kept, where registers are what is short (`renew`, once a tile, hides the
+// part's origin from the compiler, which would otherwise keep them all).
 template <typename T, int HD>
 struct RowReader {
   typedef Rows<T, HD> R;
-  int base[HD / 16];
-  __device__ __forceinline__ explicit RowReader(int lane) {
-    const int row = row_perm(lane & 31), half = lane >> 5;
-#pragma unroll
-    for (int c = 0; c < HD / 16; ++c) base[c] = R::at(row, (2 * c + half) * ((int)sizeof(T) / 2));
-  }
+  int base;
+  __device__ __forceinline__ explicit RowReader(int lane) : base(R::at(row_perm(lane & 31), (lane >> 5) * ((int)sizeof(T) / 2))) {}
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(base)); }
   // rows row0 + row_perm(lane % 32), values 16 c + 8 (lane / 32) + 0 .. 7
   __device__ __forceinline__ typename R::Frag operator()(const char* tile, int row0, int c) const {
     typename R::Frag f;
     const char* p = tile + row0 * R::kBytes;
+    const int at = base ^ (c * 16 * (int)sizeof(T));
     if constexpr (sizeof(T) == 2) {
-      f = *reinterpret_cast<const bf16x8*>(p + base[c]);
+      f = *reinterpret_cast<const bf16x8*>(p + at);
     } else {
-      const float4 lo = *reinterpret_cast<const float4*>(p + base[c]), hi = *reinterpret_cast<const float4*>(p + (base[c] ^ 16));
+      const float4 lo = *reinterpret_cast<const float4*>(p + at), hi = *reinterpret_cast<const float4*>(p + (at ^ 16));
       f[0] = lo.x, f[1] = lo.y, f[2] = lo.z, f[3] = lo.w, f[4] = hi.x, f[5] = hi.y, f[6] = hi.z, f[7] = hi.w;
     }
     return f;
@@ -137,23 +147,20 @@ struct ColReader;
 template <int HD>
 struct ColReader<uint16_t, HD> {
   typedef Rows<uint16_t, HD> R;
-  int base[2][HD / 32];
+  static constexpr int kFour = (R::swizzle(4) ^ R::swizzle(0)) << 4;  // how the swizzle of rows 4 .. 7 differs from that of 0 .. 3
+  int base;
   __device__ __forceinline__ explicit ColReader(int lane) {
     const int j = lane & 15, g = lane >> 4;
     const int q = j & 3, part = ((q & 1) << 1) | (q >> 1);  // 4-value part of the 16, in the order 0, 2, 1, 3
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const int row = 8 * (g >> 1) + 4 * r + (j >> 2);
-#pragma unroll
-      for (int d = 0; d < HD / 32; ++d) base[r][d] = R::at(row, 4 * d + 2 * (g & 1) + (part >> 1)) + 8 * (part & 1);
-    }
+    base = R::at(8 * (g >> 1) + (j >> 2), 2 * (g & 1) + (part >> 1)) + 8 * (part & 1);
   }
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(base)); }
   // rows row0 + 8 (lane / 32) + 0 .. 7 (row0 a multiple of 16) of value 32 d + row_perm(lane % 32)
   __device__ __forceinline__ bf16x8 operator()(const char* tile, int row0, int d) const {
     typedef __attribute__((address_space(3))) s16x4* Lds;
     const char* p = tile + row0 * R::kBytes;
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + base[0][d]));
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + base[1][d]));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + (base ^ (d << 6))));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 4 * R::kBytes + (base ^ (d << 6) ^ kFour)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   }
 };
@@ -163,6 +170,7 @@ struct ColReader<float, HD> {
   typedef Rows<float, HD> R;
   int col, half;
   __device__ __forceinline__ explicit ColReader(int lane) : col(row_perm(lane & 31)), half(lane >> 5) {}
+  __device__ __forceinline__ void renew() {}
   __device__ __forceinline__ f32x8 operator()(const char* tile, int row0, int d) const {
     f32x8 f;
     const int c = 32 * d + col;
@@ -191,20 +199,21 @@ __device__ __forceinline__ Sequence sequence_at(const int32_t* starts, const int
   return {a, lens ? max(0, min(lens[s], b - a)) : b - a};
 }
 
-// The tiles of B rows of all sequences are numbered start_s / B + s + (tile in s): no two have the same number, the numbers
-// ascend with s, and there are at most n / B + n_seqs of them, so no list of tiles has to be made first.  Numbers that no
-// tile has are skipped.
-__host__ __device__ __forceinline__ int tile_slots(int n, int n_seqs, int B) { return n / B + n_seqs; }
+// The query heads that share a key's are taken together: `each` of them make as many rows of a token, and a sequence of len
+// tokens is a run of len * each rows (token by token).  The tiles of B rows of all sequences are numbered
+// start_s * each / B + s + (tile in s): no two have the same number, the numbers ascend with s, and there are at most
+// n * each / B + n_seqs of them, so no list of tiles has to be made first.  Numbers that no tile has are skipped.
+__host__ __device__ __forceinline__ int tile_slots(int n, int each, int n_seqs, int B) { return n * each / B + n_seqs; }
 
 // The sequence of a tile number and the tile's first row in it; false: no such tile.  64 lanes probe at a time; whatever the
 // starts hold, only entries 0 .. n_seqs are read.
 template <int B>
-__device__ __forceinline__ bool find_tile(const int32_t* starts, const int32_t* lens, int n_seqs, int n, int slot, int lane,
+__device__ __forceinline__ bool find_tile(const int32_t* starts, const int32_t* lens, int n_seqs, int n, int each, int slot, int lane,
                                           int* seq, Sequence* sq, int* row) {
   int lo = 0, hi = n_seqs;
   do {
     const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
-    const bool before = s < hi && max(0, min(starts[s], n)) / B + s <= slot;
+    const bool before = s < hi && max(0, min(starts[s], n)) * each / B + s <= slot;
     const int k = __popcll(__ballot(before)) - 1;
     if (k < 0) return false;
     lo += k * step;
@@ -212,8 +221,50 @@ __device__ __forceinline__ bool find_tile(const int32_t* starts, const int32_t* 
   } while (hi - lo > 1);
   *seq = __builtin_amdgcn_readfirstlane(lo);
   *sq = sequence_at(starts, lens, *seq, n);
-  *row = (slot - (sq->start / B + *seq)) * B;
-  return *row >= 0 && *row < sq->len;
+  *row = (slot - (sq->start * each / B + *seq)) * B;
+  return *row >= 0 && *row < sq->len * each;
+}
+
+// Tiles 0 .. n - 1 pass through S buffers in LDS, S - 1 of them on the way at a time.  load(buffer, tile) issues a tile's loads,
+// LOADS of each wave at least as its last ones; step(buffer, tile) works on one.  The buffer is a compile-time number, so that
+// it is part of the LDS instructions' offsets.
+template <int S, int LOADS, int B = 0, typename Load, typename Step>
+__device__ __forceinline__ bool one_tile(int it, int n, Load& load, Step& step) {
+  if (it >= n) return false;
+  // the tile is there for every wave, and nobody reads the buffer before it any more
+  if (S > 2 && it + 1 < n)
+    dma_wait_barrier<(S - 2) * LOADS>();
+  else
+    dma_wait_barrier<0>();
+  if (it + S - 1 < n) load(std::integral_constant<int, (B + S - 1) % S>(), it + S - 1);
+  step(std::integral_constant<int, B>(), it);
+  if constexpr (B + 1 < S) return one_tile<S, LOADS, B + 1>(it + 1, n, load, step);
+  return true;
+}
+template <int S, int LOADS, typename Load, typename Step>
+__device__ __forceinline__ void through_tiles(int n, Load load, Step step) {
+  static_assert(S == 2 || S == 3, "the wait before the last tile but one is for all");
+  if (n > 0) load(std::integral_constant<int, 0>(), 0);
+  if (S > 2 && n > 1) load(std::integral_constant<int, 1>(), 1);
+  for (int it = 0; one_tile<S, LOADS>(it, n, load, step); it += S) {
+  }
+}
+
+// N groups of W operands from LDS, each group's loads on the way while the products of the one before it run.  load(g, f) reads
+// group g, use(g, f) multiplies by it; the first group may have been read before (read_ahead).  Left to itself the compiler
+// reads every operand into the same registers just before its product, whose time then is that of the read.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }  // (of products and memory; other VALU and SALU may move)
+template <int N, int W, int g, typename Frag, typename Load, typename Use>
+__device__ __forceinline__ void group(Frag (&f)[2][W], Load& load, Use& use) {
+  if constexpr (g + 1 < N) load(std::integral_constant<int, g + 1>(), f[(g + 1) & 1]);
+  keep_order();
+  use(std::integral_constant<int, g>(), f[g & 1]);
+  keep_order();
+  if constexpr (g + 1 < N) group<N, W, g + 1>(f, load, use);
+}
+template <int N, int W, typename Frag, typename Load, typename Use>
+__device__ __forceinline__ void groups(Frag (&f)[2][W], Load load, Use use) {
+  group<N, W, 0>(f, load, use);
 }
 
 // Workgroups are dealt out to the eight dies in turn; numbered so that a die's are neighbours.  -1: none.

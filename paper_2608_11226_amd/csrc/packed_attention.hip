@@ -2,10 +2,12 @@
 //
 //   s_ij = scale q_i k_j  (keys j <= i + len_k - len_q if causal);  lse_i = log sum_j e^s_ij;  o_i = sum_j e^(s_ij - lse_i) v_j
 //
-// A workgroup takes 128 queries of a head, a wave 32 of them, and walks over tiles of 64 keys once, with the running maximum
-// and sum of each query in 32 bits.  Scores are formed transposed (keys as rows, queries as columns), so that a lane holds one
-// query's: maximum and sum are the lane's own but for one exchange with the lane 32 away, and the probabilities' registers are
-// the operand of the product with the values.
+// A workgroup takes 128 rows, a row being a token's query of one of the heads that share a key's, a wave 32 of them, and walks
+// over tiles of 64 keys once, with the running maximum and sum of each row in 32 bits.  Scores are formed transposed (keys as
+// rows, queries as columns), so that a lane holds one query's: maximum and sum are the lane's own but for one exchange with the
+// lane 32 away, and the probabilities' registers are the operand of the product with the values.
+//
+// Where there are few rows for the card, the keys of each are dealt out to several workgroups, whose sums a second kernel joins.
 #include "packed_attention.h"
 
 namespace rollout {
@@ -24,69 +26,96 @@ __device__ __forceinline__ float pair_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
+// partial: HD sums, then the maximum and the sum, of every part, token and head.
+template <int HD>
+__device__ __forceinline__ size_t partial_at(int part, const AttentionArgs& A, size_t row, int head) {
+  return (((size_t)part * A.n_q + row) * A.heads + head) * (HD + 4);
+}
+
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_attention(AttentionArgs A, int slots) {
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_attention(AttentionArgs A, int slots, int parts,
+                                                                                     float* __restrict__ partial) {
   typedef Rows<T, HD> R;
+  typedef typename R::Frag Frag;
   __shared__ __align__(16) char s_k[2][kKeys * R::kBytes];
   __shared__ __align__(16) char s_v[2][kKeys * R::kBytes];
-  const int w = neighbours_on_die(slots * A.heads);
+  const int w = neighbours_on_die(slots * A.kv_heads * parts);
   if (w < 0) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = w / slots, kvh = head / (A.heads / A.kv_heads);
+  const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
   int seq, t0;
   Sequence sq;
   // a sequence's last queries, which have the most keys, first
-  if (!find_tile<kQueries>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, slots - 1 - w % slots, lane, &seq, &sq, &t0)) return;
+  if (!find_tile<kQueries>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, slots - 1 - w / parts % slots, lane, &seq, &sq, &t0)) return;
   const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
 
-  const int behind = sk.len - sq.len;  // causal: query i attends keys 0 .. i + behind
-  const int w_first = t0 + 32 * wave, qi = w_first + a;
-  const size_t row = (size_t)sq.start + min(qi, sq.len - 1);
-  typename R::Frag qf[HD / 16];
+  const int behind = sk.len - sq.len, n_rows = sq.len * each;  // causal: token i attends keys 0 .. i + behind
+  const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
+  const int token = r / each, head = kvh * each + r % each;
+  const size_t row = (size_t)sq.start + token;
+  Frag qf[HD / 16];
   const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
 #pragma unroll
   for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c);
-  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, min(i, sq.len - 1) + behind + 1)) : sk.len; };
-  const int mine = keys_to(qi);                                    // of this lane's query
-  const int w_least = keys_to(w_first), w_most = keys_to(w_first + 31);  // of the wave's
-  const int tiles = (keys_to(t0 + kQueries - 1) + kKeys - 1) / kKeys;
+  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
+  const int mine = keys_to(token);  // of this lane's query
+  // of the wave's; a wave behind the last row has nothing to do
+  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
+  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
+  const int all = (keys_to((min(t0 + kQueries, n_rows) - 1) / each) + kKeys - 1) / kKeys;
+  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
 
   const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
   const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
   const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
-  auto load = [&](int buf, int it) {
-    const int last = sk.len - 1 - it * kKeys;
-    R::template load<kKeys, kWaves>(s_k[buf], kb + (size_t)it * kKeys * k_stride, k_stride, last, wave, lane);
-    R::template load<kKeys, kWaves>(s_v[buf], vb + (size_t)it * kKeys * v_stride, v_stride, last, wave, lane);
+  auto load = [&](auto buf, int it) {
+    const int k0 = (first + it) * kKeys, last = sk.len - 1 - k0;
+    R::template load<kKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
+    R::template load<kKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
   };
-  const RowReader<T, HD> rows(lane);
-  const ColReader<T, HD> cols(lane);
+#pragma unroll
+  for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]));  // here: no wait for it among the tiles
+  RowReader<T, HD> rows(lane);
+  ColReader<T, HD> cols(lane);
 
   f32x16 o[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) clear(o[d]);
   const float c2 = A.scale * kLog2e;  // scores are kept in units of log 2
   float m_run = -3.4e38f, l_run = 0.f;
-  if (tiles) load(0, 0);
-  for (int it = 0; it < tiles; ++it) {
-    dma_wait_barrier();  // tile `it` is there for every wave, and nobody reads the other buffer any more
-    if (it + 1 < tiles) load((it + 1) & 1, it + 1);
-    const int k0 = it * kKeys;
-    if (k0 >= w_most) continue;  // (the same for the whole wave)
-    f32x16 s[kKeys / 32];
+  through_tiles<2, 2 * R::loads(kKeys, kWaves)>(tiles, load, [&](auto buf, int it) {
+    const int k0 = (first + it) * kKeys;
+    if (k0 >= w_most) return;  // (the same for the whole wave)
+    rows.renew();
+    cols.renew();
+    constexpr int B = kKeys / 32, C = HD / 16, D = HD / 32;
+    f32x16 s[B];
 #pragma unroll
-    for (int b = 0; b < kKeys / 32; ++b) {
-      clear(s[b]);
+    for (int b = 0; b < B; ++b) clear(s[b]);
+    Frag fr[2][2], fc[2][D];
+    auto read_row = [&](auto g, Frag(&f)[2]) {
 #pragma unroll
-      for (int c = 0; c < HD / 16; ++c) mma(rows(s_k[it & 1], 32 * b, c), qf[c], s[b]);
-    }
+      for (int k = 0; k < 2; ++k) f[k] = rows(s_k[buf], 32 * (2 * g / C), (2 * g + k) % C);
+    };
+    auto read_col = [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) f[d] = cols(s_v[buf], 16 * g, d);
+    };
+    read_row(std::integral_constant<int, 0>(), fr[0]);
+    groups<B * C / 2, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) mma(f[k], qf[(2 * g + k) % C], s[2 * g / C]);
+    });
+    read_col(std::integral_constant<int, 0>(), fc[0]);
     if (k0 + kKeys > w_least) {
+      int limit = mine;
+      asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
 #pragma unroll
       for (int b = 0; b < kKeys / 32; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (k0 + 32 * b + 16 * (e >> 3) + 8 * half + (e & 7) >= mine) s[b][e] = -INFINITY;
+          if (k0 + 32 * b + 16 * (e >> 3) + 8 * half + (e & 7) >= limit) s[b][e] = -INFINITY;
     }
     float mx = s[0][0];
 #pragma unroll
@@ -104,26 +133,35 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
     }
+    // bf16 probabilities: each is off by at most 2^-9 of itself, as far as the output's own rounding moves it, and the
+    // errors of many keys largely cancel; their sum is that of the unrounded ones
+    Frag p[2 * B];
 #pragma unroll
-    for (int b = 0; b < kKeys / 32; ++b) {
+    for (int b = 0; b < B; ++b) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         s[b][e] = __builtin_amdgcn_exp2f(fmaf(s[b][e], c2, -m_run));
         l_run += s[b][e];
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        // bf16 probabilities: each is off by at most 2^-9 of itself, as far as the output's own rounding moves it, and the
-        // errors of many keys largely cancel; their sum is that of the unrounded ones
-        typename R::Frag p;
-        operand_of(s[b], i, p);
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) mma(cols(s_v[it & 1], 32 * b + 16 * i, d), p, o[d]);
-      }
+      for (int i = 0; i < 2; ++i) operand_of(s[b], i, p[2 * b + i]);
     }
-  }
-  if (qi >= sq.len) return;
+    groups<2 * B, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) mma(f[d], p[g], o[d]);
+    });
+  });
+  if (w_first + a >= n_rows) return;
   const float l = l_run + __shfl_xor(l_run, 32, 64);
+  if (parts > 1) {
+    float* p = partial + partial_at<HD>(part, A, row, head);
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) store8(p + 32 * d + 16 * i + 8 * half, o[d], i, 1.f);
+    if (half == 0) *reinterpret_cast<float2*>(p + HD) = make_float2(m_run, l);
+    return;
+  }
   // a query without keys: nothing, and the logarithm of nothing
   const float by = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
   T* op = (T*)A.out + row * A.out_stride + (size_t)head * HD + 8 * half;
@@ -134,24 +172,77 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   if (half == 0) A.lse[(size_t)head * A.n_q + row] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+// The parts of the rows of a tile, in order: a thread takes four values of a row.
 template <typename T, int HD>
-hipError_t launch(hipStream_t s, const AttentionArgs& a) {
-  const int slots = tile_slots(a.n_q, a.n_seqs, kQueries);
-  k_packed_attention<T, HD><<<die_grid(slots * a.heads), 64 * kWaves, 0, s>>>(a, slots);
+__global__ __launch_bounds__(256) void k_attention_merge(AttentionArgs A, int slots, int parts, const float* __restrict__ partial) {
+  const int each = A.heads / A.kv_heads, kvh = (int)blockIdx.x / slots;
+  int seq, t0;
+  Sequence sq;
+  if (!find_tile<kQueries>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, (int)blockIdx.x % slots, threadIdx.x & 63, &seq, &sq, &t0)) return;
+  constexpr int kLanes = HD / 4;
+  const int r = t0 + (int)blockIdx.y * (256 / kLanes) + threadIdx.x / kLanes, c = 4 * (threadIdx.x % kLanes);
+  if (r >= sq.len * each) return;
+  const size_t row = (size_t)sq.start + r / each;
+  const int head = kvh * each + r % each;
+  float m = -INFINITY;
+  for (int k = 0; k < parts; ++k) m = fmaxf(m, partial[partial_at<HD>(k, A, row, head) + HD]);
+  float l = 0.f, o[4] = {};
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) {
+    const float* p = partial + partial_at<HD>(k, A, row, head);
+    const float2 ml = *reinterpret_cast<const float2*>(p + HD);
+    const float4 x = *reinterpret_cast<const float4*>(p + c);
+    const float by = __builtin_amdgcn_exp2f(ml.x - m);
+    l = fmaf(ml.y, by, l);
+    o[0] = fmaf(x.x, by, o[0]), o[1] = fmaf(x.y, by, o[1]), o[2] = fmaf(x.z, by, o[2]), o[3] = fmaf(x.w, by, o[3]);
+  }
+  const float by = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] *= by;
+  T* op = (T*)A.out + row * A.out_stride + (size_t)head * HD + c;
+  if constexpr (sizeof(T) == 2) {
+    const uint2 u = make_uint2((uint32_t)round_bf16(o[0]) | (uint32_t)round_bf16(o[1]) << 16,
+                               (uint32_t)round_bf16(o[2]) | (uint32_t)round_bf16(o[3]) << 16);
+    *reinterpret_cast<uint2*>(op) = u;
+  } else {
+    *reinterpret_cast<float4*>(op) = make_float4(o[0], o[1], o[2], o[3]);
+  }
+  if (c == 0) A.lse[(size_t)head * A.n_q + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The keys' parts where the rows alone give fewer workgroups than kEnough: as many as make that many, but parts of 4 tiles where a
+// sequence has its share of the keys.
+constexpr int kEnough = 1024, kMaxParts = 64;
+int key_parts(const AttentionArgs& a) {
+  const int64_t groups = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries) * a.kv_heads;
+  const int64_t tiles = (int64_t)a.n_k / a.n_seqs / (4 * kKeys);
+  return (int)std::max<int64_t>(1, std::min({(kEnough + groups - 1) / groups, tiles, (int64_t)kMaxParts}));
+}
+
+template <typename T, int HD>
+hipError_t launch(hipStream_t s, const AttentionArgs& a, float* partial) {
+  const int slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries), parts = key_parts(a);
+  k_packed_attention<T, HD><<<die_grid(slots * a.kv_heads * parts), 64 * kWaves, 0, s>>>(a, slots, parts, partial);
+  if (parts > 1) k_attention_merge<T, HD><<<dim3(slots * a.kv_heads, kQueries * HD / 1024), 256, 0, s>>>(a, slots, parts, partial);
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_of(hipStream_t s, const AttentionArgs& a) {
-  return a.head_dim == 32 ? launch<T, 32>(s, a) : a.head_dim == 64 ? launch<T, 64>(s, a) : launch<T, 128>(s, a);
+hipError_t launch_of(hipStream_t s, const AttentionArgs& a, float* partial) {
+  return a.head_dim == 32   ? launch<T, 32>(s, a, partial)
+         : a.head_dim == 64 ? launch<T, 64>(s, a, partial)
+                            : launch<T, 128>(s, a, partial);
 }
 
 }  // namespace
 
-size_t packed_attention_workspace(const AttentionArgs&) { return 0; }
+size_t packed_attention_workspace(const AttentionArgs& a) {
+  const int parts = key_parts(a);
+  return parts > 1 ? (size_t)parts * a.n_q * a.heads * (a.head_dim + 4) * 4 : 0;
+}
 
-hipError_t launch_packed_attention(hipStream_t s, int dtype, const AttentionArgs& a, void*) {
-  return dtype == ROLLOUT_DTYPE_BF16 ? launch_of<uint16_t>(s, a) : launch_of<float>(s, a);
+hipError_t launch_packed_attention(hipStream_t s, int dtype, const AttentionArgs& a, void* ws) {
+  return dtype == ROLLOUT_DTYPE_BF16 ? launch_of<uint16_t>(s, a, (float*)ws) : launch_of<float>(s, a, (float*)ws);
 }
 
 }  // namespace rollout

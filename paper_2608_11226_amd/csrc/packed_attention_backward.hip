@@ -16,10 +16,10 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// lse in units of log 2 (+inf where a query has no keys: its probabilities are then 0) and D of every row and head.  A wave
-// takes 64 * 16 bytes of rows at a time.
+// lse in units of log 2 (+inf where a query has no keys: its probabilities are then 0) and D of every token and head,
+// [n_q][heads].  A wave takes 64 * 16 bytes of rows at a time.
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_attention_delta(AttentionGradArgs A, float* __restrict__ lse2, float* __restrict__ delta) {
+__global__ __launch_bounds__(256) void k_attention_delta(AttentionGradArgs A, float2* __restrict__ stats) {
   constexpr int kLanes = HD / Chunk16<T>::N;  // of a row of a head
   const int64_t total = (int64_t)A.n_q * A.heads;
   const int64_t at = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
@@ -37,112 +37,162 @@ __global__ __launch_bounds__(256) void k_attention_delta(AttentionGradArgs A, fl
   for (int i = kLanes / 2; i > 0; i >>= 1) sum += __shfl_xor(sum, i, 64);
   if (threadIdx.x % kLanes == 0) {
     const float l = A.lse[(size_t)head * A.n_q + row];
-    lse2[(size_t)head * A.n_q + row] = l == -INFINITY ? INFINITY : l * kLog2e;
-    delta[(size_t)head * A.n_q + row] = sum;
+    stats[at] = make_float2(l == -INFINITY ? INFINITY : l * kLog2e, sum);
   }
 }
 
 // Keys' gradients.  A workgroup takes 128 keys, a wave 32 of them, whose k and v stay in registers, and walks over tiles of 32
-// queries of every head that shares them.  Scores have queries as rows and keys as columns, so that a lane holds one key's.
-constexpr int kBackKeys = 32 * kWaves, kBackQueries = 32;
+// rows, a row being a token's query of one of the heads that share the keys.  Scores have queries as rows and keys as columns,
+// so that a lane holds one key's.
+constexpr int kBackKeys = 32 * kWaves, kBackRows = 32;
 
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dkv(AttentionGradArgs A, int slots, int parts,
-                                                                                  const float* __restrict__ lse2,
-                                                                                  const float* __restrict__ delta,
+                                                                                  const float2* __restrict__ stats,
                                                                                   float* __restrict__ partial) {
   typedef Rows<T, HD> R;
-  __shared__ __align__(16) char s_q[2][kBackQueries * R::kBytes];
-  __shared__ __align__(16) char s_do[2][kBackQueries * R::kBytes];
-  __shared__ __align__(16) float s_stat[2][2][kBackQueries];
+  typedef typename R::Frag Frag;
+  constexpr int S = sizeof(T) == 2 ? 3 : 2;
+  __shared__ __align__(16) char s_q[S][kBackRows * R::kBytes];
+  __shared__ __align__(16) char s_do[S][kBackRows * R::kBytes];
+  __shared__ __align__(16) float2 s_stat[S][kBackRows];
+  // 128 dimensions in bf16: registers for all of k and v are some 20 too many, and six of v's eight operands lie in LDS (as
+  // much as two workgroups of a compute unit have room for)
+  constexpr int C = HD / 16, D = HD / 32, kKept = sizeof(T) == 2 && HD == 128 ? 2 : C;
+  __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
   const int w = neighbours_on_die(slots * A.kv_heads * parts);
   if (w < 0) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = A.heads / A.kv_heads, kvh = w / slots / parts, part = w / slots % parts;
+  const int each = A.heads / A.kv_heads, kvh = w / slots / parts, part = w / slots % parts;
   int seq, t0;
   Sequence sk;
-  if (!find_tile<kBackKeys>(A.k_starts, A.k_lens, A.n_seqs, A.n_k, w % slots, lane, &seq, &sk, &t0)) return;
+  if (!find_tile<kBackKeys>(A.k_starts, A.k_lens, A.n_seqs, A.n_k, 1, w % slots, lane, &seq, &sk, &t0)) return;
   const Sequence sq = sequence_at(A.q_starts, A.q_lens, seq, A.n_q);
-  const int behind = sk.len - sq.len;
-  const int head0 = kvh * group + group * part / parts, heads = kvh * group + group * (part + 1) / parts - head0;
+  const int behind = sk.len - sq.len, n_rows = sq.len * each;
 
   const int w_first = t0 + 32 * wave, kj = w_first + a;
   const size_t row = (size_t)sk.start + min(kj, sk.len - 1);
-  typename R::Frag kf[HD / 16], vf[HD / 16];
+  Frag kf[C], vf[kKept];
   {
     const T* kp = (const T*)A.k + row * A.k_stride + (size_t)kvh * HD + 8 * half;
     const T* vp = (const T*)A.v + row * A.v_stride + (size_t)kvh * HD + 8 * half;
 #pragma unroll
-    for (int c = 0; c < HD / 16; ++c) kf[c] = load_operand(kp + 16 * c), vf[c] = load_operand(vp + 16 * c);
+    for (int c = 0; c < C; ++c) {
+      kf[c] = load_operand(kp + 16 * c);
+      if (c < kKept)
+        vf[c < kKept ? c : 0] = load_operand(vp + 16 * c);
+      else
+        s_v[wave][c - kKept][lane] = load_operand(vp + 16 * c);
+    }
   }
-  // causal: key j is attended from query j - behind on
-  auto from = [&](int j) { return A.causal ? max(0, j - behind) : 0; };
-  const int first = min(from(t0), sq.len) / kBackQueries;
-  const int tiles = (sq.len + kBackQueries - 1) / kBackQueries - first;  // of a head
-  const int total = tiles * heads;
+  // causal: key j is attended from token j - behind on
+  auto from = [&](int j) { return A.causal ? max(0, min(j - behind, sq.len)) * each : 0; };
+  const int head_tile = from(t0) / kBackRows, all = (n_rows + kBackRows - 1) / kBackRows - head_tile;
+  const int first = head_tile + (int)((int64_t)all * part / parts);
+  const int tiles = head_tile + (int)((int64_t)all * (part + 1) / parts) - first;
+  const int mine = from(kj);
+  // a wave behind the last key has nothing to do
+  const int w_least = w_first < sk.len ? from(w_first) : INT32_MAX, w_most = from(w_first + 31);
 
   const uint32_t q_stride = (uint32_t)(A.q_stride * sizeof(T)), do_stride = (uint32_t)(A.dout_stride * sizeof(T));
-  const char* qb = (const char*)((const T*)A.q + (size_t)sq.start * A.q_stride);
-  const char* dob = (const char*)((const T*)A.dout + (size_t)sq.start * A.dout_stride);
-  int l_head = head0, l_tile = first;  // what is loaded next
-  auto load = [&](int buf) {
-    const int i0 = l_tile * kBackQueries, last = sq.len - 1 - i0;
-    R::template load<kBackQueries, kWaves>(s_q[buf], qb + (size_t)i0 * q_stride + (size_t)l_head * R::kBytes, q_stride, last, wave, lane);
-    R::template load<kBackQueries, kWaves>(s_do[buf], dob + (size_t)i0 * do_stride + (size_t)l_head * R::kBytes, do_stride, last, wave, lane);
-    float x = half ? 0.f : INFINITY;  // behind the last query: no probability
-    if (wave == 0 && a <= last) x = (half ? delta : lse2)[(size_t)l_head * A.n_q + sq.start + i0 + a];
-    if (++l_tile == first + tiles) l_tile = first, ++l_head;
-    return x;
+  const size_t head = (size_t)kvh * each;
+  const char* qb = (const char*)((const T*)A.q + (size_t)sq.start * A.q_stride + head * HD);
+  const char* dob = (const char*)((const T*)A.dout + (size_t)sq.start * A.dout_stride + head * HD);
+  const float2* sb = stats + (size_t)sq.start * A.heads + head;
+  const uint32_t inverse = 65536 / each + 1;  // x / each = x inverse / 65536 for 0 <= x < 96, each <= 64
+  int token = first * kBackRows / each, over = first * kBackRows - token * each;  // of the first row that is loaded next
+  const int more = kBackRows / each, more_over = kBackRows - more * each;
+  auto load = [&](auto buf, int it) {
+    const int last = n_rows - 1 - (first + it) * kBackRows;
+    const char* q0 = qb + (size_t)token * q_stride;
+    const char* do0 = dob + (size_t)token * do_stride;
+    if (wave == 0) {
+      const uint32_t x = (uint32_t)(min(lane >> 1, last) + over), t = x * inverse >> 16;
+      dma_lds4_at(sb + (size_t)token * A.heads, (t * (uint32_t)(A.heads - each) + x) * 8 + 4 * (lane & 1), s_stat[buf]);
+    }
+    R::template load_with<kBackRows, kWaves>(wave, lane, [&](int row, uint32_t offset, int place) {
+      const uint32_t x = (uint32_t)(min(row, last) + over), t = x * inverse >> 16;
+      const uint32_t at = (x - t * (uint32_t)each) * R::kBytes + offset;
+      dma_lds16_at(q0, t * q_stride + at, s_q[buf] + place);
+      dma_lds16_at(do0, t * do_stride + at, s_do[buf] + place);
+    });
+    token += more, over += more_over;
+    if (over >= each) over -= each, ++token;
   };
-  const RowReader<T, HD> rows(lane);
-  const ColReader<T, HD> cols(lane);
+  RowReader<T, HD> rows(lane);
+  ColReader<T, HD> cols(lane);
+  // here: no wait for them among the tiles
+#pragma unroll
+  for (int c = 0; c < C; ++c) asm volatile("" : "+v"(kf[c]));
+#pragma unroll
+  for (int c = 0; c < kKept; ++c) asm volatile("" : "+v"(vf[c]));
 
   f32x16 dk[HD / 32], dv[HD / 32];
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) clear(dk[d]), clear(dv[d]);
   const float c2 = A.scale * kLog2e;
-  if (total > 0) {
-    const float x = load(0);
-    if (wave == 0) s_stat[0][half][a] = x;
-  }
-  int tile = first;
-  for (int it = 0; it < total; ++it) {
-    const int buf = it & 1, i0 = tile * kBackQueries;
-    if (++tile == first + tiles) tile = first;
-    dma_wait_barrier();
-    float next = 0.f;
-    if (it + 1 < total) next = load(buf ^ 1);
-    if (i0 + kBackQueries > from(w_first)) {  // (the same for the whole wave)
-      f32x16 s, dp;
-      clear(s);
-      clear(dp);
+  through_tiles<S, 2 * R::loads(kBackRows, kWaves)>(tiles, load, [&](auto buf, int it) {
+    const int i0 = (first + it) * kBackRows;
+    if (i0 + kBackRows <= w_least) return;  // (the same for the whole wave)
+    rows.renew();
+    cols.renew();
+    f32x16 s, dp;
+    clear(s);
+    clear(dp);
+    Frag fr[2][4], fc[2][D];
+    auto read_row = [&](auto g, Frag(&f)[4]) {
 #pragma unroll
-      for (int c = 0; c < HD / 16; ++c) mma(rows(s_q[buf], 0, c), kf[c], s);
+      for (int k = 0; k < 2; ++k) {
+        const int c = (2 * g + k) % C;
+        f[k] = rows(2 * g < C ? s_q[buf] : s_do[buf], 0, c);
+        if (2 * g >= C && c >= kKept) f[2 + k] = s_v[wave][c - kKept][lane];
+      }
+    };
+    auto read_col = [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-      for (int c = 0; c < HD / 16; ++c) mma(rows(s_do[buf], 0, c), vf[c], dp);
-      const bool edge = i0 < from(w_first + 31);
+      for (int d = 0; d < D; ++d) f[d] = cols(g % 2 ? s_q[buf] : s_do[buf], 16 * (g / 2), d);
+    };
+    read_row(std::integral_constant<int, 0>(), fr[0]);
+    groups<C, 4>(fr, read_row, [&](auto g, Frag(&f)[4]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int c = (2 * g + k) % C;
+        if constexpr (2 * g < C)
+          mma(f[k], kf[c], s);
+        else
+          mma(f[k], c < kKept ? vf[c < kKept ? c : 0] : f[2 + k], dp);
+      }
+    });
+    read_col(std::integral_constant<int, 0>(), fc[0]);
+    if (i0 < w_most || i0 + kBackRows > n_rows) {
+      int limit = mine;
+      asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const int i = 16 * (e >> 3) + 8 * half + (e & 7);
-        s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -s_stat[buf][0][i]));
-        if (edge && i0 + i < from(kj)) s[e] = 0.f;
-        dp[e] = s[e] * (dp[e] - s_stat[buf][1][i]);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        typename R::Frag p, ds;
-        operand_of(s, i, p);
-        operand_of(dp, i, ds);
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d) {
-          mma(cols(s_do[buf], 16 * i, d), p, dv[d]);
-          mma(cols(s_q[buf], 16 * i, d), ds, dk[d]);
-        }
+        const int i = i0 + 16 * (e >> 3) + 8 * half + (e & 7);
+        if (i < limit || i >= n_rows) s[e] = -INFINITY;
       }
     }
-    if (wave == 0) s_stat[buf ^ 1][half][a] = next;
-  }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float2 x = s_stat[buf][16 * (e >> 3) + 8 * half + (e & 7)];
+      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -x.x));
+      dp[e] = s[e] * (dp[e] - x.y);
+    }
+    Frag p[2], ds[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) operand_of(s, i, p[i]), operand_of(dp, i, ds[i]);
+    groups<4, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        if constexpr (g % 2)
+          mma(f[d], ds[g / 2], dk[d]);
+        else
+          mma(f[d], p[g / 2], dv[d]);
+      }
+    });
+  });
   if (kj >= sk.len) return;
   if (parts > 1) {
     const size_t width = (size_t)A.kv_heads * HD, all = (size_t)A.n_k * width;
@@ -161,12 +211,151 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     for (int i = 0; i < 2; ++i) store8(dkp + 32 * d + 16 * i, dk[d], i, A.scale), store8(dvp + 32 * d + 16 * i, dv[d], i, 1.f);
 }
 
-// The parts' sums of a tile of keys, in order.
+// Queries' gradients.  A workgroup takes 128 rows, a wave 32 of them, whose q and do stay in registers, and walks over tiles of
+// 32 keys.  Scores have keys as rows and queries as columns, as in the forward pass, and where there are few rows the keys are
+// dealt out to several workgroups as there.
+constexpr int kDqRows = 32 * kWaves, kDqKeys = 32;
+
+template <typename T, int HD>
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, int slots, int parts,
+                                                                                 const float2* __restrict__ stats,
+                                                                                 float* __restrict__ partial) {
+  typedef Rows<T, HD> R;
+  typedef typename R::Frag Frag;
+  constexpr int S = sizeof(T) == 2 ? 3 : 2;
+  __shared__ __align__(16) char s_k[S][kDqKeys * R::kBytes];
+  __shared__ __align__(16) char s_v[S][kDqKeys * R::kBytes];
+  const int w = neighbours_on_die(slots * A.kv_heads * parts);
+  if (w < 0) return;
+  const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
+  int seq, t0;
+  Sequence sq;
+  if (!find_tile<kDqRows>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, slots - 1 - w / parts % slots, lane, &seq, &sq, &t0)) return;
+  const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
+  const int behind = sk.len - sq.len, n_rows = sq.len * each;
+  const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
+  const int token = r / each, head = kvh * each + r % each;
+  const size_t row = (size_t)sq.start + token;
+  Frag qf[HD / 16], df[HD / 16];
+  {
+    const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
+    const T* dp = (const T*)A.dout + row * A.dout_stride + (size_t)head * HD + 8 * half;
+#pragma unroll
+    for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c), df[c] = load_operand(dp + 16 * c);
+  }
+  const float2 my = stats[row * A.heads + head];
+  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
+  const int mine = keys_to(token);
+  // a wave behind the last row has nothing to do
+  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
+  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
+  const int all = (keys_to((min(t0 + kDqRows, n_rows) - 1) / each) + kDqKeys - 1) / kDqKeys;
+  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
+
+  const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
+  const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
+  const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
+  auto load = [&](auto buf, int it) {
+    const int k0 = (first + it) * kDqKeys, last = sk.len - 1 - k0;
+    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
+    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
+  };
+  RowReader<T, HD> rows(lane);
+  ColReader<T, HD> cols(lane);
+#pragma unroll
+  for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]), "+v"(df[c]));  // here: no wait for them among the tiles
+
+  f32x16 dq[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) clear(dq[d]);
+  const float c2 = A.scale * kLog2e;
+  through_tiles<S, 2 * R::loads(kDqKeys, kWaves)>(tiles, load, [&](auto buf, int it) {
+    const int k0 = (first + it) * kDqKeys;
+    if (k0 >= w_most) return;  // (the same for the whole wave)
+    rows.renew();
+    cols.renew();
+    f32x16 s, dp;
+    clear(s);
+    clear(dp);
+    constexpr int C = HD / 16, D = HD / 32;
+    Frag fr[2][2], fc[2][D];
+    auto read_row = [&](auto g, Frag(&f)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_k[buf] : s_v[buf], 0, (2 * g + k) % C);
+    };
+    auto read_col = [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) f[d] = cols(s_k[buf], 16 * g, d);
+    };
+    read_row(std::integral_constant<int, 0>(), fr[0]);
+    groups<C, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if constexpr (2 * g < C)
+          mma(f[k], qf[(2 * g + k) % C], s);
+        else
+          mma(f[k], df[(2 * g + k) % C], dp);
+      }
+    });
+    read_col(std::integral_constant<int, 0>(), fc[0]);
+    if (k0 + kDqKeys > w_least) {
+      int limit = mine;
+      asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (k0 + 16 * (e >> 3) + 8 * half + (e & 7) >= limit) s[e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dp[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my.x)) * (dp[e] - my.y);
+    Frag ds[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) operand_of(dp, i, ds[i]);
+    groups<2, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
+    });
+  });
+  if (w_first + a >= n_rows) return;
+  if (parts > 1) {
+    float* out = partial + (((size_t)part * A.n_q + row) * A.heads + head) * HD + 8 * half;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
+    return;
+  }
+  T* out = (T*)A.dq + row * A.dq_stride + (size_t)head * HD + 8 * half;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
+}
+
+// Eight neighbours of the parts' sums, in order, to an output.
 template <typename T>
-__global__ __launch_bounds__(256) void k_attention_join(AttentionGradArgs A, int slots, int parts, const float* __restrict__ partial) {
+__device__ __forceinline__ void join8(T* out, const float* p, size_t apart, int parts) {
+  float t[8], x[8];
+  ld8(p, 0, t);
+#pragma unroll 4
+  for (int k = 1; k < parts; ++k) {
+    ld8(p + k * apart, 0, x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] += x[e];
+  }
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<u32x4*>(out) = pack16(t);
+  else
+    st8(out, 0, t);
+}
+
+// The parts' sums of a tile of keys.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_join_dkv(AttentionGradArgs A, int slots, int parts, const float* __restrict__ partial) {
   int seq, t0;
   Sequence sk;
-  if (!find_tile<kBackKeys>(A.k_starts, A.k_lens, A.n_seqs, A.n_k, (int)blockIdx.x, threadIdx.x & 63, &seq, &sk, &t0)) return;
+  if (!find_tile<kBackKeys>(A.k_starts, A.k_lens, A.n_seqs, A.n_k, 1, (int)blockIdx.x, threadIdx.x & 63, &seq, &sk, &t0)) return;
   const int width = A.kv_heads * A.head_dim, chunks = width / 8, rows = min(kBackKeys, sk.len - t0);
   const size_t all = (size_t)A.n_k * width;
   const bool v = blockIdx.y & 1;
@@ -175,133 +364,52 @@ __global__ __launch_bounds__(256) void k_attention_join(AttentionGradArgs A, int
   for (int i = (int)(blockIdx.y >> 1) * 256 + threadIdx.x; i < rows * chunks; i += (int)(gridDim.y >> 1) * 256) {
     const size_t row = (size_t)sk.start + t0 + i / chunks;
     const int c = i % chunks * 8;
-    const float* p = partial + (v ? all : 0) + row * width + c;
-    float t[8], x[8];
-    ld8(p, 0, t);
-    for (int k = 1; k < parts; ++k) {
-      ld8(p + 2 * k * all, 0, x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] += x[e];
-    }
-    T* q = out + row * stride + c;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<u32x4*>(q) = pack16(t);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) q[e] = t[e];
-    }
+    join8(out + row * stride + c, partial + (v ? all : 0) + row * width + c, 2 * all, parts);
   }
 }
 
-// Queries' gradients.  A workgroup takes 128 queries of a head, a wave 32 of them, whose q and do stay in registers, and walks
-// over tiles of 32 keys.  Scores have keys as rows and queries as columns, as in the forward pass.
-constexpr int kDqQueries = 32 * kWaves, kDqKeys = 32;
-
-template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, int slots,
-                                                                                 const float* __restrict__ lse2,
-                                                                                 const float* __restrict__ delta) {
-  typedef Rows<T, HD> R;
-  __shared__ __align__(16) char s_k[2][kDqKeys * R::kBytes];
-  __shared__ __align__(16) char s_v[2][kDqKeys * R::kBytes];
-  const int w = neighbours_on_die(slots * A.heads);
-  if (w < 0) return;
-  const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = w / slots, kvh = head / (A.heads / A.kv_heads);
+// The parts' sums of a tile of 128 tokens.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_join_dq(AttentionGradArgs A, int parts, const float* __restrict__ partial) {
   int seq, t0;
   Sequence sq;
-  if (!find_tile<kDqQueries>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, slots - 1 - w % slots, lane, &seq, &sq, &t0)) return;
-  const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
-  const int behind = sk.len - sq.len;
-  const int w_first = t0 + 32 * wave, qi = w_first + a;
-  const size_t row = (size_t)sq.start + min(qi, sq.len - 1);
-  typename R::Frag qf[HD / 16], df[HD / 16];
-  {
-    const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
-    const T* dp = (const T*)A.dout + row * A.dout_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-    for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c), df[c] = load_operand(dp + 16 * c);
+  if (!find_tile<128>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, 1, (int)blockIdx.x, threadIdx.x & 63, &seq, &sq, &t0)) return;
+  const int width = A.heads * A.head_dim, chunks = width / 8, rows = min(128, sq.len - t0);
+  for (int i = (int)blockIdx.y * 256 + threadIdx.x; i < rows * chunks; i += (int)gridDim.y * 256) {
+    const size_t row = (size_t)sq.start + t0 + i / chunks;
+    const int c = i % chunks * 8;
+    join8((T*)A.dq + row * A.dq_stride + c, partial + row * width + c, (size_t)A.n_q * width, parts);
   }
-  const float my_lse = lse2[(size_t)head * A.n_q + row], my_delta = delta[(size_t)head * A.n_q + row];
-  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, min(i, sq.len - 1) + behind + 1)) : sk.len; };
-  const int mine = keys_to(qi);
-  const int w_least = keys_to(w_first), w_most = keys_to(w_first + 31);
-  const int tiles = (keys_to(t0 + kDqQueries - 1) + kDqKeys - 1) / kDqKeys;
-
-  const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
-  const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
-  const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
-  auto load = [&](int buf, int it) {
-    const int last = sk.len - 1 - it * kDqKeys;
-    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)it * kDqKeys * k_stride, k_stride, last, wave, lane);
-    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)it * kDqKeys * v_stride, v_stride, last, wave, lane);
-  };
-  const RowReader<T, HD> rows(lane);
-  const ColReader<T, HD> cols(lane);
-
-  f32x16 dq[HD / 32];
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d) clear(dq[d]);
-  const float c2 = A.scale * kLog2e;
-  if (tiles) load(0, 0);
-  for (int it = 0; it < tiles; ++it) {
-    const int buf = it & 1, k0 = it * kDqKeys;
-    dma_wait_barrier();
-    if (it + 1 < tiles) load(buf ^ 1, it + 1);
-    if (k0 >= w_most) continue;  // (the same for the whole wave)
-    f32x16 s, dp;
-    clear(s);
-    clear(dp);
-#pragma unroll
-    for (int c = 0; c < HD / 16; ++c) mma(rows(s_k[buf], 0, c), qf[c], s);
-#pragma unroll
-    for (int c = 0; c < HD / 16; ++c) mma(rows(s_v[buf], 0, c), df[c], dp);
-    const bool edge = k0 + kDqKeys > w_least;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my_lse));
-      if (edge && k0 + 16 * (e >> 3) + 8 * half + (e & 7) >= mine) s[e] = 0.f;
-      dp[e] = s[e] * (dp[e] - my_delta);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      typename R::Frag ds;
-      operand_of(dp, i, ds);
-#pragma unroll
-      for (int d = 0; d < HD / 32; ++d) mma(cols(s_k[buf], 16 * i, d), ds, dq[d]);
-    }
-  }
-  if (qi >= sq.len) return;
-  T* out = (T*)A.dq + row * A.dq_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
 }
 
-// The heads that share a key's are dealt out to this many workgroups, whose sums are joined afterwards, where there are few
-// tiles of keys.
-int head_parts(const AttentionArgs& a) {
-  const int group = a.heads / a.kv_heads;
-  const int64_t tiles = (int64_t)tile_slots(a.n_k, a.n_seqs, kBackKeys) * a.kv_heads;
-  return (int)std::min<int64_t>(group, (1024 + tiles - 1) / tiles);
+// The rows' parts of a tile of keys, and the keys' parts of a tile of rows, where the tiles alone give fewer workgroups than
+// kEnough; each part has 4 tiles where a sequence has its share of the tokens.
+constexpr int kEnough = 1024, kMaxParts = 64;
+int parts_of(int64_t groups, int64_t tiles) {
+  return (int)std::max<int64_t>(1, std::min({(kEnough + groups - 1) / groups, tiles / 4, (int64_t)kMaxParts}));
+}
+int row_parts(const AttentionArgs& a) {
+  const int each = a.heads / a.kv_heads;
+  return parts_of((int64_t)tile_slots(a.n_k, 1, a.n_seqs, kBackKeys) * a.kv_heads, (int64_t)a.n_q * each / a.n_seqs / kBackRows);
+}
+int key_parts(const AttentionArgs& a) {
+  return parts_of((int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows) * a.kv_heads, (int64_t)a.n_k / a.n_seqs / kDqKeys);
 }
 
-size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 4 + 15) / 16 * 16; }
+size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
 
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
-  float* lse2 = (float*)ws;
-  float* delta = (float*)(ws + stats_bytes(a));
-  float* partial = (float*)(ws + 2 * stats_bytes(a));
+  float2* stats = (float2*)ws;
+  float* partial = (float*)(ws + stats_bytes(a));  // of the keys, then of the queries
   const int per = 256 / (HD / Chunk16<T>::N);
-  k_attention_delta<T, HD><<<(unsigned)(((int64_t)a.n_q * a.heads + per - 1) / per), 256, 0, s>>>(a, lse2, delta);
-  const int slots = tile_slots(a.n_k, a.n_seqs, kBackKeys), parts = head_parts(a);
-  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * parts), 64 * kWaves, 0, s>>>(a, slots, parts, lse2, delta, partial);
-  if (parts > 1) k_attention_join<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, slots, parts, partial);
-  const int q_slots = tile_slots(a.n_q, a.n_seqs, kDqQueries);
-  k_attention_dq<T, HD><<<die_grid(q_slots * a.heads), 64 * kWaves, 0, s>>>(a, q_slots, lse2, delta);
+  k_attention_delta<T, HD><<<(unsigned)(((int64_t)a.n_q * a.heads + per - 1) / per), 256, 0, s>>>(a, stats);
+  const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys), rp = row_parts(a);
+  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, slots, rp, stats, partial);
+  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, slots, rp, partial);
+  const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts(a);
+  k_attention_dq<T, HD><<<die_grid(q_slots * a.kv_heads * kp), 64 * kWaves, 0, s>>>(a, q_slots, kp, stats, partial);
+  if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
   return hipGetLastError();
 }
 
@@ -313,8 +421,10 @@ hipError_t launch_of(hipStream_t s, const AttentionGradArgs& a, char* ws) {
 }  // namespace
 
 size_t packed_attention_backward_workspace(const AttentionArgs& a) {
-  const int parts = head_parts(a);
-  return 2 * stats_bytes(a) + (parts > 1 ? (size_t)parts * 2 * a.n_k * a.kv_heads * a.head_dim * 4 : 0);
+  const int rp = row_parts(a), kp = key_parts(a);
+  const size_t keys = rp > 1 ? (size_t)rp * 2 * a.n_k * a.kv_heads * a.head_dim * 4 : 0;
+  const size_t rows = kp > 1 ? (size_t)kp * a.n_q * a.heads * a.head_dim * 4 : 0;
+  return stats_bytes(a) + std::max(keys, rows);
 }
 
 hipError_t launch_packed_attention_backward(hipStream_t s, int dtype, const AttentionGradArgs& a, void* ws) {

@@ -79,6 +79,7 @@ inline bool embedding_backward_fits(int n, int dim) { return (int64_t)n * (((int
 size_t embedding_backward_workspace(int n, int vocab, int dim);
 hipError_t launch_embedding_backward(hipStream_t s, int grad_dtype, int table_dtype, const EmbeddingGradArgs& a, void* ws);
 
+constexpr int kMaxHeadsPerKey = 64;
 // Strides are in elements.  k_starts and k_lens are never NULL: the queries' where the sequences' keys are their own.
 struct AttentionArgs {
   int heads, kv_heads, head_dim, n_seqs, n_q, n_k;

@@ -18,6 +18,7 @@ rollout_status check_shape(const rollout_attention_shape* s) {
   if (!is_float_type(s->dtype)) return fail(ROLLOUT_EINVAL, "dtype must be 0 (fp32) or 1 (bf16)");
   if (s->n_heads < 1 || s->n_kv_heads < 1 || s->n_heads % s->n_kv_heads)
     return fail(ROLLOUT_EINVAL, "n_heads must be a multiple of n_kv_heads, both >= 1");
+  if (s->n_heads / s->n_kv_heads > kMaxHeadsPerKey) return fail(ROLLOUT_EUNSUPPORTED, "more than 64 query heads for a key's");
   if (s->head_dim != 32 && s->head_dim != 64 && s->head_dim != 128)
     return fail(ROLLOUT_EUNSUPPORTED, "head_dim must be 32, 64 or 128");
   if (s->n_seqs < 1 || s->n_q < 1 || s->n_k < 1) return fail(ROLLOUT_EINVAL, "n_seqs, n_q and n_k must be >= 1");
