@@ -273,6 +273,21 @@ __device__ __forceinline__ int neighbours_on_die(int total) {
   const int w = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
   return (int)(blockIdx.x >> 3) < per && w < total ? w : -1;
 }
+// Into how many parts the walks of a launch over `tiles` tiles each are cut, whose sums a second launch joins: by what a whole
+// walk takes (alone_us a tile, or shared_us a tile in every one of the card's 512 places where there are more walks than
+// places), the third of a walk that the last ones run on, and the parts' sums, which are written and read again.
+inline int walk_parts(int64_t walks, double tiles, bool triangle, double alone_us, double shared_us, double part_bytes) {
+  const double places = 512.0, all = (triangle ? 0.55 : 1.0) * (double)walks * tiles * shared_us / places;
+  int best = 1;
+  double least = 0.0;
+  for (int p = 1; p <= 64 && (p == 1 || tiles >= 4.0 * p); ++p) {
+    const double walk = alone_us * tiles / p + 3.0;
+    const double cost = std::max(walk, all) + 0.35 * walk + (p > 1 ? 5.0 + 2.0 * p * part_bytes / 4.5e6 : 0.0);
+    if (p == 1 || cost < least) best = p, least = cost;
+  }
+  return best;
+}
+
 inline unsigned die_grid(int total) { return (unsigned)((total + 7) / 8 * 8); }
 
 }  // namespace rollout

@@ -210,13 +210,10 @@ __global__ __launch_bounds__(256) void k_attention_merge(AttentionArgs A, int sl
   if (c == 0) A.lse[(size_t)head * A.n_q + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-// The keys' parts where the rows alone give fewer workgroups than kEnough: as many as make that many, but parts of 4 tiles where a
-// sequence has its share of the keys.
-constexpr int kEnough = 1024, kMaxParts = 64;
 int key_parts(const AttentionArgs& a) {
-  const int64_t groups = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries) * a.kv_heads;
-  const int64_t tiles = (int64_t)a.n_k / a.n_seqs / (4 * kKeys);
-  return (int)std::max<int64_t>(1, std::min({(kEnough + groups - 1) / groups, tiles, (int64_t)kMaxParts}));
+  const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries) * a.kv_heads;
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kKeys, a.causal && a.n_q == a.n_k, 1.0, 1.6,
+                    4.0 * a.n_q * a.heads * (a.head_dim + 4));
 }
 
 template <typename T, int HD>

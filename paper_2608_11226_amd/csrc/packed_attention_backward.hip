@@ -16,33 +16,142 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// lse in units of log 2 (+inf where a query has no keys: its probabilities are then 0) and D of every token and head,
-// [n_q][heads].  A wave takes 64 * 16 bytes of rows at a time.
+// Queries' gradients.  A workgroup takes 128 rows, a row being a token's query of one of the heads that share a key's, a wave 32 of
+// them, whose q and do stay in registers, and walks over tiles of 32 keys.  Scores have keys as rows and queries as columns, as
+// in the forward pass, and where there are few rows the keys are dealt out to several workgroups as there.  It leaves lse and D
+// of every row behind ([n_q][heads]), which the keys' gradients need.
+constexpr int kDqRows = 32 * kWaves, kDqKeys = 32;
+
 template <typename T, int HD>
-__global__ __launch_bounds__(256) void k_attention_delta(AttentionGradArgs A, float2* __restrict__ stats) {
-  constexpr int kLanes = HD / Chunk16<T>::N;  // of a row of a head
-  const int64_t total = (int64_t)A.n_q * A.heads;
-  const int64_t at = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
-  if (at >= total) return;
-  const int64_t row = at / A.heads;
-  const int head = (int)(at - row * A.heads);
-  const int c = head * HD + (int)(threadIdx.x % kLanes) * Chunk16<T>::N;
-  float o[Chunk16<T>::N], d[Chunk16<T>::N];
-  unpack16(load16((const T*)A.out + row * A.out_stride + c), o);
-  unpack16(load16((const T*)A.dout + row * A.dout_stride + c), d);
-  float sum = 0.f;
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, int slots, int parts,
+                                                                                 float2* __restrict__ stats,
+                                                                                 float* __restrict__ partial) {
+  typedef Rows<T, HD> R;
+  typedef typename R::Frag Frag;
+  constexpr int S = sizeof(T) == 2 ? 3 : 2;
+  __shared__ __align__(16) char s_k[S][kDqKeys * R::kBytes];
+  __shared__ __align__(16) char s_v[S][kDqKeys * R::kBytes];
+  const int w = neighbours_on_die(slots * A.kv_heads * parts);
+  if (w < 0) return;
+  const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
+  int seq, t0;
+  Sequence sq;
+  if (!find_tile<kDqRows>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, slots - 1 - w / parts % slots, lane, &seq, &sq, &t0)) return;
+  const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
+  const int behind = sk.len - sq.len, n_rows = sq.len * each;
+  const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
+  const int token = r / each, head = kvh * each + r % each;
+  const size_t row = (size_t)sq.start + token;
+  Frag qf[HD / 16], df[HD / 16];
+  float2 my = make_float2(0.f, 0.f);  // lse in units of log 2, and D
+  {
+    const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
+    const T* dp = (const T*)A.dout + row * A.dout_stride + (size_t)head * HD + 8 * half;
+    const T* op = (const T*)A.out + row * A.out_stride + (size_t)head * HD + 8 * half;
 #pragma unroll
-  for (int i = 0; i < Chunk16<T>::N; ++i) sum = fmaf(o[i], d[i], sum);
+    for (int c = 0; c < HD / 16; ++c) {
+      qf[c] = load_operand(qp + 16 * c), df[c] = load_operand(dp + 16 * c);
+      const Frag o = load_operand(op + 16 * c);
 #pragma unroll
-  for (int i = kLanes / 2; i > 0; i >>= 1) sum += __shfl_xor(sum, i, 64);
-  if (threadIdx.x % kLanes == 0) {
-    const float l = A.lse[(size_t)head * A.n_q + row];
-    stats[at] = make_float2(l == -INFINITY ? INFINITY : l * kLog2e, sum);
+      for (int e = 0; e < 8; ++e) my.y = fmaf((float)o[e], (float)df[c][e], my.y);
+    }
+    my.y += __shfl_xor(my.y, 32, 64);
+    // a query without keys: no probabilities
+    const float lse = A.lse[(size_t)head * A.n_q + row];
+    my.x = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    if (part == 0 && half == 0 && w_first + a < n_rows) stats[row * A.heads + head] = my;
   }
+  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
+  const int mine = keys_to(token);
+  // a wave behind the last row has nothing to do
+  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
+  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
+  const int all = (keys_to((min(t0 + kDqRows, n_rows) - 1) / each) + kDqKeys - 1) / kDqKeys;
+  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
+
+  const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
+  const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
+  const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
+  auto load = [&](auto buf, int it) {
+    const int k0 = (first + it) * kDqKeys, last = sk.len - 1 - k0;
+    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
+    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
+  };
+  RowReader<T, HD> rows(lane);
+  ColReader<T, HD> cols(lane);
+#pragma unroll
+  for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]), "+v"(df[c]));  // here: no wait for them among the tiles
+
+  f32x16 dq[HD / 32];
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d) clear(dq[d]);
+  const float c2 = A.scale * kLog2e;
+  through_tiles<S, 2 * R::loads(kDqKeys, kWaves)>(tiles, load, [&](auto buf, int it) {
+    const int k0 = (first + it) * kDqKeys;
+    if (k0 >= w_most) return;  // (the same for the whole wave)
+    rows.renew();
+    cols.renew();
+    f32x16 s, dp;
+    clear(s);
+    clear(dp);
+    constexpr int C = HD / 16, D = HD / 32;
+    Frag fr[2][2], fc[2][D];
+    auto read_row = [&](auto g, Frag(&f)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_k[buf] : s_v[buf], 0, (2 * g + k) % C);
+    };
+    auto read_col = [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) f[d] = cols(s_k[buf], 16 * g, d);
+    };
+    read_row(std::integral_constant<int, 0>(), fr[0]);
+    groups<C, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        if constexpr (2 * g < C)
+          mma(f[k], qf[(2 * g + k) % C], s);
+        else
+          mma(f[k], df[(2 * g + k) % C], dp);
+      }
+    });
+    read_col(std::integral_constant<int, 0>(), fc[0]);
+    if (k0 + kDqKeys > w_least) {
+      int limit = mine;
+      asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (k0 + 16 * (e >> 3) + 8 * half + (e & 7) >= limit) s[e] = -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dp[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my.x)) * (dp[e] - my.y);
+    Frag ds[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) operand_of(dp, i, ds[i]);
+    groups<2, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
+    });
+  });
+  if (w_first + a >= n_rows) return;
+  if (parts > 1) {
+    float* out = partial + (((size_t)part * A.n_q + row) * A.heads + head) * HD + 8 * half;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
+    return;
+  }
+  T* out = (T*)A.dq + row * A.dq_stride + (size_t)head * HD + 8 * half;
+#pragma unroll
+  for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
 }
 
 // Keys' gradients.  A workgroup takes 128 keys, a wave 32 of them, whose k and v stay in registers, and walks over tiles of 32
-// rows, a row being a token's query of one of the heads that share the keys.  Scores have queries as rows and keys as columns,
+// rows.  Scores have queries as rows and keys as columns,
 // so that a lane holds one key's.
 constexpr int kBackKeys = 32 * kWaves, kBackRows = 32;
 
@@ -211,128 +320,6 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     for (int i = 0; i < 2; ++i) store8(dkp + 32 * d + 16 * i, dk[d], i, A.scale), store8(dvp + 32 * d + 16 * i, dv[d], i, 1.f);
 }
 
-// Queries' gradients.  A workgroup takes 128 rows, a wave 32 of them, whose q and do stay in registers, and walks over tiles of
-// 32 keys.  Scores have keys as rows and queries as columns, as in the forward pass, and where there are few rows the keys are
-// dealt out to several workgroups as there.
-constexpr int kDqRows = 32 * kWaves, kDqKeys = 32;
-
-template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, int slots, int parts,
-                                                                                 const float2* __restrict__ stats,
-                                                                                 float* __restrict__ partial) {
-  typedef Rows<T, HD> R;
-  typedef typename R::Frag Frag;
-  constexpr int S = sizeof(T) == 2 ? 3 : 2;
-  __shared__ __align__(16) char s_k[S][kDqKeys * R::kBytes];
-  __shared__ __align__(16) char s_v[S][kDqKeys * R::kBytes];
-  const int w = neighbours_on_die(slots * A.kv_heads * parts);
-  if (w < 0) return;
-  const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
-  int seq, t0;
-  Sequence sq;
-  if (!find_tile<kDqRows>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, slots - 1 - w / parts % slots, lane, &seq, &sq, &t0)) return;
-  const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
-  const int behind = sk.len - sq.len, n_rows = sq.len * each;
-  const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
-  const int token = r / each, head = kvh * each + r % each;
-  const size_t row = (size_t)sq.start + token;
-  Frag qf[HD / 16], df[HD / 16];
-  {
-    const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
-    const T* dp = (const T*)A.dout + row * A.dout_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-    for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c), df[c] = load_operand(dp + 16 * c);
-  }
-  const float2 my = stats[row * A.heads + head];
-  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
-  const int mine = keys_to(token);
-  // a wave behind the last row has nothing to do
-  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
-  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
-  const int all = (keys_to((min(t0 + kDqRows, n_rows) - 1) / each) + kDqKeys - 1) / kDqKeys;
-  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
-
-  const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
-  const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
-  const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
-  auto load = [&](auto buf, int it) {
-    const int k0 = (first + it) * kDqKeys, last = sk.len - 1 - k0;
-    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
-    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
-  };
-  RowReader<T, HD> rows(lane);
-  ColReader<T, HD> cols(lane);
-#pragma unroll
-  for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]), "+v"(df[c]));  // here: no wait for them among the tiles
-
-  f32x16 dq[HD / 32];
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d) clear(dq[d]);
-  const float c2 = A.scale * kLog2e;
-  through_tiles<S, 2 * R::loads(kDqKeys, kWaves)>(tiles, load, [&](auto buf, int it) {
-    const int k0 = (first + it) * kDqKeys;
-    if (k0 >= w_most) return;  // (the same for the whole wave)
-    rows.renew();
-    cols.renew();
-    f32x16 s, dp;
-    clear(s);
-    clear(dp);
-    constexpr int C = HD / 16, D = HD / 32;
-    Frag fr[2][2], fc[2][D];
-    auto read_row = [&](auto g, Frag(&f)[2]) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_k[buf] : s_v[buf], 0, (2 * g + k) % C);
-    };
-    auto read_col = [&](auto g, Frag(&f)[D]) {
-#pragma unroll
-      for (int d = 0; d < D; ++d) f[d] = cols(s_k[buf], 16 * g, d);
-    };
-    read_row(std::integral_constant<int, 0>(), fr[0]);
-    groups<C, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if constexpr (2 * g < C)
-          mma(f[k], qf[(2 * g + k) % C], s);
-        else
-          mma(f[k], df[(2 * g + k) % C], dp);
-      }
-    });
-    read_col(std::integral_constant<int, 0>(), fc[0]);
-    if (k0 + kDqKeys > w_least) {
-      int limit = mine;
-      asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (k0 + 16 * (e >> 3) + 8 * half + (e & 7) >= limit) s[e] = -INFINITY;
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) dp[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my.x)) * (dp[e] - my.y);
-    Frag ds[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) operand_of(dp, i, ds[i]);
-    groups<2, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
-#pragma unroll
-      for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
-    });
-  });
-  if (w_first + a >= n_rows) return;
-  if (parts > 1) {
-    float* out = partial + (((size_t)part * A.n_q + row) * A.heads + head) * HD + 8 * half;
-#pragma unroll
-    for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
-    return;
-  }
-  T* out = (T*)A.dq + row * A.dq_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
-}
-
 // Eight neighbours of the parts' sums, in order, to an output.
 template <typename T>
 __device__ __forceinline__ void join8(T* out, const float* p, size_t apart, int parts) {
@@ -382,18 +369,15 @@ __global__ __launch_bounds__(256) void k_attention_join_dq(AttentionGradArgs A, 
   }
 }
 
-// The rows' parts of a tile of keys, and the keys' parts of a tile of rows, where the tiles alone give fewer workgroups than
-// kEnough; each part has 4 tiles where a sequence has its share of the tokens.
-constexpr int kEnough = 1024, kMaxParts = 64;
-int parts_of(int64_t groups, int64_t tiles) {
-  return (int)std::max<int64_t>(1, std::min({(kEnough + groups - 1) / groups, tiles / 4, (int64_t)kMaxParts}));
-}
 int row_parts(const AttentionArgs& a) {
-  const int each = a.heads / a.kv_heads;
-  return parts_of((int64_t)tile_slots(a.n_k, 1, a.n_seqs, kBackKeys) * a.kv_heads, (int64_t)a.n_q * each / a.n_seqs / kBackRows);
+  const int64_t walks = (int64_t)tile_slots(a.n_k, 1, a.n_seqs, kBackKeys) * a.kv_heads;
+  return walk_parts(walks, (double)a.n_q * (a.heads / a.kv_heads) / a.n_seqs / kBackRows, a.causal && a.n_q == a.n_k, 1.3, 2.0,
+                    8.0 * a.n_k * a.kv_heads * a.head_dim);
 }
 int key_parts(const AttentionArgs& a) {
-  return parts_of((int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows) * a.kv_heads, (int64_t)a.n_k / a.n_seqs / kDqKeys);
+  const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows) * a.kv_heads;
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k, 1.0, 1.4,
+                    4.0 * a.n_q * a.heads * a.head_dim);
 }
 
 size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
@@ -401,15 +385,13 @@ size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   float2* stats = (float2*)ws;
-  float* partial = (float*)(ws + stats_bytes(a));  // of the keys, then of the queries
-  const int per = 256 / (HD / Chunk16<T>::N);
-  k_attention_delta<T, HD><<<(unsigned)(((int64_t)a.n_q * a.heads + per - 1) / per), 256, 0, s>>>(a, stats);
-  const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys), rp = row_parts(a);
-  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, slots, rp, stats, partial);
-  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, slots, rp, partial);
+  float* partial = (float*)(ws + stats_bytes(a));  // of the queries, then of the keys
   const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts(a);
   k_attention_dq<T, HD><<<die_grid(q_slots * a.kv_heads * kp), 64 * kWaves, 0, s>>>(a, q_slots, kp, stats, partial);
   if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
+  const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys), rp = row_parts(a);
+  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, slots, rp, stats, partial);
+  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, slots, rp, partial);
   return hipGetLastError();
 }
 
