@@ -72,7 +72,8 @@ __device__ __forceinline__ void store8(float* p, const f32x16& c, int i, float b
 }
 
 // A run of rows in LDS, HD values each, without gaps.  The 16-byte chunks of a row stand in an order of its own (chunk c at
-// c ^ swizzle(row)), so that the 16 rows of a row read and the four rows of a transposing read fall on different banks.
+// c ^ swizzle(row)): the 16 rows that a row read takes at a time differ in it, and the four rows of two neighbouring transposing
+// reads fall on banks of their own.
 template <typename T, int HD>
 struct Rows {
   static constexpr int kBytes = HD * (int)sizeof(T);  // of a row
@@ -80,8 +81,8 @@ struct Rows {
   typedef typename Operand<T>::Frag Frag;
 
   static __host__ __device__ constexpr int swizzle(int row) {
-    if constexpr (kChunks >= 16) return ((row & 7) << 1) | ((row >> 3) & 1);
-    if constexpr (kChunks == 8) return (row & 6) | ((row >> 3) & 1);
+    if constexpr (kChunks >= 16) return ((row & 3) << 2) | ((row >> 2) & 3);
+    if constexpr (kChunks == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
     return (row >> 2) & 3;
   }
   // byte offset of chunk c of a row
@@ -205,29 +206,43 @@ __device__ __forceinline__ Sequence sequence_at(const int32_t* starts, const int
 // n * each / B + n_seqs of them, so no list of tiles has to be made first.  Numbers that no tile has are skipped.
 __host__ __device__ __forceinline__ int tile_slots(int n, int each, int n_seqs, int B) { return n * each / B + n_seqs; }
 
-// The sequence of a tile number and the tile's first row in it; false: no such tile.  64 lanes probe at a time; whatever the
-// starts hold, only entries 0 .. n_seqs are read.
+// A tile of one side's rows (`mine`, with `each` rows a token): its sequence, there and on the other side, and its first row.
+struct Place {
+  Sequence mine, other;
+  int row;
+};
+struct Side {
+  const int32_t *starts, *lens;
+  int n;
+};
+__device__ __forceinline__ Side queries_of(const AttentionArgs& A) { return {A.q_starts, A.q_lens, A.n_q}; }
+__device__ __forceinline__ Side keys_of(const AttentionArgs& A) { return {A.k_starts, A.k_lens, A.n_k}; }
+
+// false: no tile has the number.  64 lanes probe at a time, each with all that there is to know of its sequence, so that the last
+// probe's answer is at hand without another trip to memory.  Whatever the starts hold, only entries 0 .. n_seqs are read.
 template <int B>
-__device__ __forceinline__ bool find_tile(const int32_t* starts, const int32_t* lens, int n_seqs, int n, int each, int slot, int lane,
-                                          int* seq, Sequence* sq, int* row) {
+__device__ __forceinline__ bool find_tile(const Side& mine, const Side& other, int n_seqs, int each, int slot, int lane, Place* p) {
   int lo = 0, hi = n_seqs;
-  do {
-    const int step = (hi - lo + 63) >> 6, s = lo + lane * step;
-    const bool before = s < hi && max(0, min(starts[s], n)) * each / B + s <= slot;
-    const int k = __popcll(__ballot(before)) - 1;
+  for (;;) {
+    const int step = (hi - lo + 63) >> 6, at = lo + lane * step, s = min(at, hi - 1);
+    const Sequence x = sequence_at(mine.starts, mine.lens, s, mine.n), y = sequence_at(other.starts, other.lens, s, other.n);
+    const int first = x.start * each / B + s;
+    const int k = __popcll(__ballot(at < hi && first <= slot)) - 1;
     if (k < 0) return false;
+    if (step == 1) {
+      p->mine = {__builtin_amdgcn_readlane(x.start, k), __builtin_amdgcn_readlane(x.len, k)};
+      p->other = {__builtin_amdgcn_readlane(y.start, k), __builtin_amdgcn_readlane(y.len, k)};
+      p->row = (slot - __builtin_amdgcn_readlane(first, k)) * B;
+      return p->row >= 0 && p->row < p->mine.len * each;
+    }
     lo += k * step;
     hi = min(lo + step, hi);
-  } while (hi - lo > 1);
-  *seq = __builtin_amdgcn_readfirstlane(lo);
-  *sq = sequence_at(starts, lens, *seq, n);
-  *row = (slot - (sq->start * each / B + *seq)) * B;
-  return *row >= 0 && *row < sq->len * each;
+  }
 }
 
 // Tiles 0 .. n - 1 pass through S buffers in LDS, S - 1 of them on the way at a time.  load(buffer, tile) issues a tile's loads,
 // LOADS of each wave at least as its last ones; step(buffer, tile) works on one.  The buffer is a compile-time number, so that
-// it is part of the LDS instructions' offsets.
+// it is part of the LDS instructions' offsets.  first_tiles comes before what else a workgroup has to read.
 template <int S, int LOADS, int B = 0, typename Load, typename Step>
 __device__ __forceinline__ bool one_tile(int it, int n, Load& load, Step& step) {
   if (it >= n) return false;
@@ -241,11 +256,14 @@ __device__ __forceinline__ bool one_tile(int it, int n, Load& load, Step& step) 
   if constexpr (B + 1 < S) return one_tile<S, LOADS, B + 1>(it + 1, n, load, step);
   return true;
 }
-template <int S, int LOADS, typename Load, typename Step>
-__device__ __forceinline__ void through_tiles(int n, Load load, Step step) {
+template <int S, typename Load>
+__device__ __forceinline__ void first_tiles(int n, Load& load) {
   static_assert(S == 2 || S == 3, "the wait before the last tile but one is for all");
   if (n > 0) load(std::integral_constant<int, 0>(), 0);
   if (S > 2 && n > 1) load(std::integral_constant<int, 1>(), 1);
+}
+template <int S, int LOADS, typename Load, typename Step>
+__device__ __forceinline__ void through_tiles(int n, Load& load, Step step) {
   for (int it = 0; one_tile<S, LOADS>(it, n, load, step); it += S) {
   }
 }
@@ -276,13 +294,19 @@ __device__ __forceinline__ int neighbours_on_die(int total) {
 // Into how many parts the walks of a launch over `tiles` tiles each are cut, whose sums a second launch joins: by what a whole
 // walk takes (alone_us a tile, or shared_us a tile in every one of the card's 512 places where there are more walks than
 // places), the third of a walk that the last ones run on, and the parts' sums, which are written and read again.
-inline int walk_parts(int64_t walks, double tiles, bool triangle, double alone_us, double shared_us, double part_bytes) {
+// No more parts than their sums have room for: the workspace of a large call has to do for small ones, which have more parts, so
+// it goes by the size of a part's sums alone.
+constexpr int kMaxParts = 64;
+constexpr uint64_t kPartsRoom = 256ull << 20;
+inline uint64_t parts_room(uint64_t part_bytes) { return std::min(kMaxParts * part_bytes, kPartsRoom); }
+inline int walk_parts(int64_t walks, double tiles, bool triangle, double alone_us, double shared_us, uint64_t part_bytes) {
   const double places = 512.0, all = (triangle ? 0.55 : 1.0) * (double)walks * tiles * shared_us / places;
+  const int most = (int)std::max<uint64_t>(1, parts_room(part_bytes) / part_bytes);
   int best = 1;
   double least = 0.0;
-  for (int p = 1; p <= 64 && (p == 1 || tiles >= 4.0 * p); ++p) {
+  for (int p = 1; p <= most && (p == 1 || tiles >= 4.0 * p); ++p) {
     const double walk = alone_us * tiles / p + 3.0;
-    const double cost = std::max(walk, all) + 0.35 * walk + (p > 1 ? 5.0 + 2.0 * p * part_bytes / 4.5e6 : 0.0);
+    const double cost = std::max(walk, all) + 0.35 * walk + (p > 1 ? 5.0 + 2.0 * p * (double)part_bytes / 4.5e6 : 0.0);
     if (p == 1 || cost < least) best = p, least = cost;
   }
   return best;

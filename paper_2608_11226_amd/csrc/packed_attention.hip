@@ -44,20 +44,16 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
-  int seq, t0;
-  Sequence sq;
+  Place at;
   // a sequence's last queries, which have the most keys, first
-  if (!find_tile<kQueries>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, slots - 1 - w / parts % slots, lane, &seq, &sq, &t0)) return;
-  const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
+  if (!find_tile<kQueries>(queries_of(A), keys_of(A), A.n_seqs, each, slots - 1 - w / parts % slots, lane, &at)) return;
+  const Sequence sq = at.mine, sk = at.other;
+  const int t0 = at.row;
 
   const int behind = sk.len - sq.len, n_rows = sq.len * each;  // causal: token i attends keys 0 .. i + behind
   const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
   const int token = r / each, head = kvh * each + r % each;
   const size_t row = (size_t)sq.start + token;
-  Frag qf[HD / 16];
-  const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-  for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c);
   auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
   const int mine = keys_to(token);  // of this lane's query
   // of the wave's; a wave behind the last row has nothing to do
@@ -74,6 +70,11 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
     R::template load<kKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
     R::template load<kKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
   };
+  first_tiles<2>(tiles, load);
+  Frag qf[HD / 16];
+  const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
+#pragma unroll
+  for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c);
 #pragma unroll
   for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]));  // here: no wait for it among the tiles
   RowReader<T, HD> rows(lane);
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] *= shrink;
     }
-    // bf16 probabilities: each is off by at most 2^-9 of itself, as far as the output's own rounding moves it, and the
+    // bf16 probabilities: each is off by at most 2^-8 of itself, as far as the output's own rounding moves it, and the
     // errors of many keys largely cancel; their sum is that of the unrounded ones
     Frag p[2 * B];
 #pragma unroll
@@ -176,11 +177,11 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void k_attention_merge(AttentionArgs A, int slots, int parts, const float* __restrict__ partial) {
   const int each = A.heads / A.kv_heads, kvh = (int)blockIdx.x / slots;
-  int seq, t0;
-  Sequence sq;
-  if (!find_tile<kQueries>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, (int)blockIdx.x % slots, threadIdx.x & 63, &seq, &sq, &t0)) return;
+  Place at;
+  if (!find_tile<kQueries>(queries_of(A), keys_of(A), A.n_seqs, each, (int)blockIdx.x % slots, threadIdx.x & 63, &at)) return;
+  const Sequence sq = at.mine;
   constexpr int kLanes = HD / 4;
-  const int r = t0 + (int)blockIdx.y * (256 / kLanes) + threadIdx.x / kLanes, c = 4 * (threadIdx.x % kLanes);
+  const int r = at.row + (int)blockIdx.y * (256 / kLanes) + threadIdx.x / kLanes, c = 4 * (threadIdx.x % kLanes);
   if (r >= sq.len * each) return;
   const size_t row = (size_t)sq.start + r / each;
   const int head = kvh * each + r % each;
@@ -210,10 +211,10 @@ __global__ __launch_bounds__(256) void k_attention_merge(AttentionArgs A, int sl
   if (c == 0) A.lse[(size_t)head * A.n_q + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
+uint64_t part_bytes(const AttentionArgs& a) { return 4ull * a.n_q * a.heads * (a.head_dim + 4); }
 int key_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries) * a.kv_heads;
-  return walk_parts(walks, (double)a.n_k / a.n_seqs / kKeys, a.causal && a.n_q == a.n_k, 1.0, 1.6,
-                    4.0 * a.n_q * a.heads * (a.head_dim + 4));
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kKeys, a.causal && a.n_q == a.n_k, 1.0, 1.6, part_bytes(a));
 }
 
 template <typename T, int HD>
@@ -233,10 +234,7 @@ hipError_t launch_of(hipStream_t s, const AttentionArgs& a, float* partial) {
 
 }  // namespace
 
-size_t packed_attention_workspace(const AttentionArgs& a) {
-  const int parts = key_parts(a);
-  return parts > 1 ? (size_t)parts * a.n_q * a.heads * (a.head_dim + 4) * 4 : 0;
-}
+size_t packed_attention_workspace(const AttentionArgs& a) { return parts_room(part_bytes(a)); }
 
 hipError_t launch_packed_attention(hipStream_t s, int dtype, const AttentionArgs& a, void* ws) {
   return dtype == ROLLOUT_DTYPE_BF16 ? launch_of<uint16_t>(s, a, (float*)ws) : launch_of<float>(s, a, (float*)ws);

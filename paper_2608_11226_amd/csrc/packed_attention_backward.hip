@@ -7,7 +7,7 @@
 // do so, one for the keys' gradients and one for the queries': seven products of the size of q k^T where one that adds up
 // queries' gradients atomically has five, but every sum has an order of its own that does not depend on scheduling.
 //
-// Probabilities and ds enter the second products as bf16 where the inputs are bf16: each is off by at most 2^-9 of itself, as
+// Probabilities and ds enter the second products as bf16 where the inputs are bf16: each is off by at most 2^-8 of itself, as
 // far as the result's own rounding moves it.
 #include "packed_attention.h"
 
@@ -18,8 +18,8 @@ constexpr int kWaves = 4;
 
 // Queries' gradients.  A workgroup takes 128 rows, a row being a token's query of one of the heads that share a key's, a wave 32 of
 // them, whose q and do stay in registers, and walks over tiles of 32 keys.  Scores have keys as rows and queries as columns, as
-// in the forward pass, and where there are few rows the keys are dealt out to several workgroups as there.  It leaves lse and D
-// of every row behind ([n_q][heads]), which the keys' gradients need.
+// in the forward pass, and where there are few rows the keys are dealt out to several workgroups as there.  It leaves
+// -lse / scale and -D of every row behind ([n_q][heads]), which the keys' gradients need.
 constexpr int kDqRows = 32 * kWaves, kDqKeys = 32;
 
 template <typename T, int HD>
@@ -36,14 +36,31 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
-  int seq, t0;
-  Sequence sq;
-  if (!find_tile<kDqRows>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, each, slots - 1 - w / parts % slots, lane, &seq, &sq, &t0)) return;
-  const Sequence sk = sequence_at(A.k_starts, A.k_lens, seq, A.n_k);
+  Place at;
+  if (!find_tile<kDqRows>(queries_of(A), keys_of(A), A.n_seqs, each, slots - 1 - w / parts % slots, lane, &at)) return;
+  const Sequence sq = at.mine, sk = at.other;
+  const int t0 = at.row;
   const int behind = sk.len - sq.len, n_rows = sq.len * each;
   const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
   const int token = r / each, head = kvh * each + r % each;
   const size_t row = (size_t)sq.start + token;
+  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
+  const int mine = keys_to(token);
+  // a wave behind the last row has nothing to do
+  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
+  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
+  const int all = (keys_to((min(t0 + kDqRows, n_rows) - 1) / each) + kDqKeys - 1) / kDqKeys;
+  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
+
+  const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
+  const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
+  const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
+  auto load = [&](auto buf, int it) {
+    const int k0 = (first + it) * kDqKeys, last = sk.len - 1 - k0;
+    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
+    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
+  };
+  first_tiles<S>(tiles, load);
   Frag qf[HD / 16], df[HD / 16];
   float2 my = make_float2(0.f, 0.f);  // lse in units of log 2, and D
   {
@@ -61,24 +78,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     // a query without keys: no probabilities
     const float lse = A.lse[(size_t)head * A.n_q + row];
     my.x = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    if (part == 0 && half == 0 && w_first + a < n_rows) stats[row * A.heads + head] = my;
+    if (part == 0 && half == 0 && w_first + a < n_rows) stats[row * A.heads + head] = make_float2(lse == -INFINITY ? lse : -lse / A.scale, -my.y);
   }
-  auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
-  const int mine = keys_to(token);
-  // a wave behind the last row has nothing to do
-  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
-  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
-  const int all = (keys_to((min(t0 + kDqRows, n_rows) - 1) / each) + kDqKeys - 1) / kDqKeys;
-  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
-
-  const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
-  const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
-  const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
-  auto load = [&](auto buf, int it) {
-    const int k0 = (first + it) * kDqKeys, last = sk.len - 1 - k0;
-    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
-    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
-  };
   RowReader<T, HD> rows(lane);
   ColReader<T, HD> cols(lane);
 #pragma unroll
@@ -164,37 +165,24 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   constexpr int S = sizeof(T) == 2 ? 3 : 2;
   __shared__ __align__(16) char s_q[S][kBackRows * R::kBytes];
   __shared__ __align__(16) char s_do[S][kBackRows * R::kBytes];
-  __shared__ __align__(16) float2 s_stat[S][kBackRows];
-  // 128 dimensions in bf16: registers for all of k and v are some 20 too many, and six of v's eight operands lie in LDS (as
-  // much as two workgroups of a compute unit have room for)
-  constexpr int C = HD / 16, D = HD / 32, kKept = sizeof(T) == 2 && HD == 128 ? 2 : C;
+  __shared__ __align__(16) float s_stat[S][2][kBackRows];
+  // 128 dimensions: registers for all of k and v are some 20 too many, and six of v's eight operands lie in LDS (as much as two
+  // workgroups of a compute unit have room for), in fp32, with one workgroup there, all of them
+  constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 ? 2 : 0;
   __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
   const int w = neighbours_on_die(slots * A.kv_heads * parts);
   if (w < 0) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = A.heads / A.kv_heads, kvh = w / slots / parts, part = w / slots % parts;
-  int seq, t0;
-  Sequence sk;
-  if (!find_tile<kBackKeys>(A.k_starts, A.k_lens, A.n_seqs, A.n_k, 1, w % slots, lane, &seq, &sk, &t0)) return;
-  const Sequence sq = sequence_at(A.q_starts, A.q_lens, seq, A.n_q);
+  Place at;
+  if (!find_tile<kBackKeys>(keys_of(A), queries_of(A), A.n_seqs, 1, w % slots, lane, &at)) return;
+  const Sequence sk = at.mine, sq = at.other;
+  const int t0 = at.row;
   const int behind = sk.len - sq.len, n_rows = sq.len * each;
 
   const int w_first = t0 + 32 * wave, kj = w_first + a;
   const size_t row = (size_t)sk.start + min(kj, sk.len - 1);
-  Frag kf[C], vf[kKept];
-  {
-    const T* kp = (const T*)A.k + row * A.k_stride + (size_t)kvh * HD + 8 * half;
-    const T* vp = (const T*)A.v + row * A.v_stride + (size_t)kvh * HD + 8 * half;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      kf[c] = load_operand(kp + 16 * c);
-      if (c < kKept)
-        vf[c < kKept ? c : 0] = load_operand(vp + 16 * c);
-      else
-        s_v[wave][c - kKept][lane] = load_operand(vp + 16 * c);
-    }
-  }
   // causal: key j is attended from token j - behind on
   auto from = [&](int j) { return A.causal ? max(0, min(j - behind, sq.len)) * each : 0; };
   const int head_tile = from(t0) / kBackRows, all = (n_rows + kBackRows - 1) / kBackRows - head_tile;
@@ -217,8 +205,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     const char* q0 = qb + (size_t)token * q_stride;
     const char* do0 = dob + (size_t)token * do_stride;
     if (wave == 0) {
-      const uint32_t x = (uint32_t)(min(lane >> 1, last) + over), t = x * inverse >> 16;
-      dma_lds4_at(sb + (size_t)token * A.heads, (t * (uint32_t)(A.heads - each) + x) * 8 + 4 * (lane & 1), s_stat[buf]);
+      const uint32_t x = (uint32_t)(min(a, last) + over), t = x * inverse >> 16;
+      dma_lds4_at(sb + (size_t)token * A.heads, (t * (uint32_t)(A.heads - each) + x) * 8 + 4 * half, s_stat[buf]);
     }
     R::template load_with<kBackRows, kWaves>(wave, lane, [&](int row, uint32_t offset, int place) {
       const uint32_t x = (uint32_t)(min(row, last) + over), t = x * inverse >> 16;
@@ -229,6 +217,20 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     token += more, over += more_over;
     if (over >= each) over -= each, ++token;
   };
+  first_tiles<S>(tiles, load);
+  Frag kf[C], vf[kKept ? kKept : 1];
+  {
+    const T* kp = (const T*)A.k + row * A.k_stride + (size_t)kvh * HD + 8 * half;
+    const T* vp = (const T*)A.v + row * A.v_stride + (size_t)kvh * HD + 8 * half;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      kf[c] = load_operand(kp + 16 * c);
+      if (c < kKept)
+        vf[c < kKept ? c : 0] = load_operand(vp + 16 * c);
+      else
+        s_v[wave][c - kKept][lane] = load_operand(vp + 16 * c);
+    }
+  }
   RowReader<T, HD> rows(lane);
   ColReader<T, HD> cols(lane);
   // here: no wait for them among the tiles
@@ -246,9 +248,14 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     if (i0 + kBackRows <= w_least) return;  // (the same for the whole wave)
     rows.renew();
     cols.renew();
+    // bf16: the sums start from -lse / scale and -D, which costs their last bits and no register
+    constexpr bool kStart = sizeof(T) == 2;
     f32x16 s, dp;
-    clear(s);
-    clear(dp);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      s[e] = kStart ? s_stat[buf][0][16 * (e >> 3) + 8 * half + (e & 7)] : 0.f;
+      dp[e] = kStart ? s_stat[buf][1][16 * (e >> 3) + 8 * half + (e & 7)] : 0.f;
+    }
     Frag fr[2][4], fc[2][D];
     auto read_row = [&](auto g, Frag(&f)[4]) {
 #pragma unroll
@@ -285,9 +292,9 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     }
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      const float2 x = s_stat[buf][16 * (e >> 3) + 8 * half + (e & 7)];
-      s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -x.x));
-      dp[e] = s[e] * (dp[e] - x.y);
+      const int i = 16 * (e >> 3) + 8 * half + (e & 7);
+      s[e] = __builtin_amdgcn_exp2f((kStart ? s[e] : s[e] + s_stat[buf][0][i]) * c2);
+      dp[e] = s[e] * (kStart ? dp[e] : dp[e] + s_stat[buf][1][i]);
     }
     Frag p[2], ds[2];
 #pragma unroll
@@ -339,10 +346,11 @@ __device__ __forceinline__ void join8(T* out, const float* p, size_t apart, int 
 
 // The parts' sums of a tile of keys.
 template <typename T>
-__global__ __launch_bounds__(256) void k_attention_join_dkv(AttentionGradArgs A, int slots, int parts, const float* __restrict__ partial) {
-  int seq, t0;
-  Sequence sk;
-  if (!find_tile<kBackKeys>(A.k_starts, A.k_lens, A.n_seqs, A.n_k, 1, (int)blockIdx.x, threadIdx.x & 63, &seq, &sk, &t0)) return;
+__global__ __launch_bounds__(256) void k_attention_join_dkv(AttentionGradArgs A, int parts, const float* __restrict__ partial) {
+  Place at;
+  if (!find_tile<kBackKeys>(keys_of(A), queries_of(A), A.n_seqs, 1, (int)blockIdx.x, threadIdx.x & 63, &at)) return;
+  const Sequence sk = at.mine;
+  const int t0 = at.row;
   const int width = A.kv_heads * A.head_dim, chunks = width / 8, rows = min(kBackKeys, sk.len - t0);
   const size_t all = (size_t)A.n_k * width;
   const bool v = blockIdx.y & 1;
@@ -358,9 +366,10 @@ __global__ __launch_bounds__(256) void k_attention_join_dkv(AttentionGradArgs A,
 // The parts' sums of a tile of 128 tokens.
 template <typename T>
 __global__ __launch_bounds__(256) void k_attention_join_dq(AttentionGradArgs A, int parts, const float* __restrict__ partial) {
-  int seq, t0;
-  Sequence sq;
-  if (!find_tile<128>(A.q_starts, A.q_lens, A.n_seqs, A.n_q, 1, (int)blockIdx.x, threadIdx.x & 63, &seq, &sq, &t0)) return;
+  Place at;
+  if (!find_tile<128>(queries_of(A), keys_of(A), A.n_seqs, 1, (int)blockIdx.x, threadIdx.x & 63, &at)) return;
+  const Sequence sq = at.mine;
+  const int t0 = at.row;
   const int width = A.heads * A.head_dim, chunks = width / 8, rows = min(128, sq.len - t0);
   for (int i = (int)blockIdx.y * 256 + threadIdx.x; i < rows * chunks; i += (int)gridDim.y * 256) {
     const size_t row = (size_t)sq.start + t0 + i / chunks;
@@ -369,15 +378,16 @@ __global__ __launch_bounds__(256) void k_attention_join_dq(AttentionGradArgs A, 
   }
 }
 
+uint64_t dkv_part_bytes(const AttentionArgs& a) { return 8ull * a.n_k * a.kv_heads * a.head_dim; }
+uint64_t dq_part_bytes(const AttentionArgs& a) { return 4ull * a.n_q * a.heads * a.head_dim; }
 int row_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_k, 1, a.n_seqs, kBackKeys) * a.kv_heads;
   return walk_parts(walks, (double)a.n_q * (a.heads / a.kv_heads) / a.n_seqs / kBackRows, a.causal && a.n_q == a.n_k, 1.3, 2.0,
-                    8.0 * a.n_k * a.kv_heads * a.head_dim);
+                    dkv_part_bytes(a));
 }
 int key_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows) * a.kv_heads;
-  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k, 1.0, 1.4,
-                    4.0 * a.n_q * a.heads * a.head_dim);
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k, 1.0, 1.4, dq_part_bytes(a));
 }
 
 size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
@@ -389,9 +399,10 @@ hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts(a);
   k_attention_dq<T, HD><<<die_grid(q_slots * a.kv_heads * kp), 64 * kWaves, 0, s>>>(a, q_slots, kp, stats, partial);
   if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
-  const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys), rp = row_parts(a);
+  const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys);
+  const int rp = row_parts(a);
   k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, slots, rp, stats, partial);
-  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, slots, rp, partial);
+  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, rp, partial);
   return hipGetLastError();
 }
 
@@ -403,10 +414,7 @@ hipError_t launch_of(hipStream_t s, const AttentionGradArgs& a, char* ws) {
 }  // namespace
 
 size_t packed_attention_backward_workspace(const AttentionArgs& a) {
-  const int rp = row_parts(a), kp = key_parts(a);
-  const size_t keys = rp > 1 ? (size_t)rp * 2 * a.n_k * a.kv_heads * a.head_dim * 4 : 0;
-  const size_t rows = kp > 1 ? (size_t)kp * a.n_q * a.heads * a.head_dim * 4 : 0;
-  return stats_bytes(a) + std::max(keys, rows);
+  return stats_bytes(a) + std::max(parts_room(dkv_part_bytes(a)), parts_room(dq_part_bytes(a)));
 }
 
 hipError_t launch_packed_attention_backward(hipStream_t s, int dtype, const AttentionGradArgs& a, void* ws) {
