@@ -91,8 +91,8 @@ struct Rows {
   // loads of a wave for N rows by NW waves (some waves have none where there are fewer than waves)
   static constexpr int loads(int N, int NW) { return N * kChunks / 64 >= NW ? N * kChunks / 64 / NW : 1; }
 
-  // Loads N rows from global memory straight into LDS, by NW waves.  issue(row, offset, place): what lane has to load of row
-  // `row`, 16 bytes at `offset` of it, and the bytes behind the tile's beginning where the wave's lands.
+  // N rows dealt out to loads of NW waves.  issue(row, offset, place): the row that the lane has 16 bytes of, at `offset` of it,
+  // and the bytes behind the tile's beginning where the wave's lie, the lane's 16 lane bytes behind that.
   template <int N, int NW, typename F>
   static __device__ __forceinline__ void load_with(int wave, int lane, F issue) {
     constexpr int kPer = 64 / kChunks;  // rows of an instruction
@@ -239,6 +239,67 @@ __device__ __forceinline__ bool find_tile(const Side& mine, const Side& other, i
     hi = min(lo + step, hi);
   }
 }
+
+// A wave's 32 rows of a sequence from row `first` on (n_rows of them in all), a row being a token's values of one of the `each`
+// heads that share a key's.  They come and go through LDS, whole rows at a time: lanes that read and wrote their own row, 16 bytes
+// of it with each instruction, would touch 32 lines with every one.
+template <typename T, int HD>
+struct WaveRows {
+  typedef Rows<T, HD> R;
+  int token, over, last;  // of the first row, the heads before it there, and the last row (< 32; rows behind it are copies of it)
+  uint32_t each, inverse;
+  __device__ __forceinline__ WaveRows(int first, int n_rows, int each)
+      : token(first / each), over(first - token * each), last(min(31, n_rows - 1 - first)), each((uint32_t)each), inverse(65536 / (uint32_t)each + 1) {}
+  // where row i lies behind the first token's first head, for tokens `stride` bytes apart (x / each = x inverse / 65536 for
+  // 0 <= x < 96, each <= 64)
+  __device__ __forceinline__ uint32_t offset(int i, uint32_t stride) const {
+    const uint32_t x = (uint32_t)(i + over), t = x * inverse >> 16;
+    return t * stride + (x - t * each) * R::kBytes;
+  }
+  // into the wave's 32 rows of LDS; p: the sequence's first token, at the first of the heads
+  __device__ __forceinline__ void load(char* lds, const T* p, int64_t stride, int lane) const {
+    const char* base = (const char*)(p + (size_t)token * stride);
+    R::template load_with<32, 1>(0, lane, [&](int row, uint32_t at, int place) {
+      dma_lds16_at(base, offset(min(row, last), (uint32_t)(stride * sizeof(T))) + at, lds + place);
+    });
+  }
+  // lane's row as an operand, once it is there
+  static __device__ __forceinline__ typename R::Frag operand(const char* lds, int lane, int c) {
+    const char* p = lds + R::at(lane & 31, (2 * c + (lane >> 5)) * ((int)sizeof(T) / 2));
+    if constexpr (sizeof(T) == 2) {
+      return *reinterpret_cast<const bf16x8*>(p);
+    } else {
+      const float4 lo = *reinterpret_cast<const float4*>(p);
+      const float4 hi = *reinterpret_cast<const float4*>(lds + R::at(lane & 31, (2 * c + (lane >> 5)) * 2 + 1));
+      return f32x8{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    }
+  }
+  // results with a row per lane, `by` times, through the wave's 32 rows of LDS
+  __device__ __forceinline__ void store(char* lds, const f32x16 (&o)[HD / 32], float by, T* p, int64_t stride, int lane) const {
+    const int a = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int c = (4 * d + 2 * i + half) * ((int)sizeof(T) / 2);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = o[d][8 * i + e] * by;
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<u32x4*>(lds + R::at(a, c)) = pack16(v);
+        } else {
+          *reinterpret_cast<float4*>(lds + R::at(a, c)) = make_float4(v[0], v[1], v[2], v[3]);
+          *reinterpret_cast<float4*>(lds + R::at(a, c + 1)) = make_float4(v[4], v[5], v[6], v[7]);
+        }
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    char* base = (char*)(p + (size_t)token * stride);
+    R::template load_with<32, 1>(0, lane, [&](int row, uint32_t at, int place) {
+      if (row > last) return;
+      *reinterpret_cast<u32x4*>(base + offset(row, (uint32_t)(stride * sizeof(T))) + at) = *reinterpret_cast<const u32x4*>(lds + place + 16 * lane);
+    });
+  }
+};
 
 // Tiles 0 .. n - 1 pass through S buffers in LDS, S - 1 of them on the way at a time.  load(buffer, tile) issues a tile's loads,
 // LOADS of each wave at least as its last ones; step(buffer, tile) works on one.  The buffer is a compile-time number, so that

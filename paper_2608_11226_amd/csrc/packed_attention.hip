@@ -37,8 +37,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
                                                                                      float* __restrict__ partial) {
   typedef Rows<T, HD> R;
   typedef typename R::Frag Frag;
-  __shared__ __align__(16) char s_k[2][kKeys * R::kBytes];
-  __shared__ __align__(16) char s_v[2][kKeys * R::kBytes];
+  __shared__ __align__(16) char s_kv[2][2][kKeys * R::kBytes];
+  static_assert(2 * kKeys == kQueries, "a tile's place holds the workgroup's rows");
   const int w = neighbours_on_die(slots * A.kv_heads * parts);
   if (w < 0) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
@@ -67,16 +67,19 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
   auto load = [&](auto buf, int it) {
     const int k0 = (first + it) * kKeys, last = sk.len - 1 - k0;
-    R::template load<kKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
-    R::template load<kKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
+    R::template load<kKeys, kWaves>(s_kv[buf][0], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
+    R::template load<kKeys, kWaves>(s_kv[buf][1], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
   };
   first_tiles<2>(tiles, load);
+  // the rows by way of the second tile's place
+  char* place = s_kv[1][0] + 32 * wave * R::kBytes;
+  const size_t heads = (size_t)kvh * each * HD;
+  const WaveRows<T, HD> my(min(w_first, n_rows - 1), n_rows, each);
   Frag qf[HD / 16];
-  const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
+  my.load(place, (const T*)A.q + (size_t)sq.start * A.q_stride + heads, A.q_stride, lane);
+  dma_wait();
 #pragma unroll
-  for (int c = 0; c < HD / 16; ++c) qf[c] = load_operand(qp + 16 * c);
-#pragma unroll
-  for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]));  // here: no wait for it among the tiles
+  for (int c = 0; c < HD / 16; ++c) qf[c] = my.operand(place, lane, c);
   RowReader<T, HD> rows(lane);
   ColReader<T, HD> cols(lane);
 
@@ -97,11 +100,11 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
     Frag fr[2][2], fc[2][D];
     auto read_row = [&](auto g, Frag(&f)[2]) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) f[k] = rows(s_k[buf], 32 * (2 * g / C), (2 * g + k) % C);
+      for (int k = 0; k < 2; ++k) f[k] = rows(s_kv[buf][0], 32 * (2 * g / C), (2 * g + k) % C);
     };
     auto read_col = [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-      for (int d = 0; d < D; ++d) f[d] = cols(s_v[buf], 16 * g, d);
+      for (int d = 0; d < D; ++d) f[d] = cols(s_kv[buf][1], 16 * g, d);
     };
     read_row(std::integral_constant<int, 0>(), fr[0]);
     groups<B * C / 2, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
@@ -152,9 +155,9 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
       for (int d = 0; d < D; ++d) mma(f[d], p[g], o[d]);
     });
   });
-  if (w_first + a >= n_rows) return;
   const float l = l_run + __shfl_xor(l_run, 32, 64);
   if (parts > 1) {
+    if (w_first + a >= n_rows) return;
     float* p = partial + partial_at<HD>(part, A, row, head);
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
@@ -165,12 +168,10 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   }
   // a query without keys: nothing, and the logarithm of nothing
   const float by = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
-  T* op = (T*)A.out + row * A.out_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) store8(op + 32 * d + 16 * i, o[d], i, by);
-  if (half == 0) A.lse[(size_t)head * A.n_q + row] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * kLn2;
+  lds_barrier();  // nobody reads tiles any more
+  if (w_first >= n_rows) return;
+  my.store(place, o, by, (T*)A.out + (size_t)sq.start * A.out_stride + heads, A.out_stride, lane);
+  if (half == 0 && w_first + a < n_rows) A.lse[(size_t)head * A.n_q + row] = l == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // The parts of the rows of a tile, in order: a thread takes four values of a row.

@@ -29,8 +29,9 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   typedef Rows<T, HD> R;
   typedef typename R::Frag Frag;
   constexpr int S = sizeof(T) == 2 ? 3 : 2;
-  __shared__ __align__(16) char s_k[S][kDqKeys * R::kBytes];
-  __shared__ __align__(16) char s_v[S][kDqKeys * R::kBytes];
+  __shared__ __align__(16) char s_kv[S][2][kDqKeys * R::kBytes];
+  __shared__ __align__(16) char s_rows[kDqRows * R::kBytes];
+  static_assert(4 * kDqKeys == kDqRows, "two tiles' places hold the workgroup's rows");
   const int w = neighbours_on_die(slots * A.kv_heads * parts);
   if (w < 0) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
@@ -57,33 +58,37 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   const char* vb = (const char*)((const T*)A.v + (size_t)sk.start * A.v_stride + (size_t)kvh * HD);
   auto load = [&](auto buf, int it) {
     const int k0 = (first + it) * kDqKeys, last = sk.len - 1 - k0;
-    R::template load<kDqKeys, kWaves>(s_k[buf], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
-    R::template load<kDqKeys, kWaves>(s_v[buf], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
+    R::template load<kDqKeys, kWaves>(s_kv[buf][0], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
+    R::template load<kDqKeys, kWaves>(s_kv[buf][1], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
   };
-  first_tiles<S>(tiles, load);
+  // the rows by way of LDS: q and do at once, out with the first tiles
+  char *place = s_rows + 32 * wave * R::kBytes, *other = s_kv[0][0] + 32 * wave * R::kBytes;
+  const size_t heads = (size_t)kvh * each * HD;
+  const WaveRows<T, HD> mine_of(min(w_first, n_rows - 1), n_rows, each);
+  mine_of.load(place, (const T*)A.q + (size_t)sq.start * A.q_stride + heads, A.q_stride, lane);
+  mine_of.load(other, (const T*)A.dout + (size_t)sq.start * A.dout_stride + heads, A.dout_stride, lane);
+  const float lse = A.lse[(size_t)head * A.n_q + row];
+  dma_wait();
   Frag qf[HD / 16], df[HD / 16];
+#pragma unroll
+  for (int c = 0; c < HD / 16; ++c) qf[c] = mine_of.operand(place, lane, c), df[c] = mine_of.operand(other, lane, c);
+  lds_barrier();
+  mine_of.load(place, (const T*)A.out + (size_t)sq.start * A.out_stride + heads, A.out_stride, lane);
+  first_tiles<S>(tiles, load);
   float2 my = make_float2(0.f, 0.f);  // lse in units of log 2, and D
-  {
-    const T* qp = (const T*)A.q + row * A.q_stride + (size_t)head * HD + 8 * half;
-    const T* dp = (const T*)A.dout + row * A.dout_stride + (size_t)head * HD + 8 * half;
-    const T* op = (const T*)A.out + row * A.out_stride + (size_t)head * HD + 8 * half;
+  dma_wait();
 #pragma unroll
-    for (int c = 0; c < HD / 16; ++c) {
-      qf[c] = load_operand(qp + 16 * c), df[c] = load_operand(dp + 16 * c);
-      const Frag o = load_operand(op + 16 * c);
+  for (int c = 0; c < HD / 16; ++c) {
+    const Frag o = mine_of.operand(place, lane, c);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) my.y = fmaf((float)o[e], (float)df[c][e], my.y);
-    }
-    my.y += __shfl_xor(my.y, 32, 64);
-    // a query without keys: no probabilities
-    const float lse = A.lse[(size_t)head * A.n_q + row];
-    my.x = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    if (part == 0 && half == 0 && w_first + a < n_rows) stats[row * A.heads + head] = make_float2(lse == -INFINITY ? lse : -lse / A.scale, -my.y);
+    for (int e = 0; e < 8; ++e) my.y = fmaf((float)o[e], (float)df[c][e], my.y);
   }
+  my.y += __shfl_xor(my.y, 32, 64);
+  // a query without keys: no probabilities
+  my.x = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  if (part == 0 && half == 0 && w_first + a < n_rows) stats[row * A.heads + head] = make_float2(lse == -INFINITY ? lse : -lse / A.scale, -my.y);
   RowReader<T, HD> rows(lane);
   ColReader<T, HD> cols(lane);
-#pragma unroll
-  for (int c = 0; c < HD / 16; ++c) asm volatile("" : "+v"(qf[c]), "+v"(df[c]));  // here: no wait for them among the tiles
 
   f32x16 dq[HD / 32];
 #pragma unroll
@@ -101,11 +106,11 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     Frag fr[2][2], fc[2][D];
     auto read_row = [&](auto g, Frag(&f)[2]) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_k[buf] : s_v[buf], 0, (2 * g + k) % C);
+      for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_kv[buf][0] : s_kv[buf][1], 0, (2 * g + k) % C);
     };
     auto read_col = [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-      for (int d = 0; d < D; ++d) f[d] = cols(s_k[buf], 16 * g, d);
+      for (int d = 0; d < D; ++d) f[d] = cols(s_kv[buf][0], 16 * g, d);
     };
     read_row(std::integral_constant<int, 0>(), fr[0]);
     groups<C, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
@@ -135,8 +140,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
       for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
     });
   });
-  if (w_first + a >= n_rows) return;
   if (parts > 1) {
+    if (w_first + a >= n_rows) return;
     float* out = partial + (((size_t)part * A.n_q + row) * A.heads + head) * HD + 8 * half;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
@@ -144,11 +149,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
       for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
     return;
   }
-  T* out = (T*)A.dq + row * A.dq_stride + (size_t)head * HD + 8 * half;
-#pragma unroll
-  for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
+  if (w_first >= n_rows) return;
+  mine_of.store(place, dq, A.scale, (T*)A.dq + (size_t)sq.start * A.dq_stride + heads, A.dq_stride, lane);
 }
 
 // Keys' gradients.  A workgroup takes 128 keys, a wave 32 of them, whose k and v stay in registers, and walks over tiles of 32
