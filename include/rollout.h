@@ -492,7 +492,7 @@ rollout_status rollout_attention_backward(const rollout_attention_shape* shape, 
  * the smallest power of two, 2^-126 at least, for which no |y| of the row, over it, is above 448, and d_y the codes of y over it, to
  * nearest, ties to even (NaN where y is not finite).  Matrices are dense, and rows may start at any element.
  * Errors: EINVAL (sizes, types, alignment, NULL buffers, overlap), EUNSUPPORTED (dim above 32,768,
- * rows whose launch would have 2^32 threads: 2^26 up to dim 2,048, 2^24 up to 8,192, 2^22 above), EDEVICE.
+ * rows whose launch would have 2^32 threads: 2^26 up to dim 1,024, 2^22 from 4,097 on), EDEVICE.
  */
 rollout_status rollout_rms_norm(const void* d_x, int32_t x_dtype, const void* d_delta, int32_t delta_dtype,
                                 const float* d_gain, int32_t n_rows, int32_t dim, float eps, void* d_h, void* d_y,
@@ -529,7 +529,7 @@ rollout_status rollout_rms_norm_backward(const void* d_grad_y, int32_t grad_y_dt
  * of a counter hash of (seed, t, the tensor's place in the table, the element): bf16 drops 16 bits of
  * the fp32 value's magnitude after adding r, e4m3 drops 20 after adding 16 r + 8 (below 2^-6, where values are 2^-9 apart,
  * from the magnitude plus 2^-6).  A scale is the smallest power of two, 2^-126 at least, that leaves no magnitude of
- * its 128 above 448; a second moment above 0 keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the
+ * its 128 above 448; a second moment of 2^-126 or more keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the
  * low 16 bits and v the high ones; a weight the low ones of f(h + (k >> 32)).  f is MurmurHash3's 32-bit
  * finaliser, k = F(F(seed + G t) + G (1 + tensor + 2^20 floor(i / 2^32))) with SplitMix64's finaliser F and constant G.
  * d_grad_scale fp32 [1] (a clipping factor, say; NULL: 1): where it is not finite nothing changes.  d_lr fp32 [1] and d_step

@@ -159,15 +159,16 @@ __device__ __forceinline__ void update(const AdamwEntry& E, const Factors& F, in
       const float d = g[e] * F.grad;
       m[e] = F.b1 * m[e] + F.c1 * d;
       v[e] = F.b2 * v[e] + F.c2 * (d * d);
-      root[e] = sqrtf(v[e]);
-      // (a reciprocal that is off by one unit moves the weight by that part of its step)
+      // (roots and reciprocals that are off by one unit: that part of a weight's step, or of a state's rounding)
+      root[e] = __builtin_amdgcn_sqrtf(v[e]);
       p[e] = p[e] * keep - F.step * m[e] * __builtin_amdgcn_rcpf(root[e] * F.root + F.eps);
       if constexpr (kEight) most_m = fmaxf(most_m, fabsf(m[e])), most_v = fmaxf(most_v, root[e]);
     }
     if constexpr (kEight || kCoarse) {
       uint32_t h[8];
+      const uint32_t start = (uint32_t)i * 0x9E3779B1u + (uint32_t)key;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) h[e] = finish32((uint32_t)(i + e) * 0x9E3779B1u + (uint32_t)key);
+      for (int e = 0; e < 8; ++e) h[e] = finish32(start + (uint32_t)e * 0x9E3779B1u);
       if constexpr (kEight) {
         const float ms = e4m3_scale(row_max(most_m)), vs = e4m3_scale(row_max(most_v));
         const float mb = 1.f / ms, vb = 1.f / vs;  // exact

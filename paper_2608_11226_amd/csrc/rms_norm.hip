@@ -3,15 +3,13 @@
 //   h = x + delta (rounded to x's type),  r = 1 / sqrt(mean h^2 + eps),  y = h r gain
 //   dx_i = r (t_i - xhat_i mean_k(t_k xhat_k)) + inner_i,  t = dy gain, xhat = h r;   dgain_i = sum over rows of dy_i xhat_i
 //
-// A row is read once and stays in registers, 8 neighbours of it per thread and step: of one wave up to 2,048 values, of four
-// up to 8,192, of sixteen up to 32,768.  An output in 8 bits (e4m3) takes a second reduction, the largest |y|, and has the
+// A row is read once and stays in registers, 8 neighbours of it per thread and step: of one wave up to 1,024 values, above that
+// of as many waves as make it one step, up to sixteen.  An output in 8 bits (e4m3) takes a second reduction, the largest |y|, and has the
 // smallest power of two as scale that brings it to at most 448: a power of two takes nothing from the 4 bits of a value.
 #include "update.h"
 
 namespace rollout {
 namespace {
-
-constexpr int kSteps = 4;  // of 8 values that a thread holds
 
 struct None {};
 
@@ -79,8 +77,8 @@ __device__ __forceinline__ float row_reduce(float v, float* red, F f) {
   return v;
 }
 
-// W threads a row (64: four rows in a workgroup).  D: type of what is added, or None.
-template <typename X, typename D, typename Y, int W>
+// W threads a row (64: four rows in a workgroup), S steps of 8 values each.  D: type of what is added, or None.
+template <typename X, typename D, typename Y, int W, int S>
 __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   constexpr bool kAdds = !std::is_same<D, None>::value;
   __shared__ float red[2][W / 64];
@@ -88,9 +86,9 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   const int64_t row = (int64_t)blockIdx.x * (W < 256 ? 256 / W : 1) + threadIdx.x / W;
   if (row >= A.rows) return;  // (a whole wave)
   const X* x = (const X*)A.x + row * A.dim;
-  float h[kSteps][8];
+  float h[S][8];
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
+  for (int s = 0; s < S; ++s) {
     const int i = 8 * (t + s * W);
     if (i < A.dim) read8(x + i, A.dim - i, h[s]);
   }
@@ -98,7 +96,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
     const D* d = (const D*)A.delta + row * A.dim;
     X* to = (X*)A.h + row * A.dim;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
+    for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
       float v[8];
@@ -113,7 +111,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   }
   float sum = 0.f;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s)
+  for (int s = 0; s < S; ++s)
     if (8 * (t + s * W) < A.dim)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum = fmaf(h[s][e], h[s][e], sum);
@@ -122,7 +120,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   if (A.rstd && t == 0) A.rstd[row] = r;
   float most = 0.f;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
+  for (int s = 0; s < S; ++s) {
     const int i = 8 * (t + s * W);
     if (i >= A.dim) continue;
     float g[8];
@@ -143,7 +141,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   }
   Y* y = (Y*)A.y + row * A.dim;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
+  for (int s = 0; s < S; ++s) {
     const int i = 8 * (t + s * W);
     if (i >= A.dim) continue;
     if constexpr (sizeof(Y) == 1)
@@ -155,30 +153,31 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
 
 // Rows `worker`, `worker` + workers, ... of the gradient; the worker's sum of dy xhat stays in registers and ends in
 // partial[worker].
-template <typename X, typename G, typename O, int W>
+template <typename X, typename G, typename O, int W, int S>
 __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm_backward(NormGradArgs A, int workers, float* __restrict__ partial) {
   __shared__ float red[2][W / 64];
   const int t = threadIdx.x % W;
   const int worker = (int)blockIdx.x * (W < 256 ? 256 / W : 1) + threadIdx.x / W;
   if (worker >= workers) return;  // (a whole wave)
-  float sum[kSteps][8] = {};
+  float sum[S][8] = {};
   float* turn = red[0];
   float* other = red[1];
   for (int64_t row = worker; row < A.rows; row += workers) {
     const X* hp = (const X*)A.h + row * A.dim;
     const G* dyp = (const G*)A.dy + row * A.dim;
     const float r = A.rstd[row];
-    float xhat[kSteps][8], g[kSteps][8];
+    float xhat[S][8], g[S][8], v[S][8] = {};
     float dot = 0.f;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
+    for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
       read8(hp + i, A.dim - i, xhat[s]);
       read8(dyp + i, A.dim - i, g[s]);
+      if (A.inner) read8((const O*)A.inner + row * A.dim + i, A.dim - i, v[s]);  // (in flight with the others)
     }
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
+    for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
       float gain[8];
@@ -197,56 +196,84 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm_backward(NormGra
     other = swap;
     O* to = (O*)A.dx + row * A.dim;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
+    for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
-      float v[8] = {};
-      if (A.inner) read8((const O*)A.inner + row * A.dim + i, A.dim - i, v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = fmaf(r, g[s][e] - xhat[s][e] * dot, v[e]);
-      write8(to + i, A.dim - i, v);
+      for (int e = 0; e < 8; ++e) v[s][e] = fmaf(r, g[s][e] - xhat[s][e] * dot, v[s][e]);
+      write8(to + i, A.dim - i, v[s]);
     }
   }
   if (!partial) return;
 #pragma unroll
-  for (int s = 0; s < kSteps; ++s) {
+  for (int s = 0; s < S; ++s) {
     const int i = 8 * (t + s * W);
     if (i < A.dim) write8(partial + (int64_t)worker * A.dim + i, A.dim - i, sum[s]);
   }
 }
 
-// Sums of the workers' columns in a fixed order: 32 columns a workgroup, every 8th worker a thread row.
-__global__ __launch_bounds__(256) void k_norm_join(const float* __restrict__ partial, int workers, int dim, int accumulate,
-                                                   float* __restrict__ dgain) {
-  __shared__ float red[8][32];
-  const int c = threadIdx.x & 31, k = threadIdx.x >> 5, col = (int)blockIdx.x * 32 + c;
-  float sum = 0.f;
-  if (col < dim)
-#pragma unroll 8
-    for (int w = k; w < workers; w += 8) sum += partial[(int64_t)w * dim + col];
-  red[k][c] = sum;
-  __syncthreads();
-  if (k || col >= dim) return;
+// Sums of the workers' columns in a fixed order: 32 columns a workgroup, four of them a thread, every 64th worker a row of
+// threads.
+constexpr int kJoinRows = 64;
+__global__ __launch_bounds__(8 * kJoinRows) void k_norm_join(const float* __restrict__ partial, int workers, int dim, int accumulate,
+                                                            float* __restrict__ dgain) {
+  __shared__ float red[kJoinRows][33];
+  const int c = threadIdx.x & 7, k = threadIdx.x >> 3, col = (int)blockIdx.x * 32 + 4 * c;
+  float sum[4] = {};
+#pragma unroll 4
+  for (int w = k; w < workers; w += kJoinRows) {
+    const float* p = partial + (int64_t)w * dim + col;
+    float v[4] = {};
+    if (col + 4 <= dim)
+      unpack16(load16(p), v);
+    else
+      for (int e = 0; e < dim - col; ++e) v[e] = p[e];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) sum += red[i][c];
-  dgain[col] = accumulate ? dgain[col] + sum : sum;
+    for (int e = 0; e < 4; ++e) sum[e] += v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) red[k][4 * c + e] = sum[e];
+  __syncthreads();
+  const int mine = (int)blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x >= 32 || mine >= dim) return;
+  float total = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < kJoinRows; ++i) total += red[i][threadIdx.x];
+  dgain[mine] = accumulate ? dgain[mine] + total : total;
 }
 
 }  // namespace
 
-int norm_threads(int dim) { return dim <= 64 * 8 * kSteps ? 64 : dim <= 256 * 8 * kSteps ? 256 : 1024; }
+int norm_threads(int dim) { return dim <= 1024 ? 64 : dim <= 2048 ? 256 : dim <= 4096 ? 512 : 1024; }
 
 namespace {
 
+// f(W, S) with the threads of a row and the steps of 8 values that they take, as constants
+template <typename F>
+void by_dim(int dim, F f) {
+  using std::integral_constant;
+  if (dim <= 512)
+    f(integral_constant<int, 64>(), integral_constant<int, 1>());
+  else if (dim <= 1024)
+    f(integral_constant<int, 64>(), integral_constant<int, 2>());
+  else if (dim <= 2048)
+    f(integral_constant<int, 256>(), integral_constant<int, 1>());
+  else if (dim <= 4096)
+    f(integral_constant<int, 512>(), integral_constant<int, 1>());
+  else if (dim <= 8192)
+    f(integral_constant<int, 1024>(), integral_constant<int, 1>());
+  else if (dim <= 16384)
+    f(integral_constant<int, 1024>(), integral_constant<int, 2>());
+  else
+    f(integral_constant<int, 1024>(), integral_constant<int, 4>());
+}
+
 template <typename X, typename D, typename Y>
 hipError_t forward(hipStream_t s, const NormArgs& a) {
-  const int w = norm_threads(a.dim);
-  if (w == 64)
-    k_rms_norm<X, D, Y, 64><<<(a.rows + 3) / 4, 256, 0, s>>>(a);
-  else if (w == 256)
-    k_rms_norm<X, D, Y, 256><<<a.rows, 256, 0, s>>>(a);
-  else
-    k_rms_norm<X, D, Y, 1024><<<a.rows, 1024, 0, s>>>(a);
+  by_dim(a.dim, [&](auto W, auto S) {
+    constexpr int kRows = W < 256 ? 256 / W : 1;
+    k_rms_norm<X, D, Y, W, S><<<(a.rows + kRows - 1) / kRows, kRows * W, 0, s>>>(a);
+  });
   return hipGetLastError();
 }
 template <typename X, typename D>
@@ -266,15 +293,12 @@ int workers_of(int rows, int dim) { return std::min(rows, norm_threads(dim) == 6
 
 template <typename X, typename G, typename O>
 hipError_t backward(hipStream_t s, const NormGradArgs& a, float* partial) {
-  const int w = norm_threads(a.dim), n = workers_of(a.rows, a.dim);
-  float* p = a.dgain ? partial : nullptr;
-  if (w == 64)
-    k_rms_norm_backward<X, G, O, 64><<<(n + 3) / 4, 256, 0, s>>>(a, n, p);
-  else if (w == 256)
-    k_rms_norm_backward<X, G, O, 256><<<n, 256, 0, s>>>(a, n, p);
-  else
-    k_rms_norm_backward<X, G, O, 1024><<<n, 1024, 0, s>>>(a, n, p);
-  if (a.dgain) k_norm_join<<<(a.dim + 31) / 32, 256, 0, s>>>(partial, n, a.dim, a.accumulate, a.dgain);
+  const int n = workers_of(a.rows, a.dim);
+  by_dim(a.dim, [&](auto W, auto S) {
+    constexpr int kRows = W < 256 ? 256 / W : 1;
+    k_rms_norm_backward<X, G, O, W, S><<<(n + kRows - 1) / kRows, kRows * W, 0, s>>>(a, n, a.dgain ? partial : nullptr);
+  });
+  if (a.dgain) k_norm_join<<<(a.dim + 31) / 32, 8 * kJoinRows, 0, s>>>(partial, n, a.dim, a.accumulate, a.dgain);
   return hipGetLastError();
 }
 template <typename X, typename G>
