@@ -492,7 +492,7 @@ rollout_status rollout_attention_backward(const rollout_attention_shape* shape, 
  * the smallest power of two, 2^-126 at least, for which no |y| of the row, over it, is above 448, and d_y the codes of y over it, to
  * nearest, ties to even (NaN where y is not finite).  Matrices are dense, and rows may start at any element.
  * Errors: EINVAL (sizes, types, alignment, NULL buffers, overlap), EUNSUPPORTED (dim above 32,768,
- * rows whose launch would have 2^32 threads: 2^26 up to dim 1,024, 2^22 from 4,097 on), EDEVICE.
+ * rows whose launch would have 2^32 threads: some 2^26 up to dim 1,024, 2^22 from 4,097 on), EDEVICE.
  */
 rollout_status rollout_rms_norm(const void* d_x, int32_t x_dtype, const void* d_delta, int32_t delta_dtype,
                                 const float* d_gain, int32_t n_rows, int32_t dim, float eps, void* d_h, void* d_y,

@@ -98,6 +98,11 @@ class AttentionShape(ctypes.Structure):
         ("scale", ctypes.c_float),
     ]
 
+    def __setattr__(self, name, value):  # (ctypes would keep the low bits of what an int32 does not hold)
+        if name != "scale" and not -(1 << 31) <= value < 1 << 31:
+            raise RolloutError(EINVAL if value < 0 else EUNSUPPORTED, f"{name}: {value} does not fit an int32")
+        super().__setattr__(name, value)
+
 
 class AdamwTensor(ctypes.Structure):
     _fields_ = [
@@ -551,7 +556,9 @@ def rollout_adamw(table, n_tensors: int, n_chunks: int, lr: float, beta1: float,
                   grad_scale=None, lr_now=None, step_now=None, stream=None):
     """lr_now fp32 [1] and step_now int64 [1], on the device, replace lr and step."""
     if (n_tensors | n_chunks | step | seed) >> 31:
-        _sizes((n_tensors,), (n_chunks, step), seed)
+        _sizes((n_tensors,), (n_chunks, step))
+        if not 0 <= seed < 1 << 64:
+            raise RolloutError(EINVAL, f"the seed {seed} does not fit a uint64")
     dev = _device()
     need = ctypes.c_uint64(0)
     _check(lib.rollout_adamw_table_bytes(n_tensors, ctypes.byref(need)))

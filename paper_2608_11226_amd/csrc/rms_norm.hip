@@ -317,7 +317,11 @@ hipError_t launch_rms_norm(hipStream_t s, int x_dtype, int delta_dtype, int y_dt
                                        : forward_from<uint16_t>(s, delta_dtype, y_dtype, a);
 }
 
-size_t rms_norm_backward_workspace(int rows, int dim) { return (size_t)workers_of(rows, dim) * dim * 4; }
+// (that of a large call does for small ones, which may have more workers)
+size_t rms_norm_backward_workspace(int rows, int dim) {
+  const int narrow = std::min(dim, 1024);
+  return std::max((size_t)workers_of(rows, dim) * dim, (size_t)workers_of(rows, narrow) * narrow) * 4;
+}
 
 hipError_t launch_rms_norm_backward(hipStream_t s, int h_dtype, int dy_dtype, int dx_dtype, const NormGradArgs& a, void* ws) {
   return h_dtype == ROLLOUT_DTYPE_FP32 ? backward_from<float>(s, dy_dtype, dx_dtype, a, (float*)ws)

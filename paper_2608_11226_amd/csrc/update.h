@@ -106,7 +106,10 @@ hipError_t launch_packed_attention_backward(hipStream_t s, int dtype, const Atte
 
 constexpr int kMaxNormDim = 32768;
 int norm_threads(int dim);  // of a row
-inline bool norm_fits(int rows, int dim) { return (int64_t)rows * norm_threads(dim) < (int64_t)1 << 32; }
+inline bool norm_fits(int rows, int dim) {
+  const int64_t t = norm_threads(dim), each = t < 256 ? 256 / t : 1;  // rows of a workgroup
+  return (rows + each - 1) / each * each * t < (int64_t)1 << 32;
+}
 struct NormArgs {
   const void *x, *delta;  // delta may be NULL
   const float* gain;      // may be NULL
