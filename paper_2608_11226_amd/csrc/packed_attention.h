@@ -200,6 +200,18 @@ __device__ __forceinline__ Sequence sequence_at(const int32_t* starts, const int
   return {a, lens ? max(0, min(lens[s], b - a)) : b - a};
 }
 
+// How many query heads share a key's, and division by it: x / each = x inverse / 2^32 for x < 2^26, each <= 64.  (What a
+// workgroup works out before its first tile is as much as some tiles take: few divisions, none of them in 64 bits.)
+struct Group {
+  int each;
+  uint32_t inverse;
+  __device__ __forceinline__ int tokens(int rows) const { return each == 1 ? rows : (int)__umulhi((uint32_t)rows, inverse); }
+};
+inline Group group_of(const AttentionArgs& a) {
+  const int each = a.heads / a.kv_heads;
+  return {each, (uint32_t)(((uint64_t)1 << 32) / (uint64_t)each + 1)};
+}
+
 // The query heads that share a key's are taken together: `each` of them make as many rows of a token, and a sequence of len
 // tokens is a run of len * each rows (token by token).  The tiles of B rows of all sequences are numbered
 // start_s * each / B + s + (tile in s): no two have the same number, the numbers ascend with s, and there are at most
@@ -226,7 +238,7 @@ __device__ __forceinline__ bool find_tile(const Side& mine, const Side& other, i
   for (;;) {
     const int step = (hi - lo + 63) >> 6, at = lo + lane * step, s = min(at, hi - 1);
     const Sequence x = sequence_at(mine.starts, mine.lens, s, mine.n), y = sequence_at(other.starts, other.lens, s, other.n);
-    const int first = x.start * each / B + s;
+    const int first = (int)((uint32_t)(x.start * each) / B) + s;
     const int k = __popcll(__ballot(at < hi && first <= slot)) - 1;
     if (k < 0) return false;
     if (step == 1) {
@@ -247,14 +259,13 @@ template <typename T, int HD>
 struct WaveRows {
   typedef Rows<T, HD> R;
   int token, over, last;  // of the first row, the heads before it there, and the last row (< 32; rows behind it are copies of it)
-  uint32_t each, inverse;
-  __device__ __forceinline__ WaveRows(int first, int n_rows, int each)
-      : token(first / each), over(first - token * each), last(min(31, n_rows - 1 - first)), each((uint32_t)each), inverse(65536 / (uint32_t)each + 1) {}
-  // where row i lies behind the first token's first head, for tokens `stride` bytes apart (x / each = x inverse / 65536 for
-  // 0 <= x < 96, each <= 64)
+  Group group;
+  __device__ __forceinline__ WaveRows(int first, int n_rows, const Group& g)
+      : token(g.tokens(first)), over(first - token * g.each), last(min(31, n_rows - 1 - first)), group(g) {}
+  // where row i lies behind the first token's first head, for tokens `stride` bytes apart
   __device__ __forceinline__ uint32_t offset(int i, uint32_t stride) const {
-    const uint32_t x = (uint32_t)(i + over), t = x * inverse >> 16;
-    return t * stride + (x - t * each) * R::kBytes;
+    const int x = i + over, t = group.tokens(x);
+    return (uint32_t)t * stride + (uint32_t)(x - t * group.each) * R::kBytes;
   }
   // into the wave's 32 rows of LDS; p: the sequence's first token, at the first of the heads
   __device__ __forceinline__ void load(char* lds, const T* p, int64_t stride, int lane) const {
@@ -346,12 +357,24 @@ __device__ __forceinline__ void groups(Frag (&f)[2][W], Load load, Use use) {
   group<N, W, 0>(f, load, use);
 }
 
-// Workgroups are dealt out to the eight dies in turn; numbered so that a die's are neighbours.  -1: none.
-__device__ __forceinline__ int neighbours_on_die(int total) {
-  const int per = (total + 7) >> 3;
-  const int w = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
-  return (int)(blockIdx.x >> 3) < per && w < total ? w : -1;
+// A workgroup's walk: a number of a tile, and the part of it, for a key's head.  Workgroups are dealt out to the eight dies in
+// turn; numbered so that a die's are neighbours, the tiles of a head's part one behind the other.  false: none.
+struct Walk {
+  int slot, part, kvh;
+};
+__device__ __forceinline__ bool find_walk(int slots, int parts, int kv_heads, Walk* w) {
+  const uint32_t total = (uint32_t)(slots * kv_heads * parts), per = (total + 7) >> 3, mine = blockIdx.x >> 3;
+  const uint32_t at = (blockIdx.x & 7) * per + mine;
+  if (mine >= per || at >= total) return false;
+  const uint32_t k = at / (uint32_t)slots;
+  w->slot = (int)(at - k * (uint32_t)slots);
+  w->kvh = parts == 1 ? (int)k : (int)(k / (uint32_t)parts);
+  w->part = parts == 1 ? 0 : (int)(k - (uint32_t)w->kvh * (uint32_t)parts);
+  return true;
 }
+// the share of a part of n tiles: n parts is less than 2^31
+__device__ __forceinline__ int part_from(int n, int part, int parts) { return parts == 1 ? n * part : (int)((uint32_t)(n * part) / (uint32_t)parts); }
+
 // Into how many parts the walks of a launch over `tiles` tiles each are cut, whose sums a second launch joins: by what a whole
 // walk takes (alone_us a tile, or shared_us a tile in every one of the card's 512 places where there are more walks than
 // places), the third of a walk that the last ones run on, and the parts' sums, which are written and read again.

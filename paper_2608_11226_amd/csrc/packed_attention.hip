@@ -33,34 +33,34 @@ __device__ __forceinline__ size_t partial_at(int part, const AttentionArgs& A, s
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_attention(AttentionArgs A, int slots, int parts,
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_attention(AttentionArgs A, Group group, int slots, int parts,
                                                                                      float* __restrict__ partial) {
   typedef Rows<T, HD> R;
   typedef typename R::Frag Frag;
   __shared__ __align__(16) char s_kv[2][2][kKeys * R::kBytes];
   static_assert(2 * kKeys == kQueries, "a tile's place holds the workgroup's rows");
-  const int w = neighbours_on_die(slots * A.kv_heads * parts);
-  if (w < 0) return;
+  Walk walk;
+  if (!find_walk(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
+  const int kvh = walk.kvh, part = walk.part;
   Place at;
   // a sequence's last queries, which have the most keys, first
-  if (!find_tile<kQueries>(queries_of(A), keys_of(A), A.n_seqs, each, slots - 1 - w / parts % slots, lane, &at)) return;
+  if (!find_tile<kQueries>(queries_of(A), keys_of(A), A.n_seqs, group.each, slots - 1 - walk.slot, lane, &at)) return;
   const Sequence sq = at.mine, sk = at.other;
   const int t0 = at.row;
 
-  const int behind = sk.len - sq.len, n_rows = sq.len * each;  // causal: token i attends keys 0 .. i + behind
+  const int behind = sk.len - sq.len, n_rows = sq.len * group.each;  // causal: token i attends keys 0 .. i + behind
   const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
-  const int token = r / each, head = kvh * each + r % each;
+  const int token = group.tokens(r), head = kvh * group.each + r - token * group.each;
   const size_t row = (size_t)sq.start + token;
   auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
   const int mine = keys_to(token);  // of this lane's query
   // of the wave's; a wave behind the last row has nothing to do
-  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
-  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
-  const int all = (keys_to((min(t0 + kQueries, n_rows) - 1) / each) + kKeys - 1) / kKeys;
-  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
+  const int w_least = keys_to(group.tokens(min(w_first, n_rows - 1)));
+  const int w_most = w_first < n_rows ? keys_to(group.tokens(min(w_first + 31, n_rows - 1))) : 0;
+  const int all = (keys_to(group.tokens(min(t0 + kQueries, n_rows) - 1)) + kKeys - 1) / kKeys;
+  const int first = part_from(all, part, parts), tiles = part_from(all, part + 1, parts) - first;
 
   const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
   const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
@@ -73,8 +73,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   first_tiles<2>(tiles, load);
   // the rows by way of the second tile's place
   char* place = s_kv[1][0] + 32 * wave * R::kBytes;
-  const size_t heads = (size_t)kvh * each * HD;
-  const WaveRows<T, HD> my(min(w_first, n_rows - 1), n_rows, each);
+  const size_t heads = (size_t)kvh * group.each * HD;
+  const WaveRows<T, HD> my(min(w_first, n_rows - 1), n_rows, group);
   Frag qf[HD / 16];
   my.load(place, (const T*)A.q + (size_t)sq.start * A.q_stride + heads, A.q_stride, lane);
   dma_wait();
@@ -221,7 +221,7 @@ int key_parts(const AttentionArgs& a) {
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionArgs& a, float* partial) {
   const int slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries), parts = key_parts(a);
-  k_packed_attention<T, HD><<<die_grid(slots * a.kv_heads * parts), 64 * kWaves, 0, s>>>(a, slots, parts, partial);
+  k_packed_attention<T, HD><<<die_grid(slots * a.kv_heads * parts), 64 * kWaves, 0, s>>>(a, group_of(a), slots, parts, partial);
   if (parts > 1) k_attention_merge<T, HD><<<dim3(slots * a.kv_heads, kQueries * HD / 1024), 256, 0, s>>>(a, slots, parts, partial);
   return hipGetLastError();
 }

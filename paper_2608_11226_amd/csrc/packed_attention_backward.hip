@@ -23,7 +23,7 @@ constexpr int kWaves = 4;
 constexpr int kDqRows = 32 * kWaves, kDqKeys = 32;
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, int slots, int parts,
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, Group group, int slots, int parts,
                                                                                  float2* __restrict__ stats,
                                                                                  float* __restrict__ partial) {
   typedef Rows<T, HD> R;
@@ -32,26 +32,26 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   __shared__ __align__(16) char s_kv[S][2][kDqKeys * R::kBytes];
   __shared__ __align__(16) char s_rows[kDqRows * R::kBytes];
   static_assert(4 * kDqKeys == kDqRows, "two tiles' places hold the workgroup's rows");
-  const int w = neighbours_on_die(slots * A.kv_heads * parts);
-  if (w < 0) return;
+  Walk walk;
+  if (!find_walk(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int each = A.heads / A.kv_heads, kvh = w / parts / slots, part = w % parts;
+  const int kvh = walk.kvh, part = walk.part;
   Place at;
-  if (!find_tile<kDqRows>(queries_of(A), keys_of(A), A.n_seqs, each, slots - 1 - w / parts % slots, lane, &at)) return;
+  if (!find_tile<kDqRows>(queries_of(A), keys_of(A), A.n_seqs, group.each, slots - 1 - walk.slot, lane, &at)) return;
   const Sequence sq = at.mine, sk = at.other;
   const int t0 = at.row;
-  const int behind = sk.len - sq.len, n_rows = sq.len * each;
+  const int behind = sk.len - sq.len, n_rows = sq.len * group.each;
   const int w_first = t0 + 32 * wave, r = min(w_first + a, n_rows - 1);
-  const int token = r / each, head = kvh * each + r % each;
+  const int token = group.tokens(r), head = kvh * group.each + r - token * group.each;
   const size_t row = (size_t)sq.start + token;
   auto keys_to = [&](int i) { return A.causal ? max(0, min(sk.len, i + behind + 1)) : sk.len; };
   const int mine = keys_to(token);
   // a wave behind the last row has nothing to do
-  const int w_least = keys_to(min(w_first, n_rows - 1) / each);
-  const int w_most = w_first < n_rows ? keys_to(min(w_first + 31, n_rows - 1) / each) : 0;
-  const int all = (keys_to((min(t0 + kDqRows, n_rows) - 1) / each) + kDqKeys - 1) / kDqKeys;
-  const int first = (int)((int64_t)all * part / parts), tiles = (int)((int64_t)all * (part + 1) / parts) - first;
+  const int w_least = keys_to(group.tokens(min(w_first, n_rows - 1)));
+  const int w_most = w_first < n_rows ? keys_to(group.tokens(min(w_first + 31, n_rows - 1))) : 0;
+  const int all = (keys_to(group.tokens(min(t0 + kDqRows, n_rows) - 1)) + kDqKeys - 1) / kDqKeys;
+  const int first = part_from(all, part, parts), tiles = part_from(all, part + 1, parts) - first;
 
   const uint32_t k_stride = (uint32_t)(A.k_stride * sizeof(T)), v_stride = (uint32_t)(A.v_stride * sizeof(T));
   const char* kb = (const char*)((const T*)A.k + (size_t)sk.start * A.k_stride + (size_t)kvh * HD);
@@ -63,8 +63,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   };
   // the rows by way of LDS: q and do at once, out with the first tiles
   char *place = s_rows + 32 * wave * R::kBytes, *other = s_kv[0][0] + 32 * wave * R::kBytes;
-  const size_t heads = (size_t)kvh * each * HD;
-  const WaveRows<T, HD> mine_of(min(w_first, n_rows - 1), n_rows, each);
+  const size_t heads = (size_t)kvh * group.each * HD;
+  const WaveRows<T, HD> mine_of(min(w_first, n_rows - 1), n_rows, group);
   mine_of.load(place, (const T*)A.q + (size_t)sq.start * A.q_stride + heads, A.q_stride, lane);
   mine_of.load(other, (const T*)A.dout + (size_t)sq.start * A.dout_stride + heads, A.dout_stride, lane);
   const float lse = A.lse[(size_t)head * A.n_q + row];
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
 constexpr int kBackKeys = 32 * kWaves, kBackRows = 32;
 
 template <typename T, int HD>
-__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dkv(AttentionGradArgs A, int slots, int parts,
+__global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dkv(AttentionGradArgs A, Group group, int slots, int parts,
                                                                                   const float2* __restrict__ stats,
                                                                                   float* __restrict__ partial) {
   typedef Rows<T, HD> R;
@@ -172,13 +172,13 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   // workgroups of a compute unit have room for), in fp32, with one workgroup there, all of them
   constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 ? 2 : 0;
   __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
-  const int w = neighbours_on_die(slots * A.kv_heads * parts);
-  if (w < 0) return;
+  Walk walk;
+  if (!find_walk(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int each = A.heads / A.kv_heads, kvh = w / slots / parts, part = w / slots % parts;
+  const int each = group.each, kvh = walk.kvh, part = walk.part;
   Place at;
-  if (!find_tile<kBackKeys>(keys_of(A), queries_of(A), A.n_seqs, 1, w % slots, lane, &at)) return;
+  if (!find_tile<kBackKeys>(keys_of(A), queries_of(A), A.n_seqs, 1, walk.slot, lane, &at)) return;
   const Sequence sk = at.mine, sq = at.other;
   const int t0 = at.row;
   const int behind = sk.len - sq.len, n_rows = sq.len * each;
@@ -188,8 +188,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   // causal: key j is attended from token j - behind on
   auto from = [&](int j) { return A.causal ? max(0, min(j - behind, sq.len)) * each : 0; };
   const int head_tile = from(t0) / kBackRows, all = (n_rows + kBackRows - 1) / kBackRows - head_tile;
-  const int first = head_tile + (int)((int64_t)all * part / parts);
-  const int tiles = head_tile + (int)((int64_t)all * (part + 1) / parts) - first;
+  const int first = head_tile + part_from(all, part, parts), tiles = head_tile + part_from(all, part + 1, parts) - first;
   const int mine = from(kj);
   // a wave behind the last key has nothing to do
   const int w_least = w_first < sk.len ? from(w_first) : INT32_MAX, w_most = from(w_first + 31);
@@ -199,19 +198,18 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   const char* qb = (const char*)((const T*)A.q + (size_t)sq.start * A.q_stride + head * HD);
   const char* dob = (const char*)((const T*)A.dout + (size_t)sq.start * A.dout_stride + head * HD);
   const float2* sb = stats + (size_t)sq.start * A.heads + head;
-  const uint32_t inverse = 65536 / each + 1;  // x / each = x inverse / 65536 for 0 <= x < 96, each <= 64
-  int token = first * kBackRows / each, over = first * kBackRows - token * each;  // of the first row that is loaded next
-  const int more = kBackRows / each, more_over = kBackRows - more * each;
+  int token = group.tokens(first * kBackRows), over = first * kBackRows - token * each;  // of the first row that is loaded next
+  const int more = group.tokens(kBackRows), more_over = kBackRows - more * each;
   auto load = [&](auto buf, int it) {
     const int last = n_rows - 1 - (first + it) * kBackRows;
     const char* q0 = qb + (size_t)token * q_stride;
     const char* do0 = dob + (size_t)token * do_stride;
     if (wave == 0) {
-      const uint32_t x = (uint32_t)(min(a, last) + over), t = x * inverse >> 16;
+      const uint32_t x = (uint32_t)(min(a, last) + over), t = (uint32_t)group.tokens((int)x);
       dma_lds4_at(sb + (size_t)token * A.heads, (t * (uint32_t)(A.heads - each) + x) * 8 + 4 * half, s_stat[buf]);
     }
     R::template load_with<kBackRows, kWaves>(wave, lane, [&](int row, uint32_t offset, int place) {
-      const uint32_t x = (uint32_t)(min(row, last) + over), t = x * inverse >> 16;
+      const uint32_t x = (uint32_t)(min(row, last) + over), t = (uint32_t)group.tokens((int)x);
       const uint32_t at = (x - t * (uint32_t)each) * R::kBytes + offset;
       dma_lds16_at(q0, t * q_stride + at, s_q[buf] + place);
       dma_lds16_at(do0, t * do_stride + at, s_do[buf] + place);
@@ -399,11 +397,11 @@ hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   float2* stats = (float2*)ws;
   float* partial = (float*)(ws + stats_bytes(a));  // of the queries, then of the keys
   const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts(a);
-  k_attention_dq<T, HD><<<die_grid(q_slots * a.kv_heads * kp), 64 * kWaves, 0, s>>>(a, q_slots, kp, stats, partial);
+  k_attention_dq<T, HD><<<die_grid(q_slots * a.kv_heads * kp), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
   if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
   const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys);
   const int rp = row_parts(a);
-  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, slots, rp, stats, partial);
+  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
   if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, rp, partial);
   return hipGetLastError();
 }
