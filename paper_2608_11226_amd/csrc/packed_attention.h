@@ -358,18 +358,20 @@ __device__ __forceinline__ void groups(Frag (&f)[2][W], Load load, Use use) {
 }
 
 // A workgroup's walk: a number of a tile, and the part of it, for a key's head.  Workgroups are dealt out to the eight dies in
-// turn; numbered so that a die's are neighbours, the tiles of a head's part one behind the other.  false: none.
+// turn; numbered so that a die's are neighbours.  Beside a walk are the other parts of its tile (kParts) or the other tiles'
+// walks of its part.  false: none.
 struct Walk {
   int slot, part, kvh;
 };
+template <bool kParts>
 __device__ __forceinline__ bool find_walk(int slots, int parts, int kv_heads, Walk* w) {
   const uint32_t total = (uint32_t)(slots * kv_heads * parts), per = (total + 7) >> 3, mine = blockIdx.x >> 3;
   const uint32_t at = (blockIdx.x & 7) * per + mine;
   if (mine >= per || at >= total) return false;
-  const uint32_t k = at / (uint32_t)slots;
-  w->slot = (int)(at - k * (uint32_t)slots);
-  w->kvh = parts == 1 ? (int)k : (int)(k / (uint32_t)parts);
-  w->part = parts == 1 ? 0 : (int)(k - (uint32_t)w->kvh * (uint32_t)parts);
+  const uint32_t inner = (uint32_t)(kParts ? parts : slots), outer = (uint32_t)(kParts ? slots : parts);
+  const uint32_t k = inner == 1 ? at : at / inner, i = at - k * inner;
+  const uint32_t h = outer == 1 ? k : k / outer, o = k - h * outer;
+  w->slot = (int)(kParts ? o : i), w->part = (int)(kParts ? i : o), w->kvh = (int)h;
   return true;
 }
 // the share of a part of n tiles: n parts is less than 2^31

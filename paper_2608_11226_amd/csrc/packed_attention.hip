@@ -40,7 +40,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   __shared__ __align__(16) char s_kv[2][2][kKeys * R::kBytes];
   static_assert(2 * kKeys == kQueries, "a tile's place holds the workgroup's rows");
   Walk walk;
-  if (!find_walk(slots, parts, A.kv_heads, &walk)) return;
+  if (!find_walk<true>(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = walk.kvh, part = walk.part;

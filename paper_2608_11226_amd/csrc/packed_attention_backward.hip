@@ -33,7 +33,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   __shared__ __align__(16) char s_rows[kDqRows * R::kBytes];
   static_assert(4 * kDqKeys == kDqRows, "two tiles' places hold the workgroup's rows");
   Walk walk;
-  if (!find_walk(slots, parts, A.kv_heads, &walk)) return;
+  if (!find_walk<true>(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = walk.kvh, part = walk.part;
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 ? 2 : 0;
   __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
   Walk walk;
-  if (!find_walk(slots, parts, A.kv_heads, &walk)) return;
+  if (!find_walk<false>(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int each = group.each, kvh = walk.kvh, part = walk.part;
