@@ -358,21 +358,48 @@ __device__ __forceinline__ void groups(Frag (&f)[2][W], Load load, Use use) {
 }
 
 // A workgroup's walk: a number of a tile, and the part of it, for a key's head.  Workgroups are dealt out to the eight dies in
-// turn; numbered so that a die's are neighbours.  Beside a walk are the other parts of its tile (kParts) or the other tiles'
-// walks of its part.  false: none.
+// turn, and each die has its own cache: a die takes whole runs (the walks of a head, or of a head's part) as far as they can be
+// shared out evenly, and of the others every die (or every die of two or four) takes walks in turn, so that each has as many
+// long ones.  Walks of a run: its tiles, with their parts beside each other (kParts) or of one part alone.  false: none.
 struct Walk {
   int slot, part, kvh;
 };
 template <bool kParts>
+__host__ __device__ __forceinline__ void walk_runs(int slots, int parts, int kv_heads, uint32_t* length, uint32_t* runs, uint32_t* whole, uint32_t* rest) {
+  *length = (uint32_t)(kParts ? slots * parts : slots);
+  *runs = (uint32_t)(kParts ? kv_heads : kv_heads * parts);
+  *whole = *runs / 8 * *length;                  // walks of a die in whole runs
+  *rest = (*runs % 8 * *length + 7) / 8;         // in the others, at most
+  if (*runs % 8 == 1 || *runs % 8 == 2 || *runs % 8 == 4) *rest = (*length + 8 / (*runs % 8) - 1) / (8 / (*runs % 8));
+}
+template <bool kParts>
 __device__ __forceinline__ bool find_walk(int slots, int parts, int kv_heads, Walk* w) {
-  const uint32_t total = (uint32_t)(slots * kv_heads * parts), per = (total + 7) >> 3, mine = blockIdx.x >> 3;
-  const uint32_t at = (blockIdx.x & 7) * per + mine;
-  if (mine >= per || at >= total) return false;
-  const uint32_t inner = (uint32_t)(kParts ? parts : slots), outer = (uint32_t)(kParts ? slots : parts);
-  const uint32_t k = inner == 1 ? at : at / inner, i = at - k * inner;
-  const uint32_t h = outer == 1 ? k : k / outer, o = k - h * outer;
-  w->slot = (int)(kParts ? o : i), w->part = (int)(kParts ? i : o), w->kvh = (int)h;
+  uint32_t length, runs, whole, rest;
+  walk_runs<kParts>(slots, parts, kv_heads, &length, &runs, &whole, &rest);
+  const uint32_t die = blockIdx.x & 7, mine = blockIdx.x >> 3, left = runs & 7;
+  uint32_t run, at;
+  if (mine < whole) {
+    const uint32_t k = mine / length;
+    run = 8 * k + die, at = mine - k * length;
+  } else if (left == 1 || left == 2 || left == 4) {
+    const uint32_t dies = 8 / left;  // of a run
+    run = runs - left + die / dies, at = (mine - whole) * dies + die % dies;
+    if (at >= length) return false;
+  } else {
+    const uint32_t i = (mine - whole) * 8 + die, k = i / length;
+    if (k >= left) return false;
+    run = runs - left + k, at = i - k * length;
+  }
+  const uint32_t k = parts == 1 ? (kParts ? at : run) : (kParts ? at : run) / (uint32_t)parts;
+  w->part = (int)((kParts ? at : run) - k * (uint32_t)parts);
+  w->slot = (int)(kParts ? k : at), w->kvh = (int)(kParts ? run : k);
   return true;
+}
+template <bool kParts>
+inline unsigned walk_grid(int slots, int parts, int kv_heads) {
+  uint32_t length, runs, whole, rest;
+  walk_runs<kParts>(slots, parts, kv_heads, &length, &runs, &whole, &rest);
+  return 8 * (whole + rest);
 }
 // the share of a part of n tiles: n parts is less than 2^31
 __device__ __forceinline__ int part_from(int n, int part, int parts) { return parts == 1 ? n * part : (int)((uint32_t)(n * part) / (uint32_t)parts); }
@@ -397,7 +424,5 @@ inline int walk_parts(int64_t walks, double tiles, bool triangle, double alone_u
   }
   return best;
 }
-
-inline unsigned die_grid(int total) { return (unsigned)((total + 7) / 8 * 8); }
 
 }  // namespace rollout

@@ -221,7 +221,7 @@ int key_parts(const AttentionArgs& a) {
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionArgs& a, float* partial) {
   const int slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries), parts = key_parts(a);
-  k_packed_attention<T, HD><<<die_grid(slots * a.kv_heads * parts), 64 * kWaves, 0, s>>>(a, group_of(a), slots, parts, partial);
+  k_packed_attention<T, HD><<<walk_grid<true>(slots, parts, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, parts, partial);
   if (parts > 1) k_attention_merge<T, HD><<<dim3(slots * a.kv_heads, kQueries * HD / 1024), 256, 0, s>>>(a, slots, parts, partial);
   return hipGetLastError();
 }

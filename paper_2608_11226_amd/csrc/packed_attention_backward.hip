@@ -397,11 +397,11 @@ hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   float2* stats = (float2*)ws;
   float* partial = (float*)(ws + stats_bytes(a));  // of the queries, then of the keys
   const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts(a);
-  k_attention_dq<T, HD><<<die_grid(q_slots * a.kv_heads * kp), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
+  k_attention_dq<T, HD><<<walk_grid<true>(q_slots, kp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
   if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
   const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys);
   const int rp = row_parts(a);
-  k_attention_dkv<T, HD><<<die_grid(slots * a.kv_heads * rp), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
+  k_attention_dkv<T, HD><<<walk_grid<false>(slots, rp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
   if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, rp, partial);
   return hipGetLastError();
 }
