@@ -186,17 +186,31 @@ __global__ __launch_bounds__(256) void k_attention_merge(AttentionArgs A, int sl
   if (r >= sq.len * each) return;
   const size_t row = (size_t)sq.start + r / each;
   const int head = kvh * each + r % each;
-  float m = -INFINITY;
-  for (int k = 0; k < parts; ++k) m = fmaxf(m, partial[partial_at<HD>(k, A, row, head) + HD]);
-  float l = 0.f, o[4] = {};
-#pragma unroll 4
-  for (int k = 0; k < parts; ++k) {
-    const float* p = partial + partial_at<HD>(k, A, row, head);
-    const float2 ml = *reinterpret_cast<const float2*>(p + HD);
-    const float4 x = *reinterpret_cast<const float4*>(p + c);
-    const float by = __builtin_amdgcn_exp2f(ml.x - m);
-    l = fmaf(ml.y, by, l);
-    o[0] = fmaf(x.x, by, o[0]), o[1] = fmaf(x.y, by, o[1]), o[2] = fmaf(x.z, by, o[2]), o[3] = fmaf(x.w, by, o[3]);
+  // eight parts' loads at a time, all of them on the way together
+  float m = -3.4e38f, l = 0.f, o[4] = {};
+  for (int k0 = 0; k0 < parts; k0 += 8) {
+    float2 ml[8];
+    float4 x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float* p = partial + partial_at<HD>(min(k0 + k, parts - 1), A, row, head);
+      ml[k] = *reinterpret_cast<const float2*>(p + HD);
+      x[k] = *reinterpret_cast<const float4*>(p + c);
+    }
+    float most = m;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) most = fmaxf(most, ml[k].x);
+    const float old = __builtin_amdgcn_exp2f(m - most);
+    m = most;
+    l *= old;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= old;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float by = k0 + k < parts ? __builtin_amdgcn_exp2f(ml[k].x - m) : 0.f;
+      l = fmaf(ml[k].y, by, l);
+      o[0] = fmaf(x[k].x, by, o[0]), o[1] = fmaf(x[k].y, by, o[1]), o[2] = fmaf(x[k].z, by, o[2]), o[3] = fmaf(x[k].w, by, o[3]);
+    }
   }
   const float by = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
 #pragma unroll

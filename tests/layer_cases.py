@@ -120,7 +120,7 @@ class Attention:
                 assert (err <= bound).all(), f"out: head {h} of the sequence at {a}: {np.nanmax(err / bound):.3g} of the bound"
                 empty = np.isneginf(z[h, A])
                 assert (np.isneginf(got_z[h, A]) == empty).all() and (got[A, h][empty] == 0).all()
-                err = np.abs(got_z[h, A] - z[h, A])[~empty]
+                err = np.abs(got_z[h, A][~empty] - z[h, A][~empty])
                 bound = (es.max(1, initial=0.0) + (nk + nk / 32 + 8) * U + 4 * U * np.abs(z[h, A]) + 2.0 ** -21)[~empty]
                 assert (err <= bound).all(), f"lse: head {h} of the sequence at {a}"
         free = self.unused(self.q_seqs, self.n_q).cpu().numpy()
