@@ -455,7 +455,7 @@ typedef struct {
   int32_t n_seqs;
   int32_t n_q, n_k;            /* rows of the queries' and of the keys' matrices */
   int32_t causal;              /* 0 or 1 */
-  float scale;                 /* of the products, > 0 */
+  float scale;                 /* of the products, in [2^-100, 2^100] */
 } rollout_attention_shape;
 
 rollout_status rollout_attention_workspace(const rollout_attention_shape* shape, uint64_t* h_bytes);
@@ -489,8 +489,8 @@ rollout_status rollout_attention_backward(const rollout_attention_shape* shape, 
  * d_x [n_rows, dim] of x_dtype, d_delta of delta_dtype with d_h of x_dtype (which may be d_x), or both NULL (h = x);
  * d_gain fp32 [dim], NULL: 1; d_y of y_dtype; d_rstd fp32 [n_rows], NULL if not wanted (the gradient needs it).
  * x and delta are FP32 or BF16.  y is FP32, BF16 or E4M3: then d_scales [n_rows] (otherwise NULL) receives
- * the smallest power of two, 2^-126 at least, for which no |y| of the row, over it, is above 448, and d_y the codes of y over it, to
- * nearest, ties to even (NaN where y is not finite).  Matrices are dense, and rows may start at any element.
+ * the smallest power of two, 2^-126 at least, for which no finite |y| of the row, over it, is above 448, and d_y the codes of
+ * y over it, to nearest, ties to even (NaN where y is not finite).  Matrices are dense, and rows may start at any element.
  * Errors: EINVAL (sizes, types, alignment, NULL buffers, overlap), EUNSUPPORTED (dim above 32,768,
  * rows whose launch would have 2^32 threads: some 2^26 up to dim 1,024, 2^22 from 4,097 on), EDEVICE.
  */
@@ -528,8 +528,8 @@ rollout_status rollout_rms_norm_backward(const void* d_grad_y, int32_t grad_y_dt
  * the probability that keeps their expectation (to nearest they would not move by steps that are small beside them), by 16 bits r
  * of a counter hash of (seed, t, the tensor's place in the table, the element): bf16 drops 16 bits of
  * the fp32 value's magnitude after adding r, e4m3 drops 20 after adding 16 r + 8 (below 2^-6, where values are 2^-9 apart,
- * from the magnitude plus 2^-6).  A scale is the smallest power of two, 2^-126 at least, that leaves no magnitude of
- * its 128 above 448; a second moment of 2^-126 or more keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the
+ * from the magnitude plus 2^-6).  A scale is the smallest power of two, 2^-126 at least, that leaves no finite magnitude of
+ * its 128 above 448 (a moment that is not finite becomes NaN, and no other one of the 128 changes by it); a second moment of 2^-126 or more keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the
  * low 16 bits and v the high ones; a weight the low ones of f(h + (k >> 32)).  f is MurmurHash3's 32-bit
  * finaliser, k = F(F(seed + G t) + G (1 + tensor + 2^20 floor(i / 2^32))) with SplitMix64's finaliser F and constant G.
  * d_grad_scale fp32 [1] (a clipping factor, say; NULL: 1): where it is not finite nothing changes.  d_lr fp32 [1] and d_step

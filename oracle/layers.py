@@ -114,10 +114,15 @@ def _finish32(h):
 
 
 def adamw_bits(seed, step, tensor, index):
-    """16 random bits each for the first moment, the second and the weight of elements `index` (below 2^32) of a tensor."""
-    key = _finish64((_finish64((seed + _GOLD * step) & _M64) + _GOLD * (tensor + 1)) & _M64)
-    h = _finish32((np.asarray(index, dtype=np.uint64) * np.uint64(0x9E3779B1) + np.uint64(key & 0xFFFFFFFF)) & np.uint64(0xFFFFFFFF))
-    w = _finish32((h + np.uint64(key >> 32)) & np.uint64(0xFFFFFFFF))
+    """16 random bits each for the first moment, the second and the weight of elements `index` of a tensor."""
+    index = np.asarray(index, dtype=np.uint64)
+    first = _finish64((seed + _GOLD * step) & _M64)
+    high = index >> np.uint64(32)
+    keys = {int(r): _finish64((first + _GOLD * (tensor + (int(r) << 20) + 1)) & _M64) for r in np.unique(high)}
+    pick = lambda f: np.array([f(keys[int(r)]) for r in np.unique(high)], dtype=np.uint64)[np.unique(high, return_inverse=True)[1]]  # noqa: E731
+    low = np.uint64(0xFFFFFFFF)
+    h = _finish32(((index & low) * np.uint64(0x9E3779B1) + pick(lambda k: k & 0xFFFFFFFF)) & low)
+    w = _finish32((h + pick(lambda k: k >> 32)) & low)
     return (h & np.uint64(0xFFFF)).astype(np.int64), (h >> np.uint64(16)).astype(np.int64), (w & np.uint64(0xFFFF)).astype(np.int64)
 
 

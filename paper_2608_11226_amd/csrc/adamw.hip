@@ -162,7 +162,7 @@ __device__ __forceinline__ void update(const AdamwEntry& E, const Factors& F, in
       // (roots and reciprocals that are off by one unit: that part of a weight's step, or of a state's rounding)
       root[e] = __builtin_amdgcn_sqrtf(v[e]);
       p[e] = p[e] * keep - F.step * m[e] * __builtin_amdgcn_rcpf(root[e] * F.root + F.eps);
-      if constexpr (kEight) most_m = fmaxf(most_m, fabsf(m[e])), most_v = fmaxf(most_v, root[e]);
+      if constexpr (kEight) most_m = larger(most_m, fabsf(m[e])), most_v = larger(most_v, root[e]);
     }
     if constexpr (kEight || kCoarse) {
       uint32_t h[8];

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
     for (int e = 0; e < 8; ++e) {
       h[s][e] *= r;
       if (A.gain) h[s][e] *= g[e];
-      if constexpr (sizeof(Y) == 1) most = fmaxf(most, fabsf(h[s][e]));
+      if constexpr (sizeof(Y) == 1) most = larger(most, fabsf(h[s][e]));
     }
   }
   float by = 1.f;

@@ -228,10 +228,13 @@ __device__ __forceinline__ u32x4 pack16(const float (&v)[8]) {
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(uint16_t* p, float v) { *p = round_bf16(v); }
 
-// Smallest power of two that brings `most` (>= 0) to at most 448, the largest e4m3 value; 2^-126 at least.  448 is 1.75 2^8.
+// max(a, b) where b is a number: one infinite value shall not make its neighbours' codes 0
+__device__ __forceinline__ float larger(float a, float b) { return b > a && b < INFINITY ? b : a; }
+
+// Smallest power of two that brings `most` (>= 0, finite) to at most 448, the largest e4m3 value; 2^-126 at least.  448 is 1.75 2^8.
 __device__ __forceinline__ float e4m3_scale(float most) {
   const uint32_t u = __float_as_uint(most);
-  const int e = min((int)(u >> 23), 254) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  const int e = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return __uint_as_float((uint32_t)max(e, 1) << 23);
 }
 

@@ -23,7 +23,8 @@ rollout_status check_shape(const rollout_attention_shape* s) {
     return fail(ROLLOUT_EUNSUPPORTED, "head_dim must be 32, 64 or 128");
   if (s->n_seqs < 1 || s->n_q < 1 || s->n_k < 1) return fail(ROLLOUT_EINVAL, "n_seqs, n_q and n_k must be >= 1");
   if (s->causal != 0 && s->causal != 1) return fail(ROLLOUT_EINVAL, "causal must be 0 or 1");
-  if (!(s->scale > 0.f) || !std::isfinite(s->scale * 2.f)) return fail(ROLLOUT_EINVAL, "scale must be > 0 and finite");
+  // (the gradient forms lse / scale)
+  if (!(s->scale >= 0x1p-100f && s->scale <= 0x1p100f)) return fail(ROLLOUT_EINVAL, "scale must be in [2^-100, 2^100]");
   if ((int64_t)s->n_heads * std::max(s->n_q, s->n_k) > kMaxHeadRows)
     return fail(ROLLOUT_EUNSUPPORTED, "n_heads times tokens above 2^26");
   if ((int64_t)s->n_heads * (s->n_seqs + (int64_t)std::max(s->n_q, s->n_k) / 32) > kMaxGroups)

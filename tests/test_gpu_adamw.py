@@ -188,14 +188,21 @@ def test_gradients_that_are_not_finite():
         for bad in (float("nan"), float("inf"), -float("inf")):
             step_of(handle, 2, 0, grad_scale=torch.full((1,), bad, device=DEV))
             assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(t.all(), first))
-        t.g[3], t.g[200] = float("nan"), float("inf")
+        step_of(handle, 2, 0)
+        clean = [x.clone() for x in t.all()]
+        for x, y in zip(t.all(), first):
+            x.copy_(y)
+        # elements that are not the largest of their 128
+        i, j = (int(t.v[k:k + 128].float().argmin()) + k for k in (0, 128))
+        t.g[i], t.g[j] = float("nan"), float("inf")
         step_of(handle, 2, 0)
         # they stay where they are
         bad = torch.zeros(500, dtype=torch.bool, device=DEV)
-        bad[3] = bad[200] = True
-        assert t.p[bad].isnan().all() and t.p[~bad].isfinite().all()
-        m = t.m.float()
-        assert m[3].isnan() and not m[200].isfinite() and m[~bad].isfinite().all() and t.v.float()[~bad].isfinite().all()
+        bad[i] = bad[j] = True
+        assert t.p[bad].isnan().all() and t.m.float()[i].isnan() and not t.m.float()[j].isfinite()
+        for x, y in zip(t.all(), clean):
+            keep = ~bad if x.numel() == 500 else slice(None)
+            assert torch.equal(x.float()[keep], y.float()[keep])
 
 
 def test_a_step_that_changes_nothing():
@@ -230,6 +237,30 @@ def test_rate_and_step_from_the_device_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         check_step(tensors, k, 42, before, float(np.float32(1.0 / k)), float(np.float32(LR / k)))
+
+
+def test_elements_behind_the_first_2_to_the_32():
+    n = (1 << 32) + 2000
+    new = lambda t: torch.zeros(n, dtype=t, device=DEV)  # noqa: E731
+    g = torch.Generator(device=DEV).manual_seed(11)
+    p, grad, m, v = new(torch.bfloat16), new(torch.bfloat16), new(torch.uint8), new(torch.uint8)
+    ms, vs = (torch.zeros((n + 127) // 128, device=DEV) for _ in range(2))
+    at = torch.cat([torch.arange(1000), torch.arange(n - 2500, n)]).to(DEV)
+    p[at] = torch.randn(3500, generator=g, device=DEV).bfloat16()
+    grad[at] = torch.randn(3500, generator=g, device=DEV).bfloat16()
+    before, gw = wide(p[at]), wide(grad[at])
+    table, chunks = R.rollout_adamw_table([R.adamw_tensor(p, grad, m, v, 0.0, ms, vs)])
+    step_of((table.to(DEV), 1, chunks), 1, 77)
+    torch.cuda.synchronize()
+    want, wm, _ = L.adamw(before, gw, 0.0, 0.0, LR, B1, B2, EPS, 1, 0.0)
+    _, _, rp = L.adamw_bits(77, 1, 0, at.cpu().numpy())
+    e = 2.0 ** (np.floor(np.log2(np.maximum(np.abs(want), 2.0 ** -126))) - 7)
+    pos = np.abs(want) / e + rp / 2.0 ** 16
+    settled = np.abs(pos - np.round(pos)) > 2.0 ** -9  # (8 to 16 spacings of 2^-24 each, and a step of 2^-8 off by 20 of them)
+    assert settled.mean() > 0.9 and (np.abs(wide(p[at]))[settled] == (np.floor(pos) * e)[settled]).all()
+    mw = wide(m.view(E4M3)[at]) * wide(ms[at // 128])
+    assert (np.abs(mw - wm) <= L.spacing(np.abs(wm) / wide(ms[at // 128])) * wide(ms[at // 128]) * 1.001).all()
+    assert not m[1000:n - 2500].any() and not p[1000:n - 2500].any()
 
 
 def test_on_another_stream():

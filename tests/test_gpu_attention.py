@@ -180,6 +180,55 @@ def test_large_values_of_masked_keys_do_not_matter():
     c.check_backward(c.backward(out, lse), out, lse)
 
 
+def test_rows_behind_4_gib():
+    """Keys and queries whose places are more than 2^32 bytes behind the first, in rows far apart."""
+    H, K, hd, stride, n = 4, 2, 128, 4096, 600000
+    s = torch.cuda.current_stream().cuda_stream
+    big, grads = (torch.zeros((n, stride), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    lens, first = [70, 1, 130], [10, 550000, 599000]
+    c = Attention("bf16", H, K, hd, lens)
+    wq, wk = H * hd, K * hd
+    cols = [slice(0, wq), slice(wq, wq + wk), slice(wq + wk, wq + 2 * wk)]
+    at = 0
+    for f, m in zip(first, lens):
+        for col, x in zip(cols, (c.q, c.k, c.v)):
+            big[f:f + m, col] = x[at:at + m]
+        at += m
+    shape = R.AttentionShape(dtype=1, n_heads=H, n_kv_heads=K, head_dim=hd, n_seqs=3, n_q=n, n_k=n, causal=1, scale=c.scale)
+    starts = torch.tensor(first + [n], dtype=torch.int32, device=DEV)
+    n_lens = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out, dout = torch.zeros((n, wq), dtype=torch.bfloat16, device=DEV), torch.zeros((n, wq), dtype=torch.bfloat16, device=DEV)
+    lse = torch.zeros((H, n), device=DEV)
+    at = 0
+    for f, m in zip(first, lens):
+        dout[f:f + m] = c.grad_out[at:at + m]
+        at += m
+    need = max(R.rollout_attention_workspace(shape), R.rollout_attention_backward_workspace(shape))
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    views = [v for col in cols for v in (big[:, col], stride)]
+    R.rollout_attention(shape, *views, starts, n_lens, None, None, out, wq, lse, ws, need, s)
+    R.rollout_attention_backward(shape, *views, starts, n_lens, None, None, out, wq, lse, dout, wq,
+                                 *[v for col in cols for v in (grads[:, col], stride)], ws, need, s)
+    c_out, c_lse = c.forward()
+    c_grads = c.backward(c_out, c_lse)
+    c.check_forward(c_out, c_lse)
+    c.check_backward(c_grads, c_out, c_lse)
+    # (the two calls may cut walks into parts otherwise: within the bounds of both)
+    pick = torch.cat([torch.arange(f, f + m, device=DEV) for f, m in zip(first, lens)])
+    here = torch.full((c.n_q, wq), SENTINEL, dtype=torch.bfloat16, device=DEV)
+    here[:len(pick)] = out[pick]
+    z = torch.full((H, c.n_q), SENTINEL, device=DEV)
+    z[:, :len(pick)] = lse[:, pick]
+    c.check_forward(here, z)
+    got = []
+    for col in cols:
+        x = torch.full((c.n_q, col.stop - col.start), SENTINEL, dtype=torch.bfloat16, device=DEV)
+        x[:len(pick)] = grads[pick][:, col]
+        got.append(x)
+    c.check_backward(got, here, z)
+    assert not grads[100:500000].any() and not out[100:500000].any()
+
+
 def test_scores_of_minus_infinity():
     c = Attention("fp32", 2, 2, 32, [40])
     c.q[:, 0], c.k[:20, 0] = 1.0, -float("inf")

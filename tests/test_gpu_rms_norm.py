@@ -176,6 +176,31 @@ def test_gradients_by_differences():
     assert abs((loss(x, gain + h * way) - loss(x, gain - h * way)) / (2 * h) - slope) <= 1e-5 * abs(slope) + 1e-3
 
 
+def test_more_than_2_to_the_32_elements():
+    n, d = 540000, 8192
+    at = torch.tensor([0, 1, 262143, 524287, 524288, n - 1], device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(12)
+    x = torch.zeros((n, d), dtype=torch.bfloat16, device=DEV)
+    x[at] = _rand(g, len(at), d, t=torch.bfloat16)
+    y = torch.empty_like(x)
+    rstd = torch.empty(n, device=DEV)
+    s = torch.cuda.current_stream().cuda_stream
+    R.rollout_rms_norm(x, 1, None, 0, None, n, d, EPS, None, y, 1, None, rstd, s)
+    check_forward(x[at], None, None, "bf16", [None, y[at], None, rstd[at]])
+    assert (y[2:262143] == 0).all()
+    dgain = torch.empty(d, device=DEV)
+    need = R.rollout_rms_norm_backward_workspace(n, d)
+    ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+    dx = torch.empty_like(x)
+    R.rollout_rms_norm_backward(x, 1, x, 1, None, rstd, n, d, None, dx, 1, dgain, 0, ws, need, s)
+    few = [t[at].contiguous() for t in (x, rstd)]
+    want = backward(few[0], few[0], None, few[1], None, "bf16", torch.empty(d, device=DEV))
+    assert torch.equal(dx[at], want) and (dx[2:262143] == 0).all()
+    w = wide(few[0])
+    total = (w * w * wide(few[1])[:, None]).sum(0)
+    assert (np.abs(wide(dgain) - total) <= 600 * U * total).all()  # a worker's 528 rows, most of them 0, and the join
+
+
 def test_streams_and_graph():
     g = torch.Generator(device=DEV).manual_seed(10)
     x, delta, gain = _rand(g, 300, 1001), _rand(g, 300, 1001, t=torch.bfloat16), 1.0 + _rand(g, 1001, by=0.1)

@@ -29,6 +29,7 @@ SHAPES = [
     (R.EINVAL, dict(n_seqs=0), "n_seqs"), (R.EINVAL, dict(n_q=0), "n_q"), (R.EINVAL, dict(n_k=-1), "n_k"),
     (R.EINVAL, dict(causal=2), "causal"), (R.EINVAL, dict(scale=0.0), "scale"), (R.EINVAL, dict(scale=-1.0), "scale"),
     (R.EINVAL, dict(scale=float("nan")), "scale"), (R.EINVAL, dict(scale=float("inf")), "scale"), (R.EINVAL, dict(scale=3e38), "scale"),
+    (R.EINVAL, dict(scale=1e-31), "scale"), (R.EINVAL, dict(scale=1.3e30), "scale"),
     (R.EUNSUPPORTED, dict(n_q=(1 << 23) + 1), "2^26"), (R.EUNSUPPORTED, dict(n_k=1 << 30), "2^26"),
     (R.EUNSUPPORTED, dict(n_seqs=1 << 22), "2^23"),
 ]
