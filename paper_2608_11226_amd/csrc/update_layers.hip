@@ -9,8 +9,10 @@ using namespace rollout;
 
 namespace {
 
-// rows times heads, and workgroups of 256 threads: a launch has less than 2^32 threads
-constexpr int64_t kMaxHeadRows = 1 << 26, kMaxGroups = (1 << 24) - 8;
+// A launch has less than 2^32 threads, in workgroups of 256.  Attention has one for some 32 rows of a head at least, and one more
+// for a head and sequence.
+constexpr int64_t kMaxGroups = (1 << 24) - 8, kMaxHeadRows = 1 << 26, kMaxHeadSeqs = 1 << 23;
+static_assert(kMaxHeadRows / 32 + kMaxHeadSeqs < kMaxGroups, "a launch of attention");
 constexpr int64_t kMaxRowBytes = 1 << 25;
 
 rollout_status check_shape(const rollout_attention_shape* s) {
@@ -27,8 +29,7 @@ rollout_status check_shape(const rollout_attention_shape* s) {
   if (!(s->scale >= 0x1p-100f && s->scale <= 0x1p100f)) return fail(ROLLOUT_EINVAL, "scale must be in [2^-100, 2^100]");
   if ((int64_t)s->n_heads * std::max(s->n_q, s->n_k) > kMaxHeadRows)
     return fail(ROLLOUT_EUNSUPPORTED, "n_heads times tokens above 2^26");
-  if ((int64_t)s->n_heads * (s->n_seqs + (int64_t)std::max(s->n_q, s->n_k) / 32) > kMaxGroups)
-    return fail(ROLLOUT_EUNSUPPORTED, "n_heads times sequences above 2^23");
+  if ((int64_t)s->n_heads * s->n_seqs > kMaxHeadSeqs) return fail(ROLLOUT_EUNSUPPORTED, "n_heads times sequences above 2^23");
   return ROLLOUT_OK;
 }
 
@@ -331,9 +332,11 @@ rollout_status rollout_adamw(const void* d_table, int32_t n_tensors, int64_t n_c
   if (n_chunks < 0 || n_chunks > kMaxGroups) return fail(ROLLOUT_EINVAL, "n_chunks is not what the table's making gave");
   if (!d_table) return fail(ROLLOUT_EINVAL, "the table is NULL");
   if (!aligned_to(d_table, 8)) return fail(ROLLOUT_EINVAL, "the table must be aligned to 8 bytes");
-  if (!std::isfinite(lr)) return fail(ROLLOUT_EINVAL, "lr must be finite");
+  if (!std::isfinite((float)lr)) return fail(ROLLOUT_EINVAL, "lr must be finite in fp32");
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(ROLLOUT_EINVAL, "beta1 and beta2 must be in [0, 1)");
-  if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(ROLLOUT_EINVAL, "eps must be >= 0 and finite");
+  // (the reciprocal of a smaller one is not finite, and 0 times that no number)
+  if (!(eps == 0.0 || eps >= 0x1p-126) || !std::isfinite((float)eps))
+    return fail(ROLLOUT_EINVAL, "eps must be 0 or at least 2^-126, and finite in fp32");
   if (!d_step && step < 1) return fail(ROLLOUT_EINVAL, "step must be >= 1");
   if ((st = check_words({d_grad_scale, d_lr})) != ROLLOUT_OK) return st;
   if (!aligned_to(d_step, 8)) return fail(ROLLOUT_EINVAL, "d_step must be aligned to 8 bytes");

@@ -31,7 +31,7 @@ SHAPES = [
     (R.EINVAL, dict(scale=float("nan")), "scale"), (R.EINVAL, dict(scale=float("inf")), "scale"), (R.EINVAL, dict(scale=3e38), "scale"),
     (R.EINVAL, dict(scale=1e-31), "scale"), (R.EINVAL, dict(scale=1.3e30), "scale"),
     (R.EUNSUPPORTED, dict(n_q=(1 << 23) + 1), "2^26"), (R.EUNSUPPORTED, dict(n_k=1 << 30), "2^26"),
-    (R.EUNSUPPORTED, dict(n_seqs=1 << 22), "2^23"),
+    (R.EUNSUPPORTED, dict(n_seqs=1 << 22), "2^23"), (R.EUNSUPPORTED, dict(n_seqs=(1 << 20) + 1), "2^23"),
 ]
 
 
@@ -249,6 +249,7 @@ STEP = dict(table=A, tensors=3, chunks=5, lr=1e-3, b1=0.9, b2=0.95, eps=1e-8, st
     (R.EUNSUPPORTED, dict(tensors=BIG + 3), "int32"), (R.EUNSUPPORTED, dict(tensors=(1 << 20) + 1), "2^20"), (R.EINVAL, dict(chunks=-1), "n_chunks"),
     (R.EINVAL, dict(chunks=1 << 24), "n_chunks"), (R.EINVAL, dict(lr=float("nan")), "lr"), (R.EINVAL, dict(b1=1.0), "beta"),
     (R.EINVAL, dict(b1=-0.1), "beta"), (R.EINVAL, dict(b2=1.5), "beta"), (R.EINVAL, dict(b2=float("nan")), "beta"), (R.EINVAL, dict(eps=-1.0), "eps"),
+    (R.EINVAL, dict(eps=1e-40), "2^-126"), (R.EINVAL, dict(eps=1e39), "eps"), (R.EINVAL, dict(lr=1e39), "lr"),
     (R.EINVAL, dict(eps=float("inf")), "eps"), (R.EINVAL, dict(step=0), "step"), (R.EINVAL, dict(step=-3), "step"),
     (R.EUNSUPPORTED, dict(step=1 << 64), "int64"), (R.EINVAL, dict(seed=-1), "seed"), (R.EINVAL, dict(seed=1 << 64), "seed"),
     (R.EINVAL, dict(scale=B + 2), "4 bytes"), (R.EINVAL, dict(step_now=D + 4), "8 bytes"),
