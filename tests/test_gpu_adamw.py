@@ -138,11 +138,16 @@ def test_kinds_in_one_table_and_many_tensors():
     check_step(tensors, 3, 5, before)
 
 
-def test_large_table_takes_larger_chunks():
+def test_chunks_of_four_steps():
+    """As tables of more than 2^34 elements have them: a small table is given that chunk."""
     g = torch.Generator(device=DEV).manual_seed(4)
     tensors = [Tensor(g, n, "fp32", "bf16", "e4m3", True) for n in (3000001, 128, 2000003)]
-    handle = table_of(tensors)
-    assert handle[2] < 1000  # larger ones than the 2,048 elements of small tables
+    table, n, chunks = table_of(tensors)
+    entries = table.cpu().view(torch.int64).view(n, -1)  # 7 addresses, n, first, chunk, ...
+    assert entries[:, 9].tolist() == [2048] * n and entries[:, 8].tolist() == [0, 1465, 1466] and chunks == 2443
+    entries[:, 9] = 8192
+    entries[:, 8] = torch.tensor([0, 367, 368])
+    handle = entries.view(torch.uint8).flatten().to(DEV), n, 613
     before = [(wide(t.p), *t.moments()) for t in tensors]
     step_of(handle, 2, 9)
     torch.cuda.synchronize()
