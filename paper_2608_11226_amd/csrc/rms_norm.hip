@@ -13,22 +13,34 @@ namespace {
 
 struct None {};
 
+// Eight neighbours of a row from p on, of which n are the row's.  A row's last ones are read with those before them, in the same
+// 16-byte loads as all others, and moved to their places by `settle` once everything is on the way: read one by one they would
+// be a chain of trips to memory.  Rows of fewer than eight (`narrow`) have none before them.
 template <typename T>
-__device__ __forceinline__ void read8(const T* p, int n, float (&v)[8]) {
-  if (n >= 8) {
-    if constexpr (sizeof(T) == 2) {
-      unpack16(load16(p), v);
-    } else {
-      float a[4], b[4];
-      unpack16(load16(p), a);
-      unpack16(load16(p + 4), b);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-    }
-  } else {
+__device__ __forceinline__ void read8(const T* p, int n, bool narrow, float (&v)[8]) {
+  if (narrow) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < n ? ldf(p, i) : 0.f;
+    return;
   }
+  p += min(0, n - 8);
+  if constexpr (sizeof(T) == 2) {
+    unpack16(load16(p), v);
+  } else {
+    float a[4], b[4];
+    unpack16(load16(p), a);
+    unpack16(load16(p + 4), b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  }
+}
+__device__ __forceinline__ void settle(int n, bool narrow, float (&v)[8]) {
+  if (n >= 8 || narrow) return;
+#pragma unroll
+  for (int by = 4; by > 0; by /= 2)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((8 - n) & by) v[i] = i + by < 8 ? v[i + by < 8 ? i + by : 0] : 0.f;
 }
 template <typename T>
 __device__ __forceinline__ void write8(T* p, int n, const float (&v)[8]) {
@@ -86,27 +98,27 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   const int64_t row = (int64_t)blockIdx.x * (W < 256 ? 256 / W : 1) + threadIdx.x / W;
   if (row >= A.rows) return;  // (a whole wave)
   const X* x = (const X*)A.x + row * A.dim;
-  float h[S][8];
+  const D* d = (const D*)A.delta + row * A.dim;
+  X* to = (X*)A.h + row * A.dim;
+  const bool narrow = A.dim < 8;
+  float h[S][8], g[S][8];
 #pragma unroll
   for (int s = 0; s < S; ++s) {
-    const int i = 8 * (t + s * W);
-    if (i < A.dim) read8(x + i, A.dim - i, h[s]);
-  }
-  if constexpr (kAdds) {
-    const D* d = (const D*)A.delta + row * A.dim;
-    X* to = (X*)A.h + row * A.dim;
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int i = 8 * (t + s * W);
-      if (i >= A.dim) continue;
-      float v[8];
-      read8(d + i, A.dim - i, v);
+    const int i = 8 * (t + s * W), n = A.dim - i;
+    if (n <= 0) continue;
+    float v[8];
+    read8(x + i, n, narrow, h[s]);
+    if constexpr (kAdds) read8(d + i, n, narrow, v);
+    if (A.gain) read8(A.gain + i, n, narrow, g[s]);  // (in flight with the others)
+    settle(n, narrow, h[s]);
+    if constexpr (kAdds) {
+      settle(n, narrow, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         h[s][e] += v[e];
         if constexpr (sizeof(X) == 2) h[s][e] = bf16_to_f32(round_bf16(h[s][e]));  // the norm is of what is stored
       }
-      write8(to + i, A.dim - i, h[s]);
+      write8(to + i, n, h[s]);
     }
   }
   float sum = 0.f;
@@ -123,12 +135,11 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   for (int s = 0; s < S; ++s) {
     const int i = 8 * (t + s * W);
     if (i >= A.dim) continue;
-    float g[8];
-    if (A.gain) read8(A.gain + i, A.dim - i, g);
+    if (A.gain) settle(A.dim - i, narrow, g[s]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       h[s][e] *= r;
-      if (A.gain) h[s][e] *= g[e];
+      if (A.gain) h[s][e] *= g[s][e];
       if constexpr (sizeof(Y) == 1) most = larger(most, fabsf(h[s][e]));
     }
   }
@@ -151,17 +162,18 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
   }
 }
 
-// Rows `worker`, `worker` + workers, ... of the gradient; the worker's sum of dy xhat stays in registers and ends in
-// partial[worker].
+// Rows `worker`, `worker` + workers, ... of the gradient; the worker's sum of dy xhat stays in registers, and the workgroup's (of
+// four workers where a row is a wave's) ends in partial[workgroup].
 template <typename X, typename G, typename O, int W, int S>
 __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm_backward(NormGradArgs A, int workers, float* __restrict__ partial) {
   __shared__ float red[2][W / 64];
   const int t = threadIdx.x % W;
   const int worker = (int)blockIdx.x * (W < 256 ? 256 / W : 1) + threadIdx.x / W;
-  if (worker >= workers) return;  // (a whole wave)
   float sum[S][8] = {};
   float* turn = red[0];
   float* other = red[1];
+  const bool narrow = A.dim < 8;
+  constexpr bool kEarly = S < 4;  // the inner gradient is in flight with the others, where registers allow
   for (int64_t row = worker; row < A.rows; row += workers) {
     const X* hp = (const X*)A.h + row * A.dim;
     const G* dyp = (const G*)A.dy + row * A.dim;
@@ -172,16 +184,20 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm_backward(NormGra
     for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
-      read8(hp + i, A.dim - i, xhat[s]);
-      read8(dyp + i, A.dim - i, g[s]);
-      if (A.inner) read8((const O*)A.inner + row * A.dim + i, A.dim - i, v[s]);  // (in flight with the others)
+      read8(hp + i, A.dim - i, narrow, xhat[s]);
+      read8(dyp + i, A.dim - i, narrow, g[s]);
+      if (kEarly && A.inner) read8((const O*)A.inner + row * A.dim + i, A.dim - i, narrow, v[s]);
     }
 #pragma unroll
     for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
       float gain[8];
-      if (A.gain) read8(A.gain + i, A.dim - i, gain);
+      if (A.gain) read8(A.gain + i, A.dim - i, narrow, gain);
+      settle(A.dim - i, narrow, xhat[s]);
+      settle(A.dim - i, narrow, g[s]);
+      if (kEarly) settle(A.dim - i, narrow, v[s]);
+      if (A.gain) settle(A.dim - i, narrow, gain);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         xhat[s][e] *= r;
@@ -199,29 +215,51 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm_backward(NormGra
     for (int s = 0; s < S; ++s) {
       const int i = 8 * (t + s * W);
       if (i >= A.dim) continue;
+      if (!kEarly && A.inner) {
+        read8((const O*)A.inner + row * A.dim + i, A.dim - i, narrow, v[s]);
+        settle(A.dim - i, narrow, v[s]);
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[s][e] = fmaf(r, g[s][e] - xhat[s][e] * dot, v[s][e]);
       write8(to + i, A.dim - i, v[s]);
     }
   }
   if (!partial) return;
+  if constexpr (W == 64) {
+    __shared__ float all[3][S][8][64];
+    const int wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (wave) all[wave - 1][s][e][t] = sum[s][e];
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[s][e] = ((sum[s][e] + all[0][s][e][t]) + all[1][s][e][t]) + all[2][s][e][t];
+  }
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     const int i = 8 * (t + s * W);
-    if (i < A.dim) write8(partial + (int64_t)worker * A.dim + i, A.dim - i, sum[s]);
+    if (i < A.dim) write8(partial + (int64_t)blockIdx.x * A.dim + i, A.dim - i, sum[s]);
   }
 }
 
-// Sums of the workers' columns in a fixed order: 32 columns a workgroup, four of them a thread, every 64th worker a row of
-// threads.
+// Sums of the workgroups' columns in a fixed order: 32 columns a workgroup here, four of them a thread, every 64th row of them a
+// row of threads, of which a wave holds eight.
 constexpr int kJoinRows = 64;
-__global__ __launch_bounds__(8 * kJoinRows) void k_norm_join(const float* __restrict__ partial, int workers, int dim, int accumulate,
+__global__ __launch_bounds__(8 * kJoinRows) void k_norm_join(const float* __restrict__ partial, int rows, int dim, int accumulate,
                                                             float* __restrict__ dgain) {
-  __shared__ float red[kJoinRows][33];
+  __shared__ float red[kJoinRows / 8][32];
   const int c = threadIdx.x & 7, k = threadIdx.x >> 3, col = (int)blockIdx.x * 32 + 4 * c;
+  const int mine = (int)blockIdx.x * 32 + threadIdx.x;
+  const bool ends = threadIdx.x < 32 && mine < dim;
+  const float before = ends && accumulate ? dgain[mine] : 0.f;
   float sum[4] = {};
 #pragma unroll 4
-  for (int w = k; w < workers; w += kJoinRows) {
+  for (int w = k; w < rows; w += kJoinRows) {
     const float* p = partial + (int64_t)w * dim + col;
     float v[4] = {};
     if (col + 4 <= dim)
@@ -232,14 +270,17 @@ __global__ __launch_bounds__(8 * kJoinRows) void k_norm_join(const float* __rest
     for (int e = 0; e < 4; ++e) sum[e] += v[e];
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) red[k][4 * c + e] = sum[e];
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int apart = 8; apart < 64; apart *= 2) sum[e] += __shfl_xor(sum[e], apart, 64);
+    if ((threadIdx.x & 63) < 8) red[threadIdx.x >> 6][4 * c + e] = sum[e];
+  }
   __syncthreads();
-  const int mine = (int)blockIdx.x * 32 + threadIdx.x;
-  if (threadIdx.x >= 32 || mine >= dim) return;
+  if (!ends) return;
   float total = 0.f;
-#pragma unroll 8
-  for (int i = 0; i < kJoinRows; ++i) total += red[i][threadIdx.x];
-  dgain[mine] = accumulate ? dgain[mine] + total : total;
+#pragma unroll
+  for (int i = 0; i < kJoinRows / 8; ++i) total += red[i][threadIdx.x];
+  dgain[mine] = accumulate ? before + total : total;
 }
 
 }  // namespace
@@ -289,16 +330,25 @@ hipError_t forward_from(hipStream_t s, int delta_dtype, int y_dtype, const NormA
                                              : forward_to<X, uint16_t>(s, y_dtype, a);
 }
 
-int workers_of(int rows, int dim) { return std::min(rows, norm_threads(dim) == 64 ? 4096 : 1024); }
+// As many as the card holds at a time, by the registers that they take: more would wait for the others' places, and each has as
+// many rows as they (12,288 x 3,584 114 us with 512, 120 with 768, 131 with 1,024; 8,192 x 8,192 172 with 256, 177 with 512;
+// 65,536 x 640 124 with 4,096, 146 with 6,144; 60,000 x 300 83 with 6,144, 88 with 4,096, 107 with 8,192).
+int workers_of(int rows, int dim) {
+  return std::min(rows, dim <= 512 ? 6144 : dim <= 1024 ? 4096 : dim <= 2048 ? 1536 : dim <= 4096 ? 512 : 256);
+}
+int groups_of(int rows, int dim) {
+  const int each = norm_threads(dim) == 64 ? 4 : 1;
+  return (workers_of(rows, dim) + each - 1) / each;
+}
 
 template <typename X, typename G, typename O>
 hipError_t backward(hipStream_t s, const NormGradArgs& a, float* partial) {
-  const int n = workers_of(a.rows, a.dim);
+  const int n = workers_of(a.rows, a.dim), groups = groups_of(a.rows, a.dim);
   by_dim(a.dim, [&](auto W, auto S) {
     constexpr int kRows = W < 256 ? 256 / W : 1;
-    k_rms_norm_backward<X, G, O, W, S><<<(n + kRows - 1) / kRows, kRows * W, 0, s>>>(a, n, a.dgain ? partial : nullptr);
+    k_rms_norm_backward<X, G, O, W, S><<<groups, kRows * W, 0, s>>>(a, n, a.dgain ? partial : nullptr);
+    if (a.dgain) k_norm_join<<<(a.dim + 31) / 32, 8 * kJoinRows, 0, s>>>(partial, groups, a.dim, a.accumulate, a.dgain);
   });
-  if (a.dgain) k_norm_join<<<(a.dim + 31) / 32, 8 * kJoinRows, 0, s>>>(partial, n, a.dim, a.accumulate, a.dgain);
   return hipGetLastError();
 }
 template <typename X, typename G>
@@ -319,8 +369,9 @@ hipError_t launch_rms_norm(hipStream_t s, int x_dtype, int delta_dtype, int y_dt
 
 // (that of a large call does for small ones, which may have more workers)
 size_t rms_norm_backward_workspace(int rows, int dim) {
-  const int narrow = std::min(dim, 1024);
-  return std::max((size_t)workers_of(rows, dim) * dim, (size_t)workers_of(rows, narrow) * narrow) * 4;
+  size_t most = 0;
+  for (int d : {512, 1024, 2048, 4096, kMaxNormDim}) most = std::max(most, (size_t)groups_of(rows, std::min(d, dim)) * std::min(d, dim));
+  return 4 * most;
 }
 
 hipError_t launch_rms_norm_backward(hipStream_t s, int h_dtype, int dy_dtype, int dx_dtype, const NormGradArgs& a, void* ws) {
