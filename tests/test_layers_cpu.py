@@ -227,7 +227,7 @@ def test_adamw_tables_that_are_taken():
     table, chunks = R.rollout_adamw_table([entry(**EIGHT, d_copy=G, n=5000), entry(d_param=A + 20000, d_grad=B + 10000, d_m=C + 5000 + 3000,
                                                                                      d_v=D + 8000)])
     assert chunks == 4
-    assert R.rollout_adamw_table([entry(n=1 << 30), entry(d_param=G, d_grad=H, d_m=I, d_v=J, n=1)])[1] == (1 << 17) + 1
+    assert R.rollout_adamw_table([entry(n=1 << 30), entry(d_param=G, d_grad=H, d_m=I, d_v=J, n=1)])[1] == (1 << 19) + 1
     tight = [entry(d_param=A, d_grad=A + 4000, d_m=A + 6000, d_v=A + 10000)]
     assert R.rollout_adamw_table(tight)[1] == 1
     out, need = ctypes.c_int64(), ctypes.c_uint64()
