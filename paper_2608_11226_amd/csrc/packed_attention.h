@@ -88,9 +88,6 @@ struct Rows {
   // byte offset of chunk c of a row
   static __device__ __forceinline__ int at(int row, int c) { return row * kBytes + ((c ^ swizzle(row)) << 4); }
 
-  // loads of a wave for N rows by NW waves (some waves have none where there are fewer than waves)
-  static constexpr int loads(int N, int NW) { return N * kChunks / 64 >= NW ? N * kChunks / 64 / NW : 1; }
-
   // N rows dealt out to loads of NW waves.  issue(row, offset, place): the row that the lane has 16 bytes of, at `offset` of it,
   // and the bytes behind the tile's beginning where the wave's lie, the lane's 16 lane bytes behind that.
   template <int N, int NW, typename F>
@@ -312,31 +309,25 @@ struct WaveRows {
   }
 };
 
-// Tiles 0 .. n - 1 pass through S buffers in LDS, S - 1 of them on the way at a time.  load(buffer, tile) issues a tile's loads,
-// LOADS of each wave at least as its last ones; step(buffer, tile) works on one.  The buffer is a compile-time number, so that
-// it is part of the LDS instructions' offsets.  first_tiles comes before what else a workgroup has to read.
-template <int S, int LOADS, int B = 0, typename Load, typename Step>
+// Tiles 0 .. n - 1 pass through two buffers in LDS: while one is worked on, the next is on the way.  load(buffer, tile) issues a
+// tile's loads, step(buffer, tile) works on it.  The buffer is a compile-time number, so that it is part of the LDS
+// instructions' offsets.  first_tile comes before what else a workgroup has to read.  (Three buffers of half a tile, two of them
+// on the way, took the 14B gradient of 8,192 tokens from 2,204 to 2,240 us: a tile's products take longer than its way.)
+template <int B, typename Load, typename Step>
 __device__ __forceinline__ bool one_tile(int it, int n, Load& load, Step& step) {
   if (it >= n) return false;
-  // the tile is there for every wave, and nobody reads the buffer before it any more
-  if (S > 2 && it + 1 < n)
-    dma_wait_barrier<(S - 2) * LOADS>();
-  else
-    dma_wait_barrier<0>();
-  if (it + S - 1 < n) load(std::integral_constant<int, (B + S - 1) % S>(), it + S - 1);
+  dma_wait_barrier<0>();  // the tile is there for every wave, and nobody reads the one before it any more
+  if (it + 1 < n) load(std::integral_constant<int, 1 - B>(), it + 1);
   step(std::integral_constant<int, B>(), it);
-  if constexpr (B + 1 < S) return one_tile<S, LOADS, B + 1>(it + 1, n, load, step);
   return true;
 }
-template <int S, typename Load>
-__device__ __forceinline__ void first_tiles(int n, Load& load) {
-  static_assert(S == 2 || S == 3, "the wait before the last tile but one is for all");
+template <typename Load>
+__device__ __forceinline__ void first_tile(int n, Load& load) {
   if (n > 0) load(std::integral_constant<int, 0>(), 0);
-  if (S > 2 && n > 1) load(std::integral_constant<int, 1>(), 1);
 }
-template <int S, int LOADS, typename Load, typename Step>
+template <typename Load, typename Step>
 __device__ __forceinline__ void through_tiles(int n, Load& load, Step step) {
-  for (int it = 0; one_tile<S, LOADS>(it, n, load, step); it += S) {
+  for (int it = 0; one_tile<0>(it, n, load, step) && one_tile<1>(it + 1, n, load, step); it += 2) {
   }
 }
 

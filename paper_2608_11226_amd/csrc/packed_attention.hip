@@ -70,7 +70,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
     R::template load<kKeys, kWaves>(s_kv[buf][0], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
     R::template load<kKeys, kWaves>(s_kv[buf][1], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
   };
-  first_tiles<2>(tiles, load);
+  first_tile(tiles, load);
   // the rows by way of the second tile's place
   char* place = s_kv[1][0] + 32 * wave * R::kBytes;
   const size_t heads = (size_t)kvh * group.each * HD;
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
   for (int d = 0; d < HD / 32; ++d) clear(o[d]);
   const float c2 = A.scale * kLog2e;  // scores are kept in units of log 2
   float m_run = -3.4e38f, l_run = 0.f;
-  through_tiles<2, 2 * R::loads(kKeys, kWaves)>(tiles, load, [&](auto buf, int it) {
+  through_tiles(tiles, load, [&](auto buf, int it) {
     const int k0 = (first + it) * kKeys;
     if (k0 >= w_most) return;  // (the same for the whole wave)
     rows.renew();

@@ -17,10 +17,10 @@ namespace {
 constexpr int kWaves = 4;
 
 // Queries' gradients.  A workgroup takes 128 rows, a row being a token's query of one of the heads that share a key's, a wave 32 of
-// them, whose q and do stay in registers, and walks over tiles of 32 keys.  Scores have keys as rows and queries as columns, as
+// them, whose q and do stay in registers, and walks over tiles of 64 keys.  Scores have keys as rows and queries as columns, as
 // in the forward pass, and where there are few rows the keys are dealt out to several workgroups as there.  It leaves
 // -lse / scale and -D of every row behind ([n_q][heads]), which the keys' gradients need.
-constexpr int kDqRows = 32 * kWaves, kDqKeys = 32;
+constexpr int kDqRows = 32 * kWaves, kDqKeys = 64;
 
 template <typename T, int HD>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, Group group, int slots, int parts,
@@ -28,10 +28,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
                                                                                  float* __restrict__ partial) {
   typedef Rows<T, HD> R;
   typedef typename R::Frag Frag;
-  constexpr int S = sizeof(T) == 2 ? 3 : 2;
-  __shared__ __align__(16) char s_kv[S][2][kDqKeys * R::kBytes];
-  __shared__ __align__(16) char s_rows[kDqRows * R::kBytes];
-  static_assert(4 * kDqKeys == kDqRows, "two tiles' places hold the workgroup's rows");
+  __shared__ __align__(16) char s_kv[2][2][kDqKeys * R::kBytes];
+  static_assert(2 * kDqKeys == kDqRows, "a tile's place holds the workgroup's rows");
   Walk walk;
   if (!find_walk<true>(slots, parts, A.kv_heads, &walk)) return;
   const int lane = threadIdx.x & 63, a = lane & 31, half = lane >> 5;
@@ -61,8 +59,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     R::template load<kDqKeys, kWaves>(s_kv[buf][0], kb + (size_t)k0 * k_stride, k_stride, last, wave, lane);
     R::template load<kDqKeys, kWaves>(s_kv[buf][1], vb + (size_t)k0 * v_stride, v_stride, last, wave, lane);
   };
-  // the rows by way of LDS: q and do at once, out with the first tiles
-  char *place = s_rows + 32 * wave * R::kBytes, *other = s_kv[0][0] + 32 * wave * R::kBytes;
+  // the rows by way of LDS: q and do at once, out with the first tile
+  char *place = s_kv[1][0] + 32 * wave * R::kBytes, *other = s_kv[0][0] + 32 * wave * R::kBytes;
   const size_t heads = (size_t)kvh * group.each * HD;
   const WaveRows<T, HD> mine_of(min(w_first, n_rows - 1), n_rows, group);
   mine_of.load(place, (const T*)A.q + (size_t)sq.start * A.q_stride + heads, A.q_stride, lane);
@@ -74,7 +72,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   for (int c = 0; c < HD / 16; ++c) qf[c] = mine_of.operand(place, lane, c), df[c] = mine_of.operand(other, lane, c);
   lds_barrier();
   mine_of.load(place, (const T*)A.out + (size_t)sq.start * A.out_stride + heads, A.out_stride, lane);
-  first_tiles<S>(tiles, load);
+  first_tile(tiles, load);
   float2 my = make_float2(0.f, 0.f);  // lse in units of log 2, and D
   dma_wait();
 #pragma unroll
@@ -94,51 +92,54 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) clear(dq[d]);
   const float c2 = A.scale * kLog2e;
-  through_tiles<S, 2 * R::loads(kDqKeys, kWaves)>(tiles, load, [&](auto buf, int it) {
-    const int k0 = (first + it) * kDqKeys;
-    if (k0 >= w_most) return;  // (the same for the whole wave)
-    rows.renew();
-    cols.renew();
-    f32x16 s, dp;
-    clear(s);
-    clear(dp);
-    constexpr int C = HD / 16, D = HD / 32;
-    Frag fr[2][2], fc[2][D];
-    auto read_row = [&](auto g, Frag(&f)[2]) {
+  through_tiles(tiles, load, [&](auto buf, int it) {
+    constexpr int C = HD / 16, D = HD / 32, kUnroll = sizeof(T) == 2 ? kDqKeys / 32 : 1;  // (fp32: registers)
+#pragma unroll kUnroll
+    for (int b = 0; b < kDqKeys / 32; ++b) {
+      const int k0 = (first + it) * kDqKeys + 32 * b;
+      if (k0 >= w_most) return;  // (the same for the whole wave)
+      rows.renew();
+      cols.renew();
+      f32x16 s, dp;
+      clear(s);
+      clear(dp);
+      Frag fr[2][2], fc[2][D];
+      auto read_row = [&](auto g, Frag(&f)[2]) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_kv[buf][0] : s_kv[buf][1], 0, (2 * g + k) % C);
-    };
-    auto read_col = [&](auto g, Frag(&f)[D]) {
+        for (int k = 0; k < 2; ++k) f[k] = rows(2 * g < C ? s_kv[buf][0] : s_kv[buf][1], 32 * b, (2 * g + k) % C);
+      };
+      auto read_col = [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-      for (int d = 0; d < D; ++d) f[d] = cols(s_kv[buf][0], 16 * g, d);
-    };
-    read_row(std::integral_constant<int, 0>(), fr[0]);
-    groups<C, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
+        for (int d = 0; d < D; ++d) f[d] = cols(s_kv[buf][0], 32 * b + 16 * g, d);
+      };
+      read_row(std::integral_constant<int, 0>(), fr[0]);
+      groups<C, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if constexpr (2 * g < C)
-          mma(f[k], qf[(2 * g + k) % C], s);
-        else
-          mma(f[k], df[(2 * g + k) % C], dp);
+        for (int k = 0; k < 2; ++k) {
+          if constexpr (2 * g < C)
+            mma(f[k], qf[(2 * g + k) % C], s);
+          else
+            mma(f[k], df[(2 * g + k) % C], dp);
+        }
+      });
+      read_col(std::integral_constant<int, 0>(), fc[0]);
+      if (k0 + 32 > w_least) {
+        int limit = mine;
+        asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (k0 + 16 * (e >> 3) + 8 * half + (e & 7) >= limit) s[e] = -INFINITY;
       }
-    });
-    read_col(std::integral_constant<int, 0>(), fc[0]);
-    if (k0 + kDqKeys > w_least) {
-      int limit = mine;
-      asm volatile("" : "+v"(limit));  // (a branch, and not a comparison per score in every tile)
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (k0 + 16 * (e >> 3) + 8 * half + (e & 7) >= limit) s[e] = -INFINITY;
+      for (int e = 0; e < 16; ++e) dp[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my.x)) * (dp[e] - my.y);
+      Frag ds[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) operand_of(dp, i, ds[i]);
+      groups<2, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
+      });
     }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) dp[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my.x)) * (dp[e] - my.y);
-    Frag ds[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) operand_of(dp, i, ds[i]);
-    groups<2, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
-#pragma unroll
-      for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
-    });
   });
   if (parts > 1) {
     if (w_first + a >= n_rows) return;
@@ -149,13 +150,13 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
       for (int i = 0; i < 2; ++i) store8(out + 32 * d + 16 * i, dq[d], i, A.scale);
     return;
   }
+  lds_barrier();  // nobody reads tiles any more
   if (w_first >= n_rows) return;
   mine_of.store(place, dq, A.scale, (T*)A.dq + (size_t)sq.start * A.dq_stride + heads, A.dq_stride, lane);
 }
 
 // Keys' gradients.  A workgroup takes 128 keys, a wave 32 of them, whose k and v stay in registers, and walks over tiles of 32
-// rows.  Scores have queries as rows and keys as columns,
-// so that a lane holds one key's.
+// rows.  Scores have queries as rows and keys as columns, so that a lane holds one key's.
 constexpr int kBackKeys = 32 * kWaves, kBackRows = 32;
 
 template <typename T, int HD>
@@ -164,10 +165,9 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
                                                                                   float* __restrict__ partial) {
   typedef Rows<T, HD> R;
   typedef typename R::Frag Frag;
-  constexpr int S = sizeof(T) == 2 ? 3 : 2;
-  __shared__ __align__(16) char s_q[S][kBackRows * R::kBytes];
-  __shared__ __align__(16) char s_do[S][kBackRows * R::kBytes];
-  __shared__ __align__(16) float s_stat[S][2][kBackRows];
+  __shared__ __align__(16) char s_q[2][kBackRows * R::kBytes];
+  __shared__ __align__(16) char s_do[2][kBackRows * R::kBytes];
+  __shared__ __align__(16) float s_stat[2][2][kBackRows];
   // 128 dimensions: registers for all of k and v are some 20 too many, and six of v's eight operands lie in LDS (as much as two
   // workgroups of a compute unit have room for), in fp32, with one workgroup there, all of them
   constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 ? 2 : 0;
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     token += more, over += more_over;
     if (over >= each) over -= each, ++token;
   };
-  first_tiles<S>(tiles, load);
+  first_tile(tiles, load);
   Frag kf[C], vf[kKept ? kKept : 1];
   {
     const T* kp = (const T*)A.k + row * A.k_stride + (size_t)kvh * HD + 8 * half;
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
 #pragma unroll
   for (int d = 0; d < HD / 32; ++d) clear(dk[d]), clear(dv[d]);
   const float c2 = A.scale * kLog2e;
-  through_tiles<S, 2 * R::loads(kBackRows, kWaves)>(tiles, load, [&](auto buf, int it) {
+  through_tiles(tiles, load, [&](auto buf, int it) {
     const int i0 = (first + it) * kBackRows;
     if (i0 + kBackRows <= w_least) return;  // (the same for the whole wave)
     rows.renew();
@@ -387,7 +387,7 @@ int row_parts(const AttentionArgs& a) {
 }
 int key_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows) * a.kv_heads;
-  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k, 1.0, 1.4, dq_part_bytes(a));
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k, 2.0, 2.8, dq_part_bytes(a));
 }
 
 size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
