@@ -244,8 +244,16 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const AdamwEntry* __restrict
 
 }  // namespace
 
-// (7B layer in fp32 1,207 us, with chunks of four steps 1,252; longer ones only where a launch would have too many)
-int64_t adamw_chunk(int64_t all) { return all <= (int64_t)1 << 34 ? kStep : 4 * kStep; }
+// What a workgroup finds out before its first element (its tensor, factors, the hash's keys) costs nothing where memory is the
+// bound, and short chunks spread the load: a 7B layer with fp32 states 1,206 us with one step a workgroup, 1,231 with two and
+// 1,250 with four, its bf16 weights with fp32 states 909, 943 and 965.  Rounding by hashes makes arithmetic the bound: states in 8
+// bits 734, 728 and 738, bf16 weights with them 663, 639 and 597.  A table of few elements needs every workgroup (300 x 1,200 in two
+// layers 12.7 us with one step, 16.5 with four), and one of more than 2^34 takes four, for a launch of less than 2^32 threads.
+int64_t adamw_chunk(int64_t all, int kind) {
+  if (all > (int64_t)1 << 34) return 4 * kStep;
+  if (all <= (int64_t)1 << 24 || !(kind & 4)) return kStep;
+  return kind & 1 ? 4 * kStep : 2 * kStep;
+}
 
 hipError_t launch_adamw(hipStream_t s, const void* table, int tensors, int64_t chunks, const AdamwArgs& a) {
   k_adamw<<<(unsigned)chunks, kThreads, 0, s>>>((const AdamwEntry*)table, tensors, a);

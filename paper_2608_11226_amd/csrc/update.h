@@ -117,6 +117,7 @@ struct NormArgs {
   float eps;
   void *h, *y;
   float *scales, *rstd;
+  double per_value;  // 1 / dim
 };
 hipError_t launch_rms_norm(hipStream_t s, int x_dtype, int delta_dtype, int y_dtype, const NormArgs& a);
 
@@ -145,8 +146,8 @@ struct AdamwEntry {
 };
 constexpr int kMaxAdamwTensors = 1 << 20;
 constexpr int64_t kMaxAdamwElements = (int64_t)1 << 36;
-// elements that a workgroup takes of a tensor, by the number of all
-int64_t adamw_chunk(int64_t all);
+// elements that a workgroup takes of a tensor of a kind, by the number of all tensors' elements
+int64_t adamw_chunk(int64_t all, int kind);
 struct AdamwArgs {
   float b1, c1, b2, c2, eps, lr;
   double log_b1, log_b2, unbias1;  // 1 / (1 - b1^step)

@@ -207,7 +207,7 @@ rollout_status rollout_rms_norm(const void* d_x, int32_t x_dtype, const void* d_
                    {{"d_delta", d_delta, d_delta ? n * type_bytes(delta_dtype) : 0}, {"d_gain", d_gain, 4 * (size_t)dim}});
   if (st != ROLLOUT_OK) return st;
   if ((st = check_stream(hip_stream)) != ROLLOUT_OK) return st;
-  const NormArgs a = {d_x, d_delta, d_gain, n_rows, dim, eps, d_h, d_y, d_scales, d_rstd};
+  const NormArgs a = {d_x, d_delta, d_gain, n_rows, dim, eps, d_h, d_y, d_scales, d_rstd, 1.0 / dim};
   return launched(launch_rms_norm((hipStream_t)hip_stream, x_dtype, delta_dtype, y_dtype, a), "rms norm");
 }
 
@@ -303,14 +303,14 @@ rollout_status rollout_adamw_table(const rollout_adamw_tensor* h_tensors, int32_
         return fail(ROLLOUT_EINVAL, "tensor " + std::to_string(p.tensor) + ": a buffer overlaps another one of the table");
       (p.written ? written_to : read_to) = std::max(p.written ? written_to : read_to, p.hi);
     }
-    const int64_t chunk = adamw_chunk(all);
     int64_t chunks = 0;
     AdamwEntry* out = static_cast<AdamwEntry*>(h_table);
     for (int i = 0; i < n_tensors; ++i) {
       const rollout_adamw_tensor& t = h_tensors[i];
-      AdamwEntry e = {t.d_param, t.d_grad, t.d_m, t.d_v, t.d_m_scales, t.d_v_scales, t.d_copy, t.n, chunks, chunk, t.weight_decay, 0};
-      e.kind = (t.param_dtype == ROLLOUT_DTYPE_BF16 ? 1 : 0) | (t.grad_dtype == ROLLOUT_DTYPE_BF16 ? 2 : 0) |
-               (t.state_dtype == ROLLOUT_DTYPE_E4M3 ? 4 : 0);
+      const int32_t kind = (t.param_dtype == ROLLOUT_DTYPE_BF16 ? 1 : 0) | (t.grad_dtype == ROLLOUT_DTYPE_BF16 ? 2 : 0) |
+                           (t.state_dtype == ROLLOUT_DTYPE_E4M3 ? 4 : 0);
+      const int64_t chunk = adamw_chunk(all, kind);
+      const AdamwEntry e = {t.d_param, t.d_grad, t.d_m, t.d_v, t.d_m_scales, t.d_v_scales, t.d_copy, t.n, chunks, chunk, t.weight_decay, kind};
       std::copy_n(reinterpret_cast<const char*>(&e), sizeof e, reinterpret_cast<char*>(out + i));
       chunks += (t.n + chunk - 1) / chunk;
     }
