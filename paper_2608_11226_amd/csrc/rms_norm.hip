@@ -76,17 +76,27 @@ __device__ __forceinline__ void write8(uint8_t* p, int n, const float (&v)[8]) {
   }
 }
 
-// Sum (or maximum) over the W threads of a row, the same in all of them; red: 2 W / 64 values, used in turn.
-template <int W, typename F>
-__device__ __forceinline__ float row_reduce(float v, float* red, F f) {
+// Sum (or maximum) over the W threads of a row, of which v is a wave's, the same in all of them; red: W / 64 values.
+template <int W, typename A = float, typename F>
+__device__ __forceinline__ A row_reduce(float v, float* red, F f) {
+  A all = v;
   if constexpr (W > 64) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = red[0];
+    all = red[0];
 #pragma unroll
-    for (int i = 1; i < W / 64; ++i) v = f(v, red[i]);
+    for (int i = 1; i < W / 64; ++i) all = f(all, (A)red[i]);
   }
-  return v;
+  return all;
+}
+
+// 1 / sqrt(x), rounded once: a step of Newton's from the instruction's result, where that is within a unit (fp32's three
+// roundings, of the mean, the root and its reciprocal, moved 1.4 times as many e4m3 codes over a border)
+__device__ __forceinline__ float inverse_root(double x) {
+  const float f = (float)x;
+  if (!(f >= 0x1p-126f && f < INFINITY)) return 1.f / sqrtf(f);
+  const double r = __builtin_amdgcn_rsqf(f);
+  return (float)fma(0.5 * r, fma(-x * r, r, 1.0), r);
 }
 
 // W threads a row (64: four rows in a workgroup), S steps of 8 values each.  D: type of what is added, or None.
@@ -127,8 +137,8 @@ __global__ __launch_bounds__(W < 256 ? 256 : W) void k_rms_norm(NormArgs A) {
     if (8 * (t + s * W) < A.dim)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum = fmaf(h[s][e], h[s][e], sum);
-  sum = row_reduce<W>(wave_sum_f32(sum), red[0], [](float a, float b) { return a + b; });
-  const float r = 1.f / sqrtf(sum / (float)A.dim + A.eps);
+  const double all = row_reduce<W, double>(wave_sum_f32(sum), red[0], [](double a, double b) { return a + b; });
+  const float r = inverse_root(all * A.per_value + (double)A.eps);
   if (A.rstd && t == 0) A.rstd[row] = r;
   float most = 0.f;
 #pragma unroll
