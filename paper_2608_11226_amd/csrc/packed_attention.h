@@ -334,7 +334,8 @@ __device__ __forceinline__ void through_tiles(int n, Load& load, Step step) {
 // N groups of W operands from LDS, each group's loads on the way while the products of the one before it run.  load(g, f) reads
 // group g, use(g, f) multiplies by it; the first group may have been read before (read_ahead).  Left to itself the compiler
 // reads every operand into the same registers just before its product, whose time then is that of the read.
-__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }  // (of products and memory; other VALU and SALU may move)
+// (of products and memory; other VALU and SALU may move)
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0x6); }
 template <int N, int W, int g, typename Frag, typename Load, typename Use>
 __device__ __forceinline__ void group(Frag (&f)[2][W], Load& load, Use& use) {
   if constexpr (g + 1 < N) load(std::integral_constant<int, g + 1>(), f[(g + 1) & 1]);
@@ -357,7 +358,8 @@ struct Walk {
   int slot, part, kvh;
 };
 template <bool kParts>
-__host__ __device__ __forceinline__ void walk_runs(int slots, int parts, int kv_heads, uint32_t* length, uint32_t* runs, uint32_t* whole, uint32_t* rest) {
+__host__ __device__ __forceinline__ void walk_runs(int slots, int parts, int kv_heads, uint32_t* length, uint32_t* runs, uint32_t* whole,
+                                                   uint32_t* rest) {
   *length = (uint32_t)(kParts ? slots * parts : slots);
   *runs = (uint32_t)(kParts ? kv_heads : kv_heads * parts);
   *whole = *runs / 8 * *length;                  // walks of a die in whole runs

@@ -7,6 +7,13 @@
 // do so, one for the keys' gradients and one for the queries': seven products of the size of q k^T where one that adds up
 // queries' gradients atomically has five, but every sum has an order of its own that does not depend on scheduling.
 //
+// Bound by the matrix products and what feeds them: 8,192 tokens at 40 on 8 heads of 128 take 900 us for the queries and 1,286 for
+// the keys (products are at work in 0.70 and 0.65 of the compute units' cycles) and 59 to join the keys' parts; the 7B update's 16
+// sequences 88, 137 and 14 (0.32 and 0.38: short walks, and the longest ones end alone); fp32 at the 7B heads 1,003, 1,509 and 23.
+// Did not pay: the scores' exponentials issued beside the other product (7B 230 us, so 244), workgroups of eight waves that share
+// out a tile's rows and add up in LDS instead of half of the parts (7B 222, so 241; 14B 2,120, so 2,125), and as many parts as a
+// walk's own length asks for (some dies then wait for the others).
+//
 // Probabilities and ds enter the second products as bf16 where the inputs are bf16: each is off by at most 2^-8 of itself, as
 // far as the result's own rounding moves it.
 #include "packed_attention.h"
@@ -168,8 +175,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   __shared__ __align__(16) char s_q[2][kBackRows * R::kBytes];
   __shared__ __align__(16) char s_do[2][kBackRows * R::kBytes];
   __shared__ __align__(16) float s_stat[2][2][kBackRows];
-  // 128 dimensions: registers for all of k and v are some 20 too many, and six of v's eight operands lie in LDS (as much as two
-  // workgroups of a compute unit have room for), in fp32, with one workgroup there, all of them
+  // 128 dimensions: registers for all of k and v are some 20 too many, and what the compiler then keeps in scratch memory waits for
+  // the tiles on their way: six of v's eight operands lie in LDS, in fp32, with one workgroup in a compute unit, all of them
   constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 ? 2 : 0;
   __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
   Walk walk;
