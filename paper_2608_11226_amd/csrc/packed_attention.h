@@ -408,13 +408,24 @@ __device__ __forceinline__ int part_from(int n, int part, int parts) { return pa
 constexpr int kMaxParts = 64;
 constexpr uint64_t kPartsRoom = 256ull << 20;
 inline uint64_t parts_room(uint64_t part_bytes) { return std::min(kMaxParts * part_bytes, kPartsRoom); }
-inline int walk_parts(int64_t walks, double tiles, bool triangle, double alone_us, double shared_us, uint64_t part_bytes) {
-  const double places = 512.0, all = (triangle ? 0.55 : 1.0) * (double)walks * tiles * shared_us / places;
+struct WalkCost {
+  double alone_us, shared_us;
+  double least;  // tiles of a part
+};
+// bf16, as measured with 128 dimensions.  fp32: products of 32 x 32 x 2 values take 64 cycles, and are all that counts.
+template <typename T>
+inline WalkCost walk_cost(double alone_us, double shared_us, int products, int head_dim) {
+  if (sizeof(T) == 2) return {alone_us, shared_us, 4.0};
+  const double us = products * head_dim / 2 * 64 / 2400.0;
+  return {us, 2.0 * us, 1.0};
+}
+inline int walk_parts(int64_t walks, double tiles, bool triangle, const WalkCost& each, uint64_t part_bytes) {
+  const double places = 512.0, all = (triangle ? 0.55 : 1.0) * (double)walks * tiles * each.shared_us / places;
   const int most = (int)std::max<uint64_t>(1, parts_room(part_bytes) / part_bytes);
   int best = 1;
   double least = 0.0;
-  for (int p = 1; p <= most && (p == 1 || tiles >= 4.0 * p); ++p) {
-    const double walk = alone_us * tiles / p + 3.0;
+  for (int p = 1; p <= most && (p == 1 || tiles >= each.least * p); ++p) {
+    const double walk = each.alone_us * tiles / p + 3.0;
     const double cost = std::max(walk, all) + 0.35 * walk + (p > 1 ? 5.0 + 2.0 * p * (double)part_bytes / 4.5e6 : 0.0);
     if (p == 1 || cost < least) best = p, least = cost;
   }

@@ -237,14 +237,16 @@ __global__ __launch_bounds__(256) void k_attention_merge(AttentionArgs A, int sl
 }
 
 uint64_t part_bytes(const AttentionArgs& a) { return 4ull * a.n_q * a.heads * (a.head_dim + 4); }
+template <typename T>
 int key_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries) * a.kv_heads;
-  return walk_parts(walks, (double)a.n_k / a.n_seqs / kKeys, a.causal && a.n_q == a.n_k, 1.0, 1.6, part_bytes(a));
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kKeys, a.causal && a.n_q == a.n_k,
+                    walk_cost<T>(1.0, 1.6, 4, a.head_dim), part_bytes(a));
 }
 
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionArgs& a, float* partial) {
-  const int slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries), parts = key_parts(a);
+  const int slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries), parts = key_parts<T>(a);
   k_packed_attention<T, HD><<<walk_grid<true>(slots, parts, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, parts, partial);
   if (parts > 1) k_attention_merge<T, HD><<<dim3(slots * a.kv_heads, kQueries * HD / 1024), 256, 0, s>>>(a, slots, parts, partial);
   return hipGetLastError();

@@ -387,14 +387,17 @@ __global__ __launch_bounds__(256) void k_attention_join_dq(AttentionGradArgs A, 
 
 uint64_t dkv_part_bytes(const AttentionArgs& a) { return 8ull * a.n_k * a.kv_heads * a.head_dim; }
 uint64_t dq_part_bytes(const AttentionArgs& a) { return 4ull * a.n_q * a.heads * a.head_dim; }
+template <typename T>
 int row_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_k, 1, a.n_seqs, kBackKeys) * a.kv_heads;
-  return walk_parts(walks, (double)a.n_q * (a.heads / a.kv_heads) / a.n_seqs / kBackRows, a.causal && a.n_q == a.n_k, 1.3, 2.0,
-                    dkv_part_bytes(a));
+  return walk_parts(walks, (double)a.n_q * (a.heads / a.kv_heads) / a.n_seqs / kBackRows, a.causal && a.n_q == a.n_k,
+                    walk_cost<T>(1.3, 2.0, 4, a.head_dim), dkv_part_bytes(a));
 }
+template <typename T>
 int key_parts(const AttentionArgs& a) {
   const int64_t walks = (int64_t)tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows) * a.kv_heads;
-  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k, 2.0, 2.8, dq_part_bytes(a));
+  return walk_parts(walks, (double)a.n_k / a.n_seqs / kDqKeys, a.causal && a.n_q == a.n_k,
+                    walk_cost<T>(2.0, 2.8, 6, a.head_dim), dq_part_bytes(a));
 }
 
 size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
@@ -403,11 +406,11 @@ template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   float2* stats = (float2*)ws;
   float* partial = (float*)(ws + stats_bytes(a));  // of the queries, then of the keys
-  const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts(a);
+  const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts<T>(a);
   k_attention_dq<T, HD><<<walk_grid<true>(q_slots, kp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
   if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
   const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys);
-  const int rp = row_parts(a);
+  const int rp = row_parts<T>(a);
   k_attention_dkv<T, HD><<<walk_grid<false>(slots, rp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
   if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, rp, partial);
   return hipGetLastError();
