@@ -13,7 +13,7 @@
 // 8,192 keys at 64 on 8 heads of 128 takes 61 us and the join 5 (302 MB read at 5.0 TB/s, memory the bound; 428 us with a head
 // a workgroup and without parts).  Long sequences are bound by the matrix products: 8,192 tokens at 40 on 8 heads 655 us, 1,050
 // TFLOP/s in bf16 (products are at work in 0.61 of the compute units' cycles; exponentials and maxima fill much of the rest), at 64
-// dimensions 680; fp32 100 of the 154 that fp32 products reach.  Short ones, 16 of 257 to 768 tokens at 28 on 4 heads, 60 us, 545
+// dimensions 680; fp32 102 of the 154 that fp32 products reach.  Short ones, 16 of 257 to 768 tokens at 28 on 4 heads, 60 us, 545
 // TFLOP/s: walks of some five tiles, whose beginning (its place, rows and first tile, a trip to memory after the other) and end are
 // hidden by the compute unit's other workgroup alone (464 sequences of 18 tokens, a tile each, 40 us).  Exponentials issued between the products of the tile before them took the long case from 655 to 694 us, a
 // higher priority of waves at their products changed nothing, and half tiles with four on the way took few tokens' from 29 to 32.
@@ -103,6 +103,10 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
     rows.renew();
     cols.renew();
     constexpr int B = kKeys / 32, C = HD / 16, D = HD / 32;
+    // blocks of 32 keys at a time: fp32's long products are left out where no row of the wave has keys
+    constexpr int kAt = sizeof(T) == 2 ? B : 1;
+    const bool all_blocks = k0 + 32 * (B - 1) < w_most;
+    static_assert(B == 2, "one block or both");
     f32x16 s[B];
 #pragma unroll
     for (int b = 0; b < B; ++b) clear(s[b]);
@@ -115,11 +119,19 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
 #pragma unroll
       for (int d = 0; d < D; ++d) f[d] = cols(s_kv[buf][1], 16 * g, d);
     };
-    read_row(std::integral_constant<int, 0>(), fr[0]);
-    groups<B * C / 2, 2>(fr, read_row, [&](auto g, Frag(&f)[2]) {
+    auto scores = [&](auto b) {
+      read_row(std::integral_constant<int, b * C / 2>(), fr[0]);
+      groups<kAt * C / 2, 2>(
+          fr, [&](auto g, Frag(&f)[2]) { read_row(std::integral_constant<int, g + b * C / 2>(), f); },
+          [&](auto g, Frag(&f)[2]) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) mma(f[k], qf[(2 * g + k) % C], s[2 * g / C]);
-    });
+            for (int k = 0; k < 2; ++k) mma(f[k], qf[(2 * g + k) % C], s[b + 2 * g / C]);
+          });
+    };
+    scores(std::integral_constant<int, 0>());
+    if constexpr (kAt < B) {
+      if (all_blocks) scores(std::integral_constant<int, 1>());
+    }
     read_col(std::integral_constant<int, 0>(), fc[0]);
     if (k0 + kKeys > w_least) {
       int limit = mine;
@@ -159,10 +171,21 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
 #pragma unroll
       for (int i = 0; i < 2; ++i) operand_of(s[b], i, p[2 * b + i]);
     }
-    groups<2 * B, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
+    auto values = [&](auto b) {
+      groups<2 * kAt, D>(
+          fc, [&](auto g, Frag(&f)[D]) { read_col(std::integral_constant<int, g + 2 * b>(), f); },
+          [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-      for (int d = 0; d < D; ++d) mma(f[d], p[g], o[d]);
-    });
+            for (int d = 0; d < D; ++d) mma(f[d], p[g + 2 * b], o[d]);
+          });
+    };
+    values(std::integral_constant<int, 0>());
+    if constexpr (kAt < B) {
+      if (all_blocks) {
+        read_col(std::integral_constant<int, 2>(), fc[0]);
+        values(std::integral_constant<int, 1>());
+      }
+    }
   });
   const float l = l_run + __shfl_xor(l_run, 32, 64);
   if (parts > 1) {
