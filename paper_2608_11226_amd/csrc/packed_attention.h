@@ -412,10 +412,15 @@ struct WalkCost {
   double alone_us, shared_us;
   double least;  // tiles of a part
 };
-// bf16, as measured with 128 dimensions.  fp32: products of 32 x 32 x 2 values take 64 cycles, and are all that counts.
+// bf16: as measured with 128 dimensions, and 0.7 and 0.55 of that with 64 and 32 (the gradient of 2 x 500 to 1,500 tokens at 16 heads
+// of 64 63 us, at 1.0 of it 72, of 4 x 500 to 1,000 at 14 on 2 heads 56 and 66).  fp32: a product of 32 x 32 x 2 values takes 64
+// cycles, and those are all that counts (one token over 500 to 1,000 keys 28 us, with bf16's figures 77).
 template <typename T>
 inline WalkCost walk_cost(double alone_us, double shared_us, int products, int head_dim) {
-  if (sizeof(T) == 2) return {alone_us, shared_us, 4.0};
+  if (sizeof(T) == 2) {
+    const double share = head_dim == 128 ? 1.0 : head_dim == 64 ? 0.7 : 0.55;
+    return {share * alone_us, share * shared_us, 4.0};
+  }
   const double us = products * head_dim / 2 * 64 / 2400.0;
   return {us, 2.0 * us, 1.0};
 }
