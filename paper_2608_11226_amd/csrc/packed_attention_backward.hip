@@ -334,16 +334,20 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
     for (int i = 0; i < 2; ++i) store8(dkp + 32 * d + 16 * i, dk[d], i, A.scale), store8(dvp + 32 * d + 16 * i, dv[d], i, 1.f);
 }
 
-// Eight neighbours of the parts' sums, in order, to an output.
+// Eight neighbours of the parts' sums, in order, to an output; eight parts' are on the way together.
 template <typename T>
 __device__ __forceinline__ void join8(T* out, const float* p, size_t apart, int parts) {
-  float t[8], x[8];
-  ld8(p, 0, t);
-#pragma unroll 4
-  for (int k = 1; k < parts; ++k) {
-    ld8(p + k * apart, 0, x);
+  float t[8] = {};
+  for (int k0 = 0; k0 < parts; k0 += 8) {
+    float x[8][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] += x[e];
+    for (int k = 0; k < 8; ++k)
+      if (k0 + k < parts) ld8(p + (k0 + k) * apart, 0, x[k]);  // (the same for the whole wave)
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k0 + k < parts)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] += x[k][e];
   }
   if constexpr (sizeof(T) == 2)
     *reinterpret_cast<u32x4*>(out) = pack16(t);
@@ -400,6 +404,9 @@ int key_parts(const AttentionArgs& a) {
                     walk_cost<T>(2.0, 2.8, 6, a.head_dim), dq_part_bytes(a));
 }
 
+// workgroups for a tile's 128 rows of `width` values: a thread takes one chunk of eight, or several where there are many tiles
+int join_groups(int slots, int width) { return std::max(1, std::min(width / 16, std::max(8, 4096 / slots))); }
+
 size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
 
 template <typename T, int HD>
@@ -407,12 +414,13 @@ hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   float2* stats = (float2*)ws;
   float* partial = (float*)(ws + stats_bytes(a));  // of the queries, then of the keys
   const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts<T>(a);
+  const int join_slots = tile_slots(a.n_q, 1, a.n_seqs, 128);
   k_attention_dq<T, HD><<<walk_grid<true>(q_slots, kp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
-  if (kp > 1) k_attention_join_dq<T><<<dim3(tile_slots(a.n_q, 1, a.n_seqs, 128), 16), 256, 0, s>>>(a, kp, partial);
+  if (kp > 1) k_attention_join_dq<T><<<dim3(join_slots, join_groups(join_slots, a.heads * HD)), 256, 0, s>>>(a, kp, partial);
   const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys);
   const int rp = row_parts<T>(a);
   k_attention_dkv<T, HD><<<walk_grid<false>(slots, rp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
-  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * 8), 256, 0, s>>>(a, rp, partial);
+  if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * join_groups(slots, a.kv_heads * HD)), 256, 0, s>>>(a, rp, partial);
   return hipGetLastError();
 }
 
