@@ -410,7 +410,7 @@ constexpr uint64_t kPartsRoom = 256ull << 20;
 inline uint64_t parts_room(uint64_t part_bytes) { return std::min(kMaxParts * part_bytes, kPartsRoom); }
 struct WalkCost {
   double alone_us, shared_us;
-  double least;  // tiles of a part
+  double least;  // tiles of a part (one query of 1,024 to 4,096 keys, gradient: 38 us with 3, 40 with 4, 42 with 2)
 };
 // bf16: as measured with 128 dimensions, and 0.7 and 0.55 of that with 64 and 32 (the gradient of 2 x 500 to 1,500 tokens at 16 heads
 // of 64 63 us, at 1.0 of it 72, of 4 x 500 to 1,000 at 14 on 2 heads 56 and 66).  fp32: a product of 32 x 32 x 2 values takes 64
@@ -419,7 +419,7 @@ template <typename T>
 inline WalkCost walk_cost(double alone_us, double shared_us, int products, int head_dim) {
   if (sizeof(T) == 2) {
     const double share = head_dim == 128 ? 1.0 : head_dim == 64 ? 0.7 : 0.55;
-    return {share * alone_us, share * shared_us, 4.0};
+    return {share * alone_us, share * shared_us, 3.0};
   }
   const double us = products * head_dim / 2 * 64 / 2400.0;
   return {us, 2.0 * us, 1.0};
