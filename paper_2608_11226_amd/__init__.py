@@ -426,9 +426,9 @@ def rollout_embedding_backward(grad, grad_dtype: int, tokens, n_tokens: int, voc
 
 def _matrix(name: str, x, kind, n: int, stride: int, width: int, device: int):
     """A matrix of n rows of width elements, stride apart."""
-    if type(x) is _torch.Tensor and x.dtype is kind and x.dim() == 2 and x.get_device() == device:
+    if type(x) is _torch.Tensor and x.dtype is kind and x.get_device() == device and x.stride() == (stride, 1):
         have, wide = x.shape
-        if have >= n and wide >= width and x.stride() == (stride, 1):
+        if have >= n and wide >= width:
             return x.data_ptr()
     return _buf(name, x, kind, (n - 1) * stride + width, device, (n, stride, width))
 

@@ -402,7 +402,7 @@ __device__ __forceinline__ int part_from(int n, int part, int parts) { return pa
 // walk takes (alone_us a tile, or shared_us a tile in every one of the card's 512 places where there are more walks than
 // places), the third of a walk that the last ones run on, and the parts' sums, which are written and read again.  The constants
 // are fitted to sweeps of the parts at a dozen shapes, and the choice is within 3% of the best there (with and without parts: 72B's
-// one token 70 and 149 us, 7B gradient 228 and 256, 1,024 tokens' gradient 97 and 264, 14B gradient 2,127 and 2,325).
+// one token 70 and 149 us, 7B gradient 228 and 256, 1,024 tokens' gradient 89 and 264, 14B gradient 2,127 and 2,325).
 // No more parts than their sums have room for: the workspace of a large call has to do for small ones, which have more parts, so
 // it goes by the size of a part's sums alone.
 constexpr int kMaxParts = 64;
