@@ -524,7 +524,7 @@ rollout_status rollout_rms_norm_backward(const void* d_grad_y, int32_t grad_y_dt
  * The step, with g = grad_scale grad and t = step:
  *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   param = param (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, with the new moments before they are rounded (one of less than 2^-126 may count as 0; eps is 0 or at least that).  BF16 weights and E4M3 states are rounded up or down with
+ * in fp32, a moment's products, sum and root each rounded to nearest, with the new moments before they are rounded further (one of less than 2^-126 may count as 0; eps is 0 or at least that).  BF16 weights and E4M3 states are rounded up or down with
  * the probability that keeps their expectation (to nearest they would not move by steps that are small beside them), by 16 bits r
  * of a counter hash of (seed, t, the tensor's place in the table, the element): bf16 drops 16 bits of
  * the fp32 value's magnitude after adding r, e4m3 drops 20 after adding 16 r + 8 (below 2^-6, where values are 2^-9 apart,

@@ -5,8 +5,8 @@
 //
 // Bound by HBM: every tensor is read and written once.  A table in device memory names the tensors; a workgroup takes a chunk
 // of one of them, which it finds in the table by probing 64 entries at a time.  A 7B layer, 233 million elements: fp32 weights with
-// a bf16 copy and bf16 gradients 735 us with states in 8 bits (5.1 TB/s), 1,206 with fp32 states (5.4); bf16 weights with states in
-// 8 bits 598 (3.9 TB/s), where two hashes and the rounding of three values an element keep the vector ALU busy.
+// a bf16 copy and bf16 gradients 748 us with states in 8 bits (5.0 TB/s), 1,206 with fp32 states (5.4); bf16 weights with states in
+// 8 bits 623 (3.8 TB/s), where two hashes and the rounding of three values an element keep the vector ALU busy.
 //
 // States in 8 bits are e4m3 with a power of two as scale for each run of 128 elements (16 lanes of 8): the first moment, and
 // the root of the second, whose range is half as wide.  To nearest, a state would not move at all where a step changes it by
@@ -124,6 +124,25 @@ __device__ __forceinline__ float towards(float x, uint32_t bits) {
   return copysignf(small ? q - 0x1p-6f : q, x);
 }
 
+// b m + c x, each product and the sum rounded: a unit's difference in a moment is enough to send it to the other one of two states
+// that are an eighth apart, and the next step with it, and no formula in fp32 says where a compiler fuses
+__device__ __forceinline__ float moment(float b, float m, float c, float x) {
+#pragma clang fp contract(off)
+  const float p = b * m, q = c * x;
+  return p + q;
+}
+
+// The instruction's root is within a unit.  It is one too large if x <= r (r - unit), and one too small if x > r (r + unit): the
+// border between two neighbours, squared, lies within a quarter of a unit squared of their product.  (0 and infinity stay: their
+// neighbours' products are 0 or no numbers.  7B layer with states in 8 bits 748 us, with the library's root, which scales small x as
+// well, 761.)
+__device__ __forceinline__ float nearest_root(float x) {
+  const float r = __builtin_amdgcn_sqrtf(x);
+  const float below = __uint_as_float(__float_as_uint(r) - 1u), above = __uint_as_float(__float_as_uint(r) + 1u);
+  const float lower = fmaf(-below, r, x), upper = fmaf(-above, r, x);
+  return lower <= 0.f ? below : upper > 0.f ? above : r;
+}
+
 struct Factors {
   float b1, c1, b2, c2, eps, lr, step, root;  // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   float grad;
@@ -159,10 +178,10 @@ __device__ __forceinline__ void update(const AdamwEntry& E, const Factors& F, in
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float d = g[e] * F.grad;
-      m[e] = F.b1 * m[e] + F.c1 * d;
-      v[e] = F.b2 * v[e] + F.c2 * (d * d);
-      // (roots and reciprocals that are off by one unit: that part of a weight's step, or of a state's rounding)
-      root[e] = __builtin_amdgcn_sqrtf(v[e]);
+      m[e] = moment(F.b1, m[e], F.c1, d);
+      v[e] = moment(F.b2, v[e], F.c2, d * d);
+      // what a weight's step is divided by may be off by a unit, and a root that becomes a state may not
+      root[e] = kEight ? nearest_root(v[e]) : __builtin_amdgcn_sqrtf(v[e]);
       p[e] = p[e] * keep - F.step * m[e] * __builtin_amdgcn_rcpf(root[e] * F.root + F.eps);
       if constexpr (kEight) most_m = larger(most_m, fabsf(m[e])), most_v = larger(most_v, root[e]);
     }
