@@ -56,6 +56,18 @@ __device__ __forceinline__ void operand_of(const f32x16& c, int i, f32x8& f) {
   for (int e = 0; e < 8; ++e) f[e] = c[8 * i + e];
 }
 
+// What operand_of's rounding took from b: with kTwice a product a b takes it as well.  So do calls of few pairs of a query and a
+// key, whose results may hang on a handful of probabilities that all lie where bf16 is coarsest: three queries of 68 keys at four
+// heads (gradient) were 1.7 times as far off as results that are rounded once, and are as near as those so, in the same 16 us.
+// Among many it is 1.4 times, and the second product would cost more than it gives (one query of 768 keys at 28 heads, gradient,
+// 21 us, so 23; 16 x 500 to 2,000 tokens at four heads of 32 32 us, so 44).
+inline bool few_pairs(const AttentionArgs& a) { return (double)a.n_q * a.heads * ((double)a.n_k / a.n_seqs) <= 16384.0; }
+__device__ __forceinline__ void rest_of(const f32x16& c, int i, const bf16x8& f, bf16x8& rest) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = (__bf16)(c[8 * i + e] - (float)f[e]);
+}
+__device__ __forceinline__ void rest_of(const f32x16&, int, const f32x8&, f32x8&) {}
+
 // eight neighbours of an output row (aligned to 16 bytes)
 __device__ __forceinline__ void store8(uint16_t* p, const f32x16& c, int i, float by) {
   float v[8];

@@ -41,7 +41,7 @@ __device__ __forceinline__ size_t partial_at(int part, const AttentionArgs& A, s
   return (((size_t)part * A.n_q + row) * A.heads + head) * (HD + 4);
 }
 
-template <typename T, int HD>
+template <typename T, int HD, bool kTwice>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_attention(AttentionArgs A, Group group, int slots, int parts,
                                                                                      float* __restrict__ partial) {
   typedef Rows<T, HD> R;
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
     }
     // bf16 probabilities: each is off by at most 2^-8 of itself, as far as the output's own rounding moves it, and the
     // errors of many keys largely cancel; their sum is that of the unrounded ones
-    Frag p[2 * B];
+    Frag p[2 * B], rest[2 * B];
 #pragma unroll
     for (int b = 0; b < B; ++b) {
 #pragma unroll
@@ -169,14 +169,20 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_packed_
         l_run += s[b][e];
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) operand_of(s[b], i, p[2 * b + i]);
+      for (int i = 0; i < 2; ++i) {
+        operand_of(s[b], i, p[2 * b + i]);
+        if constexpr (kTwice) rest_of(s[b], i, p[2 * b + i], rest[2 * b + i]);
+      }
     }
     auto values = [&](auto b) {
       groups<2 * kAt, D>(
           fc, [&](auto g, Frag(&f)[D]) { read_col(std::integral_constant<int, g + 2 * b>(), f); },
           [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-            for (int d = 0; d < D; ++d) mma(f[d], p[g + 2 * b], o[d]);
+            for (int d = 0; d < D; ++d) {
+              mma(f[d], p[g + 2 * b], o[d]);
+              if constexpr (kTwice) mma(f[d], rest[g + 2 * b], o[d]);
+            }
           });
     };
     values(std::integral_constant<int, 0>());
@@ -270,7 +276,13 @@ int key_parts(const AttentionArgs& a) {
 template <typename T, int HD>
 hipError_t launch(hipStream_t s, const AttentionArgs& a, float* partial) {
   const int slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kQueries), parts = key_parts<T>(a);
-  k_packed_attention<T, HD><<<walk_grid<true>(slots, parts, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, parts, partial);
+  auto run = [&](auto kernel) {
+    kernel<<<walk_grid<true>(slots, parts, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, parts, partial);
+  };
+  if (sizeof(T) == 2 && few_pairs(a))
+    run(k_packed_attention<T, HD, sizeof(T) == 2>);
+  else
+    run(k_packed_attention<T, HD, false>);
   if (parts > 1) k_attention_merge<T, HD><<<dim3(slots * a.kv_heads, kQueries * HD / 1024), 256, 0, s>>>(a, slots, parts, partial);
   return hipGetLastError();
 }

@@ -29,7 +29,7 @@ constexpr int kWaves = 4;
 // -lse / scale and -D of every row behind ([n_q][heads]), which the keys' gradients need.
 constexpr int kDqRows = 32 * kWaves, kDqKeys = 64;
 
-template <typename T, int HD>
+template <typename T, int HD, bool kTwice>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dq(AttentionGradArgs A, Group group, int slots, int parts,
                                                                                  float2* __restrict__ stats,
                                                                                  float* __restrict__ partial) {
@@ -139,12 +139,18 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) dp[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c2, -my.x)) * (dp[e] - my.y);
-      Frag ds[2];
+      Frag ds[2], rest[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) operand_of(dp, i, ds[i]);
+      for (int i = 0; i < 2; ++i) {
+        operand_of(dp, i, ds[i]);
+        if constexpr (kTwice) rest_of(dp, i, ds[i], rest[i]);
+      }
       groups<2, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
 #pragma unroll
-        for (int d = 0; d < D; ++d) mma(f[d], ds[g], dq[d]);
+        for (int d = 0; d < D; ++d) {
+          mma(f[d], ds[g], dq[d]);
+          if constexpr (kTwice) mma(f[d], rest[g], dq[d]);
+        }
       });
     }
   });
@@ -166,7 +172,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
 // rows.  Scores have queries as rows and keys as columns, so that a lane holds one key's.
 constexpr int kBackKeys = 32 * kWaves, kBackRows = 32;
 
-template <typename T, int HD>
+template <typename T, int HD, bool kTwice>
 __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attention_dkv(AttentionGradArgs A, Group group, int slots, int parts,
                                                                                   const float2* __restrict__ stats,
                                                                                   float* __restrict__ partial) {
@@ -177,7 +183,7 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   __shared__ __align__(16) float s_stat[2][2][kBackRows];
   // 128 dimensions: registers for all of k and v are some 20 too many, and what the compiler then keeps in scratch memory waits for
   // the tiles on their way: six of v's eight operands lie in LDS, in fp32, with one workgroup in a compute unit, all of them
-  constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 ? 2 : 0;
+  constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 && !kTwice ? 2 : 0;
   __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
   Walk walk;
   if (!find_walk<false>(slots, parts, A.kv_heads, &walk)) return;
@@ -303,16 +309,22 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
       s[e] = __builtin_amdgcn_exp2f((kStart ? s[e] : s[e] + s_stat[buf][0][i]) * c2);
       dp[e] = s[e] * (kStart ? dp[e] : dp[e] + s_stat[buf][1][i]);
     }
-    Frag p[2], ds[2];
+    Frag p[2], ds[2], p_rest[2], ds_rest[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) operand_of(s, i, p[i]), operand_of(dp, i, ds[i]);
+    for (int i = 0; i < 2; ++i) {
+      operand_of(s, i, p[i]), operand_of(dp, i, ds[i]);
+      if constexpr (kTwice) rest_of(s, i, p[i], p_rest[i]), rest_of(dp, i, ds[i], ds_rest[i]);
+    }
     groups<4, D>(fc, read_col, [&](auto g, Frag(&f)[D]) {
 #pragma unroll
       for (int d = 0; d < D; ++d) {
-        if constexpr (g % 2)
+        if constexpr (g % 2) {
           mma(f[d], ds[g / 2], dk[d]);
-        else
+          if constexpr (kTwice) mma(f[d], ds_rest[g / 2], dk[d]);
+        } else {
           mma(f[d], p[g / 2], dv[d]);
+          if constexpr (kTwice) mma(f[d], p_rest[g / 2], dv[d]);
+        }
       }
     });
   });
@@ -409,24 +421,26 @@ int join_groups(int slots, int width) { return std::max(1, std::min(width / 16, 
 
 size_t stats_bytes(const AttentionArgs& a) { return ((size_t)a.n_q * a.heads * 8 + 15) / 16 * 16; }
 
-template <typename T, int HD>
+template <typename T, int HD, bool kTwice>
 hipError_t launch(hipStream_t s, const AttentionGradArgs& a, char* ws) {
   float2* stats = (float2*)ws;
   float* partial = (float*)(ws + stats_bytes(a));  // of the queries, then of the keys
   const int q_slots = tile_slots(a.n_q, a.heads / a.kv_heads, a.n_seqs, kDqRows), kp = key_parts<T>(a);
   const int join_slots = tile_slots(a.n_q, 1, a.n_seqs, 128);
-  k_attention_dq<T, HD><<<walk_grid<true>(q_slots, kp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
+  k_attention_dq<T, HD, kTwice><<<walk_grid<true>(q_slots, kp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), q_slots, kp, stats, partial);
   if (kp > 1) k_attention_join_dq<T><<<dim3(join_slots, join_groups(join_slots, a.heads * HD)), 256, 0, s>>>(a, kp, partial);
   const int slots = tile_slots(a.n_k, 1, a.n_seqs, kBackKeys);
   const int rp = row_parts<T>(a);
-  k_attention_dkv<T, HD><<<walk_grid<false>(slots, rp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
+  k_attention_dkv<T, HD, kTwice><<<walk_grid<false>(slots, rp, a.kv_heads), 64 * kWaves, 0, s>>>(a, group_of(a), slots, rp, stats, partial);
   if (rp > 1) k_attention_join_dkv<T><<<dim3(slots, 2 * join_groups(slots, a.kv_heads * HD)), 256, 0, s>>>(a, rp, partial);
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, bool kTwice>
 hipError_t launch_of(hipStream_t s, const AttentionGradArgs& a, char* ws) {
-  return a.head_dim == 32 ? launch<T, 32>(s, a, ws) : a.head_dim == 64 ? launch<T, 64>(s, a, ws) : launch<T, 128>(s, a, ws);
+  return a.head_dim == 32   ? launch<T, 32, kTwice>(s, a, ws)
+         : a.head_dim == 64 ? launch<T, 64, kTwice>(s, a, ws)
+                            : launch<T, 128, kTwice>(s, a, ws);
 }
 
 }  // namespace
@@ -436,7 +450,8 @@ size_t packed_attention_backward_workspace(const AttentionArgs& a) {
 }
 
 hipError_t launch_packed_attention_backward(hipStream_t s, int dtype, const AttentionGradArgs& a, void* ws) {
-  return dtype == ROLLOUT_DTYPE_BF16 ? launch_of<uint16_t>(s, a, (char*)ws) : launch_of<float>(s, a, (char*)ws);
+  if (dtype == ROLLOUT_DTYPE_FP32) return launch_of<float, false>(s, a, (char*)ws);
+  return few_pairs(a) ? launch_of<uint16_t, true>(s, a, (char*)ws) : launch_of<uint16_t, false>(s, a, (char*)ws);
 }
 
 }  // namespace rollout
