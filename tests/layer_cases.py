@@ -55,7 +55,7 @@ class Attention:
             x[self.unused(seqs, n)] = float("nan")
         self.shape = R.AttentionShape(dtype=CODE[dtype], n_heads=heads, n_kv_heads=kv, head_dim=hd, n_seqs=len(q_lens), n_q=self.n_q,
                                       n_k=self.n_k, causal=int(causal), scale=self.scale)
-        self.fused = fused
+        self.fused, self.few = fused, False
 
     @staticmethod
     def unused(seqs, n):
@@ -114,7 +114,7 @@ class Attention:
                 p, es = self.score_errors(q[A, h], k[B, h // G], nq, nk)
                 # a probability: its score's error, the exponential's 2, a share of the running maximum's rescalings (2 each of
                 # at most nk / 64), the sum's nk roundings; bf16 rounds it once more
-                ep = es.max(1, initial=0.0)[:, None] * 2 + (nk + nk / 32 + 8) * U + (half if self.dtype == "bf16" else 0.0)
+                ep = es.max(1, initial=0.0)[:, None] * 2 + (nk + nk / 32 + 8) * U + self.second_rounding()
                 bound = ep * (p @ np.abs(v[B, h // G])) * 1.01 + (half + 4 * U) * np.abs(o[A, h]) * 1.01 + 1e-37
                 err = np.abs(got[A, h] - o[A, h])
                 assert (err <= bound).all(), f"out: head {h} of the sequence at {a}: {np.nanmax(err / bound):.3g} of the bound"
@@ -125,6 +125,12 @@ class Attention:
                 assert (err <= bound).all(), f"lse: head {h} of the sequence at {a}"
         free = self.unused(self.q_seqs, self.n_q).cpu().numpy()
         assert (wide(out)[free] == SENTINEL).all() and (got_z[:, free] == SENTINEL).all(), "a row of no sequence was written"
+
+    def second_rounding(self):
+        """How far a probability may be off as an operand of the second product: half a step of bf16, and where what that lost is
+        multiplied as well (calls of few pairs), half a step of the rest; nothing in fp32."""
+        half = HALF["bf16"]
+        return 0.0 if self.dtype == "fp32" else half * half if self.few else half
 
     def score_errors(self, q, k, nq, nk):
         """Probabilities, and how far the exponent of each may be off: hd + 4 roundings of the product's terms, and one of it
@@ -140,7 +146,7 @@ class Attention:
         want = L.attention_backward(q, k, v, o, z, do, self.q_seqs, self.k_seqs, self.scale, self.causal)
         got = [self.heads(x, n) for x, n in zip(grads, (self.H, self.K, self.K))]
         G, half = self.H // self.K, HALF[self.dtype]
-        rounds = half if self.dtype == "bf16" else 0.0
+        rounds = self.second_rounding()
         bounds = [np.zeros_like(w) for w in want]
         for (a, nq), (b, nk) in zip(self.q_seqs, self.k_seqs):
             A, B = slice(a, a + nq), slice(b, b + nk)
@@ -149,7 +155,7 @@ class Attention:
                 p, es = self.score_errors(q[A, h], k[B, j], nq, nk)
                 zz = np.where(np.isfinite(z[h, A]), z[h, A], 0.0)[:, None]
                 # p = 2^(s log2 e - lse log2 e): the score's error, 4 roundings of lse, 2 of the exponential
-                ep = es + 4 * U * np.abs(zz) + 4 * U
+                ep = es + 4 * U * np.abs(zz) + 4 * U + (self.hd * U * np.abs(zz) if self.few else 0.0)  # (products that start from lse)
                 dp, d = do[A, h] @ v[B, j].T, (do[A, h] * o[A, h]).sum(1, keepdims=True)
                 ds = np.abs(p * (dp - d))
                 # both products' hd + 4 roundings

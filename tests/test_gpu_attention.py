@@ -68,6 +68,18 @@ def test_the_same_bits_again(dtype):
         assert all(torch.equal(a.view(torch.uint8), b.contiguous().view(torch.uint8)) for a, b in zip(first, map(torch.clone, again)))
 
 
+@pytest.mark.parametrize("heads,kv,hd,q_lens,k_lens", [
+    (4, 4, 32, [3, 3], [68, 68]), (14, 2, 64, [1, 2, 1], [60, 200, 1]), (28, 4, 128, [5, 1, 0, 7], None), (4, 1, 128, [1], [900])])
+def test_few_pairs_lose_nothing_by_the_second_product(heads, kv, hd, q_lens, k_lens):
+    """Up to 16,384 pairs of a query and a key: what bf16 rounds off the probabilities is multiplied as well."""
+    c = Attention("bf16", heads, kv, hd, q_lens, k_lens)
+    assert c.n_q * heads * c.n_k / len(q_lens) <= 16384
+    c.few = True
+    out, lse = c.forward()
+    c.check_forward(out, lse)
+    c.check_backward(c.backward(out, lse), out, lse)
+
+
 def test_gradients_by_differences():
     """The loss sum(out * w) moves as the gradient says, along a random direction, by the kernel's own forward pass."""
     c = Attention("fp32", 4, 2, 64, [40, 70], [45, 70], scale=0.2)
