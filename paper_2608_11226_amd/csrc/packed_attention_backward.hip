@@ -8,8 +8,8 @@
 // queries' gradients atomically has five, but every sum has an order of its own that does not depend on scheduling.
 //
 // Bound by the matrix products and what feeds them: 8,192 tokens at 40 on 8 heads of 128 take 900 us for the queries and 1,286 for
-// the keys (products are at work in 0.70 and 0.65 of the compute units' cycles) and 59 to join the keys' parts; the 7B update's 16
-// sequences 88, 137 and 14 (0.32 and 0.38: short walks, and the longest ones end alone); fp32 at the 7B heads 1,003, 1,509 and 23.
+// the keys (products are at work in 0.70 and 0.65 of the compute units' cycles) and 56 to join the keys' parts; the 7B update's 16
+// sequences 87, 134 and 17 (0.32 and 0.38: short walks, and the longest ones end alone); fp32 at the 7B heads 1,015, 1,455 and 39.
 // Did not pay: the scores' exponentials issued beside the other product (7B 230 us, so 244), workgroups of eight waves that share
 // out a tile's rows and add up in LDS instead of half of the parts (7B 222, so 241; 14B 2,120, so 2,125), and as many parts as a
 // walk's own length asks for (some dies then wait for the others).
