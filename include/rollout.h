@@ -524,13 +524,14 @@ rollout_status rollout_rms_norm_backward(const void* d_grad_y, int32_t grad_y_dt
  * The step, with g = grad_scale grad and t = step:
  *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   param = param (1 - lr weight_decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, a moment's products, sum and root each rounded to nearest, with the new moments before they are rounded further (one of less than 2^-126 may count as 0; eps is 0 or at least that).  BF16 weights and E4M3 states are rounded up or down with
- * the probability that keeps their expectation (to nearest they would not move by steps that are small beside them), by 16 bits r
- * of a counter hash of (seed, t, the tensor's place in the table, the element): bf16 drops 16 bits of
+ * in fp32, a moment's products, sum and root each rounded to nearest, with the new moments before they are rounded further
+ * (one of less than 2^-126 may count as 0; eps is 0 or at least that).  BF16 weights and E4M3 states are rounded up or
+ * down with the probability that keeps their expectation (to nearest they would not move by steps that are small beside
+ * them), by 16 bits r of a counter hash of (seed, t, the tensor's place in the table, the element): bf16 drops 16 bits of
  * the fp32 value's magnitude after adding r, e4m3 drops 20 after adding 16 r + 8 (below 2^-6, where values are 2^-9 apart,
  * from the magnitude plus 2^-6).  A scale is the smallest power of two, 2^-126 at least, that leaves no finite magnitude of
- * its 128 above 448 (a moment that is not finite becomes NaN, and no other one of the 128 changes by it); a second moment of 2^-126 or more keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the
- * low 16 bits and v the high ones; a weight the low ones of f(h + (k >> 32)).  f is MurmurHash3's 32-bit
+ * its 128 above 448 (a moment that is not finite becomes NaN, and no other one of the 128 changes by it); a second moment
+ * of 2^-126 or more keeps a code above 0.  Of h = f(i * 0x9E3779B1 + k) for element i, m takes the low 16 bits and v the high ones; a weight the low ones of f(h + (k >> 32)).  f is MurmurHash3's 32-bit
  * finaliser, k = F(F(seed + G t) + G (1 + tensor + 2^20 floor(i / 2^32))) with SplitMix64's finaliser F and constant G.
  * d_grad_scale fp32 [1] (a clipping factor, say; NULL: 1): where it is not finite nothing changes.  d_lr fp32 [1] and d_step
  * int64 [1] replace lr and step if not NULL (a captured call reads them at every replay; a step below 1 counts as 1).

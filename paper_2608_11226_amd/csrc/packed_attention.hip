@@ -15,7 +15,8 @@
 // TFLOP/s in bf16 (products are at work in 0.61 of the compute units' cycles; exponentials and maxima fill much of the rest), at 64
 // dimensions 680; fp32 102 of the 154 that fp32 products reach.  Short ones, 16 of 257 to 768 tokens at 28 on 4 heads, 60 us, 545
 // TFLOP/s: walks of some five tiles, whose beginning (its place, rows and first tile, a trip to memory after the other) and end are
-// hidden by the compute unit's other workgroup alone (464 sequences of 18 tokens, a tile each, 40 us).  Exponentials issued between the products of the tile before them took the long case from 655 to 694 us, a
+// hidden by the compute unit's other workgroup alone (464 sequences of 18 tokens, a tile each, 40 us).  Exponentials issued
+// between the products of the tile before them took the long case from 655 to 694 us, a
 // higher priority of waves at their products changed nothing, and half tiles with four on the way took few tokens' from 29 to 32.
 #include "packed_attention.h"
 
