@@ -120,7 +120,8 @@ __device__ __forceinline__ float towards(float x, uint32_t bits) {
   const float a = fabsf(x);
   const bool small = a < 0x1p-6f;
   const float z = small ? a + 0x1p-6f : a;
-  const float q = __uint_as_float((__float_as_uint(z) + (bits << 4) + 8u) & 0xFFF00000u);
+  // (a NaN of any pattern as the one that the sum carries nowhere: beyond 0x7FFFFFFF it would be 0)
+  const float q = __uint_as_float((min(__float_as_uint(z), 0x7FC00000u) + (bits << 4) + 8u) & 0xFFF00000u);
   return copysignf(small ? q - 0x1p-6f : q, x);
 }
 

@@ -277,3 +277,37 @@ def test_on_another_stream():
     step_of(table_of([t]), 5, 1, stream=s.cuda_stream)
     s.synchronize()
     check_step([t], 5, 1, before)
+
+
+@pytest.mark.parametrize("grad,patterns", [("bf16", [0x7FFF, 0xFFFF, 0x7FF0, 0x7FC0, 0x7F81, 0xFF81]),
+                                           ("fp32", [0x7FFFFFFF, 0xFFFFFFFF, 0x7FF00000, 0x7FC00000, 0x7F800001, 0xFF800001])])
+def test_every_pattern_that_is_no_number_stays_one(grad, patterns):
+    """Whatever the bits of a gradient that is not a number, both moments become NaN; nothing else changes by which it is."""
+    g = torch.Generator(device=DEV).manual_seed(12)
+    t = Tensor(g, 4096, "fp32", grad, "e4m3")
+    handle, first, grads = table_of([t]), [x.clone() for x in t.all()], t.g.clone()
+    bad = torch.arange(4096, device=DEV) % 3 == 1  # (many values of the hash)
+    kind = torch.int16 if grad == "bf16" else torch.int32
+    outs = []
+    for u in patterns:
+        for x, y in zip(t.all(), first):
+            x.copy_(y)
+        t.g.copy_(grads)
+        t.g.view(kind)[bad] = u - (1 << 8 * kind.itemsize) if u >> (8 * kind.itemsize - 1) else u
+        assert t.g[bad].isnan().all()
+        step_of(handle, 2, 0)
+        for x in (t.p, t.m.float(), t.v.float()):
+            assert x[bad].isnan().all() and torch.isfinite(x[~bad]).all(), hex(u)
+        outs.append([x.float()[~bad] if x.numel() == 4096 else x.clone() for x in t.all()])
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], outs[-1])), hex(u)
+
+
+def test_states_that_are_no_numbers_stay_so():
+    g = torch.Generator(device=DEV).manual_seed(13)
+    t = Tensor(g, 2048, state="e4m3")
+    for x, code in ((t.m, 0x7F), (t.m, 0xFF), (t.v, 0x7F)):
+        keep = x.clone()
+        x.view(torch.uint8)[::2] = code
+        step_of(table_of([t]), 2, 0)
+        assert x.float()[::2].isnan().all() and torch.isfinite(x.float()[1::2]).all()
+        x.copy_(keep)
