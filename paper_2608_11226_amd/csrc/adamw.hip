@@ -120,8 +120,7 @@ __device__ __forceinline__ float towards(float x, uint32_t bits) {
   const float a = fabsf(x);
   const bool small = a < 0x1p-6f;
   const float z = small ? a + 0x1p-6f : a;
-  // (a NaN of any pattern as the one that the sum carries nowhere: beyond 0x7FFFFFFF it would be 0)
-  const float q = __uint_as_float((min(__float_as_uint(z), 0x7FC00000u) + (bits << 4) + 8u) & 0xFFF00000u);
+  const float q = __uint_as_float((__float_as_uint(z) + (bits << 4) + 8u) & 0xFFF00000u);
   return copysignf(small ? q - 0x1p-6f : q, x);
 }
 
@@ -134,15 +133,21 @@ __device__ __forceinline__ float moment(float b, float m, float c, float x) {
 }
 
 // The instruction's root is within a unit.  It is one too large if x <= r (r - unit), and one too small if x > r (r + unit): the
-// border between two neighbours, squared, lies within a quarter of a unit squared of their product.  (0 and infinity stay: their
-// neighbours' products are 0 or no numbers.  7B layer with states in 8 bits 748 us, with the library's root, which scales small x as
-// well, 761.)
+// border between two neighbours, squared, lies within a quarter of a unit squared of their product (Tuckerman's test).  x is 0, or so
+// large that fp32 holds the sign of the differences: they are multiples of a unit squared, some 2^-47 of x, and some 2^-24 of it in
+// size.  (0 and infinity stay: their neighbours' products are 0 or no numbers.)
 __device__ __forceinline__ float nearest_root(float x) {
   const float r = __builtin_amdgcn_sqrtf(x);
   const float below = __uint_as_float(__float_as_uint(r) - 1u), above = __uint_as_float(__float_as_uint(r) + 1u);
   const float lower = fmaf(-below, r, x), upper = fmaf(-above, r, x);
   return lower <= 0.f ? below : upper > 0.f ? above : r;
 }
+// Where x is smaller than 2^-100 the differences are rounded to multiples of 2^-149, and x is scaled first.
+constexpr float kSmallRoot = 0x1p-50f;
+__device__ __forceinline__ float nearest_small_root(float x) { return nearest_root(x * 0x1p64f) * 0x1p-32f; }
+
+// A NaN of any pattern as the one that `towards` carries nowhere: added to, those with high bits would be 0.
+__device__ __forceinline__ float one_nan(float x) { return x == x ? x : __builtin_nanf(""); }
 
 struct Factors {
   float b1, c1, b2, c2, eps, lr, step, root;  // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
@@ -176,6 +181,7 @@ __device__ __forceinline__ void update(const AdamwEntry& E, const Factors& F, in
     }
     float root[8];
     float most_m = 0.f, most_v = 0.f;
+    uint32_t most = 0u, least = ~0u;  // of the roots' patterns, 0 apart: as numbers in order, behind them what is none
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float d = g[e] * F.grad;
@@ -183,9 +189,28 @@ __device__ __forceinline__ void update(const AdamwEntry& E, const Factors& F, in
       v[e] = moment(F.b2, v[e], F.c2, d * d);
       // what a weight's step is divided by may be off by a unit, and a root that becomes a state may not
       root[e] = kEight ? nearest_root(v[e]) : __builtin_amdgcn_sqrtf(v[e]);
-      p[e] = p[e] * keep - F.step * m[e] * __builtin_amdgcn_rcpf(root[e] * F.root + F.eps);
-      if constexpr (kEight) most_m = larger(most_m, fabsf(m[e])), most_v = larger(most_v, root[e]);
+      if constexpr (kEight) {
+        most_m = fmaxf(most_m, fabsf(m[e]));
+        most = max(most, __float_as_uint(root[e]));
+        least = min(least, __float_as_uint(root[e]) - 1u);
+      }
     }
+    if constexpr (kEight) {
+      most_v = __uint_as_float(most);
+      // rare, and looked for in all eight at once (7B layer 746 us, bf16 weights 619; each scaled, left out or given a pattern by itself
+      // 761 and 639)
+      if (!(most_m < INFINITY) || !(most_v < INFINITY) || least < __float_as_uint(kSmallRoot)) {
+        most_m = 0.f, most_v = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (root[e] > 0.f && root[e] < 2.f * kSmallRoot) root[e] = nearest_small_root(v[e]);
+          m[e] = one_nan(m[e]), root[e] = one_nan(root[e]);
+          most_m = larger(most_m, fabsf(m[e])), most_v = larger(most_v, root[e]);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = p[e] * keep - F.step * m[e] * __builtin_amdgcn_rcpf(root[e] * F.root + F.eps);
     if constexpr (kEight || kCoarse) {
       uint32_t h[8];
       const uint32_t start = (uint32_t)i * 0x9E3779B1u + (uint32_t)key;

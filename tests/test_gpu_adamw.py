@@ -311,3 +311,39 @@ def test_states_that_are_no_numbers_stay_so():
         step_of(table_of([t]), 2, 0)
         assert x.float()[::2].isnan().all() and torch.isfinite(x.float()[1::2]).all()
         x.copy_(keep)
+
+
+@pytest.mark.parametrize("binade", [-126, -125, -124, -122, -120, -117, -112, -107, -104, -96, -60, 0, 60, 126])
+def test_roots_at_the_border_of_two_codes(binade):
+    """Second moments down to 2^-126 whose roots, rounded to nearest, lie at the border that the hash's bits put between two codes, or
+    one unit below it: a root that is off by a unit gives the other code."""
+    n, beta2, seed, step = 8192, 0.5, 99, 1
+    _, bits, _ = L.adamw_bits(seed, step, 0, np.arange(n))
+    r = np.random.default_rng(binade + 200)
+    # from fresh states v = g g / 2, each product rounded; v in [2^binade, 2^(binade + 1))
+    g = np.sqrt(2.0 * r.uniform(1.001, 1.999, 1 << 24) * 2.0 ** binade).astype(np.float32)
+    v = np.float32(0.5) * (g * g)
+    assert (v >= np.float32(2.0 ** binade)).all()
+    root = np.sqrt(v)  # (correctly rounded)
+    low = root.view(np.uint32) & 0xFFFFF
+    order = np.argsort(low, kind="stable")
+    # (16 bits + 8) added to the mantissa's last 20 carries from `border` on
+    border = (1 << 20) - (16 * bits + 8)
+    wanted = border - (np.arange(n) & 1)
+    at = np.searchsorted(low[order], wanted)
+    found = (at < len(low)) & (low[order][np.minimum(at, len(low) - 1)] == wanted)
+    assert found.mean() > 0.9
+    pick = order[np.where(found, at, 0)]
+    gn = torch.zeros(n, device=DEV)
+    gn.copy_(torch.from_numpy(g[pick]))
+    p, m, v8 = torch.zeros(n, device=DEV), torch.zeros(n, dtype=torch.uint8, device=DEV), torch.zeros(n, dtype=torch.uint8, device=DEV)
+    ms, vs = torch.zeros(n // 128, device=DEV), torch.zeros(n // 128, device=DEV)
+    table, chunks = R.rollout_adamw_table([R.adamw_tensor(p, gn, m, v8, 0.0, ms, vs)])
+    R.rollout_adamw(table.to(DEV), 1, chunks, 0.0, 0.0, beta2, EPS, step, seed, stream=torch.cuda.current_stream().cuda_stream)
+    most = root[pick].reshape(-1, 128).max(1).astype(np.float64)
+    scale = L.power_scale(most)
+    np.testing.assert_array_equal(wide(vs), scale)
+    z = (root[pick].reshape(-1, 128) / scale[:, None]).astype(np.float32)  # (exact, and above 2^-6)
+    want = ((z.view(np.uint32) + (16 * bits.reshape(-1, 128) + 8).astype(np.uint32)) & np.uint32(0xFFF00000)).view(np.float32)
+    got = wide(v8.view(E4M3)).reshape(-1, 128)
+    assert (got == want).all(), f"{(got != want).sum()} of {n} codes"
