@@ -155,6 +155,28 @@ def test_differences_of_the_chain():
         assert abs((ends[0] - ends[1]) / (2 * h) - slope) <= 4 * 2.0 ** -24 / h * 8 + 10 * h * h, (k, slope)
 
 
+def test_differences_along_the_gradients():
+    """The same where it says most: along each weight's own gradient, where the slope is its norm, and half way from there to a random
+    direction.  A gradient that is off by a tenth of its norm in either fails."""
+    w, b = weights(8), Batch(9)
+    a = forward(w, b)
+    b.old = a["logp"].clone()
+    g = backward(w, b, a)
+    gen, h = torch.Generator(device=DEV).manual_seed(10), 2.0 ** -7
+    # the loss is of size 1 and rounded to 2^-24 like every log probability in it; third order: h^2 of at most 4 (along the gradients
+    # of six such chains in float64 at most 1.9)
+    tol = 4 * 2.0 ** -24 / h * 8 + 4 * h * h
+    for k in NAMES:
+        along = g[k].double() / g[k].double().norm()
+        other = torch.randn(w[k].shape, generator=gen, device=DEV, dtype=torch.float64)
+        for way in (along, along + other / other.norm()):
+            way = (way / way.norm()).float()
+            slope = float((g[k].double() * way.double()).sum())
+            assert slope >= 10 * tol, (k, slope)
+            ends = [float(forward({**w, k: w[k] + sign * h * way}, b)["loss"]) for sign in (1, -1)]
+            assert abs((ends[0] - ends[1]) / (2 * h) - slope) <= tol, (k, slope)
+
+
 def test_steps_of_the_optimiser_follow():
     """Three steps with fp32 states against float64 on the same gradients, then with states in 8 bits: the loss of the tokens that
     are worth more than others is a number, and every weight has moved."""
