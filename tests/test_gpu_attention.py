@@ -59,6 +59,16 @@ def test_attention_backward(name):
     c.check_backward(grads, out, lse)
 
 
+@pytest.mark.parametrize("dtype,heads,kv,hd", [("bf16", 17, 1, 64), ("bf16", 66, 2, 128), ("fp32", 40, 1, 32), ("bf16", 64, 1, 32),
+                                               ("fp32", 64, 1, 128), ("bf16", 128, 2, 64)])
+def test_many_heads_to_a_keys(dtype, heads, kv, hd):
+    """More than 16 query heads share a key's, and more than the rows of a tile: a tile lies within a token, or in two."""
+    c = Attention(dtype, heads, kv, hd, [1, 19, 0, 66, 7], [40, 19, 3, 70, 2])
+    out, lse = c.forward()
+    c.check_forward(out, lse)
+    c.check_backward(c.backward(out, lse), out, lse)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_the_same_bits_again(dtype):
     c = Attention(dtype, 8, 2, 128, [300, 65, 1, 130])
