@@ -428,7 +428,8 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
 
 /*
  * The update through the layers: attention over packed sequences and its gradient, the norm of the
- * residual stream and its gradient, and the optimiser's step.  Matrix products are the caller's.
+ * residual stream and its gradient, and the optimiser's step.  What else a layer has, matrix products, rotary embedding
+ * and the gated activation, is the caller's, with its gradients.
  *
  * Attention.  Sequences lie one behind the other in matrices of tokens, d_q [n_q, n_heads * head_dim] and
  * d_k, d_v [n_k, n_kv_heads * head_dim], whose rows are a stride of elements apart (so that the three
@@ -444,7 +445,11 @@ rollout_status rollout_embedding_backward(const void* d_grad, int32_t grad_dtype
  * and none of another one's.
  * d_out as d_q, d_lse fp32 [n_heads, n_q].
  * dtype FP32 (fp32 products) or BF16 (probabilities and their gradients enter products as bf16; sums
- * and statistics are fp32).  Matrices and strides are multiples of 16 bytes, rows at most 2^25 bytes apart.
+ * and statistics are fp32; in calls of at most 16,384 pairs, n_q n_heads n_k / n_seqs, what that rounding takes is multiplied
+ * too).  A sequence's last bits depend on the shape that it is called with, not on the other sequences' values.
+ * Matrices and strides are multiples of 16 bytes, rows at most 2^25 bytes apart.
+ * The workspace is for 64 parts that a query's keys may be cut into, each n_q n_heads (head_dim + 4) fp32, and 256 MiB at most;
+ * it goes by these alone, whether or not the call is cut, so that a larger call's serves smaller ones.
  * Errors: EINVAL (shape, NULL buffers, alignment, strides, overlap), EUNSUPPORTED (head_dim not 32, 64 or
  * 128, n_heads / n_kv_heads above 64, n_heads times tokens above 2^26, n_heads times sequences above 2^23, strides), ENOMEM
  * (workspace too small), EDEVICE.
@@ -470,7 +475,8 @@ rollout_status rollout_attention(const rollout_attention_shape* shape, const voi
  *   grad_v_j = sum_i p_ij grad_out_i;  ds_ij = p_ij (grad_out_i v_j - D_i)
  *   grad_k_j = scale sum_i ds_ij q_i;  grad_q_i = scale sum_j ds_ij k_j
  * each over the query heads that share the key's.  Every row of a sequence is written (keys that no query
- * attends, and queries without keys, get 0).  The gradients' rows may be columns of one matrix.
+ * attends, and queries without keys, get 0).  The gradients' rows may be columns of one matrix.  The workspace holds 8 bytes
+ * for every query and head, and the parts' sums, 256 MiB of them at most.
  * Errors as above.
  */
 rollout_status rollout_attention_backward_workspace(const rollout_attention_shape* shape, uint64_t* h_bytes);
@@ -487,7 +493,8 @@ rollout_status rollout_attention_backward(const rollout_attention_shape* shape, 
  * Root-mean-square norm of rows of dim values, behind the addition to the residual stream:
  *   h = x + delta (rounded to x_dtype);  rstd = 1 / sqrt(mean h^2 + eps);  y = h rstd gain
  * d_x [n_rows, dim] of x_dtype, d_delta of delta_dtype with d_h of x_dtype (which may be d_x), or both NULL (h = x);
- * d_gain fp32 [dim], NULL: 1; d_y of y_dtype; d_rstd fp32 [n_rows], NULL if not wanted (the gradient needs it).
+ * d_gain fp32 [dim], NULL: 1; d_y of y_dtype; d_rstd fp32 [n_rows], NULL if not wanted (the gradient needs it).  Squares are
+ * summed in fp32: a row whose sum of squares is above 3.4e38 gets rstd 0.
  * x and delta are FP32 or BF16.  y is FP32, BF16 or E4M3: then d_scales [n_rows] (otherwise NULL) receives
  * the smallest power of two, 2^-126 at least, for which no finite |y| of the row, over it, is above 448, and d_y the codes of
  * y over it, to nearest, ties to even (NaN where y is not finite).  Matrices are dense, and rows may start at any element.
@@ -515,7 +522,8 @@ rollout_status rollout_rms_norm_backward(const void* d_grad_y, int32_t grad_y_dt
 /*
  * AdamW over many tensors in one launch.  A table names them: rollout_adamw_table writes it to host memory
  * (rollout_adamw_table_bytes of it), the caller copies it to the device once, and it serves every step as long as
- * the buffers stay where they are.  A tensor of n >= 0 elements:
+ * the buffers stay where they are, the gradients' among them (a program that allocates these anew for every step makes the
+ * table anew as well).  A tensor of n >= 0 elements:
  *   d_param of param_dtype (FP32 or BF16), d_grad of grad_dtype (FP32 or BF16);
  *   d_m, d_v: first and second moment, fp32 (state_dtype FP32), or E4M3 codes with d_m_scales, d_v_scales fp32
  *     [ceil(n / 128)], one scale for 128 elements: m = code scale, sqrt(v) = code scale.  Zeros are a fresh state;

@@ -6,7 +6,7 @@
 // Bound by HBM: every tensor is read and written once.  A table in device memory names the tensors; a workgroup takes a chunk
 // of one of them, which it finds in the table by probing 64 entries at a time.  A 7B layer, 233 million elements: fp32 weights with
 // a bf16 copy and bf16 gradients 748 us with states in 8 bits (5.0 TB/s), 1,206 with fp32 states (5.4); bf16 weights with states in
-// 8 bits 623 (3.8 TB/s), where two hashes and the rounding of three values an element keep the vector ALU busy.
+// 8 bits 614 (3.8 TB/s), where two hashes and the rounding of three values an element keep the vector ALU busy.
 //
 // States in 8 bits are e4m3 with a power of two as scale for each run of 128 elements (16 lanes of 8): the first moment, and
 // the root of the second, whose range is half as wide.  To nearest, a state would not move at all where a step changes it by
@@ -197,7 +197,7 @@ __device__ __forceinline__ void update(const AdamwEntry& E, const Factors& F, in
     }
     if constexpr (kEight) {
       most_v = __uint_as_float(most);
-      // rare, and looked for in all eight at once (7B layer 746 us, bf16 weights 619; each scaled, left out or given a pattern by itself
+      // rare, and looked for in all eight at once (7B layer 748 us, bf16 weights 614; each scaled, left out or given a pattern by itself
       // 761 and 639)
       if (!(most_m < INFINITY) || !(most_v < INFINITY) || least < __float_as_uint(kSmallRoot)) {
         most_m = 0.f, most_v = 0.f;
@@ -292,9 +292,9 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const AdamwEntry* __restrict
 }  // namespace
 
 // What a workgroup finds out before its first element (its tensor, factors, the hash's keys) costs nothing where memory is the
-// bound, and short chunks spread the load: a 7B layer with fp32 states 1,206 us with one step a workgroup, 1,231 with two and
-// 1,250 with four, its bf16 weights with fp32 states 909, 943 and 965.  Rounding by hashes makes arithmetic the bound: states in 8
-// bits 734, 728 and 738, bf16 weights with them 663, 639 and 597.  A table of few elements needs every workgroup (300 x 1,200 in two
+// bound, and short chunks spread the load: a 7B layer with fp32 states 1,197 us with one step a workgroup, 1,228 with two and
+// 1,249 with four, its bf16 weights with fp32 states 911, 948 and 967.  Rounding by hashes makes arithmetic the bound: bf16 weights
+// with states in 8 bits 719, 672 and 614, fp32 weights with them 749, 747 and 747.  A table of few elements needs every workgroup (300 x 1,200 in two
 // layers 12.7 us with one step, 16.5 with four), and one of more than 2^34 takes four, for a launch of less than 2^32 threads.
 int64_t adamw_chunk(int64_t all, int kind) {
   if (all > (int64_t)1 << 34) return 4 * kStep;

@@ -56,11 +56,13 @@ __device__ __forceinline__ void operand_of(const f32x16& c, int i, f32x8& f) {
   for (int e = 0; e < 8; ++e) f[e] = c[8 * i + e];
 }
 
-// What operand_of's rounding took from b: with kTwice a product a b takes it as well.  So do calls of few pairs of a query and a
-// key, whose results may hang on a handful of probabilities that all lie where bf16 is coarsest: three queries of 68 keys at four
-// heads (gradient) were 1.7 times as far off as results that are rounded once, and are as near as those so, in the same 16 us.
-// Among many it is 1.4 times, and the second product would cost more than it gives (one query of 768 keys at 28 heads, gradient,
-// 21 us, so 23; 16 x 500 to 2,000 tokens at four heads of 32 32 us, so 44).
+// What operand_of's rounding took from b: with kTwice a product a b takes it as well.  Without it results are farther off than
+// those that are rounded once: outputs 1.05 (2 keys) to 1.35 times (900), gradients 1.4 times whatever the number of keys, as a root
+// mean square; in calls of few pairs of a query and a key, by the luck of few roundings, 1.0 to 2.8 times (gradients; emulated calls
+// of four heads).  There the second product is in nobody's way, and they are as near as those so (three queries of 68 keys, gradient,
+// 16 us with and without); in larger ones it costs more than it gives (one query of 768 keys at 28 heads, gradient, 21 us, so 23; 16 x
+// 500 to 2,000 tokens at four heads of 32 32 us, so 44).  The rule is one on the call, by its allocated rows: a sequence that is called
+// with many others has other last bits than alone.
 inline bool few_pairs(const AttentionArgs& a) { return (double)a.n_q * a.heads * ((double)a.n_k / a.n_seqs) <= 16384.0; }
 __device__ __forceinline__ void rest_of(const f32x16& c, int i, const bf16x8& f, bf16x8& rest) {
 #pragma unroll

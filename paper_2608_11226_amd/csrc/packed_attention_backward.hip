@@ -182,7 +182,8 @@ __global__ __launch_bounds__(64 * kWaves, sizeof(T) == 2 ? 2 : 1) void k_attenti
   __shared__ __align__(16) char s_do[2][kBackRows * R::kBytes];
   __shared__ __align__(16) float s_stat[2][2][kBackRows];
   // 128 dimensions: registers for all of k and v are some 20 too many, and what the compiler then keeps in scratch memory waits for
-  // the tiles on their way: six of v's eight operands lie in LDS, in fp32, with one workgroup in a compute unit, all of them
+  // the tiles on their way: six of v's eight operands lie in LDS, in fp32, with one workgroup in a compute unit, all of them, and all
+  // where products are doubled (with 64 bytes of a lane in scratch memory all the same: calls that are a launch)
   constexpr int C = HD / 16, D = HD / 32, kKept = HD < 128 ? C : sizeof(T) == 2 && !kTwice ? 2 : 0;
   __shared__ __align__(16) Frag s_v[kKept < C ? kWaves : 1][kKept < C ? C - kKept : 1][64];
   Walk walk;
