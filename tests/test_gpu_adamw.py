@@ -321,7 +321,7 @@ def test_roots_at_the_border_of_two_codes(binade):
     _, bits, _ = L.adamw_bits(seed, step, 0, np.arange(n))
     r = np.random.default_rng(binade + 200)
     # from fresh states v = g g / 2, each product rounded; v in [2^binade, 2^(binade + 1))
-    g = np.sqrt(2.0 * r.uniform(1.001, 1.999, 1 << 24) * 2.0 ** binade).astype(np.float32)
+    g = np.sqrt(2.0 * r.uniform(1.001, 1.999, 1 << 22) * 2.0 ** binade).astype(np.float32)
     v = np.float32(0.5) * (g * g)
     assert (v >= np.float32(2.0 ** binade)).all()
     root = np.sqrt(v)  # (correctly rounded)
